@@ -386,6 +386,135 @@ typedef struct {
 int kvp_trace_generate(const kvp_trace_params* params, uint32_t* access_bitmaps, void* stream);
 
 /*
+ * ---- from a model's attention to the placement problem ----
+ * The paper's traces are attention weights recorded while a model decodes (Section IV-A). The calls below are that path on the
+ * device: keys and values go into a cache held in 4 bits (kvp_cache_append), attention reads it and notes what weight every
+ * unit received (kvp_attend), recorded weights become access bitmaps (kvp_trace_weights) for kvp_create, and they drive
+ * eviction, as one step of a serving loop (kvp_evict) or as a placement schedule (kvp_policy_accumulated). They are
+ * asynchronous on `stream`, keep nothing between calls, allocate nothing and work on the current device; all of them can be
+ * captured into a graph (lengths, tables, slots and bitmaps are read on the device).
+ *
+ * A cache held in 4 bits. [pages][kv_heads][kvp_cache_page_bytes(head_dim, page_tokens)] bytes, 16-byte aligned: a page holds
+ * page_tokens (a multiple of 16) tokens of one kv-head as page_tokens / 16 tiles of 16 tokens, so that a unit of the placement
+ * problem lies in one piece. head_dim is 64, 128 or 256. Every group of 32 dims of a token's key or value is kept as
+ * zero + scale * q with q = 0..15 in 4 bits, zero = fp16(min), scale = fp16((max - zero) / 15), q = (x - zero) / scale rounded to
+ * the nearest whole number, ties to even, and cut to 0..15, or 0 where scale is 0; each operation in fp32. Inputs beyond +-65504 count as that, NaN
+ * and -0 as 0.
+ * A tile is 20 * head_dim bytes; with N = head_dim / 32, i the token of the tile, n the group, j the dim in the group, and
+ * 4-bit numbers low half of a byte first, in this order:
+ *   keys [i][j/8][n][j%8] and values [(i/2)%2][j/4][i/4][n][i%2][j%4], 4 bits each;
+ *   scales of the keys [i][n], zeros of the keys [i][n], scales of the values [i/4][n][i%4], zeros of the values [i/4][n][i%4], fp16.
+ * 160 bytes for a token's key and value at head_dim 128, 512 in bf16: bytes_per_unit of kvp_create is 1.25 * head_dim * unit_tokens.
+ */
+#define KVP_BF16 0u
+#define KVP_F16  1u
+#define KVP_F32  2u
+
+typedef struct {
+    uint32_t pages, kv_heads, head_dim, page_tokens;
+    uint32_t reserved;          /* must be 0 */
+} kvp_cache_shape;
+
+/* Bytes of a page of one kv-head; 0 for a head_dim or page_tokens that is not served. */
+uint64_t kvp_cache_page_bytes(uint32_t head_dim, uint32_t page_tokens);
+
+/*
+ * kvp_cache_append -- quantise the keys and values of `tokens` tokens into the cache.
+ *   k, v   (device) [tokens][kv_heads][head_dim] of `dtype` (KVP_BF16, KVP_F16, KVP_F32); strides in elements, dims contiguous.
+ *          Any alignment; 16-byte aligned rows are read faster.
+ *   slots  (device) [tokens]: page * page_tokens + place in the page. A token whose slot lies outside the cache is not written
+ *          (use -1 for padding). Two tokens of one call with the same slot leave a mixture of both there.
+ * Errors: KVP_ERR_ARG (null, zero sizes, unknown dtype, page_tokens no multiple of 16), KVP_ERR_RANGE (head_dim).
+ */
+int kvp_cache_append(const kvp_cache_shape* c, void* cache, uint32_t dtype, uint32_t tokens, const void* k,
+                     int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                     const int64_t* slots, void* stream);
+
+/* kvp_cache_read -- the inverse: k, v (device) [tokens][kv_heads][head_dim], contiguous, 16-byte aligned; scale * q and the sum with
+ * zero are rounded to fp32, the result to `dtype`. A token whose slot lies outside the cache reads as 0. */
+int kvp_cache_read(const kvp_cache_shape* c, const void* cache, uint32_t dtype, uint32_t tokens, const int64_t* slots, void* k,
+                   void* v, void* stream);
+
+typedef struct {
+    kvp_cache_shape cache;
+    uint32_t batch;             /* sequences                                                                 */
+    uint32_t queries;           /* query tokens per sequence, the last ones of it: 1..1024                   */
+    uint32_t group;             /* query heads per kv-head; queries * group <= 4096                          */
+    uint32_t table_pages;       /* pages per row of the table; table_pages * page_tokens < 2^31              */
+    uint32_t unit_tokens;       /* tokens per unit: 1, 2, 4, 8 or a multiple of 16; divides page_tokens      */
+    uint32_t dtype;             /* of q and out: KVP_BF16 or KVP_F16                                         */
+    float    scale;             /* of the scores, usually 1 / sqrt(head_dim)                                 */
+    uint32_t reserved;          /* must be 0 */
+    int64_t  q_batch_stride, q_query_stride, q_head_stride; /* in elements; dims contiguous                  */
+} kvp_attend_params;
+
+/*
+ * kvp_attend -- attention of the last `queries` tokens of each sequence over its cache, and the weight every unit received.
+ *   q       (device) [batch][queries][kv_heads * group][head_dim], strided; head kv * group + j reads kv-head kv
+ *   table   (device) [batch][table_pages]: the pages of each sequence in order. Tokens of a page outside 0..pages-1 are not read.
+ *   lens    (device) [batch]: tokens of each sequence in the cache, those of the queries included (cut to 0..table_pages *
+ *           page_tokens; 0 for an idle slot). Query j sees the tokens before lens - queries + 1 + j.
+ *   units   (device) uint32 bitmap or NULL: unit u of (sequence b, kv-head h) is bit (b * kv_heads + h) * n + u of the words,
+ *           n = table_pages * page_tokens / unit_tokens; only tokens of units whose bit is set are read. With batch 1 this
+ *           is one layer's part of a row of kvp_create's access_bitmaps (word aligned where kv_heads * n is a multiple of 32).
+ *   out     (device) [batch][queries][kv_heads * group][head_dim], contiguous
+ *   lse     (device) [batch][queries][kv_heads * group] float or NULL: natural logarithm of the sum of exp(score)
+ *   weights (device) [batch][kv_heads][n] float or NULL: softmax weight of the unit's tokens, summed over the queries and heads that
+ *           share the kv-head; 0 for units that were not read
+ *   workspace (device) 256-byte aligned, kvp_attend_workspace(...) bytes, used by this call alone until its work has finished
+ * A query that sees no token gives out 0 and lse -infinity. Errors: KVP_ERR_ARG (null, zero sizes, unit_tokens, dtype, a scale that is
+ * not finite, a workspace too small), KVP_ERR_RANGE (head_dim, sizes above).
+ */
+int kvp_attend_workspace(const kvp_attend_params* params, int want_weights, int has_units, uint64_t* bytes);
+int kvp_attend(const kvp_attend_params* params, const void* q, const void* cache, const int32_t* table, const int32_t* lens,
+               const uint32_t* units, void* out, float* lse, float* weights, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * kvp_trace_weights -- access bitmaps of recorded weights: every step each group reads the `topk` units that received most.
+ *   weights        (device) [steps][groups * units_per_group]; a unit without a positive weight (0, negative, NaN) is not read,
+ *                  so a group can read fewer than topk, or nothing at the steps of other layers
+ *   access_bitmaps (device) [steps][ceil(groups * units_per_group / 32)]
+ * Ties are broken towards the lower unit index. Limits: units_per_group <= 32768 (KVP_ERR_RANGE), 1 <= topk <= units_per_group.
+ */
+int kvp_trace_weights(uint32_t groups, uint32_t units_per_group, uint32_t steps, uint32_t topk, const float* weights,
+                      uint32_t* access_bitmaps, void* stream);
+
+/*
+ * Eviction from a cache by accumulated attention weight. Per unit acc = floor(acc * decay_q / 65536) + round(min(max(w, 0), 128) * 2^24)
+ * (ties to even, NaN counts as 0, acc is cut to 0..2^48 - 1). Of the units 0 .. exist-1 of a group the first `sink` and the last `recent` are always
+ * kept; the rest of the `budget` goes to those with the largest acc among the others that kept_in still holds, ties to the lower index.
+ */
+typedef struct {
+    uint32_t groups, units_per_group, steps;
+    uint32_t budget;            /* units kept per group, sink + recent <= budget <= units_per_group */
+    uint32_t sink, recent;
+    uint32_t decay_q;           /* decay per step * 2^16, 0..65536 (65536 = none)                   */
+    uint32_t reserved;          /* must be 0 */
+} kvp_evict_params;
+
+/*
+ * kvp_evict -- `steps` steps: add the step's weights, then choose.
+ *   weights  (device) [steps][groups * units_per_group], as kvp_attend gives them
+ *   acc_in   (device) [groups * units_per_group] int64 or NULL (= 0);  acc_out (device) the same, may be acc_in itself
+ *   kept_in  (device) [W32] bitmap or NULL (= every unit): the units that may be kept besides the protected ones; in a serving
+ *            loop the row the call before gave, so that what was evicted stays evicted
+ *   exist    (device) [groups] int32 or NULL (= units_per_group): units the group has by now (cut to 0..units_per_group)
+ *   kept_out (device) [steps][W32]: the units kept after each step; overlap with kept_in is KVP_ERR_ARG
+ * Limit: units_per_group <= 32768 (KVP_ERR_RANGE).
+ */
+int kvp_evict(const kvp_evict_params* params, const float* weights, const int64_t* acc_in, int64_t* acc_out,
+              const uint32_t* kept_in, const int32_t* exist, uint32_t* kept_out, void* stream);
+
+/*
+ * kvp_policy_accumulated -- the same rule as a schedule generator beside the other strategies: before each step s the units with the
+ * largest weight accumulated over steps 0 .. s-1 are in HBM (`budget` per group; a unit that was moved out is still read from off-package
+ * DRAM, receives weight and may return). Step 0 starts from the protected units and the lowest indices.
+ *   params: steps and groups * units_per_group as in the problem; groups * budget <= hbm_capacity_units (KVP_ERR_CAPACITY otherwise)
+ *   weights (device) [steps][U];  schedule (device) [steps][W32]. Asynchronous on `stream`.
+ */
+int kvp_policy_accumulated(kvp_problem* p, const kvp_evict_params* params, const float* weights, uint32_t* schedule, void* stream);
+
+/*
  * The look-ahead placement policy that the paper's annealer tunes (Section III-B), as a schedule generator.
  * Window W (steps, 1..64) and migration ratio R = ratio_permille / 1000. Starting from the static placement
  * `init_mode` (KVP_INIT_STATIC_FIRST or KVP_INIT_STATIC_FREQ), before every step s:

@@ -404,11 +404,76 @@ trace_select_kernel(const TraceK k, uint32_t want, uint32_t U, const int32_t* __
     select_step<UPT, FULL>(key, k, want, k.topk, gbase, t, sm);
 }
 
+// Access bitmaps of recorded weights: the same selection, one CTA per (group, step), on the bits of positive floats, which order
+// as whole numbers do. A unit that received nothing (or NaN) has key 0 and is never picked.
+template <int UPT, bool FULL>
+__global__ void __launch_bounds__(UPT == 32 ? 1024 : 512, UPT == 32 ? 1 : 3)
+weights_select_kernel(const TraceK k, uint32_t want, uint64_t U, const float* __restrict__ weights)
+{
+    __shared__ SelectSmem sm;
+    __shared__ uint32_t received;
+    const uint32_t g = blockIdx.x % k.groups, t = blockIdx.x / k.groups, T = blockDim.x, tid = threadIdx.x;
+    const uint32_t gbase = g * k.n;
+    select_reset(sm);
+    if (tid == 0) received = 0;
+    int32_t key[UPT];
+    uint32_t here = 0;
+    const float* from = weights + t * U + gbase + tid;
+#pragma unroll
+    for (int j = 0; j < UPT; ++j) {
+        const float w = (FULL || j * T + tid < k.n) ? __ldcs(from + j * T) : 0.0f;
+        key[j] = w > 0.0f ? __float_as_int(w) : 0;
+        here += key[j] > 0;
+    }
+    __syncthreads();
+    here = block_sum(here, &received);
+    if (here) {
+        select_step<UPT, FULL>(key, k, want, min(k.topk, here), gbase, t, sm);
+    } else if (k.aligned) {                                  // an empty row
+        uint32_t* row = k.out + (size_t)t * k.W32 + (gbase >> 5);
+        for (uint32_t i = tid; i < k.n / 32; i += T) row[i] = 0;
+    }
+}
+
 }  // namespace
 
 }  // namespace kvp
 
 using namespace kvp;
+
+extern "C" int kvp_trace_weights(uint32_t groups, uint32_t units_per_group, uint32_t steps, uint32_t topk, const float* weights,
+                                 uint32_t* access_bitmaps, void* stream)
+{
+    if (!groups || !units_per_group || !steps || !topk || topk > units_per_group || !weights || !access_bitmaps) return KVP_ERR_ARG;
+    const uint64_t U = (uint64_t)groups * units_per_group;
+    if (units_per_group > 32768 || U >= (1ull << 31) || (uint64_t)groups * steps >= (1ull << 31)) return KVP_ERR_RANGE;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    TraceK k = {};
+    k.groups = groups; k.n = units_per_group; k.steps = steps; k.topk = topk;
+    k.W32 = (uint32_t)((U + 31) / 32);
+    k.out = access_bitmaps;
+    k.aligned = units_per_group % 32 == 0;
+    if (!k.aligned) KVP_CUDA(cudaMemsetAsync(access_bitmaps, 0, (size_t)steps * k.W32 * 4, st));
+    const uint32_t n = units_per_group, grid = groups * steps;
+    int su = n > 8192 ? 32 : 1;
+    while (su < 16 && (n + su - 1) / su > 128) su *= 2;
+    const uint32_t ST = ((n + su - 1) / su + 31) / 32 * 32, want = select_want(topk, ST);
+    const bool full = (uint64_t)su * ST == n;
+#define KVP_SELECT(UPT)                                                                      \
+    if (full) weights_select_kernel<UPT, true><<<grid, ST, 0, st>>>(k, want, U, weights);    \
+    else weights_select_kernel<UPT, false><<<grid, ST, 0, st>>>(k, want, U, weights)
+    switch (su) {
+        case 1: KVP_SELECT(1); break;
+        case 2: KVP_SELECT(2); break;
+        case 4: KVP_SELECT(4); break;
+        case 8: KVP_SELECT(8); break;
+        case 16: KVP_SELECT(16); break;
+        default: KVP_SELECT(32); break;
+    }
+#undef KVP_SELECT
+    KVP_CUDA(cudaGetLastError());
+    return KVP_OK;
+}
 
 extern "C" int kvp_trace_generate(const kvp_trace_params* tp, uint32_t* access_bitmaps, void* stream)
 {

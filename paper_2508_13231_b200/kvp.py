@@ -27,6 +27,8 @@ EXPORTS = [
     "kvp_anneal_chain_state", "kvp_trace_generate", "kvp_philox4x32_10", "kvp_strerror", "kvp_last_cuda_error",
     "kvp_policy_lookahead", "kvp_policy_reactive", "kvp_policy_page", "kvp_wr_grid", "kvp_wr_anneal", "kvp_set_births",
     "kvp_set_test_hooks", "kvp_anneal_exchange", "kvp_exchange_temps",
+    "kvp_cache_page_bytes", "kvp_cache_append", "kvp_cache_read", "kvp_attend", "kvp_attend_workspace", "kvp_trace_weights",
+    "kvp_evict", "kvp_policy_accumulated",
 ]
 
 
@@ -111,6 +113,11 @@ class TraceParams(C.Structure):
     ]
 
 
+class EvictParams(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in (
+        "groups", "units_per_group", "steps", "budget", "sink", "recent", "decay_q", "reserved")]
+
+
 class TestHooks(C.Structure):
     _fields_ = [("warps_per_chain", C.c_uint32), ("drop_turn", C.c_uint32), ("split_queue_plus1", C.c_uint32),
                 ("resident", C.c_uint32), ("overlay", C.c_uint32)]
@@ -131,6 +138,7 @@ def _lib():
         h.kvp_destroy.restype = None
         h.kvp_philox4x32_10.restype = None
         h.kvp_set_test_hooks.restype = None
+        h.kvp_cache_page_bytes.restype = C.c_uint64
         _handle = h
     return _handle
 
@@ -221,6 +229,75 @@ def trace_generate(groups, units_per_group, steps, topk, seed, rho_q, c_q, sigma
     if out is None:
         out = torch.empty((steps, w32), dtype=torch.int32, device="cuda")
     _chk(_lib().kvp_trace_generate(C.byref(tp), _ptr(out, torch.int32), _stream(stream)), "kvp_trace_generate")
+    return out
+
+
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _cuda_stream(stream):
+    return None if stream is None else stream.cuda_stream
+
+
+def cache_page_bytes(head_dim, page_tokens):
+    """Bytes of a page of one kv-head of a cache held in 4 bits (1.25 * head_dim a token): a cache is a uint8 CUDA tensor
+    [pages][kv_heads][cache_page_bytes]. head_dim 64, 128 or 256; page_tokens a multiple of 16."""
+    n = int(_lib().kvp_cache_page_bytes(C.c_uint32(head_dim), C.c_uint32(page_tokens)))
+    if not n:
+        raise ValueError("head_dim must be 64, 128 or 256 and page_tokens a multiple of 16")
+    return n
+
+
+def cache_append(cache, k, v, slots, stream=None):
+    """kvp_cache_append: quantises keys and values [tokens][kv_heads][head_dim] into the cache at slots (int64 [tokens], page *
+    page_tokens + place; a slot outside the cache, such as -1, writes nothing)."""
+    rc = _native().cache_append(cache, k, v, slots, _cuda_stream(stream))
+    if rc:
+        _chk(rc, "kvp_cache_append")
+
+
+def cache_read(cache, slots, head_dim, dtype=torch.bfloat16, stream=None):
+    """kvp_cache_read -> (k, v) [tokens][kv_heads][head_dim]: what the cache holds at slots (0 outside it)."""
+    if dtype not in _DTYPES:
+        raise ValueError("dtype must be bfloat16, float16 or float32")
+    out = _native().cache_read(cache, slots, head_dim, _DTYPES[dtype], _cuda_stream(stream))
+    if out.__class__ is int:
+        _chk(out, "kvp_cache_read")
+    return out
+
+
+def attend(q, cache, table, lens, unit_tokens=0, scale=None, units=None, want_lse=False, want_weights=False, weights=None, stream=None):
+    """kvp_attend -> dict(out, lse, weights): attention of the last tokens of each sequence over the cache, and what weight each
+    unit of unit_tokens tokens (default: a page) received.
+
+    q: [batch][heads][head_dim], or [batch][queries][heads][head_dim] for several tokens, bfloat16 or float16, any strides but the last;
+    table: int32 [batch][pages]; lens: int32 [batch], the tokens of the queries included; units: int32 bitmap of
+    batch * kv_heads * n bits, n = pages * page_tokens / unit_tokens, or None for all; scale: default 1 / sqrt(head_dim).
+    weights [batch][kv_heads][n] float32 are made with want_weights, or written to the tensor given as `weights` (a row of a recording)."""
+    out = _native().attend(q, cache, table, lens, unit_tokens, scale, units, want_lse, bool(want_weights) if weights is None else weights,
+                           _cuda_stream(stream))
+    if out.__class__ is int:
+        _chk(out, "kvp_attend")
+    return out
+
+
+def trace_weights(weights, groups, topk, out=None, stream=None):
+    """kvp_trace_weights: access bitmaps (int32 [steps][ceil(U/32)]) of recorded weights [steps][U]: the topk units of each group
+    that received most at each step; units without a positive weight are not read."""
+    out = _native().trace_weights(weights, groups, topk, out, _cuda_stream(stream))
+    if out.__class__ is int:
+        _chk(out, "kvp_trace_weights")
+    return out
+
+
+def evict(weights, groups, budget, sink=0, recent=0, decay_q=65536, acc=None, kept=None, exist=None, acc_out=None, stream=None):
+    """kvp_evict -> dict(kept, acc): eviction by accumulated weight. weights [steps][U] (or [U]) are added to acc (int64 [U], weight 1 =
+    2^24; None = 0) step by step, decaying by decay_q / 65536; kept (int32 [steps][ceil(U/32)]) are the `budget` units of each
+    group left after each step: the first `sink`, the last `recent` of the `exist` (int32 [groups]) units there are, and those with
+    most weight among the ones in the bitmap `kept`. acc_out: a tensor for the new sums, may be acc itself."""
+    out = _native().evict(weights, groups, budget, sink, recent, decay_q, acc, kept, exist, acc_out, _cuda_stream(stream))
+    if out.__class__ is int:
+        _chk(out, "kvp_evict")
     return out
 
 
@@ -371,6 +448,18 @@ class Problem:
         """kvp_policy_page -> CUDA int32 [S][W32]."""
         out = torch.empty((self.steps, self.w32), dtype=torch.int32, device="cuda")
         _chk(_lib().kvp_policy_page(self._h, C.c_uint32(page_units), _ptr(out), _stream(stream)), "kvp_policy_page")
+        return out
+
+    def policy_accumulated(self, weights, groups, budget=None, sink=0, recent=0, decay_q=65536, stream=None):
+        """kvp_policy_accumulated -> CUDA int32 [S][W32]: before each step the units with the largest weight accumulated so far are in
+        HBM, `budget` per group (default: the capacity divided by the groups). weights: float32 [S][U]."""
+        if weights.numel() != self.steps * self.units:
+            raise ValueError("weights must be [steps][units]")
+        ep = EvictParams(groups, self.units // groups if groups else 0, self.steps,
+                         self.cap // groups if budget is None and groups else budget or 0, sink, recent, decay_q, 0)
+        out = torch.empty((self.steps, self.w32), dtype=torch.int32, device="cuda")
+        _chk(_lib().kvp_policy_accumulated(self._h, C.byref(ep), _ptr(weights, torch.float32), _ptr(out), _stream(stream)),
+             "kvp_policy_accumulated")
         return out
 
     def wr_grid(self, w_max, n_ratio=11, init_mode=INIT_STATIC_FIRST, stream=None):
