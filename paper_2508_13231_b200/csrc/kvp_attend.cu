@@ -33,6 +33,7 @@ constexpr int kWarps = 8;
 constexpr uint32_t kThreads = kWarps * 32;
 constexpr uint32_t kRows = 8;                 // query rows of a segment
 constexpr uint32_t kListCap = 1024;           // tiles of a bitmap row that are listed at a time
+constexpr uint32_t kTop = 0x03C003C0u;        // the upper four bits of two fp16 significands
 constexpr float kNone = -3e38f;               // maximum of nothing
 constexpr float kLift = 3.0f, kSlack = 8.0f;  // weights are at most 2^(kLift + kSlack), 2^kLift right after the maximum moved
 
@@ -56,10 +57,11 @@ struct AttendK {
     uint32_t rows, segs;     // query rows of a kv-head, segments of a kv-head
     uint32_t page_tiles, table_pages, pages;
     uint32_t unit, row_units;
-    uint32_t sub;            // tokens per block of `mass`: min(unit, 16)
+    uint32_t sub;            // tokens per block of `mass`: min(unit, 16); 0: no weights asked for
+    uint32_t unit_log2;      // of a unit of at most 16 tokens; 4 for larger ones
     uint32_t ctas, least;    // CTAs of the launch, and the least tiles worth one
     float scale;
-    bool bf16;
+    bool q_aligned;          // every eight dims of a query lie at a 16-byte boundary
 };
 
 __device__ __forceinline__ uint32_t length_of(const AttendK& p, uint32_t b)
@@ -69,6 +71,11 @@ __device__ __forceinline__ uint32_t length_of(const AttendK& p, uint32_t b)
     return (uint32_t)(n < 0 ? 0 : n > most ? most : n);
 }
 __device__ __forceinline__ uint32_t tiles_of(uint32_t tokens) { return (tokens + kTileTokens - 1) / kTileTokens; }
+
+// The kernels of a call follow each other closely: the next one's CTAs come up while the last ones of this one work, and wait
+// here until all of it is done and visible.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // 32 bits of the bitmap from bit `at` on; bits behind its end read as 0
 __device__ __forceinline__ uint32_t bits_at(const AttendK& p, uint64_t at)
@@ -80,93 +87,96 @@ __device__ __forceinline__ uint32_t bits_at(const AttendK& p, uint64_t at)
     return __funnelshift_r(lo, hi, sh);
 }
 
-// which of the tiles 32 w .. 32 w + 31 of row bh hold a token that is to be read
-__device__ uint32_t tile_word(const AttendK& p, uint32_t bh, uint32_t w, uint32_t tiles)
+// The units 32 w .. 32 w + 31 of a row that are to be read, of those that hold one of the first `len` tokens. Units smaller than a
+// tile are put together: bit i (a multiple of 16 / unit) stands for a tile.
+__device__ __forceinline__ uint32_t unit_word(const AttendK& p, uint32_t bh, uint32_t w, uint32_t units)
 {
-    const uint64_t row = (uint64_t)bh * p.row_units;
-    uint32_t bits = 0;
-    if (p.unit == kTileTokens) {
-        bits = bits_at(p, row + 32ull * w);
-    } else if (p.unit < kTileTokens) {
-        const uint32_t k = kTileTokens / p.unit, mask = (1u << k) - 1u;
-        for (uint32_t i = 0; i < 32; i += 32 / k) {
-            const uint32_t x = bits_at(p, row + (32ull * w + i) * k);
-            for (uint32_t j = 0; j < 32 / k; ++j) bits |= (uint32_t)(((x >> (j * k)) & mask) != 0) << (i + j);
-        }
-    } else {
-        const uint32_t k = p.unit / kTileTokens, first = 32u * w / k;
-        const uint32_t x = bits_at(p, row + first);
-        for (uint32_t i = 0; i < 32; ++i) bits |= ((x >> ((32u * w + i) / k - first)) & 1u) << i;
+    uint32_t x = bits_at(p, (uint64_t)bh * p.row_units + 32ull * w);
+    const uint32_t left = units - 32u * w;                  // 32 w < units
+    if (left < 32u) x &= (1u << left) - 1u;
+    if (p.unit < kTileTokens) {
+        for (uint32_t k = 1; k < kTileTokens / p.unit; k <<= 1) x |= x >> k;
+        x &= p.unit == 1 ? 0x00010001u : p.unit == 2 ? 0x01010101u : p.unit == 4 ? 0x11111111u : 0x55555555u;
     }
-    const uint32_t left = tiles > 32u * w ? tiles - 32u * w : 0u;
-    return left >= 32u ? bits : bits & ((1u << left) - 1u);
+    return x;
 }
+__device__ __forceinline__ uint32_t units_of(const AttendK& p, uint32_t len) { return (len + p.unit - 1) / p.unit; }
 
-// counts[bh]: one warp per row of the bitmap
+// counts[bh]: tiles to read of a row of the bitmap; one CTA per row
 __global__ void __launch_bounds__(kThreads) count_kernel(const AttendK p)
 {
-    const uint32_t bh = blockIdx.x * kWarps + threadIdx.x / 32, lane = threadIdx.x % 32;
-    if (bh >= p.batch * p.heads) return;
-    const uint32_t tiles = tiles_of(length_of(p, bh / p.heads));
+    __shared__ uint32_t sum[kWarps];
+    let_next_start();
+    const uint32_t bh = blockIdx.x, tid = threadIdx.x;
+    const uint32_t len = length_of(p, bh / p.heads), units = units_of(p, len), tiles = tiles_of(len);
+    const uint32_t k = p.unit > kTileTokens ? p.unit / kTileTokens : 1;
     uint32_t n = 0;
-    for (uint32_t w = lane; 32u * w < tiles; w += 32) n += __popc(tile_word(p, bh, w, tiles));
+    for (uint32_t w = tid; 32u * w < units; w += kThreads) {
+        const uint32_t x = unit_word(p, bh, w, units);
+        n += __popc(x) * k;
+        if (k > 1 && units - 32u * w <= 32u && (x >> (units - 1u - 32u * w)) & 1u) n -= units * k - tiles;   // the last unit may be cut
+    }
     n = __reduce_add_sync(0xFFFFFFFFu, n);
-    if (lane == 0) p.counts[bh] = n;
+    if (tid % 32 == 0) sum[tid / 32] = n;
+    __syncthreads();
+    if (tid == 0) {
+        for (uint32_t i = 1; i < (uint32_t)kWarps; ++i) n += sum[i];
+        p.counts[bh] = n;
+    }
 }
 
 // The line of all tiles. An entry is a sequence (no bitmap) or a (sequence, kv-head) pair; the `per` segments of an entry have
-// the same number of tiles.
+// the same number of tiles. CTA c works on tiles c * chunk .. c * chunk + chunk - 1.
 struct Line {
-    uint64_t before, total;  // tiles before the entry asked for, and of all
-    uint32_t active;         // CTAs that get a part
+    uint32_t before, total;  // tiles before the entry asked for, and of all
+    uint32_t chunk;
 };
 __device__ __forceinline__ uint32_t entry_count(const AttendK& p, uint32_t e) { return p.units ? p.counts[e] : tiles_of(length_of(p, e)); }
 __device__ __forceinline__ uint32_t line_entries(const AttendK& p) { return p.units ? p.batch * p.heads : p.batch; }
 __device__ __forceinline__ uint32_t line_per(const AttendK& p) { return p.units ? p.segs : p.segs * p.heads; }
 
 struct LineSmem {
-    uint64_t warp[32], total, before;
-    uint32_t entry;
+    uint32_t warp[kWarps], before, entry;
 };
 
-// Every thread of the CTA calls it. `at`: a place in the line as a fraction of the CTAs (part `cta` of `active`), returned as the
-// entry there and the tiles before it; or, with cta = ~0, the place of entry `entry`.
-__device__ Line find_in_line(const AttendK& p, uint32_t cta, uint32_t& entry, LineSmem& sm)
+// Every thread of the CTA calls it. With a CTA's number: the entry in which its part begins (`entry`; only if it has a part) and the tiles
+// before that entry. With cta = ~0: the tiles before `entry`.
+__device__ __forceinline__ Line find_in_line(const AttendK& p, uint32_t cta, uint32_t& entry, LineSmem& sm)
 {
-    const uint32_t E = line_entries(p), per = line_per(p), tid = threadIdx.x, T = blockDim.x, lane = tid % 32, warp = tid / 32;
-    const uint32_t chunk = (E + T - 1) / T, first = min(tid * chunk, E), last = min(first + chunk, E);
-    uint64_t mine = 0;
-    for (uint32_t e = first; e < last; ++e) mine += (uint64_t)entry_count(p, e) * per;
-    uint64_t upto = mine;
+    const uint32_t E = line_entries(p), per = line_per(p), tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    const uint32_t each = E <= kThreads ? 1 : (E + kThreads - 1) / kThreads, first = min(tid * each, E), last = min(first + each, E);
+    uint32_t mine = 0;
+    for (uint32_t e = first; e < last; ++e) mine += entry_count(p, e) * per;
+    uint32_t upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const uint64_t v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
         if (lane >= (uint32_t)o) upto += v;
     }
     if (lane == 31) sm.warp[warp] = upto;
     __syncthreads();
-    uint64_t base = 0, total = 0;
-    for (uint32_t w = 0; w < T / 32; ++w) {
+    uint32_t base = 0, total = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < (uint32_t)kWarps; ++w) {
         if (w < warp) base += sm.warp[w];
         total += sm.warp[w];
     }
     Line line;
     line.total = total;
-    const uint64_t worth = (total + p.least - 1) / p.least;
-    line.active = worth < p.ctas ? (uint32_t)worth : p.ctas;
-    uint64_t before = base + upto - mine;
+    line.chunk = max((total + p.ctas - 1) / p.ctas, p.least);
+    uint32_t before = base + upto - mine;
     if (cta == ~0u) {
         if (first <= entry && entry < last) {
-            for (uint32_t e = first; e < entry; ++e) before += (uint64_t)entry_count(p, e) * per;
+            for (uint32_t e = first; e < entry; ++e) before += entry_count(p, e) * per;
             sm.before = before;
         }
-    } else if (cta < line.active) {
-        const uint64_t at = total * cta / line.active;
-        if (before <= at && at < before + mine) {
+    } else {
+        const uint64_t at = (uint64_t)line.chunk * cta;
+        if (before <= at && at < (uint64_t)before + mine) {
             uint32_t e = first;
             for (;; ++e) {
-                const uint64_t n = (uint64_t)entry_count(p, e) * per;
-                if (at < before + n) break;
+                const uint32_t n = entry_count(p, e) * per;
+                if (at < (uint64_t)before + n) break;
                 before += n;
             }
             sm.before = before;
@@ -179,11 +189,16 @@ __device__ Line find_in_line(const AttendK& p, uint32_t cta, uint32_t& entry, Li
     return line;
 }
 
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0,
+                                    float c1, float c2, float c3)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    mma(c, a0, a1, a2, a3, b0, b1, c[0], c[1], c[2], c[3]);
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x)
 {
@@ -214,19 +229,34 @@ __device__ __forceinline__ float over_rows(float x)                 // sum over 
     return x + __shfl_xor_sync(0xFFFFFFFFu, x, 16);
 }
 
-__device__ __forceinline__ float load_q(const AttendK& p, int64_t at)
+// eight dims of a query
+template <bool HALF>
+__device__ __forceinline__ void load_q(const AttendK& p, int64_t at, bool real, float (&x)[8])
 {
-    return p.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.q)[at]) : __half2float(static_cast<const __half*>(p.q)[at]);
+    alignas(16) uint16_t raw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (real) {
+        const uint16_t* from = static_cast<const uint16_t*>(p.q) + at;
+        if (p.q_aligned) {
+            *reinterpret_cast<uint4*>(raw) = __ldg(reinterpret_cast<const uint4*>(from));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) raw[i] = __ldg(from + i);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = HALF ? __half2float(__ushort_as_half(raw[i])) : __uint_as_float((uint32_t)raw[i] << 16);
 }
-__device__ __forceinline__ void store_out(const AttendK& p, uint64_t at, float x)
+template <bool HALF>
+__device__ __forceinline__ uint32_t out_pair(float a, float b)
 {
-    if (p.bf16) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(x);
-    else static_cast<__half*>(p.out)[at] = __float2half_rn(x);
+    if (HALF) return pack(a, b);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
 }
 
 template <int N>
 struct Shape {
-    static constexpr int kStages = N == 2 ? 8 : 4;                  // tiles of a warp under way
+    static constexpr int kStages = N == 2 ? 8 : 4;                  // tiles of a warp under way, two of them worked on
     static constexpr uint32_t kRing = kWarps * kStages * Tile<N>::kBytes;
     static constexpr uint32_t kJoin = kWarps * kRows * 32 * N * 4;
     static constexpr uint32_t kSmem = kRing > kJoin ? kRing : kJoin;
@@ -237,18 +267,20 @@ struct AttendSmem {
     uint32_t list[kListCap];
     uint32_t scan[kWarps];
     float2 ml[kWarps][kRows];
+    float share[kWarps][kRows];
 };
 
 // list[i] = number of the (from + i)-th tile of row bh that is to be read, i < many <= kListCap. Every thread of the CTA calls it.
-__device__ void list_tiles(const AttendK& p, uint32_t bh, uint32_t tiles, uint32_t from, uint32_t many, AttendSmem& sm)
+__device__ __forceinline__ void list_tiles(const AttendK& p, uint32_t bh, uint32_t len, uint32_t from, uint32_t many, AttendSmem& sm)
 {
-    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32, units = units_of(p, len), tiles = tiles_of(len);
+    const uint32_t k = p.unit > kTileTokens ? p.unit / kTileTokens : 1, fold = p.unit < kTileTokens ? kTileTokens / p.unit : 1;
     uint32_t seen = 0;
-    for (uint32_t w0 = 0; 32u * w0 < tiles && seen < from + many; w0 += kThreads) {
+    for (uint32_t w0 = 0; 32u * w0 < units && seen < from + many; w0 += kThreads) {
         const uint32_t w = w0 + tid;
-        uint32_t bits = 32u * w < tiles ? tile_word(p, bh, w, tiles) : 0u;
-        uint32_t upto = __popc(bits);
-        const uint32_t mine = upto;
+        uint32_t bits = 32u * w < units ? unit_word(p, bh, w, units) : 0u;
+        uint32_t mine = __popc(bits) * k;                    // the last unit may be cut, but nothing stands behind it
+        uint32_t upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
@@ -257,18 +289,25 @@ __device__ void list_tiles(const AttendK& p, uint32_t bh, uint32_t tiles, uint32
         if (lane == 31) sm.scan[warp] = upto;
         __syncthreads();
         uint32_t at = seen + upto - mine;
+#pragma unroll
         for (uint32_t i = 0; i < (uint32_t)kWarps; ++i) {
             const uint32_t n = sm.scan[i];
             if (i < warp) at += n;
             seen += n;
         }
-        for (; bits; bits &= bits - 1u, ++at)
-            if (at >= from && at - from < many) sm.list[at - from] = 32u * w + __ffs(bits) - 1u;
+        if (at < from + many && at + mine > from)
+            for (; bits; bits &= bits - 1u) {
+                const uint32_t tile = (32u * w + __ffs(bits) - 1u) / fold * k;
+                for (uint32_t j = 0; j < k; ++j, ++at)
+                    if (at >= from && at - from < many && tile + j < tiles) sm.list[at - from] = tile + j;
+            }
         __syncthreads();
     }
 }
 
-template <int N>
+// HALF: fp16 queries and outputs, else bf16. fp16 outputs keep three more bits, so there the weights enter the second product as two fp16
+// terms (22 bits).
+template <int N, bool HALF>
 __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const AttendK p)
 {
     using L = Tile<N>;
@@ -276,14 +315,16 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
     constexpr int kStages = S::kStages;
     extern __shared__ __align__(16) uint8_t ring_all[];
     __shared__ AttendSmem sm;
+    let_next_start();
     const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32, g = lane >> 2, t = lane & 3;
+    wait_for_previous();
     uint32_t entry = 0;
     const Line line = find_in_line(p, blockIdx.x, entry, sm.line);
-    if (blockIdx.x >= line.active) return;
-    uint64_t todo = line.total * (blockIdx.x + 1) / line.active - line.total * blockIdx.x / line.active;
+    const uint64_t begin = (uint64_t)line.chunk * blockIdx.x;
+    if (begin >= line.total) return;
+    uint32_t todo = min(line.chunk, line.total - (uint32_t)begin);
     const uint32_t per = line_per(p), E = line_entries(p);
-    uint64_t skip = line.total * blockIdx.x / line.active - line.before;
-    uint32_t count = entry_count(p, entry), inner = (uint32_t)(skip / count), off = (uint32_t)(skip % count);
+    uint32_t count = entry_count(p, entry), inner = ((uint32_t)begin - line.before) / count, off = ((uint32_t)begin - line.before) % count;
     uint8_t* const ring = ring_all + warp * kStages * L::kBytes;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
     // a fragment's row g is token 4 (g / 2) + g % 2 of the tile, its row g + 8 the token two further on: a thread then needs the
@@ -296,29 +337,29 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
             count = entry_count(p, entry);
             inner = 0;
         }
-        const uint32_t seg = entry * per + inner, bh = seg / p.segs, rt = seg % p.segs, b = bh / p.heads, h = bh % p.heads;
-        const uint32_t take = (uint32_t)(todo < count - off ? todo : count - off);
-        const uint32_t len = length_of(p, b), tiles = tiles_of(len);
+        const uint32_t seg = entry * per + inner, bh = seg / p.segs, rt = seg - bh * p.segs, b = bh / p.heads, h = bh - b * p.heads;
+        const uint32_t take = min(todo, count - off);
+        const uint32_t len = length_of(p, b);
         const int32_t* table = p.table + (uint64_t)b * p.table_pages;
 
-        // queries: this thread's part of row g as the right operand, divided by a power of two; sums over groups for the zeros
-        uint32_t qf[N][4], qz[2];
-        float f0, f1;
+        // This thread's part of row g's query as the right operand, divided by a power of two; the sums over groups for the zeros.
+        // The 4-bit numbers are centred by starting their products at -8 times those sums, which keeps the partial sums small.
+        uint32_t qf[N][4], qz[N == 8 ? 4 : 2];
+        float start0[N], start1[N], f0, f1;
         {
-            const uint32_t r = rt * kRows + g;
+            const uint32_t r = rt * kRows + g, query = r / p.group;
             const bool real = r < p.rows;
-            const int64_t at = real ? b * p.q_batch + (int64_t)(r / p.group) * p.q_query + (int64_t)(h * p.group + r % p.group) * p.q_head : 0;
+            const int64_t at = b * p.q_batch + (int64_t)query * p.q_query + (int64_t)(h * p.group + (r - query * p.group)) * p.q_head + t * 8;
             float x[N][8], most = 0.0f;
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+            for (int n = 0; n < N; ++n) {
+                load_q<HALF>(p, at + n * 32, real, x[n]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[n][i] = real ? load_q(p, at + n * 32 + t * 8 + i) : 0.0f;
-                    most = fmaxf(most, fabsf(x[n][i]));
-                }
+                for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[n][i]));
+            }
             most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
             most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-            const int e = most > 0.0f && most < INFINITY ? ilogbf(most) - 9 : 0;     // largest magnitude in [2^9, 2^10)
+            const int e = most > 0.0f && most < INFINITY ? ilogbf(most) - 6 : 0;     // largest magnitude in [2^6, 2^7)
             float sums[N];
 #pragma unroll
             for (int n = 0; n < N; ++n) {
@@ -330,44 +371,51 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                 }
                 sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
                 sums[n] = sum + __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+                start0[n] = __shfl_sync(0xFFFFFFFFu, sums[n], 8 * t) * -0x1p-15f;
+                start1[n] = __shfl_sync(0xFFFFFFFFu, sums[n], 8 * t + 4) * -0x1p-15f;
                 qf[n][0] = pack(x[n][0], x[n][4]);
-                qf[n][1] = pack(x[n][1] * 0.0625f, x[n][5] * 0.0625f);
+                qf[n][1] = pack(x[n][1], x[n][5]);
                 qf[n][2] = pack(x[n][2], x[n][6]);
-                qf[n][3] = pack(x[n][3] * 0.0625f, x[n][7] * 0.0625f);
+                qf[n][3] = pack(x[n][3], x[n][7]);
             }
-            // columns of the zeros' product: the sums' upper parts, then what they leave
-            float col[4];
+            // the right operand of the zeros' product, 4 N columns: zeros times the upper parts of the sums and times what those leave,
+            // and scales times 8 of the same
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t c = 2 * t + (i & 1) + 8 * (i >> 1);       // column of the operand
-                float v = 0.0f;
+            for (int j = 0; j < (N == 8 ? 4 : 2); ++j) {
+                float col[2];
 #pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const float up = __half2float(__float2half_rn(sums[n]));
-                    if (c == (uint32_t)n) v = up;
-                    if (c == (uint32_t)(N + n)) v = sums[n] - up;
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t c = 8 * j + 2 * t + i;
+                    float v = 0.0f;
+#pragma unroll
+                    for (int n = 0; n < N; ++n) {
+                        const float up = __half2float(__float2half_rn(sums[n])), low = sums[n] - up;
+                        if (c == (uint32_t)n) v = up;
+                        if (c == (uint32_t)(N + n)) v = low;
+                        if (c == (uint32_t)(2 * N + n)) v = 8.0f * up;
+                        if (c == (uint32_t)(3 * N + n)) v = 8.0f * low;
+                    }
+                    col[i] = v;
                 }
-                col[i] = v;
+                qz[j] = pack(col[0], col[1]);
             }
-            qz[0] = pack(col[0], col[1]);
-            qz[1] = pack(col[2], col[3]);
             const float f = scalbnf(p.scale * 1.4426950408889634f, e);
             f0 = __shfl_sync(0xFFFFFFFFu, f, 8 * t);
             f1 = __shfl_sync(0xFFFFFFFFu, f, 8 * t + 4);
         }
-        // rows 2 t and 2 t + 1 see the tokens before these
+        // rows 2 t and 2 t + 1 see the tokens before these, all rows those before `all`
         int32_t see0, see1, all;
         {
             const int32_t first = (int32_t)len - (int32_t)p.queries + 1;
-            see0 = first + (int32_t)((rt * kRows + 2 * t) / p.group);
-            see1 = first + (int32_t)((rt * kRows + 2 * t + 1) / p.group);
-            see0 = min(see0, (int32_t)len);
-            see1 = min(see1, (int32_t)len);
+            see0 = min(first + (int32_t)((rt * kRows + 2 * t) / p.group), (int32_t)len);
+            see1 = min(first + (int32_t)((rt * kRows + 2 * t + 1) / p.group), (int32_t)len);
             all = min(first + (int32_t)(rt * kRows / p.group), (int32_t)len);
         }
+        float* const mass = p.mass + ((uint64_t)bh * p.segs + rt) * p.row_subs * kRows + 2 * t;
 
         float o[2 * N][4], zsum[4] = {0, 0, 0, 0}, m0 = kNone, m1 = kNone, l0 = 0.0f, l1 = 0.0f;
         int ev = -14;                                              // the values' scales are divided by 2^ev
+        float vlimit = 0x1p-10f;                                   // 2^(ev + 4)
         uint32_t shrink = 0x74007400u;                             // 2^-ev, twice
 #pragma unroll
         for (int i = 0; i < 2 * N; ++i)
@@ -378,136 +426,168 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
             const uint32_t many = p.units ? min(take - done, kListCap) : take;
             if (p.units) {
                 __syncthreads();
-                list_tiles(p, bh, tiles, off + done, many, sm);
+                list_tiles(p, bh, len, off + done, many, sm);
             }
             const uint32_t mine = many > warp ? (many - warp + kWarps - 1) / kWarps : 0;      // this warp's tiles
             auto tile_no = [&](uint32_t k) { const uint32_t i = warp + k * kWarps; return p.units ? sm.list[i] : off + i; };
-            int32_t page = -1;
-            uint32_t in_page = 0, bad = 0;
+            uint32_t where = ~0u, bad = 0;
             auto issue = [&](uint32_t k) {
-                if (k < mine) {
-                    if (k % 32 == 0) {                             // the pages of the next 32 tiles, one a lane
-                        page = -1;
-                        if (k + lane < mine) {
-                            const uint32_t tile = tile_no(k + lane);
-                            page = __ldg(table + tile / p.page_tiles);
-                            in_page = tile % p.page_tiles;
-                        }
-                    }
-                    const int32_t pg = __shfl_sync(0xFFFFFFFFu, page, k % 32);
-                    const uint32_t ip = __shfl_sync(0xFFFFFFFFu, in_page, k % 32), stage = k % kStages;
-                    if (pg >= 0 && (uint32_t)pg < p.pages) {
-                        const uint8_t* from = p.cache + (((uint64_t)pg * p.heads + h) * p.page_tiles + ip) * L::kBytes;
-#pragma unroll
-                        for (uint32_t c = 0; c < L::kBytes / 16; c += 32)
-                            if (L::kBytes / 16 - c >= 32 || lane < L::kBytes / 16 - c)
-                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring_at + stage * L::kBytes + (c + lane) * 16),
-                                             "l"(from + (c + lane) * 16) : "memory");
-                        bad &= ~(1u << stage);
-                    } else {
-                        bad |= 1u << stage;
+                const uint32_t stage = k % kStages;
+                if (k % 32 == 0) {                                 // where the next 32 tiles lie, one a lane
+                    where = ~0u;
+                    if (k + lane < mine) {
+                        const uint32_t tile = tile_no(k + lane), page = tile / p.page_tiles;
+                        const uint32_t pg = (uint32_t)__ldg(table + page);
+                        if (pg < p.pages) where = (pg * p.heads + h) * p.page_tiles + (tile - page * p.page_tiles);
                     }
                 }
-                asm volatile("cp.async.commit_group;" ::: "memory");
+                const uint32_t at = __shfl_sync(0xFFFFFFFFu, where, k % 32);
+                if (at != ~0u) {
+                    const uint8_t* from = p.cache + (uint64_t)at * L::kBytes + lane * 16;
+                    const uint32_t to = ring_at + stage * L::kBytes + lane * 16;
+#pragma unroll
+                    for (uint32_t c = 0; c < L::kBytes / 16; c += 32)
+                        if (L::kBytes / 16 - c >= 32 || lane < L::kBytes / 16 - c)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + c * 16), "l"(from + c * 16) : "memory");
+                    bad &= ~(1u << stage);
+                } else {
+                    bad |= 1u << stage;                            // no tile, or in a page that is none
+                }
             };
 #pragma unroll 1
-            for (int k = 0; k < kStages - 1; ++k) issue(k);
+            for (int k = 0; k < kStages; k += 2) {
+                if (k < (int)mine) { issue(k); issue(k + 1); }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            }
 #pragma unroll 1
-            for (uint32_t k = 0; k < mine; ++k) {
-                __syncwarp();                                      // the stage written next was read by all lanes
-                issue(k + kStages - 1);
-                asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            for (uint32_t k = 0; k < mine; k += 2) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(kStages / 2 - 1) : "memory");
                 __syncwarp();
-                if ((bad >> (k % kStages)) & 1u) continue;         // a page that is none: its tokens are not read
-                const uint8_t* tile = ring + (k % kStages) * L::kBytes;
-                const uint32_t no = tile_no(k);
-                const int32_t base = (int32_t)(no * kTileTokens);
+                const uint32_t stage = k % kStages;
+                const uint8_t* const tile0 = ring + stage * L::kBytes;
+                const uint32_t none = bad >> stage & 3u;           // of the two tiles, those that are not there
+                const uint32_t no0 = tile_no(k), no1 = k + 1 < mine ? tile_no(k + 1) : no0;
 
                 // scores of tokens a and b for rows 2t and 2t + 1
-                float s[4] = {0, 0, 0, 0}, z[4] = {0, 0, 0, 0};
-                {
-                    uint32_t wa[N], wb[N];
-                    __half sa[N], sb[N];
+                float s[2][4];
 #pragma unroll
-                    for (int n = 0; n < N; n += N < 4 ? 2 : 4) {
-                        if constexpr (N < 4) {
-                            *reinterpret_cast<uint2*>(wa) = *reinterpret_cast<const uint2*>(tile + L::key_word(tok_a, t, 0));
-                            *reinterpret_cast<uint2*>(wb) = *reinterpret_cast<const uint2*>(tile + L::key_word(tok_b, t, 0));
-                        } else {
+                for (int u = 0; u < 2; ++u) {
+                    const uint8_t* tile = tile0 + u * L::kBytes;
+                    uint32_t wa[N], wb[N], sa[N / 2], sb[N / 2];
+                    float z[4], sum[4] = {0, 0, 0, 0};
+                    if constexpr (N == 2) {
+                        *reinterpret_cast<uint2*>(wa) = *reinterpret_cast<const uint2*>(tile + L::key_word(tok_a, t, 0));
+                        *reinterpret_cast<uint2*>(wb) = *reinterpret_cast<const uint2*>(tile + L::key_word(tok_b, t, 0));
+                        sa[0] = *reinterpret_cast<const uint32_t*>(tile + L::key_meta(tok_a, 0));
+                        sb[0] = *reinterpret_cast<const uint32_t*>(tile + L::key_meta(tok_b, 0));
+                    } else {
+#pragma unroll
+                        for (int n = 0; n < N; n += 4) {
                             *reinterpret_cast<uint4*>(wa + n) = *reinterpret_cast<const uint4*>(tile + L::key_word(tok_a, t, n));
                             *reinterpret_cast<uint4*>(wb + n) = *reinterpret_cast<const uint4*>(tile + L::key_word(tok_b, t, n));
+                            *reinterpret_cast<uint2*>(sa + n / 2) = *reinterpret_cast<const uint2*>(tile + L::key_meta(tok_a, n));
+                            *reinterpret_cast<uint2*>(sb + n / 2) = *reinterpret_cast<const uint2*>(tile + L::key_meta(tok_b, n));
                         }
                     }
-#pragma unroll
-                    for (int n = 0; n < N; n += 2) {
-                        *reinterpret_cast<uint32_t*>(sa + n) = *reinterpret_cast<const uint32_t*>(tile + L::key_meta(tok_a, n));
-                        *reinterpret_cast<uint32_t*>(sb + n) = *reinterpret_cast<const uint32_t*>(tile + L::key_meta(tok_b, n));
+                    {
+                        const uint8_t* meta = tile + L::kKeyZero + (2 * t % N) * 2;
+                        const uint32_t za = *reinterpret_cast<const uint32_t*>(meta + tok_a * 2 * N);
+                        const uint32_t zb = *reinterpret_cast<const uint32_t*>(meta + tok_b * 2 * N);
+                        if constexpr (N == 2) {
+                            mma(z, t < 2 ? za : sa[0], t < 2 ? zb : sb[0], 0u, 0u, qz[0], 0u, 0.0f, 0.0f, 0.0f, 0.0f);
+                        } else {
+                            const uint32_t ka = *reinterpret_cast<const uint32_t*>(meta + tok_a * 2 * N - (L::kKeyZero - L::kKeyScale));
+                            const uint32_t kb = *reinterpret_cast<const uint32_t*>(meta + tok_b * 2 * N - (L::kKeyZero - L::kKeyScale));
+                            if constexpr (N == 4) {
+                                mma(z, za, zb, ka, kb, qz[0], qz[1], 0.0f, 0.0f, 0.0f, 0.0f);
+                            } else {
+                                mma(z, za, zb, za, zb, qz[0], qz[1], 0.0f, 0.0f, 0.0f, 0.0f);
+                                mma(z, ka, kb, ka, kb, qz[2], qz[3]);
+                            }
+                        }
                     }
 #pragma unroll
                     for (int n = 0; n < N; ++n) {
-                        float acc[4] = {0, 0, 0, 0};
-                        mma(acc, wa[n] & 0x000F000Fu, wb[n] & 0x000F000Fu, wa[n] & 0x00F000F0u, wb[n] & 0x00F000F0u, qf[n][0], qf[n][1]);
+                        float acc[4];
+                        mma(acc, wa[n] * 64u & kTop, wb[n] * 64u & kTop, wa[n] * 4u & kTop, wb[n] * 4u & kTop, qf[n][0], qf[n][1],
+                            start0[n], start1[n], start0[n], start1[n]);
                         const uint32_t xa = wa[n] >> 8, xb = wb[n] >> 8;
-                        mma(acc, xa & 0x000F000Fu, xb & 0x000F000Fu, xa & 0x00F000F0u, xb & 0x00F000F0u, qf[n][2], qf[n][3]);
-                        const float fa = __half2float(sa[n]), fb = __half2float(sb[n]);
-                        s[0] = fmaf(fa, acc[0], s[0]);
-                        s[1] = fmaf(fa, acc[1], s[1]);
-                        s[2] = fmaf(fb, acc[2], s[2]);
-                        s[3] = fmaf(fb, acc[3], s[3]);
+                        mma(acc, xa * 64u & kTop, xb * 64u & kTop, xa * 4u & kTop, xb * 4u & kTop, qf[n][2], qf[n][3]);
+                        const float2 pa = __half22float2(half2_of(sa[n / 2])), pb = __half22float2(half2_of(sb[n / 2]));
+                        const float fa = n & 1 ? pa.y : pa.x, fb = n & 1 ? pb.y : pb.x;
+                        sum[0] = fmaf(fa, acc[0], sum[0]);
+                        sum[1] = fmaf(fa, acc[1], sum[1]);
+                        sum[2] = fmaf(fb, acc[2], sum[2]);
+                        sum[3] = fmaf(fb, acc[3], sum[3]);
                     }
-                    const uint32_t za = *reinterpret_cast<const uint32_t*>(tile + L::kKeyZero + tok_a * 2 * N + (2 * t % N) * 2);
-                    const uint32_t zb = *reinterpret_cast<const uint32_t*>(tile + L::kKeyZero + tok_b * 2 * N + (2 * t % N) * 2);
-                    const uint32_t zero = 0;
-                    if constexpr (N == 8) mma(z, za, zb, za, zb, qz[0], qz[1]);
-                    else mma(z, za, zb, zero, zero, qz[0], zero);
+                    s[u][0] = f0 * fmaf(sum[0], 0x1p18f, z[0]);
+                    s[u][1] = f1 * fmaf(sum[1], 0x1p18f, z[1]);
+                    s[u][2] = f0 * fmaf(sum[2], 0x1p18f, z[2]);
+                    s[u][3] = f1 * fmaf(sum[3], 0x1p18f, z[3]);
                 }
-                s[0] = f0 * fmaf(s[0], 16777216.0f, z[0]);
-                s[1] = f1 * fmaf(s[1], 16777216.0f, z[1]);
-                s[2] = f0 * fmaf(s[2], 16777216.0f, z[2]);
-                s[3] = f1 * fmaf(s[3], 16777216.0f, z[3]);
 
                 // scales and zeros of the values of tokens 4t .. 4t + 3
-                uint32_t vs[N][2], vz0 = 0, vz1 = 0;
+                uint32_t vs[2][N][2], vz[2][2] = {{0, 0}, {0, 0}};
 #pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const uint2 x = *reinterpret_cast<const uint2*>(tile + L::value_meta(4 * t, n));
-                    vs[n][0] = x.x;
-                    vs[n][1] = x.y;
-                }
-                if (g < N) {
-                    const uint2 x = *reinterpret_cast<const uint2*>(tile + L::value_meta(4 * t, g) + (L::kValueZero - L::kValueScale));
-                    vz0 = x.x;
-                    vz1 = x.y;
+                for (int u = 0; u < 2; ++u) {
+                    const uint8_t* tile = tile0 + u * L::kBytes;
+#pragma unroll
+                    for (int n = 0; n < N; n += 2) {
+                        const uint4 x = *reinterpret_cast<const uint4*>(tile + L::value_meta(4 * t, n));
+                        vs[u][n][0] = x.x;
+                        vs[u][n][1] = x.y;
+                        vs[u][n + 1][0] = x.z;
+                        vs[u][n + 1][1] = x.w;
+                    }
+                    if (g < N) {
+                        const uint2 x = *reinterpret_cast<const uint2*>(tile + L::value_meta(4 * t, g) + (L::kValueZero - L::kValueScale));
+                        vz[u][0] = x.x;
+                        vz[u][1] = x.y;
+                    }
                 }
                 const bool parts = p.units && p.unit < kTileTokens;
-                if (parts || base + (int32_t)kTileTokens > all) {
-                    // some token is not seen by some row. What lies in the cache behind the last token may be anything, also
-                    // infinite, so its scales and zeros are cleared too
-                    uint32_t bits = ~0u;
-                    if (parts) bits = bits_at(p, (uint64_t)bh * p.row_units + base / (int32_t)p.unit);
-                    auto seen = [&](uint32_t i) { return base + (int32_t)i < (int32_t)len && (!parts || ((bits >> (i / p.unit)) & 1u)); };
-                    const bool a = seen(tok_a), bb = seen(tok_b);
-                    if (!a || base + (int32_t)tok_a >= see0) s[0] = -INFINITY;
-                    if (!a || base + (int32_t)tok_a >= see1) s[1] = -INFINITY;
-                    if (!bb || base + (int32_t)tok_b >= see0) s[2] = -INFINITY;
-                    if (!bb || base + (int32_t)tok_b >= see1) s[3] = -INFINITY;
-                    const uint32_t k0 = (seen(4 * t) ? 0xFFFFu : 0u) | (seen(4 * t + 1) ? 0xFFFF0000u : 0u);
-                    const uint32_t k1 = (seen(4 * t + 2) ? 0xFFFFu : 0u) | (seen(4 * t + 3) ? 0xFFFF0000u : 0u);
+                if (none || parts || (int32_t)(max(no0, no1) * kTileTokens + kTileTokens) > all) {
+                    // Some token is not seen by some row. What lies in the cache behind the last token, or in the ring where there was
+                    // no tile, may be anything, also infinite, so its scales and zeros are cleared too.
 #pragma unroll
-                    for (int n = 0; n < N; ++n) { vs[n][0] &= k0; vs[n][1] &= k1; }
-                    vz0 &= k0;
-                    vz1 &= k1;
+                    for (int u = 0; u < 2; ++u) {
+                        const int32_t base = (int32_t)((u ? no1 : no0) * kTileTokens);
+                        uint32_t bits = 0xFFFFu;                   // of the tile's tokens
+                        if (parts) {
+                            const uint32_t x = bits_at(p, (uint64_t)bh * p.row_units + (base >> p.unit_log2));
+                            bits = 0;
+                            for (uint32_t i = 0; i < kTileTokens; ++i) bits |= (x >> (i >> p.unit_log2) & 1u) << i;
+                        }
+                        const int32_t left = (int32_t)len - base;
+                        if (left < (int32_t)kTileTokens) bits &= left > 0 ? (1u << left) - 1u : 0u;
+                        if (none >> u & 1u) bits = 0;
+                        const bool a = bits >> tok_a & 1u, c = bits >> tok_b & 1u;
+                        if (!a || base + (int32_t)tok_a >= see0) s[u][0] = -INFINITY;
+                        if (!a || base + (int32_t)tok_a >= see1) s[u][1] = -INFINITY;
+                        if (!c || base + (int32_t)tok_b >= see0) s[u][2] = -INFINITY;
+                        if (!c || base + (int32_t)tok_b >= see1) s[u][3] = -INFINITY;
+                        const uint32_t four = bits >> (4 * t);
+                        const uint32_t k0 = (four & 1u ? 0xFFFFu : 0u) | (four & 2u ? 0xFFFF0000u : 0u);
+                        const uint32_t k1 = (four & 4u ? 0xFFFFu : 0u) | (four & 8u ? 0xFFFF0000u : 0u);
+#pragma unroll
+                        for (int n = 0; n < N; ++n) { vs[u][n][0] &= k0; vs[u][n][1] &= k1; }
+                        vz[u][0] &= k0;
+                        vz[u][1] &= k1;
+                    }
                 }
                 // has a score passed the maximum by more than the slack, or a scale its power of two?
-                uint32_t top = __half2_raw(half2_of(vs[0][0])).x;
+                float vmost;
                 {
-                    __half2 v = __hmax2(half2_of(vs[0][0]), half2_of(vs[0][1]));
+                    __half2 v = __hmax2(half2_of(vs[0][0][0]), half2_of(vs[0][0][1]));
+                    v = __hmax2(v, __hmax2(half2_of(vs[1][0][0]), half2_of(vs[1][0][1])));
 #pragma unroll
-                    for (int n = 1; n < N; ++n) v = __hmax2(v, __hmax2(half2_of(vs[n][0]), half2_of(vs[n][1])));
-                    top = __half_as_ushort(__hmax(__low2half(v), __high2half(v)));
+                    for (int n = 1; n < N; ++n) {
+                        v = __hmax2(v, __hmax2(half2_of(vs[0][n][0]), half2_of(vs[0][n][1])));
+                        v = __hmax2(v, __hmax2(half2_of(vs[1][n][0]), half2_of(vs[1][n][1])));
+                    }
+                    vmost = __half2float(__hmax(__low2half(v), __high2half(v)));
                 }
-                const float t0 = fmaxf(s[0], s[2]), t1 = fmaxf(s[1], s[3]), vmost = __half2float(__ushort_as_half((unsigned short)top));
-                const float vlimit = exp2f((float)(ev + 4));
+                const float t0 = fmaxf(fmaxf(s[0][0], s[0][2]), fmaxf(s[1][0], s[1][2])), t1 = fmaxf(fmaxf(s[0][1], s[0][3]), fmaxf(s[1][1], s[1][3]));
                 if (__any_sync(0xFFFFFFFFu, t0 > m0 + kSlack || t1 > m1 + kSlack || vmost > vlimit)) {
                     float n0 = t0, n1 = t1, nv = vmost;
 #pragma unroll
@@ -524,6 +604,7 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                     m0 = n0;
                     m1 = n1;
                     ev = en;
+                    vlimit = exp2f((float)(ev + 4));
                     shrink = bits_of(__float2half2_rn(exp2f((float)-ev)));
                     l0 *= c0;
                     l1 *= c1;
@@ -538,67 +619,110 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                     }
                 }
                 const float d0 = m0 - kLift, d1 = m1 - kLift;
-                const float e0 = exp2_fast(s[0] - d0), e1 = exp2_fast(s[1] - d1), e2 = exp2_fast(s[2] - d0), e3 = exp2_fast(s[3] - d1);
-                l0 += e0 + e2;
-                l1 += e1 + e3;
-                const uint32_t p0 = transposed(pack(e0, e1)), p1 = transposed(pack(e2, e3));
+                float e[2][4];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    e[u][0] = exp2_fast(s[u][0] - d0);
+                    e[u][1] = exp2_fast(s[u][1] - d1);
+                    e[u][2] = exp2_fast(s[u][2] - d0);
+                    e[u][3] = exp2_fast(s[u][3] - d1);
+                }
+                float a0 = e[0][0] + e[0][2], a1 = e[0][1] + e[0][3], b0 = e[1][0] + e[1][2], b1 = e[1][1] + e[1][3];
+                l0 += a0 + b0;
+                l1 += a1 + b1;
 
                 // what each block of `sub` tokens received, as log2
-                if (p.sub) {
-                    float2* mass = reinterpret_cast<float2*>(p.mass) +
-                                   (((uint64_t)bh * p.segs + rt) * p.row_subs + (uint64_t)base / p.sub) * (kRows / 2) + t;
-                    if (p.sub == 1) {
-                        mass[tok_a * (kRows / 2)] = make_float2(s[0], s[1]);
-                        mass[tok_b * (kRows / 2)] = make_float2(s[2], s[3]);
-                    } else if (p.sub == 2) {
-                        float a0 = e0 + __shfl_xor_sync(0xFFFFFFFFu, e0, 4), a1 = e1 + __shfl_xor_sync(0xFFFFFFFFu, e1, 4);
-                        float b0 = e2 + __shfl_xor_sync(0xFFFFFFFFu, e2, 4), b1 = e3 + __shfl_xor_sync(0xFFFFFFFFu, e3, 4);
-                        if (!(g & 1)) {
-                            mass[g * (kRows / 2)] = make_float2(d0 + log2_fast(a0), d1 + log2_fast(a1));
-                            mass[(g + 1) * (kRows / 2)] = make_float2(d0 + log2_fast(b0), d1 + log2_fast(b1));
+                if (p.sub == kTileTokens) {
+                    // four sums over the eight rows: after two exchanges a lane holds one of them, of tile (lane / 16) and row 2 t + lane / 8 % 2
+                    const bool up = lane & 16, odd = lane & 8;
+                    float x0 = up ? b0 : a0, x1 = up ? b1 : a1;
+                    x0 += __shfl_xor_sync(0xFFFFFFFFu, up ? a0 : b0, 16);
+                    x1 += __shfl_xor_sync(0xFFFFFFFFu, up ? a1 : b1, 16);
+                    float x = (odd ? x1 : x0) + __shfl_xor_sync(0xFFFFFFFFu, odd ? x0 : x1, 8);
+                    x += __shfl_xor_sync(0xFFFFFFFFu, x, 4);
+                    if (!(lane & 4) && !(none >> (up ? 1 : 0) & 1u))
+                        mass[(uint64_t)(up ? no1 : no0) * kRows + (odd ? 1 : 0)] = (odd ? d1 : d0) + log2_fast(x);
+                } else if (p.sub) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const bool there = !(none >> u & 1u);
+                        float2* to = reinterpret_cast<float2*>(mass) + (uint64_t)((u ? no1 : no0) << (4 - p.unit_log2)) * (kRows / 2);
+                        if (p.sub == 1) {
+                            if (there) {
+                                to[tok_a * (kRows / 2)] = make_float2(s[u][0], s[u][1]);
+                                to[tok_b * (kRows / 2)] = make_float2(s[u][2], s[u][3]);
+                            }
+                        } else if (p.sub == 2) {
+                            float x[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) x[i] = e[u][i] + __shfl_xor_sync(0xFFFFFFFFu, e[u][i], 4);
+                            if (there && !(g & 1)) {
+                                to[g * (kRows / 2)] = make_float2(d0 + log2_fast(x[0]), d1 + log2_fast(x[1]));
+                                to[(g + 1) * (kRows / 2)] = make_float2(d0 + log2_fast(x[2]), d1 + log2_fast(x[3]));
+                            }
+                        } else {                                    // 4 or 8 tokens: rows 2 j, 2 j + 1, or four of them
+                            float x0 = u ? b0 : a0, x1 = u ? b1 : a1;
+                            x0 += __shfl_xor_sync(0xFFFFFFFFu, x0, 4);
+                            x1 += __shfl_xor_sync(0xFFFFFFFFu, x1, 4);
+                            const float y0 = __shfl_xor_sync(0xFFFFFFFFu, x0, 8), y1 = __shfl_xor_sync(0xFFFFFFFFu, x1, 8);
+                            if (p.sub == 8) { x0 += y0; x1 += y1; }
+                            if (there && !(g & (p.sub / 2 - 1))) to[g / (p.sub / 2) * (kRows / 2)] = make_float2(d0 + log2_fast(x0), d1 + log2_fast(x1));
                         }
-                    } else {
-                        float a0 = e0 + e2, a1 = e1 + e3;
-                        for (uint32_t d = 4; d < 2 * p.sub; d <<= 1) {
-                            a0 += __shfl_xor_sync(0xFFFFFFFFu, a0, d);
-                            a1 += __shfl_xor_sync(0xFFFFFFFFu, a1, d);
-                        }
-                        const uint32_t same = p.sub / 2;                   // rows g of one block
-                        if (g % same == 0) mass[g / same * (kRows / 2)] = make_float2(d0 + log2_fast(a0), d1 + log2_fast(a1));
                     }
                 }
 
                 // values: dims 32 n + 4 g + {0, 2} in rows g, {1, 3} in rows g + 8 (16 times too large)
-                const uint32_t zero = 0;
-                mma(zsum, vz0, zero, vz1, zero, p0, p1);
-                uint32_t x[N], y[N];
 #pragma unroll
-                for (int n = 0; n < N; n += N < 4 ? 2 : 4) {
-                    if constexpr (N < 4) {
+                for (int u = 0; u < 2; ++u) {
+                    const uint8_t* tile = tile0 + u * L::kBytes;
+                    const uint32_t h0 = pack(e[u][0], e[u][1]), h1 = pack(e[u][2], e[u][3]), p0 = transposed(h0), p1 = transposed(h1);
+                    uint32_t r0 = 0, r1 = 0;                       // what the fp16 weights leave
+                    mma(zsum, vz[u][0], 0u, vz[u][1], 0u, p0, p1);
+                    if constexpr (HALF) {
+                        const float2 q0 = __half22float2(half2_of(h0)), q1 = __half22float2(half2_of(h1));
+                        r0 = transposed(pack(e[u][0] - q0.x, e[u][1] - q0.y));
+                        r1 = transposed(pack(e[u][2] - q1.x, e[u][3] - q1.y));
+                        mma(zsum, vz[u][0], 0u, vz[u][1], 0u, r0, r1);
+                    }
+                    uint32_t x[N], y[N];
+                    if constexpr (N == 2) {
                         *reinterpret_cast<uint2*>(x) = *reinterpret_cast<const uint2*>(tile + L::value_half(4 * t, g, 0));
                         *reinterpret_cast<uint2*>(y) = *reinterpret_cast<const uint2*>(tile + L::value_half(4 * t + 2, g, 0));
                     } else {
-                        *reinterpret_cast<uint4*>(x + n) = *reinterpret_cast<const uint4*>(tile + L::value_half(4 * t, g, n));
-                        *reinterpret_cast<uint4*>(y + n) = *reinterpret_cast<const uint4*>(tile + L::value_half(4 * t + 2, g, n));
+#pragma unroll
+                        for (int n = 0; n < N; n += 4) {
+                            *reinterpret_cast<uint4*>(x + n) = *reinterpret_cast<const uint4*>(tile + L::value_half(4 * t, g, n));
+                            *reinterpret_cast<uint4*>(y + n) = *reinterpret_cast<const uint4*>(tile + L::value_half(4 * t + 2, g, n));
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < N; ++n) {
+                        const uint32_t v0 = times(vs[u][n][0], shrink), v1 = times(vs[u][n][1], shrink), w0 = times(p0, v0), w1 = times(p1, v1);
+                        const uint32_t a[4] = {x[n] & 0x000F000Fu, x[n] & 0x00F000F0u, y[n] & 0x000F000Fu, y[n] & 0x00F000F0u};
+                        const uint32_t xx = x[n] >> 8, yy = y[n] >> 8;
+                        const uint32_t c[4] = {xx & 0x000F000Fu, xx & 0x00F000F0u, yy & 0x000F000Fu, yy & 0x00F000F0u};
+                        mma(o[2 * n], a[0], a[1], a[2], a[3], w0, w1);
+                        mma(o[2 * n + 1], c[0], c[1], c[2], c[3], w0, w1);
+                        if constexpr (HALF) {
+                            const uint32_t low0 = bits_of(__hfma2(half2_of(r0), half2_of(v0), __hfma2(half2_of(p0), half2_of(v0), __hneg2(half2_of(w0)))));
+                            const uint32_t low1 = bits_of(__hfma2(half2_of(r1), half2_of(v1), __hfma2(half2_of(p1), half2_of(v1), __hneg2(half2_of(w1)))));
+                            mma(o[2 * n], a[0], a[1], a[2], a[3], low0, low1);
+                            mma(o[2 * n + 1], c[0], c[1], c[2], c[3], low0, low1);
+                        }
                     }
                 }
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const uint32_t b0 = times(p0, times(vs[n][0], shrink)), b1 = times(p1, times(vs[n][1], shrink));
-                    mma(o[2 * n], x[n] & 0x000F000Fu, x[n] & 0x00F000F0u, y[n] & 0x000F000Fu, y[n] & 0x00F000F0u, b0, b1);
-                    const uint32_t xx = x[n] >> 8, yy = y[n] >> 8;
-                    mma(o[2 * n + 1], xx & 0x000F000Fu, xx & 0x00F000F0u, yy & 0x000F000Fu, yy & 0x00F000F0u, b0, b1);
-                }
+                __syncwarp();                                      // all lanes have read the two stages
+                if (k + kStages < mine) { issue(k + kStages); issue(k + kStages + 1); }
+                asm volatile("cp.async.commit_group;" ::: "memory");
             }
             asm volatile("cp.async.wait_group 0;" ::: "memory");
             done += many;
         }
 
-        // join the warps
+        // join the warps; a row's 16-byte pieces are shuffled by its number, so that eight lanes write to eight banks
         l0 = over_rows(l0);
         l1 = over_rows(l1);
         __syncthreads();                                           // every warp is done with its ring
-        float* join = reinterpret_cast<float*>(ring_all);
         const float up = exp2f((float)(ev + 24)), up16 = exp2f((float)(ev + 20));
 #pragma unroll
         for (int n = 0; n < N; ++n) {
@@ -612,9 +736,9 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
             c.y = fmaf(o[2 * n][3], up16, z1);
             c.z = fmaf(o[2 * n + 1][1], up, z1);
             c.w = fmaf(o[2 * n + 1][3], up16, z1);
-            float* to = join + (warp * kRows + 2 * t) * L::D + n * 32 + g * 4;
-            *reinterpret_cast<float4*>(to) = a;
-            *reinterpret_cast<float4*>(to + L::D) = c;
+            float4* to = reinterpret_cast<float4*>(ring_all) + (warp * kRows + 2 * t) * (L::D / 4) + ((n * 8 + g) ^ (2 * t));
+            to[0] = a;
+            to[L::D / 4] = c;
         }
         if (g == 0) {
             sm.ml[warp][2 * t] = make_float2(m0 - kLift, l0);
@@ -623,27 +747,39 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
         __syncthreads();
         const bool whole = take == count;
         const uint64_t slot = (uint64_t)blockIdx.x + seg;
-        for (uint32_t i = tid; i < kRows * L::D; i += kThreads) {
-            const uint32_t r = i / L::D, d = i % L::D, row = rt * kRows + r;
-            if (row >= p.rows) continue;
-            float m = sm.ml[0][r].x;
+        auto place = [&](uint32_t row) {
+            const uint32_t query = row / p.group;
+            return ((uint64_t)b * p.queries + query) * (p.heads * p.group) + h * p.group + (row - query * p.group);
+        };
+        if (tid < kRows) {
+            const uint32_t r = tid, row = rt * kRows + r;
+            float m = sm.ml[0][r].x, l = 0.0f;
 #pragma unroll
             for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sm.ml[w][r].x);
-            float sum = 0.0f, l = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) l = fmaf(sm.ml[w][r].y, exp2_fast(sm.ml[w][r].x - m), l);
+            const float by = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) sm.share[w][r] = exp2_fast(sm.ml[w][r].x - m) * by;
+            p.ml[slot * kRows + r] = make_float2(m, l);
+            if (whole && p.lse && row < p.rows) p.lse[place(row)] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        }
+        __syncthreads();
+        for (uint32_t i = tid; i < kRows * L::D / 4; i += kThreads) {
+            const uint32_t r = i / (L::D / 4), c = i % (L::D / 4), row = rt * kRows + r;
+            if (row >= p.rows) continue;
+            float4 sum = make_float4(0, 0, 0, 0);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                const float c = exp2_fast(sm.ml[w][r].x - m);
-                l = fmaf(sm.ml[w][r].y, c, l);
-                sum = fmaf(join[(w * kRows + r) * L::D + d], c, sum);
+                const float4 x = reinterpret_cast<const float4*>(ring_all)[(w * kRows + r) * (L::D / 4) + (c ^ (r & 6))];
+                const float k = sm.share[w][r];
+                sum.x = fmaf(x.x, k, sum.x);
+                sum.y = fmaf(x.y, k, sum.y);
+                sum.z = fmaf(x.z, k, sum.z);
+                sum.w = fmaf(x.w, k, sum.w);
             }
-            if (d == 0) p.ml[slot * kRows + r] = make_float2(m, l);
-            if (whole) {
-                const uint64_t at = ((uint64_t)b * p.queries + row / p.group) * (p.heads * p.group) + h * p.group + row % p.group;
-                store_out(p, at * L::D + d, l == 0.0f ? 0.0f : sum / l);
-                if (d == 0 && p.lse) p.lse[at] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-            } else {
-                p.part[(slot * kRows + r) * L::D + d] = sum;
-            }
+            if (whole) reinterpret_cast<uint2*>(p.out)[place(row) * (L::D / 4) + c] = make_uint2(out_pair<HALF>(sum.x, sum.y), out_pair<HALF>(sum.z, sum.w));
+            else reinterpret_cast<float4*>(p.part)[(slot * kRows + r) * (L::D / 4) + c] = sum;
         }
         __syncthreads();                                           // the ring is free again
         todo -= take;
@@ -654,72 +790,95 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
 
 // Joins the parts of segments that several CTAs worked on, and turns the blocks' masses into weights.
 // Blocks 0 .. batch * heads * rows - 1: one query row each. The rest: kThreads units of a (sequence, kv-head) each.
-template <int N>
+template <int N, bool HALF>
 __global__ void __launch_bounds__(kThreads) join_kernel(const AttendK p)
 {
-    constexpr uint32_t D = 32 * N;
+    constexpr uint32_t D = 32 * N, kPart = kThreads / (D / 4);     // threads for four dims each share the CTAs' parts
     __shared__ LineSmem sm;
     __shared__ float lse2[64];
     __shared__ float2 ml[kThreads];
-    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32, per = line_per(p);
-    const uint64_t out_blocks = (uint64_t)p.batch * p.heads * p.rows;
+    __shared__ float4 sums[kThreads];
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32, per = line_per(p);
+    const uint32_t out_blocks = p.batch * p.heads * p.rows;
     const bool is_out = blockIdx.x < out_blocks;
     const uint32_t chunks = p.weights ? (p.row_units + kThreads - 1) / kThreads : 1;
-    const uint32_t bh = is_out ? blockIdx.x / p.rows : (uint32_t)((blockIdx.x - out_blocks) / chunks);
-    const uint32_t b = bh / p.heads, h = bh % p.heads;
+    const uint32_t bh = is_out ? blockIdx.x / p.rows : (blockIdx.x - out_blocks) / chunks;
+    const uint32_t b = bh / p.heads, h = bh - b * p.heads;
     const uint32_t entry0 = p.units ? bh : b;
     uint32_t entry = entry0;
+    wait_for_previous();
     const Line line = find_in_line(p, ~0u, entry, sm);
     const uint32_t count = entry_count(p, entry0);
     // the CTAs that worked on segment seg: first and last
-    auto cta_of = [&](uint64_t tile) { return (uint32_t)(((tile + 1) * line.active - 1) / line.total); };
-    auto first_tile = [&](uint32_t seg) { return line.before + (uint64_t)(seg - entry0 * per) * count; };
+    auto first_tile = [&](uint32_t seg) { return line.before + (seg - entry0 * per) * count; };
     if (is_out) {
-        const uint32_t row = blockIdx.x % p.rows, rt = row / kRows, r = row % kRows, seg = bh * p.segs + rt;
-        const uint64_t at = ((uint64_t)b * p.queries + row / p.group) * (p.heads * p.group) + h * p.group + row % p.group;
+        const uint32_t row = blockIdx.x - bh * p.rows, rt = row / kRows, r = row % kRows, seg = bh * p.segs + rt, query = row / p.group;
+        const uint64_t at = ((uint64_t)b * p.queries + query) * (p.heads * p.group) + h * p.group + (row - query * p.group);
         if (!count) {
-            for (uint32_t d = tid; d < D; d += kThreads) store_out(p, at * D + d, 0.0f);
+            if (tid < D / 4) reinterpret_cast<uint2*>(p.out)[at * (D / 4) + tid] = make_uint2(0u, 0u);
             if (tid == 0 && p.lse) p.lse[at] = -INFINITY;
             return;
         }
-        const uint32_t c0 = cta_of(first_tile(seg)), c1 = cta_of(first_tile(seg) + count - 1);
+        const uint32_t c0 = first_tile(seg) / line.chunk, c1 = (first_tile(seg) + count - 1) / line.chunk;
         if (c0 == c1) return;                                      // written by its one CTA
-        float m = kNone, l = 0.0f, sum = 0.0f;
+        const uint32_t d4 = tid % (D / 4), mine = tid / (D / 4);
+        float m = kNone, l = 0.0f;
+        float4 sum = make_float4(0, 0, 0, 0);
         for (uint32_t c = c0; c <= c1; c += kThreads) {
-            __syncthreads();
-            if (c + tid <= c1) ml[tid] = p.ml[((uint64_t)c + tid + seg) * kRows + r];
-            __syncthreads();
             const uint32_t many = min(c1 - c + 1, kThreads);
+            __syncthreads();
+            if (tid < many) ml[tid] = p.ml[((uint64_t)c + tid + seg) * kRows + r];
+            __syncthreads();
             float up = m;
             for (uint32_t i = 0; i < many; ++i) up = fmaxf(up, ml[i].x);
             const float old = exp2_fast(m - up);
             m = up;
             l *= old;
-            sum *= old;
-            for (uint32_t i = 0; i < many; ++i) {
+            sum.x *= old;
+            sum.y *= old;
+            sum.z *= old;
+            sum.w *= old;
+            for (uint32_t i = 0; i < many; ++i) l = fmaf(ml[i].y, exp2_fast(ml[i].x - m), l);
+#pragma unroll 4
+            for (uint32_t i = mine; i < many; i += kPart) {
                 const float k = exp2_fast(ml[i].x - m);
-                l = fmaf(ml[i].y, k, l);
-                if (tid < D) sum = fmaf(p.part[(((uint64_t)c + i + seg) * kRows + r) * D + tid], k, sum);
+                const float4 x = reinterpret_cast<const float4*>(p.part)[(((uint64_t)c + i + seg) * kRows + r) * (D / 4) + d4];
+                sum.x = fmaf(x.x, k, sum.x);
+                sum.y = fmaf(x.y, k, sum.y);
+                sum.z = fmaf(x.z, k, sum.z);
+                sum.w = fmaf(x.w, k, sum.w);
             }
         }
-        if (tid < D) store_out(p, at * D + tid, l == 0.0f ? 0.0f : sum / l);
-        if (tid == 0 && p.lse) p.lse[at] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        sums[tid] = sum;
+        __syncthreads();
+        if (tid < D / 4) {
+            for (uint32_t i = 1; i < kPart; ++i) {
+                const float4 x = sums[i * (D / 4) + tid];
+                sum.x += x.x;
+                sum.y += x.y;
+                sum.z += x.z;
+                sum.w += x.w;
+            }
+            const float by = l == 0.0f ? 0.0f : 1.0f / l;
+            reinterpret_cast<uint2*>(p.out)[at * (D / 4) + tid] = make_uint2(out_pair<HALF>(sum.x * by, sum.y * by), out_pair<HALF>(sum.z * by, sum.w * by));
+            if (tid == 0 && p.lse) p.lse[at] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        }
         return;
     }
-    const uint32_t unit = (uint32_t)((blockIdx.x - out_blocks) % chunks) * kThreads + tid;
+    const uint32_t unit = (blockIdx.x - out_blocks - bh * chunks) * kThreads + tid;
     const uint32_t len = length_of(p, b);
     const uint64_t base = (uint64_t)unit * p.unit;
     bool read = unit < p.row_units && base < len && count;
     if (read && p.units) read = bits_at(p, (uint64_t)bh * p.row_units + unit) & 1u;
     float got = 0.0f;
     for (uint32_t row0 = 0; row0 < p.rows; row0 += 64) {           // rows in turns of 64
-        const uint32_t rows = min(p.rows - row0, 64u);
+        const uint32_t rows = min(p.rows - row0, 64u), padded = (rows + kRows - 1) / kRows * kRows;
         __syncthreads();
-        for (uint32_t i = warp; i < rows; i += kWarps) {           // a warp joins a row's sums
+        for (uint32_t i = warp; i < padded; i += kWarps) {         // a warp joins a row's sums
             float m = kNone, l = 0.0f;
-            if (count) {
+            if (count && i < rows) {
                 const uint32_t seg = bh * p.segs + (row0 + i) / kRows, r = (row0 + i) % kRows;
-                const uint32_t c0 = cta_of(first_tile(seg)), c1 = cta_of(first_tile(seg) + count - 1);
+                const uint32_t c0 = first_tile(seg) / line.chunk, c1 = (first_tile(seg) + count - 1) / line.chunk;
                 for (uint32_t c = c0 + lane; c <= c1; c += 32) {
                     const float2 x = p.ml[((uint64_t)c + seg) * kRows + r];
                     const float up = fmaxf(m, x.x);
@@ -743,8 +902,12 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttendK p)
             const uint32_t tile = (uint32_t)(i / kTileTokens);
             const int32_t page = __ldg(p.table + (uint64_t)b * p.table_pages + tile / p.page_tiles);
             if (page < 0 || (uint32_t)page >= p.pages) continue;
-            for (uint32_t r = 0; r < rows; ++r)
-                got += exp2_fast(p.mass[(((uint64_t)bh * p.segs + (row0 + r) / kRows) * p.row_subs + i / p.sub) * kRows + (row0 + r) % kRows] - lse2[r]);
+            for (uint32_t r = 0; r < rows; r += kRows) {           // a segment's rows lie together; rows that are none have 0
+                const float4* x = reinterpret_cast<const float4*>(p.mass + (((uint64_t)bh * p.segs + (row0 + r) / kRows) * p.row_subs + (i >> (p.unit_log2 < 4 ? p.unit_log2 : 4))) * kRows);
+                const float4 lo = x[0], hi = x[1];
+                got += exp2_fast(lo.x - lse2[r]) + exp2_fast(lo.y - lse2[r + 1]) + exp2_fast(lo.z - lse2[r + 2]) + exp2_fast(lo.w - lse2[r + 3]) +
+                       exp2_fast(hi.x - lse2[r + 4]) + exp2_fast(hi.y - lse2[r + 5]) + exp2_fast(hi.z - lse2[r + 6]) + exp2_fast(hi.w - lse2[r + 7]);
+            }
         }
     }
     if (unit < p.row_units) p.weights[(uint64_t)bh * p.row_units + unit] = got;
@@ -786,25 +949,40 @@ int check_attend(const kvp_attend_params* a)
     const uint64_t rows = (uint64_t)a->queries * a->group, bh = (uint64_t)a->batch * a->cache.kv_heads;
     const uint64_t tokens = (uint64_t)a->table_pages * a->cache.page_tokens;
     if (rows > 4096 || a->queries > 1024 || a->batch >= (1u << 24) || bh >= (1u << 24) || tokens >= (1ull << 31)) return KVP_ERR_RANGE;
+    // tiles of the line and of the cache are counted in 32 bits
+    if (bh * ((rows + kRows - 1) / kRows) * (tokens / kTileTokens) >= (1ull << 32) - (1u << 20) || (uint64_t)a->cache.pages * a->cache.kv_heads * (a->cache.page_tokens / kTileTokens) >= (1ull << 32) - 1) return KVP_ERR_RANGE;
     if (bh * rows >= (1ull << 30) || bh * ((tokens / u + kThreads - 1) / kThreads) >= (1ull << 30)) return KVP_ERR_RANGE;
     return KVP_OK;
 }
 
-template <int N>
+// `chained`: behind another kernel of the same call, whose end it waits for by itself
+template <typename... A>
+int launch(void (*kernel)(A...), uint32_t grid, uint32_t smem, bool chained, cudaStream_t st, const AttendK& k)
+{
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(grid);
+    c.blockDim = dim3(kThreads);
+    c.dynamicSmemBytes = smem;
+    c.stream = st;
+    cudaLaunchAttribute a;
+    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a.val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = &a;
+    c.numAttrs = chained ? 1 : 0;
+    KVP_CUDA(cudaLaunchKernelEx(&c, kernel, k));
+    return KVP_OK;
+}
+
+template <int N, bool HALF>
 int launch_attend(const AttendK& k, cudaStream_t st)
 {
     const uint32_t smem = Shape<N>::kSmem;
-    KVP_CUDA(cudaFuncSetAttribute(attend_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    if (k.units) {
-        count_kernel<<<(k.batch * k.heads + kWarps - 1) / kWarps, kThreads, 0, st>>>(k);
-        KVP_CUDA(cudaGetLastError());
-    }
-    attend_kernel<N><<<k.ctas, kThreads, smem, st>>>(k);
-    KVP_CUDA(cudaGetLastError());
+    KVP_CUDA(cudaFuncSetAttribute(attend_kernel<N, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    int rc = k.units ? launch(count_kernel, k.batch * k.heads, 0, false, st, k) : KVP_OK;
+    if (!rc) rc = launch(attend_kernel<N, HALF>, k.ctas, smem, k.units != nullptr, st, k);
     const uint64_t blocks = (uint64_t)k.batch * k.heads * (k.rows + (k.weights ? (k.row_units + kThreads - 1) / kThreads : 0));
-    join_kernel<N><<<(uint32_t)blocks, kThreads, 0, st>>>(k);
-    KVP_CUDA(cudaGetLastError());
-    return KVP_OK;
+    if (!rc) rc = launch(join_kernel<N, HALF>, (uint32_t)blocks, 0, true, st, k);
+    return rc;
 }
 
 }  // namespace
@@ -851,12 +1029,20 @@ extern "C" int kvp_attend(const kvp_attend_params* a, const void* q, const void*
     k.sub = weights ? sub : 0;
     k.ctas = w.ctas;
     k.least = kWarps;
+    k.unit_log2 = k.unit == 1 ? 0 : k.unit == 2 ? 1 : k.unit == 4 ? 2 : k.unit == 8 ? 3 : 4;
     k.scale = a->scale;
-    k.bf16 = a->dtype == KVP_BF16;
+    k.q_aligned = ((uint64_t)(uintptr_t)q | (uint64_t)(a->q_batch_stride * 2) | (uint64_t)(a->q_query_stride * 2) | (uint64_t)(a->q_head_stride * 2)) % 16 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a->dtype == KVP_F16) {
+        switch (a->cache.head_dim) {
+            case 64: return launch_attend<2, true>(k, st);
+            case 128: return launch_attend<4, true>(k, st);
+            default: return launch_attend<8, true>(k, st);
+        }
+    }
     switch (a->cache.head_dim) {
-        case 64: return launch_attend<2>(k, st);
-        case 128: return launch_attend<4>(k, st);
-        default: return launch_attend<8>(k, st);
+        case 64: return launch_attend<2, false>(k, st);
+        case 128: return launch_attend<4, false>(k, st);
+        default: return launch_attend<8, false>(k, st);
     }
 }
