@@ -37,6 +37,22 @@ constexpr uint32_t kTop = 0x03C003C0u;        // the upper four bits of two fp16
 constexpr float kNone = -3e38f;               // maximum of nothing
 constexpr float kLift = 3.0f, kSlack = 8.0f;  // weights are at most 2^(kLift + kSlack), 2^kLift right after the maximum moved
 
+// Division by a number known at the launch: n / d = (n * mul) >> (32 + shift) for n < 2^31 (d = 1: mul = 0)
+struct Divisor {
+    uint32_t d, mul, shift;
+    __device__ __forceinline__ uint32_t of(uint32_t n) const { return mul ? __umulhi(n, mul) >> shift : n; }
+};
+
+// mul = ceil(2^(32 + shift) / d) with 2^shift < d <= 2^(shift + 1) is below 2^32 and off by e < d; n e / (d 2^(32 + shift)) < 1 / d for n < 2^31
+Divisor divisor(uint32_t d)
+{
+    Divisor r = {d, 0, 0};
+    if (d <= 1) return r;
+    while ((2ull << r.shift) < d) ++r.shift;
+    r.mul = (uint32_t)(((1ull << (32 + r.shift)) + d - 1) / d);
+    return r;
+}
+
 struct AttendK {
     const void* q;
     void* out;
@@ -53,9 +69,12 @@ struct AttendK {
     int64_t q_batch, q_query, q_head;
     uint64_t unit_words;     // words of the bitmap
     uint64_t row_subs;       // blocks of `sub` tokens of a table row
-    uint32_t batch, queries, heads, group;
-    uint32_t rows, segs;     // query rows of a kv-head, segments of a kv-head
-    uint32_t page_tiles, table_pages, pages;
+    uint32_t batch, queries;
+    Divisor heads, group;
+    uint32_t rows;           // query rows of a kv-head
+    Divisor segs;            // segments of a kv-head
+    Divisor page_tiles;
+    uint32_t table_pages, pages;
     uint32_t unit, row_units;
     uint32_t sub;            // tokens per block of `mass`: min(unit, 16); 0: no weights asked for
     uint32_t unit_log2;      // of a unit of at most 16 tokens; 4 for larger ones
@@ -66,7 +85,7 @@ struct AttendK {
 
 __device__ __forceinline__ uint32_t length_of(const AttendK& p, uint32_t b)
 {
-    const int64_t most = (int64_t)p.table_pages * p.page_tiles * kTileTokens;
+    const int64_t most = (int64_t)p.table_pages * p.page_tiles.d * kTileTokens;
     const int64_t n = __ldg(p.lens + b);
     return (uint32_t)(n < 0 ? 0 : n > most ? most : n);
 }
@@ -108,7 +127,7 @@ __global__ void __launch_bounds__(kThreads) count_kernel(const AttendK p)
     __shared__ uint32_t sum[kWarps];
     let_next_start();
     const uint32_t bh = blockIdx.x, tid = threadIdx.x;
-    const uint32_t len = length_of(p, bh / p.heads), units = units_of(p, len), tiles = tiles_of(len);
+    const uint32_t len = length_of(p, p.heads.of(bh)), units = units_of(p, len), tiles = tiles_of(len);
     const uint32_t k = p.unit > kTileTokens ? p.unit / kTileTokens : 1;
     uint32_t n = 0;
     for (uint32_t w = tid; 32u * w < units; w += kThreads) {
@@ -126,33 +145,78 @@ __global__ void __launch_bounds__(kThreads) count_kernel(const AttendK p)
 }
 
 // The line of all tiles. An entry is a sequence (no bitmap) or a (sequence, kv-head) pair; the `per` segments of an entry have
-// the same number of tiles. CTA c works on tiles c * chunk .. c * chunk + chunk - 1.
+// the same number of tiles. A segment with tiles takes kFixed places before its first one: what a CTA spends on a segment whatever
+// its length (queries, the first tiles' way from memory, the join) is that of kFixed tiles about. CTA c works on the tiles at places
+// c * chunk .. c * chunk + chunk - 1.
+constexpr uint32_t kFixed = 16;
+
 struct Line {
-    uint32_t before, total;  // tiles before the entry asked for, and of all
+    uint32_t before, total;  // places before the entry asked for, and of all
     uint32_t chunk;
 };
 __device__ __forceinline__ uint32_t entry_count(const AttendK& p, uint32_t e) { return p.units ? p.counts[e] : tiles_of(length_of(p, e)); }
-__device__ __forceinline__ uint32_t line_entries(const AttendK& p) { return p.units ? p.batch * p.heads : p.batch; }
-__device__ __forceinline__ uint32_t line_per(const AttendK& p) { return p.units ? p.segs : p.segs * p.heads; }
+__device__ __forceinline__ uint32_t line_entries(const AttendK& p) { return p.units ? p.batch * p.heads.d : p.batch; }
+__device__ __forceinline__ uint32_t line_per(const AttendK& p) { return p.units ? p.segs.d : p.segs.d * p.heads.d; }
+__device__ __forceinline__ uint32_t entry_places(const AttendK& p, uint32_t e, uint32_t per)
+{
+    const uint32_t n = entry_count(p, e);
+    return n ? (n + kFixed) * per : 0u;
+}
+__device__ __forceinline__ uint32_t sum_upto(uint32_t x, uint32_t lane)       // over the lanes up to this one
+{
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= (uint32_t)o) x += v;
+    }
+    return x;
+}
 
 struct LineSmem {
     uint32_t warp[kWarps], before, entry;
 };
 
-// Every thread of the CTA calls it. With a CTA's number: the entry in which its part begins (`entry`; only if it has a part) and the tiles
-// before that entry. With cta = ~0: the tiles before `entry`.
+// Every thread of the CTA calls it. With a CTA's number: the entry in which its part begins (`entry`; only if it has a part) and the places
+// before that entry. With cta = ~0: the places before `entry`. Up to 128 entries every warp goes through them by itself (one load's
+// latency, no barrier), more of them are split over the CTA.
 __device__ __forceinline__ Line find_in_line(const AttendK& p, uint32_t cta, uint32_t& entry, LineSmem& sm)
 {
     const uint32_t E = line_entries(p), per = line_per(p), tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
-    const uint32_t each = E <= kThreads ? 1 : (E + kThreads - 1) / kThreads, first = min(tid * each, E), last = min(first + each, E);
-    uint32_t mine = 0;
-    for (uint32_t e = first; e < last; ++e) mine += entry_count(p, e) * per;
-    uint32_t upto = mine;
+    Line line;
+    if (E <= 128) {
+        uint32_t n[4], upto[4], base = 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-        if (lane >= (uint32_t)o) upto += v;
+        for (int i = 0; i < 4; ++i) n[i] = 32 * i + lane < E ? entry_places(p, 32 * i + lane, per) : 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            upto[i] = 0;
+            if (32 * i < (int)E) {
+                upto[i] = base + sum_upto(n[i], lane);
+                base = __shfl_sync(0xFFFFFFFFu, upto[i], 31);
+            }
+        }
+        line.total = base;
+        line.chunk = max((base + p.ctas - 1) / p.ctas, p.least);
+        line.before = 0;
+        const uint64_t at = (uint64_t)line.chunk * cta;
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (32 * i < (int)E && !found) {
+                const uint32_t here = __ballot_sync(0xFFFFFFFFu, cta == ~0u ? 32 * i + lane == entry : at < upto[i] && n[i]);
+                if (here) {
+                    const int l = __ffs(here) - 1;
+                    line.before = __shfl_sync(0xFFFFFFFFu, upto[i] - n[i], l);
+                    if (cta != ~0u) entry = 32 * i + l;
+                    found = true;
+                }
+            }
+        return line;
     }
+    const uint32_t each = (E + kThreads - 1) / kThreads, first = min(tid * each, E), last = min(first + each, E);
+    uint32_t mine = 0;
+    for (uint32_t e = first; e < last; ++e) mine += entry_places(p, e, per);
+    const uint32_t upto = sum_upto(mine, lane);
     if (lane == 31) sm.warp[warp] = upto;
     __syncthreads();
     uint32_t base = 0, total = 0;
@@ -161,13 +225,12 @@ __device__ __forceinline__ Line find_in_line(const AttendK& p, uint32_t cta, uin
         if (w < warp) base += sm.warp[w];
         total += sm.warp[w];
     }
-    Line line;
     line.total = total;
     line.chunk = max((total + p.ctas - 1) / p.ctas, p.least);
     uint32_t before = base + upto - mine;
     if (cta == ~0u) {
         if (first <= entry && entry < last) {
-            for (uint32_t e = first; e < entry; ++e) before += entry_count(p, e) * per;
+            for (uint32_t e = first; e < entry; ++e) before += entry_places(p, e, per);
             sm.before = before;
         }
     } else {
@@ -175,7 +238,7 @@ __device__ __forceinline__ Line find_in_line(const AttendK& p, uint32_t cta, uin
         if (before <= at && at < (uint64_t)before + mine) {
             uint32_t e = first;
             for (;; ++e) {
-                const uint32_t n = entry_count(p, e) * per;
+                const uint32_t n = entry_places(p, e, per);
                 if (at < (uint64_t)before + n) break;
                 before += n;
             }
@@ -322,34 +385,80 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
     const Line line = find_in_line(p, blockIdx.x, entry, sm.line);
     const uint64_t begin = (uint64_t)line.chunk * blockIdx.x;
     if (begin >= line.total) return;
-    uint32_t todo = min(line.chunk, line.total - (uint32_t)begin);
+    uint32_t todo = min(line.chunk, line.total - (uint32_t)begin);  // places
     const uint32_t per = line_per(p), E = line_entries(p);
-    uint32_t count = entry_count(p, entry), inner = ((uint32_t)begin - line.before) / count, off = ((uint32_t)begin - line.before) % count;
+    uint32_t count = entry_count(p, entry), inner = ((uint32_t)begin - line.before) / (count + kFixed);
+    uint32_t at_place = ((uint32_t)begin - line.before) - inner * (count + kFixed);      // in the segment
     uint8_t* const ring = ring_all + warp * kStages * L::kBytes;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
     // a fragment's row g is token 4 (g / 2) + g % 2 of the tile, its row g + 8 the token two further on: a thread then needs the
     // values of the four tokens 4 t .. 4 t + 3
     const uint32_t tok_a = 4 * (g >> 1) + (g & 1), tok_b = tok_a + 2;
 
-    while (todo) {
+    for (; todo; ++inner, at_place = 0) {
         while (inner == per || !count) {
             if (++entry >= E) return;                              // not reached: the line ends with the last part
             count = entry_count(p, entry);
             inner = 0;
         }
-        const uint32_t seg = entry * per + inner, bh = seg / p.segs, rt = seg - bh * p.segs, b = bh / p.heads, h = bh - b * p.heads;
-        const uint32_t take = min(todo, count - off);
+        const uint32_t places = min(todo, count + kFixed - at_place);
+        todo -= places;
+        if (at_place + places <= kFixed) continue;                 // no tile among them
+        const uint32_t off = at_place > kFixed ? at_place - kFixed : 0u, take = at_place + places - kFixed - off;
+        const uint32_t seg = entry * per + inner, bh = p.segs.of(seg), rt = seg - bh * p.segs.d, b = p.heads.of(bh), h = bh - b * p.heads.d;
         const uint32_t len = length_of(p, b);
         const int32_t* table = p.table + (uint64_t)b * p.table_pages;
+
+        uint32_t done = 0, many = 0, mine = 0, where = ~0u, bad = 0;   // this chunk of the segment's tiles, and this warp's part of it
+        auto tile_no = [&](uint32_t k) { const uint32_t i = warp + k * kWarps; return p.units ? sm.list[i] : off + i; };
+        auto issue = [&](uint32_t k) {
+            const uint32_t stage = k % kStages;
+            if (k % 32 == 0) {                                 // where the next 32 tiles lie, one a lane
+                where = ~0u;
+                if (k + lane < mine) {
+                    const uint32_t tile = tile_no(k + lane), page = p.page_tiles.of(tile);
+                    const uint32_t pg = (uint32_t)__ldg(table + page);
+                    if (pg < p.pages) where = (pg * p.heads.d + h) * p.page_tiles.d + (tile - page * p.page_tiles.d);
+                }
+            }
+            const uint32_t at = __shfl_sync(0xFFFFFFFFu, where, k % 32);
+            if (at != ~0u) {
+                const uint8_t* from = p.cache + (uint64_t)at * L::kBytes + lane * 16;
+                const uint32_t to = ring_at + stage * L::kBytes + lane * 16;
+#pragma unroll
+                for (uint32_t c = 0; c < L::kBytes / 16; c += 32)
+                    if (L::kBytes / 16 - c >= 32 || lane < L::kBytes / 16 - c)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + c * 16), "l"(from + c * 16) : "memory");
+                bad &= ~(1u << stage);
+            } else {
+                bad |= 1u << stage;                            // no tile, or in a page that is none
+            }
+        };
+        auto begin_chunk = [&]() {                                 // lists its tiles and sends for the first ones
+            many = p.units ? min(take - done, kListCap) : take;
+            if (p.units) {
+                __syncthreads();
+                list_tiles(p, bh, len, off + done, many, sm);
+            }
+            mine = many > warp ? (many - warp + kWarps - 1) / kWarps : 0;
+            where = ~0u;
+            bad = 0;
+#pragma unroll 1
+            for (int k = 0; k < kStages; k += 2) {
+                if (k < (int)mine) { issue(k); issue(k + 1); }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            }
+        };
+        begin_chunk();
 
         // This thread's part of row g's query as the right operand, divided by a power of two; the sums over groups for the zeros.
         // The 4-bit numbers are centred by starting their products at -8 times those sums, which keeps the partial sums small.
         uint32_t qf[N][4], qz[N == 8 ? 4 : 2];
         float start0[N], start1[N], f0, f1;
         {
-            const uint32_t r = rt * kRows + g, query = r / p.group;
+            const uint32_t r = rt * kRows + g, query = p.group.of(r);
             const bool real = r < p.rows;
-            const int64_t at = b * p.q_batch + (int64_t)query * p.q_query + (int64_t)(h * p.group + (r - query * p.group)) * p.q_head + t * 8;
+            const int64_t at = b * p.q_batch + (int64_t)query * p.q_query + (int64_t)(h * p.group.d + (r - query * p.group.d)) * p.q_head + t * 8;
             float x[N][8], most = 0.0f;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
@@ -359,14 +468,16 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
             }
             most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
             most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-            const int e = most > 0.0f && most < INFINITY ? ilogbf(most) - 6 : 0;     // largest magnitude in [2^6, 2^7)
+            // largest magnitude in [2^6, 2^7); the power of two in two factors, either of them a normal number
+            const int e = most > 0.0f && most < INFINITY ? ilogbf(most) - 6 : 0, half_e = -e / 2;
+            const float by0 = __int_as_float((half_e + 127) << 23), by1 = __int_as_float((-e - half_e + 127) << 23);
             float sums[N];
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 float sum = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    x[n][i] = scalbnf(x[n][i], -e);
+                    x[n][i] = x[n][i] * by0 * by1;
                     sum += x[n][i];
                 }
                 sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
@@ -407,11 +518,11 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
         int32_t see0, see1, all;
         {
             const int32_t first = (int32_t)len - (int32_t)p.queries + 1;
-            see0 = min(first + (int32_t)((rt * kRows + 2 * t) / p.group), (int32_t)len);
-            see1 = min(first + (int32_t)((rt * kRows + 2 * t + 1) / p.group), (int32_t)len);
-            all = min(first + (int32_t)(rt * kRows / p.group), (int32_t)len);
+            see0 = min(first + (int32_t)p.group.of(rt * kRows + 2 * t), (int32_t)len);
+            see1 = min(first + (int32_t)p.group.of(rt * kRows + 2 * t + 1), (int32_t)len);
+            all = min(first + (int32_t)p.group.of(rt * kRows), (int32_t)len);
         }
-        float* const mass = p.mass + ((uint64_t)bh * p.segs + rt) * p.row_subs * kRows + 2 * t;
+        float* const mass = p.mass + (uint64_t)seg * p.row_subs * kRows + 2 * t;
 
         float o[2 * N][4], zsum[4] = {0, 0, 0, 0}, m0 = kNone, m1 = kNone, l0 = 0.0f, l1 = 0.0f;
         int ev = -14;                                              // the values' scales are divided by 2^ev
@@ -422,43 +533,7 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
 
-        for (uint32_t done = 0; done < take;) {
-            const uint32_t many = p.units ? min(take - done, kListCap) : take;
-            if (p.units) {
-                __syncthreads();
-                list_tiles(p, bh, len, off + done, many, sm);
-            }
-            const uint32_t mine = many > warp ? (many - warp + kWarps - 1) / kWarps : 0;      // this warp's tiles
-            auto tile_no = [&](uint32_t k) { const uint32_t i = warp + k * kWarps; return p.units ? sm.list[i] : off + i; };
-            uint32_t where = ~0u, bad = 0;
-            auto issue = [&](uint32_t k) {
-                const uint32_t stage = k % kStages;
-                if (k % 32 == 0) {                                 // where the next 32 tiles lie, one a lane
-                    where = ~0u;
-                    if (k + lane < mine) {
-                        const uint32_t tile = tile_no(k + lane), page = tile / p.page_tiles;
-                        const uint32_t pg = (uint32_t)__ldg(table + page);
-                        if (pg < p.pages) where = (pg * p.heads + h) * p.page_tiles + (tile - page * p.page_tiles);
-                    }
-                }
-                const uint32_t at = __shfl_sync(0xFFFFFFFFu, where, k % 32);
-                if (at != ~0u) {
-                    const uint8_t* from = p.cache + (uint64_t)at * L::kBytes + lane * 16;
-                    const uint32_t to = ring_at + stage * L::kBytes + lane * 16;
-#pragma unroll
-                    for (uint32_t c = 0; c < L::kBytes / 16; c += 32)
-                        if (L::kBytes / 16 - c >= 32 || lane < L::kBytes / 16 - c)
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + c * 16), "l"(from + c * 16) : "memory");
-                    bad &= ~(1u << stage);
-                } else {
-                    bad |= 1u << stage;                            // no tile, or in a page that is none
-                }
-            };
-#pragma unroll 1
-            for (int k = 0; k < kStages; k += 2) {
-                if (k < (int)mine) { issue(k); issue(k + 1); }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-            }
+        while (true) {
 #pragma unroll 1
             for (uint32_t k = 0; k < mine; k += 2) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(kStages / 2 - 1) : "memory");
@@ -717,6 +792,8 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
             }
             asm volatile("cp.async.wait_group 0;" ::: "memory");
             done += many;
+            if (done >= take) break;
+            begin_chunk();
         }
 
         // join the warps; a row's 16-byte pieces are shuffled by its number, so that eight lanes write to eight banks
@@ -748,21 +825,24 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
         const bool whole = take == count;
         const uint64_t slot = (uint64_t)blockIdx.x + seg;
         auto place = [&](uint32_t row) {
-            const uint32_t query = row / p.group;
-            return ((uint64_t)b * p.queries + query) * (p.heads * p.group) + h * p.group + (row - query * p.group);
+            const uint32_t query = p.group.of(row);
+            return ((uint64_t)b * p.queries + query) * (p.heads.d * p.group.d) + h * p.group.d + (row - query * p.group.d);
         };
-        if (tid < kRows) {
-            const uint32_t r = tid, row = rt * kRows + r;
-            float m = sm.ml[0][r].x, l = 0.0f;
+        if (tid < kRows * kWarps) {                                // a row's warps in eight neighbouring lanes
+            const uint32_t r = tid / kWarps, w = tid % kWarps, row = rt * kRows + r;
+            const float2 x = sm.ml[w][r];
+            float m = x.x;
 #pragma unroll
-            for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sm.ml[w][r].x);
+            for (int o = 1; o < kWarps; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+            const float k = exp2_fast(x.x - m);
+            float l = x.y * k;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) l = fmaf(sm.ml[w][r].y, exp2_fast(sm.ml[w][r].x - m), l);
-            const float by = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) sm.share[w][r] = exp2_fast(sm.ml[w][r].x - m) * by;
-            p.ml[slot * kRows + r] = make_float2(m, l);
-            if (whole && p.lse && row < p.rows) p.lse[place(row)] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+            for (int o = 1; o < kWarps; o <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+            sm.share[w][r] = whole ? (l == 0.0f ? 0.0f : k / l) : k;
+            if (w == 0) {
+                p.ml[slot * kRows + r] = make_float2(m, l);
+                if (whole && p.lse && row < p.rows) p.lse[place(row)] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+            }
         }
         __syncthreads();
         for (uint32_t i = tid; i < kRows * L::D / 4; i += kThreads) {
@@ -781,10 +861,7 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
             if (whole) reinterpret_cast<uint2*>(p.out)[place(row) * (L::D / 4) + c] = make_uint2(out_pair<HALF>(sum.x, sum.y), out_pair<HALF>(sum.z, sum.w));
             else reinterpret_cast<float4*>(p.part)[(slot * kRows + r) * (L::D / 4) + c] = sum;
         }
-        __syncthreads();                                           // the ring is free again
-        todo -= take;
-        off = 0;
-        ++inner;
+        if (todo) __syncthreads();                                 // the ring is free again
     }
 }
 
@@ -793,74 +870,88 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
 template <int N, bool HALF>
 __global__ void __launch_bounds__(kThreads) join_kernel(const AttendK p)
 {
-    constexpr uint32_t D = 32 * N, kPart = kThreads / (D / 4);     // threads for four dims each share the CTAs' parts
+    constexpr uint32_t D = 32 * N, kQuads = D / 4;                 // 16-byte pieces of a row
+    constexpr uint32_t kOver = kQuads < 32 ? 32 / kQuads : 1;      // parts that a warp's lanes take at a time
+    constexpr uint32_t kEach = kQuads > 32 ? kQuads / 32 : 1;      // pieces of a lane
     __shared__ LineSmem sm;
     __shared__ float lse2[64];
-    __shared__ float2 ml[kThreads];
-    __shared__ float4 sums[kThreads];
+    __shared__ float4 sums[kWarps * kOver * kQuads];
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32, per = line_per(p);
-    const uint32_t out_blocks = p.batch * p.heads * p.rows;
+    const uint32_t out_blocks = p.batch * p.heads.d * p.rows;
     const bool is_out = blockIdx.x < out_blocks;
     const uint32_t chunks = p.weights ? (p.row_units + kThreads - 1) / kThreads : 1;
     const uint32_t bh = is_out ? blockIdx.x / p.rows : (blockIdx.x - out_blocks) / chunks;
-    const uint32_t b = bh / p.heads, h = bh - b * p.heads;
+    const uint32_t b = p.heads.of(bh), h = bh - b * p.heads.d;
     const uint32_t entry0 = p.units ? bh : b;
     uint32_t entry = entry0;
     wait_for_previous();
     const Line line = find_in_line(p, ~0u, entry, sm);
     const uint32_t count = entry_count(p, entry0);
     // the CTAs that worked on segment seg: first and last
-    auto first_tile = [&](uint32_t seg) { return line.before + (seg - entry0 * per) * count; };
+    auto first_cta = [&](uint32_t seg) { return (line.before + (seg - entry0 * per) * (count + kFixed) + kFixed) / line.chunk; };
+    auto last_cta = [&](uint32_t seg) { return (line.before + (seg - entry0 * per + 1) * (count + kFixed) - 1) / line.chunk; };
+    // a warp joins the maxima and sums of a row's parts
+    auto join_row = [&](uint32_t seg, uint32_t r, uint32_t c0, uint32_t c1, float& m, float& l) {
+        m = kNone;
+        l = 0.0f;
+        for (uint32_t c = c0 + lane; c <= c1; c += 32) {
+            const float2 x = p.ml[((uint64_t)c + seg) * kRows + r];
+            const float up = fmaxf(m, x.x);
+            l = fmaf(l, exp2_fast(m - up), x.y * exp2_fast(x.x - up));
+            m = up;
+        }
+        float top = m;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        l *= exp2_fast(m - top);
+        m = top;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+    };
     if (is_out) {
-        const uint32_t row = blockIdx.x - bh * p.rows, rt = row / kRows, r = row % kRows, seg = bh * p.segs + rt, query = row / p.group;
-        const uint64_t at = ((uint64_t)b * p.queries + query) * (p.heads * p.group) + h * p.group + (row - query * p.group);
+        const uint32_t row = blockIdx.x - bh * p.rows, rt = row / kRows, r = row % kRows, seg = bh * p.segs.d + rt, query = p.group.of(row);
+        const uint64_t at = ((uint64_t)b * p.queries + query) * (p.heads.d * p.group.d) + h * p.group.d + (row - query * p.group.d);
         if (!count) {
-            if (tid < D / 4) reinterpret_cast<uint2*>(p.out)[at * (D / 4) + tid] = make_uint2(0u, 0u);
+            if (tid < kQuads) reinterpret_cast<uint2*>(p.out)[at * kQuads + tid] = make_uint2(0u, 0u);
             if (tid == 0 && p.lse) p.lse[at] = -INFINITY;
             return;
         }
-        const uint32_t c0 = first_tile(seg) / line.chunk, c1 = (first_tile(seg) + count - 1) / line.chunk;
+        const uint32_t c0 = first_cta(seg), c1 = last_cta(seg);
         if (c0 == c1) return;                                      // written by its one CTA
-        const uint32_t d4 = tid % (D / 4), mine = tid / (D / 4);
-        float m = kNone, l = 0.0f;
-        float4 sum = make_float4(0, 0, 0, 0);
-        for (uint32_t c = c0; c <= c1; c += kThreads) {
-            const uint32_t many = min(c1 - c + 1, kThreads);
-            __syncthreads();
-            if (tid < many) ml[tid] = p.ml[((uint64_t)c + tid + seg) * kRows + r];
-            __syncthreads();
-            float up = m;
-            for (uint32_t i = 0; i < many; ++i) up = fmaxf(up, ml[i].x);
-            const float old = exp2_fast(m - up);
-            m = up;
-            l *= old;
-            sum.x *= old;
-            sum.y *= old;
-            sum.z *= old;
-            sum.w *= old;
-            for (uint32_t i = 0; i < many; ++i) l = fmaf(ml[i].y, exp2_fast(ml[i].x - m), l);
+        float m, l;
+        join_row(seg, r, c0, c1, m, l);
+        float4 sum[kEach];
+#pragma unroll
+        for (uint32_t j = 0; j < kEach; ++j) sum[j] = make_float4(0, 0, 0, 0);
+        const uint32_t piece = lane % kQuads;
 #pragma unroll 4
-            for (uint32_t i = mine; i < many; i += kPart) {
-                const float k = exp2_fast(ml[i].x - m);
-                const float4 x = reinterpret_cast<const float4*>(p.part)[(((uint64_t)c + i + seg) * kRows + r) * (D / 4) + d4];
-                sum.x = fmaf(x.x, k, sum.x);
-                sum.y = fmaf(x.y, k, sum.y);
-                sum.z = fmaf(x.z, k, sum.z);
-                sum.w = fmaf(x.w, k, sum.w);
+        for (uint32_t c = c0 + warp * kOver + lane / kQuads; c <= c1; c += kWarps * kOver) {
+            const float k = exp2_fast(p.ml[((uint64_t)c + seg) * kRows + r].x - m);
+            const float4* part = reinterpret_cast<const float4*>(p.part) + (((uint64_t)c + seg) * kRows + r) * kQuads + piece;
+#pragma unroll
+            for (uint32_t j = 0; j < kEach; ++j) {
+                const float4 x = part[32 * j];
+                sum[j].x = fmaf(x.x, k, sum[j].x);
+                sum[j].y = fmaf(x.y, k, sum[j].y);
+                sum[j].z = fmaf(x.z, k, sum[j].z);
+                sum[j].w = fmaf(x.w, k, sum[j].w);
             }
         }
-        sums[tid] = sum;
+#pragma unroll
+        for (uint32_t j = 0; j < kEach; ++j) sums[(warp * kOver + lane / kQuads) * kQuads + piece + 32 * j] = sum[j];
         __syncthreads();
-        if (tid < D / 4) {
-            for (uint32_t i = 1; i < kPart; ++i) {
-                const float4 x = sums[i * (D / 4) + tid];
-                sum.x += x.x;
-                sum.y += x.y;
-                sum.z += x.z;
-                sum.w += x.w;
+        if (tid < kQuads) {
+            float4 x = sums[tid];
+#pragma unroll
+            for (uint32_t i = 1; i < kWarps * kOver; ++i) {
+                const float4 y = sums[i * kQuads + tid];
+                x.x += y.x;
+                x.y += y.y;
+                x.z += y.z;
+                x.w += y.w;
             }
             const float by = l == 0.0f ? 0.0f : 1.0f / l;
-            reinterpret_cast<uint2*>(p.out)[at * (D / 4) + tid] = make_uint2(out_pair<HALF>(sum.x * by, sum.y * by), out_pair<HALF>(sum.z * by, sum.w * by));
+            reinterpret_cast<uint2*>(p.out)[at * kQuads + tid] = make_uint2(out_pair<HALF>(x.x * by, x.y * by), out_pair<HALF>(x.z * by, x.w * by));
             if (tid == 0 && p.lse) p.lse[at] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
         }
         return;
@@ -877,21 +968,8 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttendK p)
         for (uint32_t i = warp; i < padded; i += kWarps) {         // a warp joins a row's sums
             float m = kNone, l = 0.0f;
             if (count && i < rows) {
-                const uint32_t seg = bh * p.segs + (row0 + i) / kRows, r = (row0 + i) % kRows;
-                const uint32_t c0 = first_tile(seg) / line.chunk, c1 = (first_tile(seg) + count - 1) / line.chunk;
-                for (uint32_t c = c0 + lane; c <= c1; c += 32) {
-                    const float2 x = p.ml[((uint64_t)c + seg) * kRows + r];
-                    const float up = fmaxf(m, x.x);
-                    l = fmaf(l, exp2_fast(m - up), x.y * exp2_fast(x.x - up));
-                    m = up;
-                }
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const float mo = __shfl_xor_sync(0xFFFFFFFFu, m, o), lo = __shfl_xor_sync(0xFFFFFFFFu, l, o);
-                    const float up = fmaxf(m, mo);
-                    l = l * exp2_fast(m - up) + lo * exp2_fast(mo - up);
-                    m = up;
-                }
+                const uint32_t seg = bh * p.segs.d + (row0 + i) / kRows;
+                join_row(seg, (row0 + i) % kRows, first_cta(seg), last_cta(seg), m, l);
             }
             if (lane == 0) lse2[i] = l == 0.0f ? INFINITY : m + log2f(l);
         }
@@ -900,10 +978,10 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttendK p)
         const uint64_t last = min((uint64_t)len, base + p.unit);
         for (uint64_t i = base; i < last; i += p.sub) {
             const uint32_t tile = (uint32_t)(i / kTileTokens);
-            const int32_t page = __ldg(p.table + (uint64_t)b * p.table_pages + tile / p.page_tiles);
+            const int32_t page = __ldg(p.table + (uint64_t)b * p.table_pages + p.page_tiles.of(tile));
             if (page < 0 || (uint32_t)page >= p.pages) continue;
             for (uint32_t r = 0; r < rows; r += kRows) {           // a segment's rows lie together; rows that are none have 0
-                const float4* x = reinterpret_cast<const float4*>(p.mass + (((uint64_t)bh * p.segs + (row0 + r) / kRows) * p.row_subs + (i >> (p.unit_log2 < 4 ? p.unit_log2 : 4))) * kRows);
+                const float4* x = reinterpret_cast<const float4*>(p.mass + (((uint64_t)bh * p.segs.d + (row0 + r) / kRows) * p.row_subs + (i >> (p.unit_log2 < 4 ? p.unit_log2 : 4))) * kRows);
                 const float4 lo = x[0], hi = x[1];
                 got += exp2_fast(lo.x - lse2[r]) + exp2_fast(lo.y - lse2[r + 1]) + exp2_fast(lo.z - lse2[r + 2]) + exp2_fast(lo.w - lse2[r + 3]) +
                        exp2_fast(hi.x - lse2[r + 4]) + exp2_fast(hi.y - lse2[r + 5]) + exp2_fast(hi.z - lse2[r + 6]) + exp2_fast(hi.w - lse2[r + 7]);
@@ -949,8 +1027,8 @@ int check_attend(const kvp_attend_params* a)
     const uint64_t rows = (uint64_t)a->queries * a->group, bh = (uint64_t)a->batch * a->cache.kv_heads;
     const uint64_t tokens = (uint64_t)a->table_pages * a->cache.page_tokens;
     if (rows > 4096 || a->queries > 1024 || a->batch >= (1u << 24) || bh >= (1u << 24) || tokens >= (1ull << 31)) return KVP_ERR_RANGE;
-    // tiles of the line and of the cache are counted in 32 bits
-    if (bh * ((rows + kRows - 1) / kRows) * (tokens / kTileTokens) >= (1ull << 32) - (1u << 20) || (uint64_t)a->cache.pages * a->cache.kv_heads * (a->cache.page_tokens / kTileTokens) >= (1ull << 32) - 1) return KVP_ERR_RANGE;
+    // places in the line (31 bits) and tiles of the cache are counted in 32 bits
+    if (bh * ((rows + kRows - 1) / kRows) * (tokens / kTileTokens + kFixed) >= (1ull << 31) || (uint64_t)a->cache.pages * a->cache.kv_heads * (a->cache.page_tokens / kTileTokens) >= (1ull << 32) - 1) return KVP_ERR_RANGE;
     if (bh * rows >= (1ull << 30) || bh * ((tokens / u + kThreads - 1) / kThreads) >= (1ull << 30)) return KVP_ERR_RANGE;
     return KVP_OK;
 }
@@ -978,9 +1056,9 @@ int launch_attend(const AttendK& k, cudaStream_t st)
 {
     const uint32_t smem = Shape<N>::kSmem;
     KVP_CUDA(cudaFuncSetAttribute(attend_kernel<N, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    int rc = k.units ? launch(count_kernel, k.batch * k.heads, 0, false, st, k) : KVP_OK;
+    int rc = k.units ? launch(count_kernel, k.batch * k.heads.d, 0, false, st, k) : KVP_OK;
     if (!rc) rc = launch(attend_kernel<N, HALF>, k.ctas, smem, k.units != nullptr, st, k);
-    const uint64_t blocks = (uint64_t)k.batch * k.heads * (k.rows + (k.weights ? (k.row_units + kThreads - 1) / kThreads : 0));
+    const uint64_t blocks = (uint64_t)k.batch * k.heads.d * (k.rows + (k.weights ? (k.row_units + kThreads - 1) / kThreads : 0));
     if (!rc) rc = launch(join_kernel<N, HALF>, (uint32_t)blocks, 0, true, st, k);
     return rc;
 }
@@ -1018,12 +1096,12 @@ extern "C" int kvp_attend(const kvp_attend_params* a, const void* q, const void*
     k.mass = reinterpret_cast<float*>(ws + w.mass);
     k.counts = reinterpret_cast<uint32_t*>(ws + w.counts);
     k.q_batch = a->q_batch_stride; k.q_query = a->q_query_stride; k.q_head = a->q_head_stride;
-    k.batch = a->batch; k.queries = a->queries; k.heads = a->cache.kv_heads; k.group = a->group;
-    k.rows = a->queries * a->group; k.segs = (k.rows + kRows - 1) / kRows;
-    k.page_tiles = a->cache.page_tokens / kTileTokens; k.table_pages = a->table_pages; k.pages = a->cache.pages;
+    k.batch = a->batch; k.queries = a->queries; k.heads = divisor(a->cache.kv_heads); k.group = divisor(a->group);
+    k.rows = a->queries * a->group; k.segs = divisor((k.rows + kRows - 1) / kRows);
+    k.page_tiles = divisor(a->cache.page_tokens / kTileTokens); k.table_pages = a->table_pages; k.pages = a->cache.pages;
     const uint64_t tokens = (uint64_t)a->table_pages * a->cache.page_tokens;
     k.unit = a->unit_tokens; k.row_units = (uint32_t)(tokens / a->unit_tokens);
-    k.unit_words = ((uint64_t)k.batch * k.heads * k.row_units + 31) / 32;
+    k.unit_words = ((uint64_t)k.batch * k.heads.d * k.row_units + 31) / 32;
     const uint32_t sub = k.unit < kTileTokens ? k.unit : kTileTokens;
     k.row_subs = tokens / sub;
     k.sub = weights ? sub : 0;
