@@ -10,7 +10,7 @@ LIB = os.path.join(HERE, "libkvp.so")
 BINDING = os.path.join(HERE, "_kvp_torch.so")
 SOURCES = ["kvp_api.cu", "kvp_cost.cu", "kvp_layout.cu", "kvp_anneal.cu", "kvp_trace.cu", "kvp_policy.cu", "kvp_cache.cu", "kvp_attend.cu",
            "kvp_evict.cu", "kvp_table.cpp"]
-HEADERS = ["kvp_common.cuh", "kvp_chain.cuh", "kvp_narrow.cuh", "kvp_tile.cuh"]
+HEADERS = ["kvp_common.cuh", "kvp_chain.cuh", "kvp_narrow.cuh", "kvp_tile.cuh", "kvp_select.cuh"]
 
 
 def _nvcc():

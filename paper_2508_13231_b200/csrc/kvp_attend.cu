@@ -33,9 +33,9 @@ constexpr int kWarps = 8;
 constexpr uint32_t kThreads = kWarps * 32;
 constexpr uint32_t kRows = 8;                 // query rows of a segment
 constexpr uint32_t kListCap = 1024;           // tiles of a bitmap row that are listed at a time
-constexpr uint32_t kTop = 0x03C003C0u;        // the upper four bits of two fp16 significands
+constexpr uint32_t kNibble = 0x00F000F0u;     // bits 4 .. 7 of two fp16 significands
 constexpr float kNone = -3e38f;               // maximum of nothing
-constexpr float kLift = 3.0f, kSlack = 8.0f;  // weights are at most 2^(kLift + kSlack), 2^kLift right after the maximum moved
+constexpr float kLift = 13.0f, kSlack = 2.0f; // weights are at most 2^(kLift + kSlack), 2^kLift right after the maximum moved
 
 // Division by a number known at the launch: n / d = (n * mul) >> (32 + shift) for n < 2^31 (d = 1: mul = 0)
 struct Divisor {
@@ -293,21 +293,33 @@ __device__ __forceinline__ float over_rows(float x)                 // sum over 
 }
 
 // eight dims of a query
-template <bool HALF>
-__device__ __forceinline__ void load_q(const AttendK& p, int64_t at, bool real, float (&x)[8])
+__device__ __forceinline__ uint4 load_q(const AttendK& p, int64_t at, bool real)
 {
-    alignas(16) uint16_t raw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    uint4 x = make_uint4(0, 0, 0, 0);
     if (real) {
         const uint16_t* from = static_cast<const uint16_t*>(p.q) + at;
         if (p.q_aligned) {
-            *reinterpret_cast<uint4*>(raw) = __ldg(reinterpret_cast<const uint4*>(from));
+            x = __ldg(reinterpret_cast<const uint4*>(from));
         } else {
+            uint32_t e[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) raw[i] = __ldg(from + i);
+            for (int i = 0; i < 8; ++i) e[i] = __ldg(from + i);
+            x = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
         }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = HALF ? __half2float(__ushort_as_half(raw[i])) : __uint_as_float((uint32_t)raw[i] << 16);
+    return x;
+}
+template <bool HALF>
+__device__ __forceinline__ void floats_of(uint32_t x, float* to)
+{
+    if (HALF) {
+        const float2 f = __half22float2(half2_of(x));
+        to[0] = f.x;
+        to[1] = f.y;
+    } else {
+        to[0] = __uint_as_float(x << 16);
+        to[1] = __uint_as_float(x & 0xFFFF0000u);
+    }
 }
 template <bool HALF>
 __device__ __forceinline__ uint32_t out_pair(float a, float b)
@@ -449,20 +461,27 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                 asm volatile("cp.async.commit_group;" ::: "memory");
             }
         };
+        uint4 raw[N];                                              // this thread's part of row g's query: on their way before the tiles
+        {
+            const uint32_t r = rt * kRows + g, query = p.group.of(r);
+            const int64_t at = b * p.q_batch + (int64_t)query * p.q_query + (int64_t)(h * p.group.d + (r - query * p.group.d)) * p.q_head + t * 8;
+#pragma unroll
+            for (int n = 0; n < N; ++n) raw[n] = load_q(p, at + n * 32, r < p.rows);
+        }
         begin_chunk();
 
-        // This thread's part of row g's query as the right operand, divided by a power of two; the sums over groups for the zeros.
+        // The queries as the right operand, divided by a power of two; the sums over groups for the zeros.
         // The 4-bit numbers are centred by starting their products at -8 times those sums, which keeps the partial sums small.
         uint32_t qf[N][4], qz[N == 8 ? 4 : 2];
         float start0[N], start1[N], f0, f1;
         {
-            const uint32_t r = rt * kRows + g, query = p.group.of(r);
-            const bool real = r < p.rows;
-            const int64_t at = b * p.q_batch + (int64_t)query * p.q_query + (int64_t)(h * p.group.d + (r - query * p.group.d)) * p.q_head + t * 8;
             float x[N][8], most = 0.0f;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                load_q<HALF>(p, at + n * 32, real, x[n]);
+                floats_of<HALF>(raw[n].x, x[n]);
+                floats_of<HALF>(raw[n].y, x[n] + 2);
+                floats_of<HALF>(raw[n].z, x[n] + 4);
+                floats_of<HALF>(raw[n].w, x[n] + 6);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[n][i]));
             }
@@ -482,8 +501,8 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                 }
                 sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
                 sums[n] = sum + __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-                start0[n] = __shfl_sync(0xFFFFFFFFu, sums[n], 8 * t) * -0x1p-15f;
-                start1[n] = __shfl_sync(0xFFFFFFFFu, sums[n], 8 * t + 4) * -0x1p-15f;
+                start0[n] = __shfl_sync(0xFFFFFFFFu, sums[n], 8 * t) * -0x1p-17f;
+                start1[n] = __shfl_sync(0xFFFFFFFFu, sums[n], 8 * t + 4) * -0x1p-17f;
                 qf[n][0] = pack(x[n][0], x[n][4]);
                 qf[n][1] = pack(x[n][1], x[n][5]);
                 qf[n][2] = pack(x[n][2], x[n][6]);
@@ -525,13 +544,25 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
         float* const mass = p.mass + (uint64_t)seg * p.row_subs * kRows + 2 * t;
 
         float o[2 * N][4], zsum[4] = {0, 0, 0, 0}, m0 = kNone, m1 = kNone, l0 = 0.0f, l1 = 0.0f;
-        int ev = -14;                                              // the values' scales are divided by 2^ev
-        float vlimit = 0x1p-10f;                                   // 2^(ev + 4)
-        uint32_t shrink = 0x74007400u;                             // 2^-ev, twice
+        float lift = kLift, d0 = kNone, d1 = kNone;                // weights are 2^(s - d), d = m - lift
 #pragma unroll
         for (int i = 0; i < 2 * N; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
+
+        auto rescale = [&](float c0, float c1) {
+            l0 *= c0;
+            l1 *= c1;
+            zsum[0] *= c0;
+            zsum[1] *= c1;
+#pragma unroll
+            for (int i = 0; i < 2 * N; ++i) {
+                o[i][0] *= c0;
+                o[i][1] *= c1;
+                o[i][2] *= c0;
+                o[i][3] *= c1;
+            }
+        };
 
         while (true) {
 #pragma unroll 1
@@ -584,10 +615,10 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
 #pragma unroll
                     for (int n = 0; n < N; ++n) {
                         float acc[4];
-                        mma(acc, wa[n] * 64u & kTop, wb[n] * 64u & kTop, wa[n] * 4u & kTop, wb[n] * 4u & kTop, qf[n][0], qf[n][1],
+                        mma(acc, wa[n] * 16u & kNibble, wb[n] * 16u & kNibble, wa[n] & kNibble, wb[n] & kNibble, qf[n][0], qf[n][1],
                             start0[n], start1[n], start0[n], start1[n]);
                         const uint32_t xa = wa[n] >> 8, xb = wb[n] >> 8;
-                        mma(acc, xa * 64u & kTop, xb * 64u & kTop, xa * 4u & kTop, xb * 4u & kTop, qf[n][2], qf[n][3]);
+                        mma(acc, xa * 16u & kNibble, xb * 16u & kNibble, xa & kNibble, xb & kNibble, qf[n][2], qf[n][3]);
                         const float2 pa = __half22float2(half2_of(sa[n / 2])), pb = __half22float2(half2_of(sb[n / 2]));
                         const float fa = n & 1 ? pa.y : pa.x, fb = n & 1 ? pb.y : pb.x;
                         sum[0] = fmaf(fa, acc[0], sum[0]);
@@ -595,35 +626,17 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                         sum[2] = fmaf(fb, acc[2], sum[2]);
                         sum[3] = fmaf(fb, acc[3], sum[3]);
                     }
-                    s[u][0] = f0 * fmaf(sum[0], 0x1p18f, z[0]);
-                    s[u][1] = f1 * fmaf(sum[1], 0x1p18f, z[1]);
-                    s[u][2] = f0 * fmaf(sum[2], 0x1p18f, z[2]);
-                    s[u][3] = f1 * fmaf(sum[3], 0x1p18f, z[3]);
+                    s[u][0] = f0 * fmaf(sum[0], 0x1p20f, z[0]);
+                    s[u][1] = f1 * fmaf(sum[1], 0x1p20f, z[1]);
+                    s[u][2] = f0 * fmaf(sum[2], 0x1p20f, z[2]);
+                    s[u][3] = f1 * fmaf(sum[3], 0x1p20f, z[3]);
                 }
 
-                // scales and zeros of the values of tokens 4t .. 4t + 3
-                uint32_t vs[2][N][2], vz[2][2] = {{0, 0}, {0, 0}};
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint8_t* tile = tile0 + u * L::kBytes;
-#pragma unroll
-                    for (int n = 0; n < N; n += 2) {
-                        const uint4 x = *reinterpret_cast<const uint4*>(tile + L::value_meta(4 * t, n));
-                        vs[u][n][0] = x.x;
-                        vs[u][n][1] = x.y;
-                        vs[u][n + 1][0] = x.z;
-                        vs[u][n + 1][1] = x.w;
-                    }
-                    if (g < N) {
-                        const uint2 x = *reinterpret_cast<const uint2*>(tile + L::value_meta(4 * t, g) + (L::kValueZero - L::kValueScale));
-                        vz[u][0] = x.x;
-                        vz[u][1] = x.y;
-                    }
-                }
+                uint32_t live = ~0u;                               // tokens of the two tiles that some row sees
                 const bool parts = p.units && p.unit < kTileTokens;
                 if (none || parts || (int32_t)(max(no0, no1) * kTileTokens + kTileTokens) > all) {
                     // Some token is not seen by some row. What lies in the cache behind the last token, or in the ring where there was
-                    // no tile, may be anything, also infinite, so its scales and zeros are cleared too.
+                    // no tile, may be anything, also infinite, so its scales and zeros are cleared below.
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         const int32_t base = (int32_t)((u ? no1 : no0) * kTileTokens);
@@ -641,59 +654,26 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                         if (!a || base + (int32_t)tok_a >= see1) s[u][1] = -INFINITY;
                         if (!c || base + (int32_t)tok_b >= see0) s[u][2] = -INFINITY;
                         if (!c || base + (int32_t)tok_b >= see1) s[u][3] = -INFINITY;
-                        const uint32_t four = bits >> (4 * t);
-                        const uint32_t k0 = (four & 1u ? 0xFFFFu : 0u) | (four & 2u ? 0xFFFF0000u : 0u);
-                        const uint32_t k1 = (four & 4u ? 0xFFFFu : 0u) | (four & 8u ? 0xFFFF0000u : 0u);
-#pragma unroll
-                        for (int n = 0; n < N; ++n) { vs[u][n][0] &= k0; vs[u][n][1] &= k1; }
-                        vz[u][0] &= k0;
-                        vz[u][1] &= k1;
+                        live = u ? live & 0xFFFFu | bits << 16 : live & 0xFFFF0000u | bits;
                     }
                 }
-                // has a score passed the maximum by more than the slack, or a scale its power of two?
-                float vmost;
-                {
-                    __half2 v = __hmax2(half2_of(vs[0][0][0]), half2_of(vs[0][0][1]));
-                    v = __hmax2(v, __hmax2(half2_of(vs[1][0][0]), half2_of(vs[1][0][1])));
-#pragma unroll
-                    for (int n = 1; n < N; ++n) {
-                        v = __hmax2(v, __hmax2(half2_of(vs[0][n][0]), half2_of(vs[0][n][1])));
-                        v = __hmax2(v, __hmax2(half2_of(vs[1][n][0]), half2_of(vs[1][n][1])));
-                    }
-                    vmost = __half2float(__hmax(__low2half(v), __high2half(v)));
-                }
+                // has a score passed the maximum by more than the slack?
                 const float t0 = fmaxf(fmaxf(s[0][0], s[0][2]), fmaxf(s[1][0], s[1][2])), t1 = fmaxf(fmaxf(s[0][1], s[0][3]), fmaxf(s[1][1], s[1][3]));
-                if (__any_sync(0xFFFFFFFFu, t0 > m0 + kSlack || t1 > m1 + kSlack || vmost > vlimit)) {
-                    float n0 = t0, n1 = t1, nv = vmost;
+                if (__any_sync(0xFFFFFFFFu, t0 > m0 + kSlack || t1 > m1 + kSlack)) {
+                    float n0 = t0, n1 = t1;
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) {
                         n0 = fmaxf(n0, __shfl_xor_sync(0xFFFFFFFFu, n0, d));
                         n1 = fmaxf(n1, __shfl_xor_sync(0xFFFFFFFFu, n1, d));
                     }
-                    nv = fmaxf(nv, __shfl_xor_sync(0xFFFFFFFFu, nv, 1));
-                    nv = fmaxf(nv, __shfl_xor_sync(0xFFFFFFFFu, nv, 2));
                     n0 = fmaxf(m0, n0);
                     n1 = fmaxf(m1, n1);
-                    const int en = nv > 0.0f && nv < INFINITY ? max(ev, ilogbf(nv) + 1) : ev;
-                    const float c0 = exp2_fast(m0 - n0), c1 = exp2_fast(m1 - n1), ce = exp2f((float)(ev - en));
+                    rescale(exp2_fast(m0 - n0), exp2_fast(m1 - n1));
                     m0 = n0;
                     m1 = n1;
-                    ev = en;
-                    vlimit = exp2f((float)(ev + 4));
-                    shrink = bits_of(__float2half2_rn(exp2f((float)-ev)));
-                    l0 *= c0;
-                    l1 *= c1;
-                    zsum[0] *= c0;
-                    zsum[1] *= c1;
-#pragma unroll
-                    for (int i = 0; i < 2 * N; ++i) {
-                        o[i][0] *= c0 * ce;
-                        o[i][1] *= c1 * ce;
-                        o[i][2] *= c0 * ce;
-                        o[i][3] *= c1 * ce;
-                    }
+                    d0 = m0 - lift;
+                    d1 = m1 - lift;
                 }
-                const float d0 = m0 - kLift, d1 = m1 - kLift;
                 float e[2][4];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -750,14 +730,60 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const uint8_t* tile = tile0 + u * L::kBytes;
+                    uint32_t vs[N][2], vz0 = 0, vz1 = 0;           // scales and zeros of the values of tokens 4t .. 4t + 3
+#pragma unroll
+                    for (int n = 0; n < N; n += 2) {
+                        const uint4 x = *reinterpret_cast<const uint4*>(tile + L::value_meta(4 * t, n));
+                        vs[n][0] = x.x;
+                        vs[n][1] = x.y;
+                        vs[n + 1][0] = x.z;
+                        vs[n + 1][1] = x.w;
+                    }
+                    if (g < N) {
+                        const uint2 x = *reinterpret_cast<const uint2*>(tile + L::value_meta(4 * t, g) + (L::kValueZero - L::kValueScale));
+                        vz0 = x.x;
+                        vz1 = x.y;
+                    }
+                    if (live != ~0u) {
+                        const uint32_t four = live >> (16 * u + 4 * t);
+                        const uint32_t k0 = (four & 1u ? 0xFFFFu : 0u) | (four & 2u ? 0xFFFF0000u : 0u);
+                        const uint32_t k1 = (four & 4u ? 0xFFFFu : 0u) | (four & 8u ? 0xFFFF0000u : 0u);
+#pragma unroll
+                        for (int n = 0; n < N; ++n) { vs[n][0] &= k0; vs[n][1] &= k1; }
+                        vz0 &= k0;
+                        vz1 &= k1;
+                    }
+                    // A weight times a scale has to stay below 2^16. Up to scales of 2 the lift sees to that; larger ones (values
+                    // that span more than 30) take as much off the lift, for good.
+                    uint32_t large = vs[0][0] | vs[0][1];
+#pragma unroll
+                    for (int n = 1; n < N; ++n) large |= vs[n][0] | vs[n][1];
+                    if (__any_sync(0xFFFFFFFFu, large & 0x40004000u)) {
+                        __half2 v = __hmax2(half2_of(vs[0][0]), half2_of(vs[0][1]));
+#pragma unroll
+                        for (int n = 1; n < N; ++n) v = __hmax2(v, __hmax2(half2_of(vs[n][0]), half2_of(vs[n][1])));
+                        float most = __half2float(__hmax(__low2half(v), __high2half(v)));
+                        most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+                        most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+                        const float room = kLift - (float)(most < INFINITY ? ilogbf(most) : 15);
+                        if (room < lift) {
+                            const float c = exp2f(room - lift);
+                            rescale(c, c);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) { e[0][i] *= c; e[1][i] *= c; }
+                            lift = room;
+                            d0 = m0 - lift;
+                            d1 = m1 - lift;
+                        }
+                    }
                     const uint32_t h0 = pack(e[u][0], e[u][1]), h1 = pack(e[u][2], e[u][3]), p0 = transposed(h0), p1 = transposed(h1);
                     uint32_t r0 = 0, r1 = 0;                       // what the fp16 weights leave
-                    mma(zsum, vz[u][0], 0u, vz[u][1], 0u, p0, p1);
+                    mma(zsum, vz0, 0u, vz1, 0u, p0, p1);
                     if constexpr (HALF) {
                         const float2 q0 = __half22float2(half2_of(h0)), q1 = __half22float2(half2_of(h1));
                         r0 = transposed(pack(e[u][0] - q0.x, e[u][1] - q0.y));
                         r1 = transposed(pack(e[u][2] - q1.x, e[u][3] - q1.y));
-                        mma(zsum, vz[u][0], 0u, vz[u][1], 0u, r0, r1);
+                        mma(zsum, vz0, 0u, vz1, 0u, r0, r1);
                     }
                     uint32_t x[N], y[N];
                     if constexpr (N == 2) {
@@ -772,15 +798,15 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                     }
 #pragma unroll
                     for (int n = 0; n < N; ++n) {
-                        const uint32_t v0 = times(vs[u][n][0], shrink), v1 = times(vs[u][n][1], shrink), w0 = times(p0, v0), w1 = times(p1, v1);
+                        const uint32_t w0 = times(p0, vs[n][0]), w1 = times(p1, vs[n][1]);
                         const uint32_t a[4] = {x[n] & 0x000F000Fu, x[n] & 0x00F000F0u, y[n] & 0x000F000Fu, y[n] & 0x00F000F0u};
                         const uint32_t xx = x[n] >> 8, yy = y[n] >> 8;
                         const uint32_t c[4] = {xx & 0x000F000Fu, xx & 0x00F000F0u, yy & 0x000F000Fu, yy & 0x00F000F0u};
                         mma(o[2 * n], a[0], a[1], a[2], a[3], w0, w1);
                         mma(o[2 * n + 1], c[0], c[1], c[2], c[3], w0, w1);
                         if constexpr (HALF) {
-                            const uint32_t low0 = bits_of(__hfma2(half2_of(r0), half2_of(v0), __hfma2(half2_of(p0), half2_of(v0), __hneg2(half2_of(w0)))));
-                            const uint32_t low1 = bits_of(__hfma2(half2_of(r1), half2_of(v1), __hfma2(half2_of(p1), half2_of(v1), __hneg2(half2_of(w1)))));
+                            const uint32_t low0 = bits_of(__hfma2(half2_of(r0), half2_of(vs[n][0]), __hfma2(half2_of(p0), half2_of(vs[n][0]), __hneg2(half2_of(w0)))));
+                            const uint32_t low1 = bits_of(__hfma2(half2_of(r1), half2_of(vs[n][1]), __hfma2(half2_of(p1), half2_of(vs[n][1]), __hneg2(half2_of(w1)))));
                             mma(o[2 * n], a[0], a[1], a[2], a[3], low0, low1);
                             mma(o[2 * n + 1], c[0], c[1], c[2], c[3], low0, low1);
                         }
@@ -800,7 +826,7 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
         l0 = over_rows(l0);
         l1 = over_rows(l1);
         __syncthreads();                                           // every warp is done with its ring
-        const float up = exp2f((float)(ev + 24)), up16 = exp2f((float)(ev + 20));
+        constexpr float up = 0x1p24f, up16 = 0x1p20f;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const float z0 = __shfl_sync(0xFFFFFFFFu, zsum[0], n * 4 + t), z1 = __shfl_sync(0xFFFFFFFFu, zsum[1], n * 4 + t);
@@ -818,8 +844,8 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
             to[L::D / 4] = c;
         }
         if (g == 0) {
-            sm.ml[warp][2 * t] = make_float2(m0 - kLift, l0);
-            sm.ml[warp][2 * t + 1] = make_float2(m1 - kLift, l1);
+            sm.ml[warp][2 * t] = make_float2(d0, l0);
+            sm.ml[warp][2 * t + 1] = make_float2(d1, l1);
         }
         __syncthreads();
         const bool whole = take == count;

@@ -1,8 +1,14 @@
 // Eviction by accumulated attention weight (include/kvp.h, kvp_evict) and the placement policy made of it.
 //
-// Weights are accumulated as whole numbers of 2^-24, so that no order of summation shows, and the units of a group are ranked
-// by (accumulated weight, lower index first) through one 64-bit key, acc << 16 | (65535 - index), that no two units share.
-#include "kvp_common.cuh"
+// Weights are accumulated as whole numbers of 2^-24, so that no order of summation shows; the units of a group are ranked by
+// (accumulated weight, lower index first).
+//
+// Two forms. One pass: a CTA walks the steps of a group with the sums in registers; it reads every weight once and writes a bit for it, but
+// a step takes about two microseconds of barriers and latency, which only other groups on the SM hide. Two passes: one thread
+// per unit writes the sums of all steps to scratch, and the choices of the steps, independent of each other now, are made by as many CTAs as fit.
+#include <algorithm>
+
+#include "kvp_select.cuh"
 
 namespace kvp {
 
@@ -10,7 +16,6 @@ namespace {
 
 constexpr uint64_t kAccMost = (1ull << 48) - 1;
 constexpr uint32_t kEvictUnits = 32768;        // units of a group
-constexpr uint32_t kEvictThreads = 256;
 
 struct EvictK {
     const float* w;           // [steps][U]
@@ -19,91 +24,166 @@ struct EvictK {
     const uint32_t* kept;     // [W32] or null: every unit
     const int32_t* exist;     // [groups] or null: n
     uint32_t* out;            // [steps][W32]
+    uint64_t* sums;           // [steps][U], two passes only: the sums that step's choice goes by
     uint64_t U, W32;
-    uint32_t n, steps, budget, sink, recent, decay;
+    uint32_t n, steps, groups, budget, sink, recent, decay;
+    uint32_t chunk;           // steps of a CTA of the second pass
     bool aligned;             // n % 32 == 0: no word is shared by two groups
     bool before;              // a step's row is chosen before its weights are added
 };
 
-__device__ __forceinline__ uint64_t fixed_weight(float w)
-{
-    return w > 0.0f ? (uint64_t)__float2uint_rn(fminf(w, 128.0f) * 16777216.0f) : 0u;   // NaN counts as 0
-}
+__device__ __forceinline__ uint32_t fixed_weight(float w) { return __float2uint_rn(fminf(fmaxf(w, 0.0f), 128.0f) * 16777216.0f); }   // fmaxf: NaN counts as 0
 __device__ __forceinline__ uint64_t accumulated(uint64_t acc, uint32_t decay, float w)
 {
     if (decay != 65536u) acc = acc * decay >> 16;
-    return min(acc + fixed_weight(w), kAccMost);
+    acc += fixed_weight(w);
+    return acc < kAccMost ? acc : kAccMost;
 }
-__device__ __forceinline__ uint64_t key_of(uint64_t acc, uint32_t i) { return acc << 16 | (65535u - i); }
-
-__global__ void __launch_bounds__(kEvictThreads) evict_kernel(const EvictK p)
+__device__ __forceinline__ uint64_t first_sum(const EvictK& p, uint64_t u)
 {
-    __shared__ uint32_t hist[256], number, need_s;
-    __shared__ uint64_t edge;
-    const uint32_t g = blockIdx.x, tid = threadIdx.x, lane = tid % 32;
+    const int64_t a = p.acc_in ? p.acc_in[u] : 0;
+    return a < 0 ? 0u : min((uint64_t)a, kAccMost);
+}
+
+// Lane j's words of round j: who may be chosen, and who is protected
+struct Members {
+    uint32_t cand, safe, left;
+};
+__device__ __forceinline__ Members members_of(const EvictK& p, uint32_t g)
+{
+    const uint32_t T = blockDim.x, tid = threadIdx.x, lane = tid & 31;
     const uint64_t first = (uint64_t)g * p.n;
     const uint32_t e = p.exist ? (uint32_t)min(max(p.exist[g], 0), (int32_t)p.n) : p.n;
-    const uint32_t left = p.budget - min(min(e, p.sink + p.recent), p.budget);
-    auto safe = [&](uint32_t i) { return i < p.sink || i + p.recent >= e; };
-    auto old = [&](uint32_t i) { return !p.kept || (p.kept[(first + i) >> 5] >> ((first + i) & 31) & 1u); };
-    uint64_t* acc = reinterpret_cast<uint64_t*>(p.acc + first);
-    for (uint32_t i = tid; i < p.n; i += kEvictThreads) {
-        const int64_t a = p.acc_in ? p.acc_in[first + i] : 0;
-        acc[i] = a < 0 ? 0u : min((uint64_t)a, kAccMost);
+    Members m = {0, 0, p.budget - min(min(e, p.sink + p.recent), p.budget)};
+    for (uint32_t j = 0; j * T < p.n; ++j) {
+        const uint32_t i = j * T + tid;
+        const bool in = i < e, safe = in && (i < p.sink || i + p.recent >= e);
+        const bool old = in && !safe && (!p.kept || (p.kept[(first + i) >> 5] >> ((first + i) & 31) & 1u));
+        const uint32_t c = __ballot_sync(0xFFFFFFFFu, old), s = __ballot_sync(0xFFFFFFFFu, safe);
+        if (lane == j) { m.cand = c; m.safe = s; }
     }
-    for (uint32_t s = 0; s < p.steps; ++s) {
-        const float* w = p.w + s * p.U + first;
-        if (tid == 0) number = 0;
-        __syncthreads();
-        if (!p.before)
-            for (uint32_t i = tid; i < p.n; i += kEvictThreads) acc[i] = accumulated(acc[i], p.decay, w[i]);
-        uint32_t here = 0;
-        for (uint32_t i = tid; i < e; i += kEvictThreads) here += !safe(i) && old(i);
-        atomicAdd(&number, here);
-        __syncthreads();
-        uint64_t K = 0;
-        uint32_t need = left;
-        if (left == 0) {
-            K = ~0ull;
-        } else if (number > left) {
-            for (int sh = 56; sh >= 0; sh -= 8) {
-                hist[tid] = 0;
-                __syncthreads();
-                for (uint32_t i = tid; i < e; i += kEvictThreads) {
-                    const uint64_t k = key_of(acc[i], i);
-                    if (!safe(i) && old(i) && (sh == 56 || k >> (sh + 8) == K >> (sh + 8))) atomicAdd(&hist[k >> sh & 255u], 1u);
-                }
-                __syncthreads();
-                if (tid == 0) {
-                    uint32_t d = 255;
-                    while (hist[d] < need) need -= hist[d--];
-                    need_s = need;
-                    edge = K | (uint64_t)d << sh;
-                }
-                __syncthreads();
-                need = need_s;
-                K = edge;
-                __syncthreads();
-            }
-        }
-        uint32_t* row = p.out + s * p.W32;
-        for (uint32_t i = tid; i - lane < p.n; i += kEvictThreads) {
-            const bool in = i < e && (safe(i) || (left && old(i) && key_of(acc[i], i) >= K));
-            const uint32_t bits = __ballot_sync(0xFFFFFFFFu, in);
-            if (lane == 0) {
-                const uint64_t at = first + i;
-                const uint32_t sh = (uint32_t)at & 31u;
-                if (p.aligned) {
-                    row[at >> 5] = bits;
+    return m;
+}
+
+// One pass. The sums of a group, 48 bits each, are in shared memory as lower words and upper half-words (24 KB for 4096 units: seven CTAs an SM,
+// so that 1036 groups of that size are worked on at once); a step's first pass adds its weights.
+struct SumsRow {
+    const EvictK& p;
+    uint32_t* lo;
+    uint16_t* hi;
+    const float* w;           // the weights to be added, or null
+    bool plain;               // no decay, and no sum can reach 2^48
+    __device__ __forceinline__ uint64_t key(uint32_t unit) const { return (uint64_t)hi[unit] << 32 | lo[unit]; }
+    __device__ __forceinline__ void again(uint32_t j0, uint64_t (&k)[kBatch]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) k[i] = key(min((j0 + i) * blockDim.x + threadIdx.x, p.n - 1));
+    }
+    __device__ __forceinline__ void load(uint32_t j0, uint64_t (&k)[kBatch]) const
+    {
+        if (!w) return again(j0, k);
+        float x[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) x[i] = __ldcs(w + min((j0 + i) * blockDim.x + threadIdx.x, p.n - 1));
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const uint32_t unit = (j0 + i) * blockDim.x + threadIdx.x;
+            k[i] = 0;
+            if (unit < p.n) {
+                if (plain) {
+                    const uint32_t add = fixed_weight(x[i]), l = lo[unit] + add;
+                    uint32_t h = hi[unit];
+                    lo[unit] = l;
+                    if (l < add) hi[unit] = (uint16_t)++h;
+                    k[i] = (uint64_t)h << 32 | l;
                 } else {
-                    if (bits << sh) atomicOr(row + (at >> 5), bits << sh);
-                    if (sh && bits >> (32u - sh)) atomicOr(row + (at >> 5) + 1, bits >> (32u - sh));
+                    k[i] = accumulated(key(unit), p.decay, x[i]);
+                    lo[unit] = (uint32_t)k[i];
+                    hi[unit] = (uint16_t)(k[i] >> 32);
                 }
             }
         }
-        __syncthreads();
-        if (p.before)
-            for (uint32_t i = tid; i < p.n; i += kEvictThreads) acc[i] = accumulated(acc[i], p.decay, w[i]);
+    }
+};
+
+__global__ void __launch_bounds__(1024, 1) evict_kernel(const EvictK p)
+{
+    extern __shared__ uint32_t sums[];
+    __shared__ SelectShared<uint64_t> sm;
+    __shared__ uint32_t upper;
+    const uint32_t g = blockIdx.x, tid = threadIdx.x, rounds = (p.n + blockDim.x - 1) / blockDim.x;
+    const uint64_t first = (uint64_t)g * p.n;
+    if (tid == 0) upper = 0;
+    clear(sm);
+    const Members m = members_of(p, g);
+    SumsRow row = {p, sums, reinterpret_cast<uint16_t*>(sums + p.n), nullptr, false};
+    uint32_t most = 0;
+    for (uint32_t i = tid; i < p.n; i += blockDim.x) {
+        const uint64_t x = first_sum(p, first + i);
+        row.lo[i] = (uint32_t)x;
+        row.hi[i] = (uint16_t)(x >> 32);
+        most = max(most, (uint32_t)(x >> 32));
+    }
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+    if ((tid & 31) == 0) atomicMax(&upper, most);
+    __syncthreads();
+    row.plain = p.decay == 65536u && upper + (uint64_t)p.steps / 2 + 1 < 0xFFFFu;             // a step adds 2^31 at most
+    Band<uint64_t> band;
+    band.valid = band.moved = false;
+    // a row that is chosen before its weights are added is what the step before left
+    for (uint32_t s = 0; s < p.steps; ++s) {
+        row.w = !p.before ? p.w + s * p.U + first : s ? p.w + (s - 1) * p.U + first : nullptr;
+        const uint32_t word = choose<uint64_t>(row, rounds, m.cand, m.left, band, sm, s);
+        put_words(p.out + s * p.W32, first, p.n, p.aligned, word | m.safe);
+    }
+    if (p.before) return;                                          // a policy: nobody asks for the sums
+    for (uint32_t i = tid; i < p.n; i += blockDim.x) p.acc[first + i] = (int64_t)row.key(i);   // written by this thread
+}
+
+// Two passes, the first: the sums that the steps' choices go by.
+__global__ void __launch_bounds__(128) sums_kernel(const EvictK p)
+{
+    const uint64_t u = (uint64_t)blockIdx.x * 128 + threadIdx.x;
+    if (u >= p.U) return;
+    uint64_t acc = first_sum(p, u);
+    const float* w = p.w + u;
+    uint64_t* to = p.sums + u;
+#pragma unroll 32
+    for (uint32_t s = 0; s < p.steps; ++s) {
+        const uint64_t was = acc;
+        acc = accumulated(acc, p.decay, __ldcs(w + s * p.U));
+        to[s * p.U] = p.before ? was : acc;
+    }
+    if (!p.before) p.acc[u] = (int64_t)acc;
+}
+
+// The second: a CTA chooses for some consecutive steps of a group.
+struct StoredRow {
+    const uint64_t* from;
+    uint32_t n;
+    __device__ __forceinline__ uint64_t key(uint32_t unit) const { return from[unit]; }
+    __device__ __forceinline__ void load(uint32_t j0, uint64_t (&k)[kBatch]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) k[i] = from[min((j0 + i) * blockDim.x + threadIdx.x, n - 1)];
+    }
+    __device__ __forceinline__ void again(uint32_t j0, uint64_t (&k)[kBatch]) const { load(j0, k); }
+};
+
+__global__ void __launch_bounds__(1024, 1) choose_kernel(const EvictK p)
+{
+    __shared__ SelectShared<uint64_t> sm;
+    const uint32_t g = blockIdx.x % p.groups, s0 = blockIdx.x / p.groups * p.chunk, s1 = min(s0 + p.chunk, p.steps);
+    const uint32_t rounds = (p.n + blockDim.x - 1) / blockDim.x;
+    const uint64_t first = (uint64_t)g * p.n;
+    clear(sm);
+    const Members m = members_of(p, g);
+    Band<uint64_t> band;
+    band.valid = band.moved = false;
+    for (uint32_t s = s0; s < s1; ++s) {
+        StoredRow row = {p.sums + s * p.U + first, p.n};
+        const uint32_t word = choose<uint64_t>(row, rounds, m.cand, m.left, band, sm, s);
+        put_words(p.out + s * p.W32, first, p.n, p.aligned, word | m.safe);
     }
 }
 
@@ -118,16 +198,41 @@ int check_evict(const kvp_evict_params* a)
 int launch_evict(const kvp_evict_params* a, const float* weights, const int64_t* acc_in, int64_t* acc, const uint32_t* kept,
                  const int32_t* exist, uint32_t* rows, bool before, cudaStream_t st)
 {
-    EvictK k;
+    EvictK k = {};
     k.w = weights; k.acc_in = acc_in; k.acc = acc; k.kept = kept; k.exist = exist; k.out = rows;
     k.n = a->units_per_group; k.steps = a->steps; k.budget = a->budget; k.sink = a->sink; k.recent = a->recent; k.decay = a->decay_q;
     k.U = (uint64_t)a->groups * k.n;
     k.W32 = (k.U + 31) / 32;
     k.aligned = k.n % 32 == 0;
     k.before = before;
+    k.groups = a->groups;
     if (!k.aligned) KVP_CUDA(cudaMemsetAsync(rows, 0, (size_t)a->steps * k.W32 * 4, st));
-    evict_kernel<<<a->groups, kEvictThreads, 0, st>>>(k);
-    KVP_CUDA(cudaGetLastError());
+    const uint32_t n = k.n;
+    // A step of the one-pass form takes about 1.5 us as long as the groups fit the SMs' registers at once; the other form moves 24 bytes
+    // per unit and step, for which 4 ps are about right, in kernels that take 10 us at least.
+    const uint64_t waves = (k.groups + 1035) / 1036, all = k.U * a->steps;
+    const size_t bytes = all * 8;
+    const bool two = a->steps > 1 && bytes <= ((size_t)1 << 30) && 1.5e-6 * (double)(waves * a->steps) > 4e-12 * (double)all + 10e-6;
+    if (two) {
+        int dev = 0;
+        KVP_CUDA(cudaGetDevice(&dev));
+        const int prc = retain_in_pool(dev, bytes);
+        if (prc) return prc;
+        KVP_CUDA(cudaMallocAsync(&k.sums, bytes, st));
+        sums_kernel<<<(uint32_t)((k.U + 127) / 128), 128, 0, st>>>(k);
+        k.chunk = std::max(1u, (uint32_t)std::min<uint64_t>(16, (uint64_t)k.groups * a->steps / (148 * 16)));
+    }
+    const uint32_t threads = select_threads(n);
+    if (two) {
+        choose_kernel<<<k.groups * ((a->steps + k.chunk - 1) / k.chunk), threads, 0, st>>>(k);
+    } else {
+        const uint32_t smem = (n * 6 + 15) / 16 * 16;
+        if (smem > 40 * 1024) KVP_CUDA(cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        evict_kernel<<<k.groups, threads, smem, st>>>(k);
+    }
+    const cudaError_t le = cudaGetLastError();
+    if (two) KVP_CUDA(cudaFreeAsync(k.sums, st));
+    KVP_CUDA(le);
     return KVP_OK;
 }
 

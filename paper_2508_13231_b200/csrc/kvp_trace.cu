@@ -5,7 +5,9 @@
 // shared-memory histogram, the rest by ranking the keys of that bin, ties going to the lower unit index. A fused single-pass form
 // (one CTA per group walking the steps, state in registers) serves layered or growing traces and those whose score
 // matrix would exceed the scratch budget.
-#include "kvp_common.cuh"
+#include <algorithm>
+
+#include "kvp_select.cuh"
 
 namespace kvp {
 
@@ -404,34 +406,37 @@ trace_select_kernel(const TraceK k, uint32_t want, uint32_t U, const int32_t* __
     select_step<UPT, FULL>(key, k, want, k.topk, gbase, t, sm);
 }
 
-// Access bitmaps of recorded weights: the same selection, one CTA per (group, step), on the bits of positive floats, which order
-// as whole numbers do. A unit that received nothing (or NaN) has key 0 and is never picked.
-template <int UPT, bool FULL>
-__global__ void __launch_bounds__(UPT == 32 ? 1024 : 512, UPT == 32 ? 1 : 3)
-weights_select_kernel(const TraceK k, uint32_t want, uint64_t U, const float* __restrict__ weights)
-{
-    __shared__ SelectSmem sm;
-    __shared__ uint32_t received;
-    const uint32_t g = blockIdx.x % k.groups, t = blockIdx.x / k.groups, T = blockDim.x, tid = threadIdx.x;
-    const uint32_t gbase = g * k.n;
-    select_reset(sm);
-    if (tid == 0) received = 0;
-    int32_t key[UPT];
-    uint32_t here = 0;
-    const float* from = weights + t * U + gbase + tid;
+// Access bitmaps of recorded weights, on the bits of positive floats, which order as whole numbers do (a unit that received nothing, or NaN, has key
+// 0 and is never picked). A CTA takes some consecutive steps of a group, in which the threshold moves little.
+struct WeightsRow {
+    const float* from;
+    uint32_t n;
+    static __device__ __forceinline__ uint32_t key_of(float w) { return w > 0.0f ? __float_as_uint(w) : 0u; }
+    __device__ __forceinline__ void load(uint32_t j0, uint32_t (&k)[kBatch]) const
+    {
+        float w[kBatch];                                     // all loads under way at once: none depends on a condition
 #pragma unroll
-    for (int j = 0; j < UPT; ++j) {
-        const float w = (FULL || j * T + tid < k.n) ? __ldcs(from + j * T) : 0.0f;
-        key[j] = w > 0.0f ? __float_as_int(w) : 0;
-        here += key[j] > 0;
+        for (int i = 0; i < kBatch; ++i) w[i] = from[min((j0 + i) * blockDim.x + threadIdx.x, n - 1)];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) k[i] = key_of(w[i]);
     }
-    __syncthreads();
-    here = block_sum(here, &received);
-    if (here) {
-        select_step<UPT, FULL>(key, k, want, min(k.topk, here), gbase, t, sm);
-    } else if (k.aligned) {                                  // an empty row
-        uint32_t* row = k.out + (size_t)t * k.W32 + (gbase >> 5);
-        for (uint32_t i = tid; i < k.n / 32; i += T) row[i] = 0;
+    __device__ __forceinline__ void again(uint32_t j0, uint32_t (&k)[kBatch]) const { load(j0, k); }
+    __device__ __forceinline__ uint32_t key(uint32_t unit) const { return key_of(from[unit]); }
+};
+
+__global__ void __launch_bounds__(1024, 1) weights_select_kernel(const TraceK k, uint32_t chunk, uint64_t U, const float* __restrict__ weights)
+{
+    __shared__ SelectShared<uint32_t> sm;
+    const uint32_t g = blockIdx.x % k.groups, t0 = blockIdx.x / k.groups * chunk, t1 = min(t0 + chunk, k.steps);
+    const uint32_t rounds = (k.n + blockDim.x - 1) / blockDim.x, cand = units_there(k.n);
+    const uint64_t first = (uint64_t)g * k.n;
+    clear(sm);
+    Band<uint32_t> band;
+    band.valid = band.moved = false;
+    for (uint32_t t = t0; t < t1; ++t) {
+        WeightsRow row = {weights + t * U + first, k.n};
+        const uint32_t word = choose<uint32_t>(row, rounds, cand, k.topk, band, sm, t);
+        put_words(k.out + (size_t)t * k.W32, first, k.n, k.aligned, word);
     }
 }
 
@@ -454,23 +459,9 @@ extern "C" int kvp_trace_weights(uint32_t groups, uint32_t units_per_group, uint
     k.out = access_bitmaps;
     k.aligned = units_per_group % 32 == 0;
     if (!k.aligned) KVP_CUDA(cudaMemsetAsync(access_bitmaps, 0, (size_t)steps * k.W32 * 4, st));
-    const uint32_t n = units_per_group, grid = groups * steps;
-    int su = n > 8192 ? 32 : 1;
-    while (su < 16 && (n + su - 1) / su > 128) su *= 2;
-    const uint32_t ST = ((n + su - 1) / su + 31) / 32 * 32, want = select_want(topk, ST);
-    const bool full = (uint64_t)su * ST == n;
-#define KVP_SELECT(UPT)                                                                      \
-    if (full) weights_select_kernel<UPT, true><<<grid, ST, 0, st>>>(k, want, U, weights);    \
-    else weights_select_kernel<UPT, false><<<grid, ST, 0, st>>>(k, want, U, weights)
-    switch (su) {
-        case 1: KVP_SELECT(1); break;
-        case 2: KVP_SELECT(2); break;
-        case 4: KVP_SELECT(4); break;
-        case 8: KVP_SELECT(8); break;
-        case 16: KVP_SELECT(16); break;
-        default: KVP_SELECT(32); break;
-    }
-#undef KVP_SELECT
+    // several steps to a CTA once there are enough CTAs
+    const uint32_t chunk = std::max(1u, std::min(16u, groups * steps / (148u * 16u)));
+    weights_select_kernel<<<groups * ((steps + chunk - 1) / chunk), select_threads(k.n), 0, st>>>(k, chunk, U, weights);
     KVP_CUDA(cudaGetLastError());
     return KVP_OK;
 }

@@ -135,7 +135,7 @@ def check(kvp, q, cache, table, lens, units, unit, scale=None, **kw):
     assert np.all(off <= room), (off / room).max()
     half = 2.0 ** -8 if q.dtype == BF16 else 2.0 ** -11
     room = half * np.abs(want["out"]) + (2.0 ** -10 + 2.0 ** -13 + 2 * score[..., None]) * want["size"] + \
-        2.0 ** -22 * (want["count"] * want["top"] * want["vscale"])[..., None] + 2.0 ** -25
+        2.0 ** -31 * (want["count"] * want["top"] * np.maximum(want["vscale"], 1))[..., None] + 2.0 ** -25
     bad = np.abs(out - want["out"]) / room
     assert np.all(bad <= 1), bad.max()
     group = q.shape[2] // weights.shape[1]
