@@ -32,7 +32,8 @@ struct EvictK {
     bool before;              // a step's row is chosen before its weights are added
 };
 
-__device__ __forceinline__ uint32_t fixed_weight(float w) { return __float2uint_rn(fminf(fmaxf(w, 0.0f), 128.0f) * 16777216.0f); }   // fmaxf: NaN counts as 0
+// NaN and negative weights convert to 0 (fminf would make 128 of NaN)
+__device__ __forceinline__ uint32_t fixed_weight(float w) { return min(__float2uint_rn(w * 16777216.0f), 0x80000000u); }
 __device__ __forceinline__ uint64_t accumulated(uint64_t acc, uint32_t decay, float w)
 {
     if (decay != 65536u) acc = acc * decay >> 16;
@@ -67,6 +68,8 @@ __device__ __forceinline__ Members members_of(const EvictK& p, uint32_t g)
 
 // One pass. The sums of a group, 48 bits each, are in shared memory as lower words and upper half-words (24 KB for 4096 units: seven CTAs an SM,
 // so that 1036 groups of that size are worked on at once); a step's first pass adds its weights.
+// FULL: the rounds end with the last unit, and come in eights.
+template <int T, bool FULL>
 struct SumsRow {
     const EvictK& p;
     uint32_t* lo;
@@ -74,51 +77,62 @@ struct SumsRow {
     const float* w;           // the weights to be added, or null
     bool plain;               // no decay, and no sum can reach 2^48
     __device__ __forceinline__ uint64_t key(uint32_t unit) const { return (uint64_t)hi[unit] << 32 | lo[unit]; }
+    __device__ __forceinline__ uint32_t unit_of(uint32_t j) const { return FULL ? j * T + threadIdx.x : min(j * T + threadIdx.x, p.n - 1); }
     __device__ __forceinline__ void again(uint32_t j0, uint64_t (&k)[kBatch]) const
     {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) k[i] = key(min((j0 + i) * blockDim.x + threadIdx.x, p.n - 1));
+        for (int i = 0; i < kBatch; ++i) k[i] = key(unit_of(j0 + i));
     }
-    __device__ __forceinline__ void load(uint32_t j0, uint64_t (&k)[kBatch]) const
+    template <bool FIRST>
+    __device__ __forceinline__ void load(uint32_t j0, uint64_t least, uint64_t most, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
     {
-        if (!w) return again(j0, k);
-        float x[kBatch];
+        uint64_t k[kBatch];
+        if (FIRST && w) {
+            float x[kBatch];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) x[i] = __ldcs(w + min((j0 + i) * blockDim.x + threadIdx.x, p.n - 1));
+            for (int i = 0; i < kBatch; ++i) x[i] = __ldcs(w + unit_of(j0 + i));
+            if (plain) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const uint32_t unit = (j0 + i) * blockDim.x + threadIdx.x;
-            k[i] = 0;
-            if (unit < p.n) {
-                if (plain) {
-                    const uint32_t add = fixed_weight(x[i]), l = lo[unit] + add;
-                    uint32_t h = hi[unit];
-                    lo[unit] = l;
-                    if (l < add) hi[unit] = (uint16_t)++h;
+                for (int i = 0; i < kBatch; ++i) {
+                    const uint32_t unit = unit_of(j0 + i), add = fixed_weight(x[i]);
+                    const bool there = FULL || (j0 + i) * T + threadIdx.x < p.n;
+                    const uint32_t l = lo[unit] + add, h = hi[unit] + (l < add);
+                    if (there) lo[unit] = l;
+                    if (there && l < add) hi[unit] = (uint16_t)h;
                     k[i] = (uint64_t)h << 32 | l;
-                } else {
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    const uint32_t unit = unit_of(j0 + i);
                     k[i] = accumulated(key(unit), p.decay, x[i]);
-                    lo[unit] = (uint32_t)k[i];
-                    hi[unit] = (uint16_t)(k[i] >> 32);
+                    if (FULL || (j0 + i) * T + threadIdx.x < p.n) {
+                        lo[unit] = (uint32_t)k[i];
+                        hi[unit] = (uint16_t)(k[i] >> 32);
+                    }
                 }
             }
+        } else {
+            again(j0, k);
         }
+        ballots(k, least, most, a, b);
     }
 };
 
-__global__ void __launch_bounds__(1024, 1) evict_kernel(const EvictK p)
+template <int T, bool FULL>
+__global__ void __launch_bounds__(T) evict_kernel(const EvictK p)
 {
     extern __shared__ uint32_t sums[];
     __shared__ SelectShared<uint64_t> sm;
     __shared__ uint32_t upper;
-    const uint32_t g = blockIdx.x, tid = threadIdx.x, rounds = (p.n + blockDim.x - 1) / blockDim.x;
+    const uint32_t g = blockIdx.x, tid = threadIdx.x, rounds = (p.n + T - 1) / T;
     const uint64_t first = (uint64_t)g * p.n;
     if (tid == 0) upper = 0;
     clear(sm);
     const Members m = members_of(p, g);
-    SumsRow row = {p, sums, reinterpret_cast<uint16_t*>(sums + p.n), nullptr, false};
+    SumsRow<T, FULL> row = {p, sums, reinterpret_cast<uint16_t*>(sums + p.n), nullptr, false};
     uint32_t most = 0;
-    for (uint32_t i = tid; i < p.n; i += blockDim.x) {
+    for (uint32_t i = tid; i < p.n; i += T) {
         const uint64_t x = first_sum(p, first + i);
         row.lo[i] = (uint32_t)x;
         row.hi[i] = (uint16_t)(x >> 32);
@@ -133,11 +147,11 @@ __global__ void __launch_bounds__(1024, 1) evict_kernel(const EvictK p)
     // a row that is chosen before its weights are added is what the step before left
     for (uint32_t s = 0; s < p.steps; ++s) {
         row.w = !p.before ? p.w + s * p.U + first : s ? p.w + (s - 1) * p.U + first : nullptr;
-        const uint32_t word = choose<uint64_t>(row, rounds, m.cand, m.left, band, sm, s);
+        const uint32_t word = choose<uint64_t, T>(row, rounds, m.cand, m.left, band, sm, s);
         put_words(p.out + s * p.W32, first, p.n, p.aligned, word | m.safe);
     }
     if (p.before) return;                                          // a policy: nobody asks for the sums
-    for (uint32_t i = tid; i < p.n; i += blockDim.x) p.acc[first + i] = (int64_t)row.key(i);   // written by this thread
+    for (uint32_t i = tid; i < p.n; i += T) p.acc[first + i] = (int64_t)row.key(i);           // written by this thread
 }
 
 // Two passes, the first: the sums that the steps' choices go by.
@@ -158,33 +172,57 @@ __global__ void __launch_bounds__(128) sums_kernel(const EvictK p)
 }
 
 // The second: a CTA chooses for some consecutive steps of a group.
+template <int T>
 struct StoredRow {
     const uint64_t* from;
     uint32_t n;
     __device__ __forceinline__ uint64_t key(uint32_t unit) const { return from[unit]; }
-    __device__ __forceinline__ void load(uint32_t j0, uint64_t (&k)[kBatch]) const
+    __device__ __forceinline__ void again(uint32_t j0, uint64_t (&k)[kBatch]) const
     {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) k[i] = from[min((j0 + i) * blockDim.x + threadIdx.x, n - 1)];
+        for (int i = 0; i < kBatch; ++i) k[i] = from[min((j0 + i) * T + threadIdx.x, n - 1)];
     }
-    __device__ __forceinline__ void again(uint32_t j0, uint64_t (&k)[kBatch]) const { load(j0, k); }
+    template <bool FIRST>
+    __device__ __forceinline__ void load(uint32_t j0, uint64_t least, uint64_t most, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
+    {
+        uint64_t k[kBatch];
+        again(j0, k);
+        ballots(k, least, most, a, b);
+    }
 };
 
-__global__ void __launch_bounds__(1024, 1) choose_kernel(const EvictK p)
+template <int T>
+__global__ void __launch_bounds__(T) choose_kernel(const EvictK p)
 {
     __shared__ SelectShared<uint64_t> sm;
     const uint32_t g = blockIdx.x % p.groups, s0 = blockIdx.x / p.groups * p.chunk, s1 = min(s0 + p.chunk, p.steps);
-    const uint32_t rounds = (p.n + blockDim.x - 1) / blockDim.x;
+    const uint32_t rounds = (p.n + T - 1) / T;
     const uint64_t first = (uint64_t)g * p.n;
     clear(sm);
     const Members m = members_of(p, g);
     Band<uint64_t> band;
     band.valid = band.moved = false;
     for (uint32_t s = s0; s < s1; ++s) {
-        StoredRow row = {p.sums + s * p.U + first, p.n};
-        const uint32_t word = choose<uint64_t>(row, rounds, m.cand, m.left, band, sm, s);
+        StoredRow<T> row = {p.sums + s * p.U + first, p.n};
+        const uint32_t word = choose<uint64_t, T>(row, rounds, m.cand, m.left, band, sm, s);
         put_words(p.out + s * p.W32, first, p.n, p.aligned, word | m.safe);
     }
+}
+
+template <int T>
+int launch_choice(const EvictK& k, bool two, cudaStream_t st)
+{
+    if (two) {
+        choose_kernel<T><<<k.groups * ((k.steps + k.chunk - 1) / k.chunk), T, 0, st>>>(k);
+        return KVP_OK;
+    }
+    const bool full = k.n % (kBatch * T) == 0;
+    const uint32_t smem = (k.n * 6 + 15) / 16 * 16;
+    const void* f = full ? (const void*)evict_kernel<T, true> : (const void*)evict_kernel<T, false>;
+    if (smem > 40 * 1024) KVP_CUDA(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (full) evict_kernel<T, true><<<k.groups, T, smem, st>>>(k);
+    else evict_kernel<T, false><<<k.groups, T, smem, st>>>(k);
+    return KVP_OK;
 }
 
 int check_evict(const kvp_evict_params* a)
@@ -223,15 +261,11 @@ int launch_evict(const kvp_evict_params* a, const float* weights, const int64_t*
         k.chunk = std::max(1u, (uint32_t)std::min<uint64_t>(16, (uint64_t)k.groups * a->steps / (148 * 16)));
     }
     const uint32_t threads = select_threads(n);
-    if (two) {
-        choose_kernel<<<k.groups * ((a->steps + k.chunk - 1) / k.chunk), threads, 0, st>>>(k);
-    } else {
-        const uint32_t smem = (n * 6 + 15) / 16 * 16;
-        if (smem > 40 * 1024) KVP_CUDA(cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        evict_kernel<<<k.groups, threads, smem, st>>>(k);
-    }
+    const int rc = threads == 128 ? launch_choice<128>(k, two, st) : threads == 256 ? launch_choice<256>(k, two, st)
+                 : threads == 512 ? launch_choice<512>(k, two, st) : launch_choice<1024>(k, two, st);
     const cudaError_t le = cudaGetLastError();
     if (two) KVP_CUDA(cudaFreeAsync(k.sums, st));
+    if (rc) return rc;
     KVP_CUDA(le);
     return KVP_OK;
 }

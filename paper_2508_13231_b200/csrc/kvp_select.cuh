@@ -14,7 +14,10 @@ namespace kvp {
 
 constexpr uint32_t kBins256 = 256;
 constexpr uint32_t kListed = 128;             // keys that can be ranked
-constexpr uint32_t kBandGoal = 64;            // a band should hold this many keys, or up to four times as many
+constexpr uint32_t kFew = 128;                // keys of a band found by the histogram
+// A band should hold this many keys, or up to twice as many: sums move steadily, weights by a drift of their own.
+template <typename Key>
+constexpr uint32_t kBandGoal = sizeof(Key) == 8 ? 32 : 64;
 
 constexpr int kBatch = 8;                     // rounds whose keys are loaded together
 
@@ -88,8 +91,8 @@ __device__ __forceinline__ void find_bin(SelectShared<Key>& sm, uint32_t need, u
     }
 }
 
-// `Row` gives the keys: load(j0, k) those of this thread in rounds j0 .. j0 + 7 for the first time (which may change them: the weights of a
-// step are added then), again(j0, k) once more, key(unit) any unit's. Rounds behind the last unit give any key at all: `cand`, lane j's word of the
+// `Row` gives the keys: again(j0, k) those of this thread in rounds j0 .. j0 + 7, key(unit) any unit's, load<..>(j0, lo, hi, a, b) the ballots of
+// >= lo and > hi over these rounds, for the first time with FIRST (which may change the keys: the weights of a step are added then). Rounds behind the last unit give any key at all: `cand`, lane j's word of the
 // candidates in round j, says which count. 32-bit keys: of the units in it, those with key 0 are no candidates either.
 
 // One digit of the search for a band: of the candidates at a distance of at most `span` from its base, counted by distance >> sh.
@@ -164,7 +167,7 @@ __device__ Found find_band(Row& row, uint32_t rounds, uint32_t cand, uint32_t le
     const uint32_t top = sm.top;
     int rem = bits_needed(top - base);
     uint64_t span = top - base;
-    while (rem > 0 && equal > 2 * kBandGoal) {
+    while (rem > 0 && equal > kFew) {
         const int sh = max(rem - 8, 0);
         one_digit(sm, row, rounds, cand, sh, span, need, [&](Key x) { const uint32_t c = coarse(x); return c < base ? ~0ull : (uint64_t)(c - base); });
         base += (uint32_t)sm.edge << sh;
@@ -178,7 +181,7 @@ __device__ Found find_band(Row& row, uint32_t rounds, uint32_t cand, uint32_t le
     band.bits = bits_needed(hi - band.lo);
     band.valid = true;
     if (sizeof(Key) == 8 && equal > kListed) {                    // keys that share their upper 24 bits
-        while (band.bits > 0 && equal > kBandGoal) {
+        while (band.bits > 0 && equal > kFew) {
             const int sh = max(band.bits - 8, 0);
             const uint64_t wide = (1ull << band.bits) - 1;
             one_digit(sm, row, rounds, cand, sh, wide, need, [&](Key x) { return (uint64_t)(x - band.lo); });
@@ -191,23 +194,38 @@ __device__ Found find_band(Row& row, uint32_t rounds, uint32_t cand, uint32_t le
     return band.bits == 0 && equal > kListed ? Found::kTies : Found::kBand;
 }
 
-// Lane j's words of round j: keys from `lo` on and keys above `hi`, of the candidates. FIRST: by row.load
+// of eight words the one whose number is lane % 8
+__device__ __forceinline__ uint32_t own_of(const uint32_t (&x)[kBatch], uint32_t lane)
+{
+    const uint32_t a = lane & 1u ? x[1] : x[0], b = lane & 1u ? x[3] : x[2], c = lane & 1u ? x[5] : x[4], d = lane & 1u ? x[7] : x[6];
+    const uint32_t e = lane & 2u ? b : a, f = lane & 2u ? d : c;
+    return lane & 4u ? f : e;
+}
+
+// the ballots of keys at hand
+template <typename Key>
+__device__ __forceinline__ void ballots(const Key (&k)[kBatch], Key lo, Key hi, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch])
+{
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+        a[i] = __ballot_sync(0xFFFFFFFFu, k[i] >= lo);
+        b[i] = __ballot_sync(0xFFFFFFFFu, k[i] > hi);
+    }
+}
+
+// Lane j's words of round j: keys from `lo` on and keys above `hi`, of the candidates.
 template <bool FIRST, typename Key, typename Row>
 __device__ __forceinline__ void split(Row& row, uint32_t rounds, uint32_t cand, Key lo, Key hi, uint32_t& from, uint32_t& above)
 {
     const uint32_t lane = threadIdx.x & 31;
     from = above = 0;
     for (uint32_t j0 = 0; j0 < rounds; j0 += kBatch) {
-        Key k[kBatch];
-        if (FIRST) row.load(j0, k);
-        else row.again(j0, k);
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const uint32_t a = __ballot_sync(0xFFFFFFFFu, k[i] >= lo), b = __ballot_sync(0xFFFFFFFFu, k[i] > hi);
-            if (lane == j0 + i) {
-                from = a;
-                above = b;
-            }
+        uint32_t a[kBatch], b[kBatch];
+        row.template load<FIRST>(j0, lo, hi, a, b);
+        const uint32_t x = own_of(a, lane), y = own_of(b, lane);
+        if ((lane & ~7u) == j0) {
+            from = x;
+            above = y;
         }
     }
     from &= cand;
@@ -258,26 +276,25 @@ __device__ uint32_t choose_ties(Row& row, uint32_t rounds, uint32_t cand, uint32
 
 // -> lane j's word of round j: the chosen units. turn: a number that changes by one from call to call. Every thread of the CTA calls it; the
 // row's keys have all been loaded when it returns.
-template <typename Key, typename Row>
+template <typename Key, int T, typename Row>
 __device__ __forceinline__ uint32_t choose(Row& row, uint32_t rounds, uint32_t cand, uint32_t left, Band<Key>& band, SelectShared<Key>& sm,
                                            uint32_t turn)
 {
-    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32, warps = blockDim.x / 32, T = blockDim.x, now = turn & 1;
-    bool loaded = false, fresh = false;
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32, warps = T / 32, now = turn & 1;
+    bool loaded = false;
     if (left == 0 || !band.valid) {                                // loads only
-        for (uint32_t j0 = 0; j0 < rounds; j0 += kBatch) {
-            Key k[kBatch];
-            row.load(j0, k);
-        }
+        uint32_t from, above;
+        split<true>(row, rounds, cand, (Key)1, (Key)1, from, above);
+        __syncwarp();
         loaded = true;
         if (left == 0) return 0;
     }
-    while (true) {
+    // At most one band that misses, one that is found, and eight narrower ones in it
+    for (int attempt = 0; attempt < 12; ++attempt) {
         if (!band.valid) {
             const Found found = find_band(row, rounds, cand, left, band, sm);
-            fresh = true;
             if (found != Found::kBand) {
-                band.valid = band.moved = false;
+                band.valid = false;
                 if (found == Found::kTies) return choose_ties(row, rounds, cand, left, band.lo, sm);
                 if (sizeof(Key) == 8) return cand;
                 uint32_t from, above;
@@ -328,7 +345,7 @@ __device__ __forceinline__ uint32_t choose(Row& row, uint32_t rounds, uint32_t c
                 }
             }
             __syncthreads();
-            for (uint32_t e = tid; e < equal; e += T) {
+            for (uint32_t e = tid; e < equal; e += (uint32_t)T) {
                 const Key k = sm.list[e];
                 const uint32_t u = sm.unit[e];
                 uint32_t before = 0;
@@ -354,16 +371,17 @@ __device__ __forceinline__ uint32_t choose(Row& row, uint32_t rounds, uint32_t c
             band.valid = band.moved = false;
             return choose_ties(row, rounds, cand, left, edge, sm);
         }
-        // The next row's band: around the threshold, moved on by as much as it moved last, and wide enough for kBandGoal keys or more.
-        if (in_band < kBandGoal && band.bits < (int)sizeof(Key) * 8 - 4) ++band.bits;
-        else if (in_band > 4 * kBandGoal && band.bits > 0) --band.bits;
+        // The next row's band: around the threshold, moved on by as much as it moved last, and wide enough for kBandGoal keys.
+        if (in_band < kBandGoal<Key> && band.bits < (int)sizeof(Key) * 8 - 4) ++band.bits;
+        else if (in_band > 2 * kBandGoal<Key> && band.bits > 0) --band.bits;
         const Key half = ((Key)1 << band.bits) / 2;
-        const Key centre = edge + (sizeof(Key) == 8 && band.moved && !fresh ? edge - band.last : 0);    // wraps where it moved down
+        const Key centre = edge + (sizeof(Key) == 8 && band.moved ? edge - band.last : 0);    // wraps where it moved down
         band.lo = centre > half && centre < (Key)1 << (sizeof(Key) * 8 - 1) ? centre - half : sizeof(Key) == 4;
         band.last = edge;
         band.moved = true;
         return word;
     }
+    return 0;                                                      // not reached
 }
 
 // Lane j's word of round j: which units there are

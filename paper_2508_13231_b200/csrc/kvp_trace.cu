@@ -408,34 +408,56 @@ trace_select_kernel(const TraceK k, uint32_t want, uint32_t U, const int32_t* __
 
 // Access bitmaps of recorded weights, on the bits of positive floats, which order as whole numbers do (a unit that received nothing, or NaN, has key
 // 0 and is never picked). A CTA takes some consecutive steps of a group, in which the threshold moves little.
+// FULL: the rounds end with the last unit, and come in eights.
+template <int T, bool FULL>
 struct WeightsRow {
     const float* from;
     uint32_t n;
     static __device__ __forceinline__ uint32_t key_of(float w) { return w > 0.0f ? __float_as_uint(w) : 0u; }
-    __device__ __forceinline__ void load(uint32_t j0, uint32_t (&k)[kBatch]) const
+    // all loads under way at once: none depends on a condition
+    __device__ __forceinline__ void weights(uint32_t j0, float (&w)[kBatch]) const
     {
-        float w[kBatch];                                     // all loads under way at once: none depends on a condition
+        const float* at = from + j0 * T + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) w[i] = from[min((j0 + i) * blockDim.x + threadIdx.x, n - 1)];
+        for (int i = 0; i < kBatch; ++i) w[i] = FULL ? at[i * T] : from[min((j0 + i) * T + threadIdx.x, n - 1)];
+    }
+    __device__ __forceinline__ void again(uint32_t j0, uint32_t (&k)[kBatch]) const
+    {
+        float w[kBatch];
+        weights(j0, w);
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) k[i] = key_of(w[i]);
     }
-    __device__ __forceinline__ void again(uint32_t j0, uint32_t (&k)[kBatch]) const { load(j0, k); }
+    // 0 < lo <= the bits of infinity, so a comparison of floats says the same as one of keys, and NaN or a negative weight fails it; hi may lie
+    // behind infinity, even where the bits are those of negative numbers, and is cut to it
+    template <bool FIRST>
+    __device__ __forceinline__ void load(uint32_t j0, uint32_t lo, uint32_t hi, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
+    {
+        float w[kBatch];
+        const float least = __uint_as_float(lo), most = __uint_as_float(min(hi, 0x7F800000u));
+        weights(j0, w);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            a[i] = __ballot_sync(0xFFFFFFFFu, w[i] >= least);
+            b[i] = __ballot_sync(0xFFFFFFFFu, w[i] > most);
+        }
+    }
     __device__ __forceinline__ uint32_t key(uint32_t unit) const { return key_of(from[unit]); }
 };
 
-__global__ void __launch_bounds__(1024, 1) weights_select_kernel(const TraceK k, uint32_t chunk, uint64_t U, const float* __restrict__ weights)
+template <int T, bool FULL>
+__global__ void __launch_bounds__(T) weights_select_kernel(const TraceK k, uint32_t chunk, uint64_t U, const float* __restrict__ weights)
 {
     __shared__ SelectShared<uint32_t> sm;
     const uint32_t g = blockIdx.x % k.groups, t0 = blockIdx.x / k.groups * chunk, t1 = min(t0 + chunk, k.steps);
-    const uint32_t rounds = (k.n + blockDim.x - 1) / blockDim.x, cand = units_there(k.n);
+    const uint32_t rounds = (k.n + T - 1) / T, cand = units_there(k.n);
     const uint64_t first = (uint64_t)g * k.n;
     clear(sm);
     Band<uint32_t> band;
     band.valid = band.moved = false;
     for (uint32_t t = t0; t < t1; ++t) {
-        WeightsRow row = {weights + t * U + first, k.n};
-        const uint32_t word = choose<uint32_t>(row, rounds, cand, k.topk, band, sm, t);
+        WeightsRow<T, FULL> row = {weights + t * U + first, k.n};
+        const uint32_t word = choose<uint32_t, T>(row, rounds, cand, k.topk, band, sm, t);
         put_words(k.out + (size_t)t * k.W32, first, k.n, k.aligned, word);
     }
 }
@@ -461,7 +483,19 @@ extern "C" int kvp_trace_weights(uint32_t groups, uint32_t units_per_group, uint
     if (!k.aligned) KVP_CUDA(cudaMemsetAsync(access_bitmaps, 0, (size_t)steps * k.W32 * 4, st));
     // several steps to a CTA once there are enough CTAs
     const uint32_t chunk = std::max(1u, std::min(16u, groups * steps / (148u * 16u)));
-    weights_select_kernel<<<groups * ((steps + chunk - 1) / chunk), select_threads(k.n), 0, st>>>(k, chunk, U, weights);
+    const uint32_t grid = groups * ((steps + chunk - 1) / chunk);
+#define KVP_SELECT(T)                                                                                     \
+    do {                                                                                                  \
+        if (k.n % (kBatch * T)) weights_select_kernel<T, false><<<grid, T, 0, st>>>(k, chunk, U, weights);     \
+        else weights_select_kernel<T, true><<<grid, T, 0, st>>>(k, chunk, U, weights);                         \
+    } while (0)
+    switch (select_threads(k.n)) {
+        case 128: KVP_SELECT(128); break;
+        case 256: KVP_SELECT(256); break;
+        case 512: KVP_SELECT(512); break;
+        default: KVP_SELECT(1024); break;
+    }
+#undef KVP_SELECT
     KVP_CUDA(cudaGetLastError());
     return KVP_OK;
 }
