@@ -424,7 +424,7 @@ uint64_t kvp_cache_page_bytes(uint32_t head_dim, uint32_t page_tokens);
  *          Any alignment; 16-byte aligned rows are read faster.
  *   slots  (device) [tokens]: page * page_tokens + place in the page. A token whose slot lies outside the cache is not written
  *          (use -1 for padding). Two tokens of one call with the same slot leave a mixture of both there.
- * Errors: KVP_ERR_ARG (null, zero sizes, unknown dtype, page_tokens no multiple of 16), KVP_ERR_RANGE (head_dim).
+ * Errors: KVP_ERR_ARG (null, zero sizes, unknown dtype, page_tokens no multiple of 16), KVP_ERR_RANGE (head_dim, kv_heads > 65535).
  */
 int kvp_cache_append(const kvp_cache_shape* c, void* cache, uint32_t dtype, uint32_t tokens, const void* k,
                      int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,

@@ -30,7 +30,7 @@ __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162f
 
 // eight neighbouring elements; `aligned`: at a 16-byte boundary
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, bool aligned, float (&x)[8])
+__device__ __forceinline__ void load8(const T* p, bool aligned, float* x)
 {
     if (aligned) {
         alignas(16) T e[8];
@@ -46,111 +46,156 @@ __device__ __forceinline__ void load8(const T* p, bool aligned, float (&x)[8])
 
 // the tile of a slot, for one head; slot < slots_in_cache
 template <int N>
-__device__ __forceinline__ uint64_t tile_at(uint64_t slot, uint32_t head, uint32_t heads, uint32_t page_tokens)
+__device__ __forceinline__ uint64_t tile_at(uint64_t slot, uint32_t head, const RowsK& p, uint32_t& token)
 {
-    const uint64_t page = slot / page_tokens;
-    const uint32_t in_page = (uint32_t)(slot - page * page_tokens);
-    return ((page * heads + head) * (page_tokens / kTileTokens) + in_page / kTileTokens) * Tile<N>::kBytes;
+    uint64_t page;
+    uint32_t in_page;
+    if (p.slots_in_cache <= ~0u) {                                     // a 64-bit division takes as long as the rest of the kernel
+        const uint32_t q = (uint32_t)slot / p.page_tokens;
+        page = q;
+        in_page = (uint32_t)slot - q * p.page_tokens;
+    } else {
+        page = slot / p.page_tokens;
+        in_page = (uint32_t)(slot - page * p.page_tokens);
+    }
+    token = in_page % kTileTokens;
+    return ((page * p.heads + head) * (p.page_tokens / kTileTokens) + in_page / kTileTokens) * Tile<N>::kBytes;
 }
 
-// A thread quantises eight dims; the four threads of a group of 32 dims are neighbours. D / 4 threads serve a (token, head): the
-// first half of them its key, the rest its value.
+// A thread quantises the 32 dims of a group, so that nothing is exchanged and what is done once a group is done once a thread. Neighbouring threads
+// take the groups of a token, then the next tokens (whose values fill the same sectors of a tile); blockIdx.y is the head, blockIdx.z 0 for
+// keys and 1 for values. What bounds it is instructions, so the common way has ten for an element:
+// y = fl(x inv - z inv) stands for the quotient (x - z) / s; with |z inv| = b it is off from it by less than (b + 16) 2^-21 (the
+// roundings of inv, z inv and y, each 2^-24 relative, and that of x - z in the definition). Adding 1.5 * 2^23 rounds y to the nearest whole number, ties to even,
+// as the definition rounds the quotient unless y lies that close to a half; the whole number is in the low bits, and a Horner scheme packs eight of
+// them (the constant's bits leave by the top). A group in which some y lies near a half (2% of the groups of bf16 values:
+// their grid and the scale's often meet in one), or that is to be cut, is done again with a look at each number, and a division where it takes one.
 template <int N, typename T>
-__global__ void __launch_bounds__(256) append_kernel(const RowsK p, bool aligned)
+__global__ void __launch_bounds__(128) append_kernel(const RowsK p, bool aligned)
 {
     using L = Tile<N>;
-    constexpr uint32_t kPer = 4 * N;                                   // threads of a key or of a value
-    const uint64_t at = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    const uint64_t row = at / (2 * kPer);
-    const uint32_t j = (uint32_t)(at % kPer), n = j / 4, t = j % 4;
-    const bool is_value = (at / kPer) & 1;
-    const bool in = row < (uint64_t)p.tokens * p.heads;
-    const uint32_t token = (uint32_t)(in ? row / p.heads : 0), head = (uint32_t)(in ? row % p.heads : 0);
-    float x[8];
-    const T* from = is_value ? static_cast<const T*>(p.v) + token * p.v_token + head * p.v_head
-                             : static_cast<const T*>(p.k) + token * p.k_token + head * p.k_head;
-    load8(from + 8 * j, aligned, x);
-    float low = INFINITY, high = -INFINITY;
+    const uint32_t n = threadIdx.x % N, token = blockIdx.x * (128 / N) + threadIdx.x / N, head = blockIdx.y;
+    const bool is_value = blockIdx.z;
+    if (token >= p.tokens) return;
+    const int64_t slot = __ldg(p.slots + token);
+    float x[32];
+    {
+        const T* from = (is_value ? static_cast<const T*>(p.v) + token * p.v_token + head * p.v_head
+                                  : static_cast<const T*>(p.k) + token * p.k_token + head * p.k_head) + 32 * n;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        x[i] = x[i] != x[i] ? 0.0f : __fadd_rn(fminf(fmaxf(x[i], -kMost), kMost), 0.0f);     // -0 becomes 0
+        for (int i = 0; i < 32; i += 8) load8(from + i, aligned, x + i);
+    }
+    if (slot < 0 || (uint64_t)slot >= p.slots_in_cache) return;
+    float low = x[0], high = x[0], odd = 0.0f;                         // odd: NaN if some x is not finite
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
         low = fminf(low, x[i]);
         high = fmaxf(high, x[i]);
+        odd = fmaf(x[i], 0.0f, odd);
     }
+    if (odd != 0.0f || low < -kMost || high > kMost) {                 // rare: NaN becomes 0, the rest is cut
+        low = INFINITY;
+        high = -INFINITY;
 #pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-        low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, o));
-        high = fmaxf(high, __shfl_xor_sync(0xFFFFFFFFu, high, o));
+        for (int i = 0; i < 32; ++i) {
+            x[i] = x[i] != x[i] ? 0.0f : fminf(fmaxf(x[i], -kMost), kMost);
+            low = fminf(low, x[i]);
+            high = fmaxf(high, x[i]);
+        }
     }
-    const __half zero = __float2half_rn(low);
+    const __half zero = __float2half_rn(__fadd_rn(low, 0.0f));         // -0 becomes 0
     const float z = __half2float(zero);
     const __half scale = __float2half_rn(fmaxf(__fdiv_rn(__fsub_rn(high, z), 15.0f), 0.0f));
     const float s = __half2float(scale);
-    uint32_t word = 0;
+    uint32_t word[4] = {0, 0, 0, 0};
+    if (s > 0.0f) {
+        constexpr float kRound = 12582912.0f;
+        const float inv = __frcp_rn(s), back = -z * inv, room = 0.5f - (fabsf(back) + 16.0f) * 0x1p-21f;
+        float most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float q = s > 0.0f ? rintf(__fdiv_rn(__fsub_rn(x[i], z), s)) : 0.0f;
-        word |= (uint32_t)fminf(fmaxf(q, 0.0f), 15.0f) << (4 * i);
+        for (int i = 31; i >= 0; --i) {
+            const float y = fmaf(x[i], inv, back), r = __fadd_rn(y, kRound);
+            most = fmaxf(most, fabsf(__fsub_rn(y, __fsub_rn(r, kRound))));
+            word[i / 8] = word[i / 8] * 16u + (uint32_t)__float_as_int(r);
+        }
+        // 0x4B400000 is the whole number 0 here; of the sum of its multiples by powers of 16 only the first two stay within 32 bits
+        constexpr uint32_t kZero = 0x4B400000u + 0x4B400000u * 16u + 0x4B400000u * 256u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) word[i] -= kZero;
+        if (!(most < room && fmaf(low, inv, back) > -0.25f && fmaf(high, inv, back) < 15.25f)) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                word[w] = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float y = fmaf(x[8 * w + i], inv, back);
+                    float r = rintf(y);
+                    if (!(fabsf(y - r) < room)) r = rintf(__fdiv_rn(__fsub_rn(x[8 * w + i], z), s));
+                    word[w] |= (uint32_t)fminf(fmaxf(r, 0.0f), 15.0f) << (4 * i);
+                }
+            }
+        }
     }
-    const int64_t slot = in ? __ldg(p.slots + token) : -1;
-    if (slot < 0 || (uint64_t)slot >= p.slots_in_cache) return;
-    uint8_t* tile = p.cache + tile_at<N>((uint64_t)slot, head, p.heads, p.page_tokens);
-    const uint32_t i = (uint32_t)((uint64_t)slot % kTileTokens);
+    uint32_t i;
+    uint8_t* tile = p.cache + tile_at<N>((uint64_t)slot, head, p, i);
     if (is_value) {
-        *reinterpret_cast<uint16_t*>(tile + L::value_half(i, 2 * t, n)) = (uint16_t)word;
-        *reinterpret_cast<uint16_t*>(tile + L::value_half(i, 2 * t + 1, n)) = (uint16_t)(word >> 16);
+#pragma unroll
+        for (uint32_t g = 0; g < 8; ++g) *reinterpret_cast<uint16_t*>(tile + L::value_half(i, g, n)) = (uint16_t)(word[g / 2] >> (16 * (g & 1)));
     } else {
-        *reinterpret_cast<uint32_t*>(tile + L::key_word(i, t, n)) = word;
+#pragma unroll
+        for (uint32_t t = 0; t < 4; ++t) *reinterpret_cast<uint32_t*>(tile + L::key_word(i, t, n)) = word[t];
     }
-    if (t == 0) {
-        __half* meta = reinterpret_cast<__half*>(tile + (is_value ? L::value_meta(i, n) : L::key_meta(i, n)));
-        meta[0] = scale;
-        meta[(L::kKeyZero - L::kKeyScale) / 2] = zero;
-    }
+    __half* meta = reinterpret_cast<__half*>(tile + (is_value ? L::value_meta(i, n) : L::key_meta(i, n)));
+    meta[0] = scale;
+    meta[(L::kKeyZero - L::kKeyScale) / 2] = zero;
 }
 
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(__half* p, float x) { *p = __float2half_rn(x); }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-// The inverse: a thread gives eight dims back. Outputs are [tokens][heads][D]; a token of a slot outside the cache reads as 0.
+// The inverse, by the same threads. Outputs are [tokens][heads][D]; a token of a slot outside the cache reads as 0.
 template <int N, typename T>
-__global__ void __launch_bounds__(256) read_kernel(const RowsK p, T* __restrict__ k, T* __restrict__ v)
+__global__ void __launch_bounds__(128) read_kernel(const RowsK p, T* __restrict__ k, T* __restrict__ v)
 {
     using L = Tile<N>;
-    constexpr uint32_t kPer = 4 * N;
-    const uint64_t at = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    const uint64_t row = at / (2 * kPer);
-    if (row >= (uint64_t)p.tokens * p.heads) return;
-    const uint32_t j = (uint32_t)(at % kPer), n = j / 4, t = j % 4;
-    const bool is_value = (at / kPer) & 1;
-    const uint32_t token = (uint32_t)(row / p.heads), head = (uint32_t)(row % p.heads);
+    const uint32_t n = threadIdx.x % N, token = blockIdx.x * (128 / N) + threadIdx.x / N, head = blockIdx.y;
+    const bool is_value = blockIdx.z;
+    if (token >= p.tokens) return;
     const int64_t slot = __ldg(p.slots + token);
-    uint32_t word = 0;
+    uint32_t word[4] = {0, 0, 0, 0};
     float s = 0.0f, z = 0.0f;
     if (slot >= 0 && (uint64_t)slot < p.slots_in_cache) {
-        const uint8_t* tile = p.cache + tile_at<N>((uint64_t)slot, head, p.heads, p.page_tokens);
-        const uint32_t i = (uint32_t)((uint64_t)slot % kTileTokens);
-        word = is_value ? (uint32_t)*reinterpret_cast<const uint16_t*>(tile + L::value_half(i, 2 * t, n)) |
-                              (uint32_t)*reinterpret_cast<const uint16_t*>(tile + L::value_half(i, 2 * t + 1, n)) << 16
-                        : *reinterpret_cast<const uint32_t*>(tile + L::key_word(i, t, n));
+        uint32_t i;
+        const uint8_t* tile = p.cache + tile_at<N>((uint64_t)slot, head, p, i);
+#pragma unroll
+        for (uint32_t t = 0; t < 4; ++t)
+            word[t] = is_value ? (uint32_t)*reinterpret_cast<const uint16_t*>(tile + L::value_half(i, 2 * t, n)) |
+                                     (uint32_t)*reinterpret_cast<const uint16_t*>(tile + L::value_half(i, 2 * t + 1, n)) << 16
+                               : *reinterpret_cast<const uint32_t*>(tile + L::key_word(i, t, n));
         const __half* meta = reinterpret_cast<const __half*>(tile + (is_value ? L::value_meta(i, n) : L::key_meta(i, n)));
         s = __half2float(meta[0]);
         z = __half2float(meta[(L::kKeyZero - L::kKeyScale) / 2]);
     }
-    alignas(16) T e[8];
+    T* to = (is_value ? v : k) + ((uint64_t)token * p.heads + head) * L::D + 32 * n;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) put(e + i, __fadd_rn(__fmul_rn((float)((word >> (4 * i)) & 15u), s), z));
-    uint4* to = reinterpret_cast<uint4*>((is_value ? v : k) + row * L::D + 8 * j);
+    for (int t = 0; t < 4; ++t) {
+        alignas(16) T e[8];
 #pragma unroll
-    for (uint32_t i = 0; i < sizeof(e) / 16; ++i) to[i] = reinterpret_cast<const uint4*>(e)[i];
+        for (int i = 0; i < 8; ++i) {
+            const float q = __uint_as_float(0x4B000000u | (word[t] >> (4 * i) & 15u)) - 8388608.0f;  // 2^23 + q, without a conversion
+            put(e + i, __fadd_rn(__fmul_rn(q, s), z));
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(e) / 16; ++i) reinterpret_cast<uint4*>(to + 8 * t)[i] = reinterpret_cast<const uint4*>(e)[i];
+    }
 }
 
 template <int N, typename T>
 int launch_append(const RowsK& p, bool aligned, cudaStream_t st)
 {
-    const uint64_t threads = (uint64_t)p.tokens * p.heads * 8 * N, grid = (threads + 255) / 256;
-    append_kernel<N, T><<<(uint32_t)grid, 256, 0, st>>>(p, aligned);
+    constexpr uint32_t kTokens = 128 / N;
+    append_kernel<N, T><<<dim3((p.tokens + kTokens - 1) / kTokens, p.heads, 2), 128, 0, st>>>(p, aligned);
     KVP_CUDA(cudaGetLastError());
     return KVP_OK;
 }
@@ -158,8 +203,8 @@ int launch_append(const RowsK& p, bool aligned, cudaStream_t st)
 template <int N, typename T>
 int launch_read(const RowsK& p, void* k, void* v, cudaStream_t st)
 {
-    const uint64_t threads = (uint64_t)p.tokens * p.heads * 8 * N, grid = (threads + 255) / 256;
-    read_kernel<N, T><<<(uint32_t)grid, 256, 0, st>>>(p, static_cast<T*>(k), static_cast<T*>(v));
+    constexpr uint32_t kTokens = 128 / N;
+    read_kernel<N, T><<<dim3((p.tokens + kTokens - 1) / kTokens, p.heads, 2), 128, 0, st>>>(p, static_cast<T*>(k), static_cast<T*>(v));
     KVP_CUDA(cudaGetLastError());
     return KVP_OK;
 }
@@ -170,7 +215,7 @@ int check_rows(const kvp_cache_shape* c, const void* cache, uint32_t tokens, con
     if (!c->page_tokens || c->page_tokens % kTileTokens) return KVP_ERR_ARG;
     if (!head_dim_served(c->head_dim)) return KVP_ERR_RANGE;
     if (tokens && (!cache || !a || !b || !slots)) return KVP_ERR_ARG;
-    if ((uint64_t)tokens * c->kv_heads * (c->head_dim / 4) >= (1ull << 31) * 256) return KVP_ERR_RANGE;
+    if (c->kv_heads > 65535 || tokens >= (1u << 31)) return KVP_ERR_RANGE;
     return KVP_OK;
 }
 

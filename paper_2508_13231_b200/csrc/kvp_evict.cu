@@ -68,37 +68,57 @@ __device__ __forceinline__ Members members_of(const EvictK& p, uint32_t g)
 
 // One pass. The sums of a group, 48 bits each, are in shared memory as lower words and upper half-words (24 KB for 4096 units: seven CTAs an SM,
 // so that 1036 groups of that size are worked on at once); a step's first pass adds its weights.
-// FULL: the rounds end with the last unit, and come in eights.
+// FULL: n = 32 T, so that every slot of 32 rounds holds a unit; the weights of a step are then on their way while the step before is chosen for.
 template <int T, bool FULL>
 struct SumsRow {
+    typedef float Raw;
+    static constexpr int kFetch = FULL ? 32 : kBatch;
     const EvictK& p;
     uint32_t* lo;
     uint16_t* hi;
     const float* w;           // the weights to be added, or null
     bool plain;               // no decay, and no sum can reach 2^48
+    const float* next;        // the weights after those, or null
+    float ahead[FULL ? 32 : 1];
     __device__ __forceinline__ uint64_t key(uint32_t unit) const { return (uint64_t)hi[unit] << 32 | lo[unit]; }
     __device__ __forceinline__ uint32_t unit_of(uint32_t j) const { return FULL ? j * T + threadIdx.x : min(j * T + threadIdx.x, p.n - 1); }
     __device__ __forceinline__ void again(uint32_t j0, uint64_t (&k)[kBatch]) const
     {
+        const uint32_t* l = lo + j0 * T + threadIdx.x;            // the offsets from them are constants
+        const uint16_t* h = hi + j0 * T + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) k[i] = key(unit_of(j0 + i));
+        for (int i = 0; i < kBatch; ++i) k[i] = FULL ? (uint64_t)h[i * T] << 32 | l[i * T] : key(unit_of(j0 + i));
     }
     template <bool FIRST>
-    __device__ __forceinline__ void load(uint32_t j0, uint64_t least, uint64_t most, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
+    __device__ __forceinline__ void fetch(uint32_t j0, float (&x)[kFetch]) const
+    {
+        if (FIRST && w) {
+#pragma unroll
+            for (int i = 0; i < kFetch; ++i) x[i] = FULL ? ahead[FULL ? i : 0] : __ldcs(w + unit_of(j0 + i));
+        }
+    }
+    __device__ __forceinline__ void done()
+    {
+        if (FULL && next) {
+#pragma unroll
+            for (int i = 0; i < kFetch; ++i) ahead[FULL ? i : 0] = __ldcs(next + i * T + threadIdx.x);
+        }
+    }
+    template <bool FIRST>
+    __device__ __forceinline__ void split(uint32_t j0, const float* x, uint64_t least, uint64_t most, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
     {
         uint64_t k[kBatch];
         if (FIRST && w) {
-            float x[kBatch];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) x[i] = __ldcs(w + unit_of(j0 + i));
             if (plain) {
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i) {
-                    const uint32_t unit = unit_of(j0 + i), add = fixed_weight(x[i]);
+                    const uint32_t unit = FULL ? 0 : unit_of(j0 + i), add = fixed_weight(x[i]);
+                    uint32_t* const lower = FULL ? lo + j0 * T + threadIdx.x + i * T : lo + unit;
+                    uint16_t* const upper = FULL ? hi + j0 * T + threadIdx.x + i * T : hi + unit;
                     const bool there = FULL || (j0 + i) * T + threadIdx.x < p.n;
-                    const uint32_t l = lo[unit] + add, h = hi[unit] + (l < add);
-                    if (there) lo[unit] = l;
-                    if (there && l < add) hi[unit] = (uint16_t)h;
+                    const uint32_t l = *lower + add, h = *upper + (l < add);
+                    if (there) *lower = l;
+                    if (there && l < add) *upper = (uint16_t)h;
                     k[i] = (uint64_t)h << 32 | l;
                 }
             } else {
@@ -120,17 +140,18 @@ struct SumsRow {
 };
 
 template <int T, bool FULL>
-__global__ void __launch_bounds__(T) evict_kernel(const EvictK p)
+__global__ void __launch_bounds__(T, T == 128 ? 5 : 1) evict_kernel(const EvictK p)
 {
     extern __shared__ uint32_t sums[];
-    __shared__ SelectShared<uint64_t> sm;
+    __shared__ SelectShared<uint64_t, T> sm;
     __shared__ uint32_t upper;
     const uint32_t g = blockIdx.x, tid = threadIdx.x, rounds = (p.n + T - 1) / T;
     const uint64_t first = (uint64_t)g * p.n;
     if (tid == 0) upper = 0;
     clear(sm);
     const Members m = members_of(p, g);
-    SumsRow<T, FULL> row = {p, sums, reinterpret_cast<uint16_t*>(sums + p.n), nullptr, false};
+    SumsRow<T, FULL> row = {p, sums, reinterpret_cast<uint16_t*>(sums + p.n), nullptr, false, p.w + first, {}};
+    row.done();
     uint32_t most = 0;
     for (uint32_t i = tid; i < p.n; i += T) {
         const uint64_t x = first_sum(p, first + i);
@@ -146,7 +167,9 @@ __global__ void __launch_bounds__(T) evict_kernel(const EvictK p)
     band.valid = band.moved = false;
     // a row that is chosen before its weights are added is what the step before left
     for (uint32_t s = 0; s < p.steps; ++s) {
-        row.w = !p.before ? p.w + s * p.U + first : s ? p.w + (s - 1) * p.U + first : nullptr;
+        const uint32_t adds = p.before ? s - 1 : s;                // the step whose weights are added; none (wraps) before the first choice
+        row.w = adds < p.steps ? p.w + adds * p.U + first : nullptr;
+        row.next = adds + 1 < p.steps ? p.w + (adds + 1) * p.U + first : nullptr;
         const uint32_t word = choose<uint64_t, T>(row, rounds, m.cand, m.left, band, sm, s);
         put_words(p.out + s * p.W32, first, p.n, p.aligned, word | m.safe);
     }
@@ -160,13 +183,24 @@ __global__ void __launch_bounds__(128) sums_kernel(const EvictK p)
     const uint64_t u = (uint64_t)blockIdx.x * 128 + threadIdx.x;
     if (u >= p.U) return;
     uint64_t acc = first_sum(p, u);
-    const float* w = p.w + u;
-    uint64_t* to = p.sums + u;
-#pragma unroll 32
-    for (uint32_t s = 0; s < p.steps; ++s) {
-        const uint64_t was = acc;
-        acc = accumulated(acc, p.decay, __ldcs(w + s * p.U));
-        to[s * p.U] = p.before ? was : acc;
+    constexpr uint32_t kAhead = 32;                                // weights under way while those before are added
+    const uint32_t last = p.steps - 1;
+    float next[kAhead];
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i) next[i] = __ldcs(p.w + min(i, last) * p.U + u);
+    for (uint32_t s0 = 0; s0 < p.steps; s0 += kAhead) {
+        float x[kAhead];
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i) x[i] = next[i];
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i) next[i] = __ldcs(p.w + min(s0 + kAhead + i, last) * p.U + u);
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i) {
+            if (s0 + i >= p.steps) break;
+            const uint64_t was = acc;
+            acc = accumulated(acc, p.decay, x[i]);
+            p.sums[(s0 + i) * p.U + u] = p.before ? was : acc;
+        }
     }
     if (!p.before) p.acc[u] = (int64_t)acc;
 }
@@ -174,8 +208,11 @@ __global__ void __launch_bounds__(128) sums_kernel(const EvictK p)
 // The second: a CTA chooses for some consecutive steps of a group.
 template <int T>
 struct StoredRow {
+    typedef uint64_t Raw;
+    static constexpr int kFetch = 2 * kBatch;
     const uint64_t* from;
     uint32_t n;
+    __device__ __forceinline__ void done() const {}
     __device__ __forceinline__ uint64_t key(uint32_t unit) const { return from[unit]; }
     __device__ __forceinline__ void again(uint32_t j0, uint64_t (&k)[kBatch]) const
     {
@@ -183,18 +220,26 @@ struct StoredRow {
         for (int i = 0; i < kBatch; ++i) k[i] = from[min((j0 + i) * T + threadIdx.x, n - 1)];
     }
     template <bool FIRST>
-    __device__ __forceinline__ void load(uint32_t j0, uint64_t least, uint64_t most, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
+    __device__ __forceinline__ void fetch(uint32_t j0, uint64_t (&x)[kFetch]) const
     {
-        uint64_t k[kBatch];
-        again(j0, k);
-        ballots(k, least, most, a, b);
+#pragma unroll
+        for (int i = 0; i < kFetch; ++i) x[i] = from[min((j0 + i) * T + threadIdx.x, n - 1)];
+    }
+    template <bool FIRST>
+    __device__ __forceinline__ void split(uint32_t, const uint64_t* k, uint64_t least, uint64_t most, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            a[i] = __ballot_sync(0xFFFFFFFFu, k[i] >= least);
+            b[i] = __ballot_sync(0xFFFFFFFFu, k[i] > most);
+        }
     }
 };
 
 template <int T>
 __global__ void __launch_bounds__(T) choose_kernel(const EvictK p)
 {
-    __shared__ SelectShared<uint64_t> sm;
+    __shared__ SelectShared<uint64_t, T> sm;
     const uint32_t g = blockIdx.x % p.groups, s0 = blockIdx.x / p.groups * p.chunk, s1 = min(s0 + p.chunk, p.steps);
     const uint32_t rounds = (p.n + T - 1) / T;
     const uint64_t first = (uint64_t)g * p.n;
@@ -216,7 +261,7 @@ int launch_choice(const EvictK& k, bool two, cudaStream_t st)
         choose_kernel<T><<<k.groups * ((k.steps + k.chunk - 1) / k.chunk), T, 0, st>>>(k);
         return KVP_OK;
     }
-    const bool full = k.n % (kBatch * T) == 0;
+    const bool full = k.n == 32 * T;
     const uint32_t smem = (k.n * 6 + 15) / 16 * 16;
     const void* f = full ? (const void*)evict_kernel<T, true> : (const void*)evict_kernel<T, false>;
     if (smem > 40 * 1024) KVP_CUDA(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));

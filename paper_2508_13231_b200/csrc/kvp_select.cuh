@@ -21,10 +21,10 @@ constexpr uint32_t kBandGoal = sizeof(Key) == 8 ? 32 : 64;
 
 constexpr int kBatch = 8;                     // rounds whose keys are loaded together
 
-template <typename Key>
+template <typename Key, int T>
 struct SelectShared {
     uint32_t hist[kBins256];                  // zero between uses
-    uint32_t words[1024];                     // chosen keys of the list, or ties per word; zero between uses
+    uint32_t words[T];                        // chosen keys of the list, or ties per word; zero between uses
     uint32_t above[2];                        // keys above the band of this row and the next; zero before a call
     Key list[kListed];
     uint32_t unit[kListed];
@@ -58,8 +58,8 @@ __device__ __forceinline__ void count_if(bool in, uint32_t bins, uint32_t at)
 
 // One warp: the bin from the top in which the need-th key lies -> sm.edge (its number), sm.need (how many of its keys are
 // wanted), sm.equal (how many it has); sm.inside: keys in all bins. Leaves the bins zero. need = 0 or need > inside: edge is left alone.
-template <typename Key>
-__device__ __forceinline__ void find_bin(SelectShared<Key>& sm, uint32_t need, uint32_t lane)
+template <typename Key, int T>
+__device__ __forceinline__ void find_bin(SelectShared<Key, T>& sm, uint32_t need, uint32_t lane)
 {
     uint4* mine = reinterpret_cast<uint4*>(sm.hist) + 2 * lane;    // a lane owns eight neighbouring bins
     const uint4 a = mine[0], b = mine[1];
@@ -91,13 +91,14 @@ __device__ __forceinline__ void find_bin(SelectShared<Key>& sm, uint32_t need, u
     }
 }
 
-// `Row` gives the keys: again(j0, k) those of this thread in rounds j0 .. j0 + 7, key(unit) any unit's, load<..>(j0, lo, hi, a, b) the ballots of
-// >= lo and > hi over these rounds, for the first time with FIRST (which may change the keys: the weights of a step are added then). Rounds behind the last unit give any key at all: `cand`, lane j's word of the
+// `Row` gives the keys: again(j0, k) those of this thread in rounds j0 .. j0 + 7, key(unit) any unit's, fetch<..>(j0, x) gets
+// what kFetch rounds need from memory, done() is called when all rounds of FIRST were, and split<..>(j0, x, lo, hi, a, b) gives the ballots of >= lo and > hi over eight of them, with FIRST for
+// the first time (which may change the keys: the weights of a step are added then). Rounds behind the last unit give any key at all: `cand`, lane j's word of the
 // candidates in round j, says which count. 32-bit keys: of the units in it, those with key 0 are no candidates either.
 
 // One digit of the search for a band: of the candidates at a distance of at most `span` from its base, counted by distance >> sh.
-template <typename Key, typename Row, typename Distance>
-__device__ __forceinline__ void one_digit(SelectShared<Key>& sm, Row& row, uint32_t rounds, uint32_t cand, int sh, uint64_t span, uint32_t need,
+template <typename Key, int T, typename Row, typename Distance>
+__device__ __forceinline__ void one_digit(SelectShared<Key, T>& sm, Row& row, uint32_t rounds, uint32_t cand, int sh, uint64_t span, uint32_t need,
                                           Distance distance)
 {
     const uint32_t bins = (uint32_t)__cvta_generic_to_shared(sm.hist), lane = threadIdx.x & 31;
@@ -120,8 +121,8 @@ enum class Found { kAll, kBand, kTies };
 
 // A band that holds the threshold. kAll: there are no more than `left` candidates. kTies: the threshold is band.lo, and more keys
 // equal it than can be ranked. Every thread of the CTA calls it.
-template <typename Key, typename Row>
-__device__ Found find_band(Row& row, uint32_t rounds, uint32_t cand, uint32_t left, Band<Key>& band, SelectShared<Key>& sm)
+template <typename Key, int T, typename Row>
+__device__ Found find_band(Row& row, uint32_t rounds, uint32_t cand, uint32_t left, Band<Key>& band, SelectShared<Key, T>& sm)
 {
     const uint32_t tid = threadIdx.x, lane = tid & 31;
     __syncthreads();
@@ -219,13 +220,18 @@ __device__ __forceinline__ void split(Row& row, uint32_t rounds, uint32_t cand, 
 {
     const uint32_t lane = threadIdx.x & 31;
     from = above = 0;
-    for (uint32_t j0 = 0; j0 < rounds; j0 += kBatch) {
-        uint32_t a[kBatch], b[kBatch];
-        row.template load<FIRST>(j0, lo, hi, a, b);
-        const uint32_t x = own_of(a, lane), y = own_of(b, lane);
-        if ((lane & ~7u) == j0) {
-            from = x;
-            above = y;
+    for (uint32_t j0 = 0; j0 < rounds; j0 += Row::kFetch) {
+        typename Row::Raw x[Row::kFetch];
+        row.template fetch<FIRST>(j0, x);
+#pragma unroll
+        for (int i = 0; i < Row::kFetch; i += kBatch) {
+            uint32_t a[kBatch], b[kBatch];
+            row.template split<FIRST>(j0 + i, x + i, lo, hi, a, b);
+            const uint32_t c = own_of(a, lane), d = own_of(b, lane);
+            if ((lane & ~7u) == j0 + i) {
+                from = c;
+                above = d;
+            }
         }
     }
     from &= cand;
@@ -233,8 +239,8 @@ __device__ __forceinline__ void split(Row& row, uint32_t rounds, uint32_t cand, 
 }
 
 // Many keys equal the threshold `at`: the keys above it, and of the equal ones the first in the order of the units.
-template <typename Key, typename Row>
-__device__ uint32_t choose_ties(Row& row, uint32_t rounds, uint32_t cand, uint32_t left, Key at, SelectShared<Key>& sm)
+template <typename Key, int T, typename Row>
+__device__ uint32_t choose_ties(Row& row, uint32_t rounds, uint32_t cand, uint32_t left, Key at, SelectShared<Key, T>& sm)
 {
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32, warps = blockDim.x / 32;
     uint32_t from, word;
@@ -277,7 +283,7 @@ __device__ uint32_t choose_ties(Row& row, uint32_t rounds, uint32_t cand, uint32
 // -> lane j's word of round j: the chosen units. turn: a number that changes by one from call to call. Every thread of the CTA calls it; the
 // row's keys have all been loaded when it returns.
 template <typename Key, int T, typename Row>
-__device__ __forceinline__ uint32_t choose(Row& row, uint32_t rounds, uint32_t cand, uint32_t left, Band<Key>& band, SelectShared<Key>& sm,
+__device__ __forceinline__ uint32_t choose(Row& row, uint32_t rounds, uint32_t cand, uint32_t left, Band<Key>& band, SelectShared<Key, T>& sm,
                                            uint32_t turn)
 {
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32, warps = T / 32, now = turn & 1;
@@ -286,6 +292,7 @@ __device__ __forceinline__ uint32_t choose(Row& row, uint32_t rounds, uint32_t c
         uint32_t from, above;
         split<true>(row, rounds, cand, (Key)1, (Key)1, from, above);
         __syncwarp();
+        row.done();
         loaded = true;
         if (left == 0) return 0;
     }
@@ -307,6 +314,7 @@ __device__ __forceinline__ uint32_t choose(Row& row, uint32_t rounds, uint32_t c
         uint32_t word, inside;
         if (loaded) split<false>(row, rounds, cand, lo, lo + span, inside, word);
         else split<true>(row, rounds, cand, lo, lo + span, inside, word);
+        if (!loaded) row.done();                                   // the next row's keys may be sent for
         loaded = true;
         inside &= ~word;
         __syncwarp();                                              // a lane looks at keys that other lanes of its warp may have written
@@ -391,11 +399,11 @@ __device__ __forceinline__ uint32_t units_there(uint32_t n)
     return first >= n ? 0u : n - first >= 32 ? ~0u : (1u << (n - first)) - 1u;
 }
 
-template <typename Key>
-__device__ __forceinline__ void clear(SelectShared<Key>& sm)
+template <typename Key, int T>
+__device__ __forceinline__ void clear(SelectShared<Key, T>& sm)
 {
-    for (uint32_t i = threadIdx.x; i < 1024; i += blockDim.x) sm.words[i] = 0;
-    for (uint32_t i = threadIdx.x; i < kBins256; i += blockDim.x) sm.hist[i] = 0;
+    sm.words[threadIdx.x] = 0;
+    for (uint32_t i = threadIdx.x; i < kBins256; i += T) sm.hist[i] = 0;
     if (threadIdx.x < 2) sm.above[threadIdx.x] = 0;
     __syncthreads();
 }

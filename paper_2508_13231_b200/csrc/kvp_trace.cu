@@ -408,16 +408,19 @@ trace_select_kernel(const TraceK k, uint32_t want, uint32_t U, const int32_t* __
 
 // Access bitmaps of recorded weights, on the bits of positive floats, which order as whole numbers do (a unit that received nothing, or NaN, has key
 // 0 and is never picked). A CTA takes some consecutive steps of a group, in which the threshold moves little.
-// FULL: the rounds end with the last unit, and come in eights.
+// FULL: n = 32 T, so that every slot of 32 rounds holds a unit.
 template <int T, bool FULL>
 struct WeightsRow {
+    typedef float Raw;
+    // Loads under way at once: none depends on a condition. More of them, or a step ahead as kvp_evict.cu has it, cost CTAs an SM, and were slower:
+    // 640 groups of 4096 units x 64 steps 215 us with 8, 225 with 16, 298 with 32 a step ahead.
+    static constexpr int kFetch = kBatch;
     const float* from;
     uint32_t n;
     static __device__ __forceinline__ uint32_t key_of(float w) { return w > 0.0f ? __float_as_uint(w) : 0u; }
-    // all loads under way at once: none depends on a condition
     __device__ __forceinline__ void weights(uint32_t j0, float (&w)[kBatch]) const
     {
-        const float* at = from + j0 * T + threadIdx.x;
+        const float* at = from + j0 * T + threadIdx.x;       // the offsets from it are constants
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) w[i] = FULL ? at[i * T] : from[min((j0 + i) * T + threadIdx.x, n - 1)];
     }
@@ -428,14 +431,15 @@ struct WeightsRow {
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) k[i] = key_of(w[i]);
     }
+    template <bool FIRST>
+    __device__ __forceinline__ void fetch(uint32_t j0, float (&w)[kFetch]) const { weights(j0, w); }
+    __device__ __forceinline__ void done() const {}
     // 0 < lo <= the bits of infinity, so a comparison of floats says the same as one of keys, and NaN or a negative weight fails it; hi may lie
     // behind infinity, even where the bits are those of negative numbers, and is cut to it
     template <bool FIRST>
-    __device__ __forceinline__ void load(uint32_t j0, uint32_t lo, uint32_t hi, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
+    __device__ __forceinline__ void split(uint32_t, const float* w, uint32_t lo, uint32_t hi, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
     {
-        float w[kBatch];
         const float least = __uint_as_float(lo), most = __uint_as_float(min(hi, 0x7F800000u));
-        weights(j0, w);
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             a[i] = __ballot_sync(0xFFFFFFFFu, w[i] >= least);
@@ -446,9 +450,9 @@ struct WeightsRow {
 };
 
 template <int T, bool FULL>
-__global__ void __launch_bounds__(T) weights_select_kernel(const TraceK k, uint32_t chunk, uint64_t U, const float* __restrict__ weights)
+__global__ void __launch_bounds__(T, T == 1024 ? 1 : 1280 / T) weights_select_kernel(const TraceK k, uint32_t chunk, uint64_t U, const float* __restrict__ weights)
 {
-    __shared__ SelectShared<uint32_t> sm;
+    __shared__ SelectShared<uint32_t, T> sm;
     const uint32_t g = blockIdx.x % k.groups, t0 = blockIdx.x / k.groups * chunk, t1 = min(t0 + chunk, k.steps);
     const uint32_t rounds = (k.n + T - 1) / T, cand = units_there(k.n);
     const uint64_t first = (uint64_t)g * k.n;
@@ -481,12 +485,13 @@ extern "C" int kvp_trace_weights(uint32_t groups, uint32_t units_per_group, uint
     k.out = access_bitmaps;
     k.aligned = units_per_group % 32 == 0;
     if (!k.aligned) KVP_CUDA(cudaMemsetAsync(access_bitmaps, 0, (size_t)steps * k.W32 * 4, st));
-    // several steps to a CTA once there are enough CTAs
-    const uint32_t chunk = std::max(1u, std::min(16u, groups * steps / (148u * 16u)));
+    // Consecutive steps to a CTA once there are enough CTAs: a CTA begins with the search for a band, but many short ones fill the SMs better
+    // (640 groups of 4096 units x 64 steps: 8 steps to a CTA 208 us, 4 steps 224, 16 steps 213, all 64 349; with ten CTAs an SM, 224 with 16).
+    const uint32_t chunk = std::max(1u, std::min(8u, groups * steps / (148u * 16u)));
     const uint32_t grid = groups * ((steps + chunk - 1) / chunk);
 #define KVP_SELECT(T)                                                                                     \
     do {                                                                                                  \
-        if (k.n % (kBatch * T)) weights_select_kernel<T, false><<<grid, T, 0, st>>>(k, chunk, U, weights);     \
+        if (k.n != 32 * T) weights_select_kernel<T, false><<<grid, T, 0, st>>>(k, chunk, U, weights);     \
         else weights_select_kernel<T, true><<<grid, T, 0, st>>>(k, chunk, U, weights);                         \
     } while (0)
     switch (select_threads(k.n)) {
