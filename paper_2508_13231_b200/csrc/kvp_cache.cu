@@ -23,6 +23,7 @@ struct RowsK {
 };
 
 constexpr float kMost = 65504.0f;
+constexpr uint32_t kRowThreads = 128;
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
@@ -62,69 +63,76 @@ __device__ __forceinline__ uint64_t tile_at(uint64_t slot, uint32_t head, const 
     return ((page * p.heads + head) * (p.page_tokens / kTileTokens) + in_page / kTileTokens) * Tile<N>::kBytes;
 }
 
-// A thread quantises the 32 dims of a group, so that nothing is exchanged and what is done once a group is done once a thread. Neighbouring threads
-// take the groups of a token, then the next tokens (whose values fill the same sectors of a tile); blockIdx.y is the head, blockIdx.z 0 for
-// keys and 1 for values. What bounds it is instructions, so the common way has ten for an element:
+// Two neighbouring threads quantise the 32 dims of a group, 16 each: what is done once a thread counts little beside the elements' work, and there are
+// threads enough for a decode step. Next to them stand the groups of the token, then the next tokens (whose values fill the same sectors of a
+// tile); blockIdx.y is the head, blockIdx.z 0 for keys and 1 for values. What bounds it is instructions, so the common way has ten for an element:
 // y = fl(x inv - z inv) stands for the quotient (x - z) / s; with |z inv| = b it is off from it by less than (b + 16) 2^-21 (the
 // roundings of inv, z inv and y, each 2^-24 relative, and that of x - z in the definition). Adding 1.5 * 2^23 rounds y to the nearest whole number, ties to even,
 // as the definition rounds the quotient unless y lies that close to a half; the whole number is in the low bits, and a Horner scheme packs eight of
 // them (the constant's bits leave by the top). A group in which some y lies near a half (2% of the groups of bf16 values:
 // their grid and the scale's often meet in one), or that is to be cut, is done again with a look at each number, and a division where it takes one.
 template <int N, typename T>
-__global__ void __launch_bounds__(128) append_kernel(const RowsK p, bool aligned)
+__global__ void __launch_bounds__(kRowThreads) append_kernel(const RowsK p, bool aligned)
 {
     using L = Tile<N>;
-    const uint32_t n = threadIdx.x % N, token = blockIdx.x * (128 / N) + threadIdx.x / N, head = blockIdx.y;
-    const bool is_value = blockIdx.z;
-    if (token >= p.tokens) return;
-    const int64_t slot = __ldg(p.slots + token);
-    float x[32];
+    const uint32_t half = threadIdx.x % 2, n = threadIdx.x / 2 % N, row = blockIdx.x * (kRowThreads / (2 * N)) + threadIdx.x / (2 * N), head = blockIdx.y;
+    const bool is_value = blockIdx.z, in = row < p.tokens;
+    const uint32_t token = in ? row : 0;                               // both threads of a pair are in or out
+    const int64_t slot = in ? __ldg(p.slots + token) : -1;
+    float x[16];
     {
         const T* from = (is_value ? static_cast<const T*>(p.v) + token * p.v_token + head * p.v_head
-                                  : static_cast<const T*>(p.k) + token * p.k_token + head * p.k_head) + 32 * n;
-#pragma unroll
-        for (int i = 0; i < 32; i += 8) load8(from + i, aligned, x + i);
+                                  : static_cast<const T*>(p.k) + token * p.k_token + head * p.k_head) + 32 * n + 16 * half;
+        load8(from, aligned, x);
+        load8(from + 8, aligned, x + 8);
     }
-    if (slot < 0 || (uint64_t)slot >= p.slots_in_cache) return;
-    float low = x[0], high = x[0], odd = 0.0f;                         // odd: NaN if some x is not finite
+    float low, high, odd;                                              // odd: NaN if some x is not finite
+    {
+        float a[4] = {x[0], x[1], x[2], x[3]}, b[4] = {x[0], x[1], x[2], x[3]}, c[4] = {0, 0, 0, 0};     // four short chains for one long
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        low = fminf(low, x[i]);
-        high = fmaxf(high, x[i]);
-        odd = fmaf(x[i], 0.0f, odd);
+        for (int i = 0; i < 16; ++i) {
+            a[i % 4] = fminf(a[i % 4], x[i]);
+            b[i % 4] = fmaxf(b[i % 4], x[i]);
+            c[i % 4] = fmaf(x[i], 0.0f, c[i % 4]);
+        }
+        low = fminf(fminf(a[0], a[1]), fminf(a[2], a[3]));
+        high = fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3]));
+        odd = (c[0] + c[1]) + (c[2] + c[3]);
     }
     if (odd != 0.0f || low < -kMost || high > kMost) {                 // rare: NaN becomes 0, the rest is cut
         low = INFINITY;
         high = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < 16; ++i) {
             x[i] = x[i] != x[i] ? 0.0f : fminf(fmaxf(x[i], -kMost), kMost);
             low = fminf(low, x[i]);
             high = fmaxf(high, x[i]);
         }
     }
+    low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, 1));
+    high = fmaxf(high, __shfl_xor_sync(0xFFFFFFFFu, high, 1));
     const __half zero = __float2half_rn(__fadd_rn(low, 0.0f));         // -0 becomes 0
     const float z = __half2float(zero);
     const __half scale = __float2half_rn(fmaxf(__fdiv_rn(__fsub_rn(high, z), 15.0f), 0.0f));
     const float s = __half2float(scale);
-    uint32_t word[4] = {0, 0, 0, 0};
+    uint32_t word[2] = {0, 0};
     if (s > 0.0f) {
         constexpr float kRound = 12582912.0f;
         const float inv = __frcp_rn(s), back = -z * inv, room = 0.5f - (fabsf(back) + 16.0f) * 0x1p-21f;
-        float most = 0.0f;
+        float most[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int i = 31; i >= 0; --i) {
+        for (int i = 15; i >= 0; --i) {
             const float y = fmaf(x[i], inv, back), r = __fadd_rn(y, kRound);
-            most = fmaxf(most, fabsf(__fsub_rn(y, __fsub_rn(r, kRound))));
+            most[i / 8] = fmaxf(most[i / 8], fabsf(__fsub_rn(y, __fsub_rn(r, kRound))));
             word[i / 8] = word[i / 8] * 16u + (uint32_t)__float_as_int(r);
         }
-        // 0x4B400000 is the whole number 0 here; of the sum of its multiples by powers of 16 only the first two stay within 32 bits
+        // 0x4B400000 is the whole number 0 here; of the sum of its multiples by powers of 16 only the first three stay within 32 bits
         constexpr uint32_t kZero = 0x4B400000u + 0x4B400000u * 16u + 0x4B400000u * 256u;
+        word[0] -= kZero;
+        word[1] -= kZero;
+        if (!(fmaxf(most[0], most[1]) < room && fmaf(low, inv, back) > -0.25f && fmaf(high, inv, back) < 15.25f)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) word[i] -= kZero;
-        if (!(most < room && fmaf(low, inv, back) > -0.25f && fmaf(high, inv, back) < 15.25f)) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
+            for (int w = 0; w < 2; ++w) {
                 word[w] = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -136,18 +144,19 @@ __global__ void __launch_bounds__(128) append_kernel(const RowsK p, bool aligned
             }
         }
     }
+    if (slot < 0 || (uint64_t)slot >= p.slots_in_cache) return;
     uint32_t i;
     uint8_t* tile = p.cache + tile_at<N>((uint64_t)slot, head, p, i);
     if (is_value) {
 #pragma unroll
-        for (uint32_t g = 0; g < 8; ++g) *reinterpret_cast<uint16_t*>(tile + L::value_half(i, g, n)) = (uint16_t)(word[g / 2] >> (16 * (g & 1)));
+        for (uint32_t g = 0; g < 4; ++g) *reinterpret_cast<uint16_t*>(tile + L::value_half(i, 4 * half + g, n)) = (uint16_t)(word[g / 2] >> (16 * (g & 1)));
     } else {
-#pragma unroll
-        for (uint32_t t = 0; t < 4; ++t) *reinterpret_cast<uint32_t*>(tile + L::key_word(i, t, n)) = word[t];
+        *reinterpret_cast<uint32_t*>(tile + L::key_word(i, 2 * half, n)) = word[0];
+        *reinterpret_cast<uint32_t*>(tile + L::key_word(i, 2 * half + 1, n)) = word[1];
     }
     __half* meta = reinterpret_cast<__half*>(tile + (is_value ? L::value_meta(i, n) : L::key_meta(i, n)));
-    meta[0] = scale;
-    meta[(L::kKeyZero - L::kKeyScale) / 2] = zero;
+    if (half) meta[(L::kKeyZero - L::kKeyScale) / 2] = zero;
+    else meta[0] = scale;
 }
 
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
@@ -156,46 +165,57 @@ __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bf
 
 // The inverse, by the same threads. Outputs are [tokens][heads][D]; a token of a slot outside the cache reads as 0.
 template <int N, typename T>
-__global__ void __launch_bounds__(128) read_kernel(const RowsK p, T* __restrict__ k, T* __restrict__ v)
+__global__ void __launch_bounds__(kRowThreads) read_kernel(const RowsK p, T* __restrict__ k, T* __restrict__ v)
 {
     using L = Tile<N>;
-    const uint32_t n = threadIdx.x % N, token = blockIdx.x * (128 / N) + threadIdx.x / N, head = blockIdx.y;
-    const bool is_value = blockIdx.z;
-    if (token >= p.tokens) return;
-    const int64_t slot = __ldg(p.slots + token);
-    uint32_t word[4] = {0, 0, 0, 0};
+    const uint32_t half = threadIdx.x % 2, n = threadIdx.x / 2 % N, row = blockIdx.x * (kRowThreads / (2 * N)) + threadIdx.x / (2 * N), head = blockIdx.y;
+    const bool is_value = blockIdx.z, in = row < p.tokens;
+    const int64_t slot = in ? __ldg(p.slots + row) : -1;
+    uint32_t word[2] = {0, 0};
     float s = 0.0f, z = 0.0f;
     if (slot >= 0 && (uint64_t)slot < p.slots_in_cache) {
         uint32_t i;
         const uint8_t* tile = p.cache + tile_at<N>((uint64_t)slot, head, p, i);
 #pragma unroll
-        for (uint32_t t = 0; t < 4; ++t)
-            word[t] = is_value ? (uint32_t)*reinterpret_cast<const uint16_t*>(tile + L::value_half(i, 2 * t, n)) |
-                                     (uint32_t)*reinterpret_cast<const uint16_t*>(tile + L::value_half(i, 2 * t + 1, n)) << 16
-                               : *reinterpret_cast<const uint32_t*>(tile + L::key_word(i, t, n));
+        for (uint32_t t = 0; t < 2; ++t)
+            word[t] = is_value ? (uint32_t)*reinterpret_cast<const uint16_t*>(tile + L::value_half(i, 4 * half + 2 * t, n)) |
+                                     (uint32_t)*reinterpret_cast<const uint16_t*>(tile + L::value_half(i, 4 * half + 2 * t + 1, n)) << 16
+                               : *reinterpret_cast<const uint32_t*>(tile + L::key_word(i, 2 * half + t, n));
         const __half* meta = reinterpret_cast<const __half*>(tile + (is_value ? L::value_meta(i, n) : L::key_meta(i, n)));
         s = __half2float(meta[0]);
         z = __half2float(meta[(L::kKeyZero - L::kKeyScale) / 2]);
     }
-    T* to = (is_value ? v : k) + ((uint64_t)token * p.heads + head) * L::D + 32 * n;
+    constexpr int kPieces = 16 * sizeof(T) / 16;
+    uint4 piece[kPieces];
+    T* e = reinterpret_cast<T*>(piece);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        alignas(16) T e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float q = __uint_as_float(0x4B000000u | (word[t] >> (4 * i) & 15u)) - 8388608.0f;  // 2^23 + q, without a conversion
-            put(e + i, __fadd_rn(__fmul_rn(q, s), z));
+    for (int i = 0; i < 16; ++i) {
+        const float q = __uint_as_float(0x4B000000u | (word[i / 8] >> (4 * (i % 8)) & 15u)) - 8388608.0f;    // 2^23 + q, without a conversion
+        put(e + i, __fadd_rn(__fmul_rn(q, s), z));
+    }
+    uint4* to = reinterpret_cast<uint4*>((is_value ? v : k) + ((uint64_t)row * p.heads + head) * L::D + 32 * n);
+    if (kPieces == 2) {
+        // the pair's four pieces lie side by side: the threads exchange two, so that a store fills whole sectors
+        uint4 give = half ? piece[0] : piece[1], got;
+        got.x = __shfl_xor_sync(0xFFFFFFFFu, give.x, 1);
+        got.y = __shfl_xor_sync(0xFFFFFFFFu, give.y, 1);
+        got.z = __shfl_xor_sync(0xFFFFFFFFu, give.z, 1);
+        got.w = __shfl_xor_sync(0xFFFFFFFFu, give.w, 1);
+        if (in) {
+            to[half] = half ? got : piece[0];
+            to[2 + half] = half ? piece[1] : got;
         }
+    } else if (in) {
 #pragma unroll
-        for (uint32_t i = 0; i < sizeof(e) / 16; ++i) reinterpret_cast<uint4*>(to + 8 * t)[i] = reinterpret_cast<const uint4*>(e)[i];
+        for (int i = 0; i < kPieces; ++i) to[half * kPieces + i] = piece[i];
     }
 }
 
 template <int N, typename T>
 int launch_append(const RowsK& p, bool aligned, cudaStream_t st)
 {
-    constexpr uint32_t kTokens = 128 / N;
-    append_kernel<N, T><<<dim3((p.tokens + kTokens - 1) / kTokens, p.heads, 2), 128, 0, st>>>(p, aligned);
+    constexpr uint32_t kTokens = kRowThreads / (2 * N);
+    append_kernel<N, T><<<dim3((p.tokens + kTokens - 1) / kTokens, p.heads, 2), kRowThreads, 0, st>>>(p, aligned);
     KVP_CUDA(cudaGetLastError());
     return KVP_OK;
 }
@@ -203,8 +223,8 @@ int launch_append(const RowsK& p, bool aligned, cudaStream_t st)
 template <int N, typename T>
 int launch_read(const RowsK& p, void* k, void* v, cudaStream_t st)
 {
-    constexpr uint32_t kTokens = 128 / N;
-    read_kernel<N, T><<<dim3((p.tokens + kTokens - 1) / kTokens, p.heads, 2), 128, 0, st>>>(p, static_cast<T*>(k), static_cast<T*>(v));
+    constexpr uint32_t kTokens = kRowThreads / (2 * N);
+    read_kernel<N, T><<<dim3((p.tokens + kTokens - 1) / kTokens, p.heads, 2), kRowThreads, 0, st>>>(p, static_cast<T*>(k), static_cast<T*>(v));
     KVP_CUDA(cudaGetLastError());
     return KVP_OK;
 }
