@@ -153,14 +153,15 @@ constexpr uint32_t kFixed = 16;
 struct Line {
     uint32_t before, total;  // places before the entry asked for, and of all
     uint32_t chunk;
+    uint32_t count;          // tiles of a segment of that entry
 };
 __device__ __forceinline__ uint32_t entry_count(const AttendK& p, uint32_t e) { return p.units ? p.counts[e] : tiles_of(length_of(p, e)); }
 __device__ __forceinline__ uint32_t line_entries(const AttendK& p) { return p.units ? p.batch * p.heads.d : p.batch; }
 __device__ __forceinline__ uint32_t line_per(const AttendK& p) { return p.units ? p.segs.d : p.segs.d * p.heads.d; }
+__device__ __forceinline__ uint32_t places_of(uint32_t count, uint32_t per) { return count ? (count + kFixed) * per : 0u; }
 __device__ __forceinline__ uint32_t entry_places(const AttendK& p, uint32_t e, uint32_t per)
 {
-    const uint32_t n = entry_count(p, e);
-    return n ? (n + kFixed) * per : 0u;
+    return places_of(entry_count(p, e), per);
 }
 __device__ __forceinline__ uint32_t sum_upto(uint32_t x, uint32_t lane)       // over the lanes up to this one
 {
@@ -184,9 +185,11 @@ __device__ __forceinline__ Line find_in_line(const AttendK& p, uint32_t cta, uin
     const uint32_t E = line_entries(p), per = line_per(p), tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     Line line;
     if (E <= 128) {
-        uint32_t n[4], upto[4], base = 0;
+        uint32_t c[4], n[4], upto[4], base = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) n[i] = 32 * i + lane < E ? entry_places(p, 32 * i + lane, per) : 0u;
+        for (int i = 0; i < 4; ++i) c[i] = 32 * i + lane < E ? entry_count(p, 32 * i + lane) : 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n[i] = places_of(c[i], per);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             upto[i] = 0;
@@ -197,7 +200,7 @@ __device__ __forceinline__ Line find_in_line(const AttendK& p, uint32_t cta, uin
         }
         line.total = base;
         line.chunk = max((base + p.ctas - 1) / p.ctas, p.least);
-        line.before = 0;
+        line.before = line.count = 0;
         const uint64_t at = (uint64_t)line.chunk * cta;
         bool found = false;
 #pragma unroll
@@ -207,6 +210,7 @@ __device__ __forceinline__ Line find_in_line(const AttendK& p, uint32_t cta, uin
                 if (here) {
                     const int l = __ffs(here) - 1;
                     line.before = __shfl_sync(0xFFFFFFFFu, upto[i] - n[i], l);
+                    line.count = __shfl_sync(0xFFFFFFFFu, c[i], l);
                     if (cta != ~0u) entry = 32 * i + l;
                     found = true;
                 }
@@ -249,6 +253,7 @@ __device__ __forceinline__ Line find_in_line(const AttendK& p, uint32_t cta, uin
     __syncthreads();
     line.before = sm.before;
     if (cta != ~0u) entry = sm.entry;
+    if (cta == ~0u || (uint64_t)line.chunk * cta < total) line.count = entry_count(p, entry);
     return line;
 }
 
@@ -343,6 +348,8 @@ struct AttendSmem {
     uint32_t scan[kWarps];
     float2 ml[kWarps][kRows];
     float share[kWarps][kRows];
+    alignas(16) uint4 query[8][32];          // per group of 32 dims: each lane's fragments
+    float sums[8][kRows], factor[kRows];     // of the scaled queries per group and row; what scores are multiplied by
 };
 
 // list[i] = number of the (from + i)-th tile of row bh that is to be read, i < many <= kListCap. Every thread of the CTA calls it.
@@ -399,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
     if (begin >= line.total) return;
     uint32_t todo = min(line.chunk, line.total - (uint32_t)begin);  // places
     const uint32_t per = line_per(p), E = line_entries(p);
-    uint32_t count = entry_count(p, entry), inner = ((uint32_t)begin - line.before) / (count + kFixed);
+    uint32_t count = line.count, inner = ((uint32_t)begin - line.before) / (count + kFixed);
     uint32_t at_place = ((uint32_t)begin - line.before) - inner * (count + kFixed);      // in the segment
     uint8_t* const ring = ring_all + warp * kStages * L::kBytes;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
@@ -470,69 +477,70 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
         }
         begin_chunk();
 
-        // The queries as the right operand, divided by a power of two; the sums over groups for the zeros.
-        // The 4-bit numbers are centred by starting their products at -8 times those sums, which keeps the partial sums small.
-        uint32_t qf[N][4], qz[N == 8 ? 4 : 2];
-        float start0[N], start1[N], f0, f1;
+        // The queries as the right operand, divided by a power of two; the sums over groups for the zeros. The 4-bit numbers are
+        // centred by starting their products at -8 times those sums, which keeps the partial sums small. A warp prepares one group for all.
         {
-            float x[N][8], most = 0.0f;
+            float most = 0.0f;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                floats_of<HALF>(raw[n].x, x[n]);
-                floats_of<HALF>(raw[n].y, x[n] + 2);
-                floats_of<HALF>(raw[n].z, x[n] + 4);
-                floats_of<HALF>(raw[n].w, x[n] + 6);
+                float x[8];
+                floats_of<HALF>(raw[n].x, x);
+                floats_of<HALF>(raw[n].y, x + 2);
+                floats_of<HALF>(raw[n].z, x + 4);
+                floats_of<HALF>(raw[n].w, x + 6);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[n][i]));
+                for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
             }
             most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
             most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
             // largest magnitude in [2^6, 2^7); the power of two in two factors, either of them a normal number
             const int e = most > 0.0f && most < INFINITY ? ilogbf(most) - 6 : 0, half_e = -e / 2;
             const float by0 = __int_as_float((half_e + 127) << 23), by1 = __int_as_float((-e - half_e + 127) << 23);
-            float sums[N];
+            if (warp < N) {
+                uint4 mine = raw[0];
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                float sum = 0.0f;
+                for (int n = 1; n < N; ++n) mine = warp == (uint32_t)n ? raw[n] : mine;
+                float x[8], sum = 0.0f;
+                floats_of<HALF>(mine.x, x);
+                floats_of<HALF>(mine.y, x + 2);
+                floats_of<HALF>(mine.z, x + 4);
+                floats_of<HALF>(mine.w, x + 6);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    x[n][i] = x[n][i] * by0 * by1;
-                    sum += x[n][i];
+                    x[i] = x[i] * by0 * by1;
+                    sum += x[i];
                 }
                 sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
-                sums[n] = sum + __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-                start0[n] = __shfl_sync(0xFFFFFFFFu, sums[n], 8 * t) * -0x1p-17f;
-                start1[n] = __shfl_sync(0xFFFFFFFFu, sums[n], 8 * t + 4) * -0x1p-17f;
-                qf[n][0] = pack(x[n][0], x[n][4]);
-                qf[n][1] = pack(x[n][1], x[n][5]);
-                qf[n][2] = pack(x[n][2], x[n][6]);
-                qf[n][3] = pack(x[n][3], x[n][7]);
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+                sm.query[warp][lane] = make_uint4(pack(x[0], x[4]), pack(x[1], x[5]), pack(x[2], x[6]), pack(x[3], x[7]));
+                if (t == 0) sm.sums[warp][g] = sum;
             }
-            // the right operand of the zeros' product, 4 N columns: zeros times the upper parts of the sums and times what those leave,
-            // and scales times 8 of the same
-#pragma unroll
-            for (int j = 0; j < (N == 8 ? 4 : 2); ++j) {
-                float col[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t c = 8 * j + 2 * t + i;
-                    float v = 0.0f;
-#pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        const float up = __half2float(__float2half_rn(sums[n])), low = sums[n] - up;
-                        if (c == (uint32_t)n) v = up;
-                        if (c == (uint32_t)(N + n)) v = low;
-                        if (c == (uint32_t)(2 * N + n)) v = 8.0f * up;
-                        if (c == (uint32_t)(3 * N + n)) v = 8.0f * low;
-                    }
-                    col[i] = v;
-                }
-                qz[j] = pack(col[0], col[1]);
-            }
-            const float f = scalbnf(p.scale * 1.4426950408889634f, e);
-            f0 = __shfl_sync(0xFFFFFFFFu, f, 8 * t);
-            f1 = __shfl_sync(0xFFFFFFFFu, f, 8 * t + 4);
+            if (warp == 0 && t == 0) sm.factor[g] = scalbnf(p.scale * 1.4426950408889634f, e);
         }
+        __syncthreads();
+        uint32_t qf[N][4], qz[N == 8 ? 4 : 2];
+        float start0[N], start1[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            *reinterpret_cast<uint4*>(qf[n]) = sm.query[n][lane];
+            const float2 x = *reinterpret_cast<const float2*>(&sm.sums[n][2 * t]);
+            start0[n] = x.x * -0x1p-17f;
+            start1[n] = x.y * -0x1p-17f;
+        }
+        // the right operand of the zeros' product, 4 N columns: zeros times the upper parts of the sums and times what those leave,
+        // and scales times 8 of the same
+#pragma unroll
+        for (int j = 0; j < (N == 8 ? 4 : 2); ++j) {
+            float col[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t c = 8 * j + 2 * t + i, kind = c / N;
+                const float sum = sm.sums[c % N][g], up = __half2float(__float2half_rn(sum)), part = kind & 1 ? sum - up : up;
+                col[i] = kind > 3 ? 0.0f : kind & 2 ? 8.0f * part : part;
+            }
+            qz[j] = pack(col[0], col[1]);
+        }
+        const float f0 = sm.factor[2 * t], f1 = sm.factor[2 * t + 1];
         // rows 2 t and 2 t + 1 see the tokens before these, all rows those before `all`
         int32_t see0, see1, all;
         {
@@ -912,7 +920,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttendK p)
     uint32_t entry = entry0;
     wait_for_previous();
     const Line line = find_in_line(p, ~0u, entry, sm);
-    const uint32_t count = entry_count(p, entry0);
+    const uint32_t count = line.count;
     // the CTAs that worked on segment seg: first and last
     auto first_cta = [&](uint32_t seg) { return (line.before + (seg - entry0 * per) * (count + kFixed) + kFixed) / line.chunk; };
     auto last_cta = [&](uint32_t seg) { return (line.before + (seg - entry0 * per + 1) * (count + kFixed) - 1) / line.chunk; };
