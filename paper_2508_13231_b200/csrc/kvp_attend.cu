@@ -453,7 +453,14 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                 bad |= 1u << stage;                            // no tile, or in a page that is none
             }
         };
-        auto begin_chunk = [&]() {                                 // lists its tiles and sends for the first ones
+        auto send = [&](int from, int to) {
+#pragma unroll 1
+            for (int k = from; k < to; k += 2) {
+                if (k < (int)mine) { issue(k); issue(k + 1); }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            }
+        };
+        auto begin_chunk = [&]() {                                 // lists its tiles and sends for the first two
             many = p.units ? min(take - done, kListCap) : take;
             if (p.units) {
                 __syncthreads();
@@ -462,11 +469,7 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
             mine = many > warp ? (many - warp + kWarps - 1) / kWarps : 0;
             where = ~0u;
             bad = 0;
-#pragma unroll 1
-            for (int k = 0; k < kStages; k += 2) {
-                if (k < (int)mine) { issue(k); issue(k + 1); }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-            }
+            send(0, 2);
         };
         uint4 raw[N];                                              // this thread's part of row g's query: on their way before the tiles
         {
@@ -477,8 +480,8 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
         }
         begin_chunk();
 
-        // The queries as the right operand, divided by a power of two; the sums over groups for the zeros. The 4-bit numbers are
-        // centred by starting their products at -8 times those sums, which keeps the partial sums small. A warp prepares one group for all.
+        // The queries as the right operand, divided by a power of two, and their sums over groups for the zeros. A warp prepares one group for
+        // all; they stay in shared memory, which is read once for two tiles: 16 registers more would be too many.
         {
             float most = 0.0f;
 #pragma unroll
@@ -518,25 +521,16 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
             if (warp == 0 && t == 0) sm.factor[g] = scalbnf(p.scale * 1.4426950408889634f, e);
         }
         __syncthreads();
-        uint32_t qf[N][4], qz[N == 8 ? 4 : 2];
-        float start0[N], start1[N];
+        uint32_t qz[N == 8 ? 2 : 1];
+        // the right operand of the zeros' product, 2 N columns: the upper parts of the sums and what those leave
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            *reinterpret_cast<uint4*>(qf[n]) = sm.query[n][lane];
-            const float2 x = *reinterpret_cast<const float2*>(&sm.sums[n][2 * t]);
-            start0[n] = x.x * -0x1p-17f;
-            start1[n] = x.y * -0x1p-17f;
-        }
-        // the right operand of the zeros' product, 4 N columns: zeros times the upper parts of the sums and times what those leave,
-        // and scales times 8 of the same
-#pragma unroll
-        for (int j = 0; j < (N == 8 ? 4 : 2); ++j) {
+        for (int j = 0; j < (N == 8 ? 2 : 1); ++j) {
             float col[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const uint32_t c = 8 * j + 2 * t + i, kind = c / N;
                 const float sum = sm.sums[c % N][g], up = __half2float(__float2half_rn(sum)), part = kind & 1 ? sum - up : up;
-                col[i] = kind > 3 ? 0.0f : kind & 2 ? 8.0f * part : part;
+                col[i] = kind > 1 ? 0.0f : part;
             }
             qz[j] = pack(col[0], col[1]);
         }
@@ -573,6 +567,7 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
         };
 
         while (true) {
+            send(2, kStages);                                      // not sooner: the first two tiles of every warp are to come first
 #pragma unroll 1
             for (uint32_t k = 0; k < mine; k += 2) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(kStages / 2 - 1) : "memory");
@@ -607,26 +602,17 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                         const uint8_t* meta = tile + L::kKeyZero + (2 * t % N) * 2;
                         const uint32_t za = *reinterpret_cast<const uint32_t*>(meta + tok_a * 2 * N);
                         const uint32_t zb = *reinterpret_cast<const uint32_t*>(meta + tok_b * 2 * N);
-                        if constexpr (N == 2) {
-                            mma(z, t < 2 ? za : sa[0], t < 2 ? zb : sb[0], 0u, 0u, qz[0], 0u, 0.0f, 0.0f, 0.0f, 0.0f);
-                        } else {
-                            const uint32_t ka = *reinterpret_cast<const uint32_t*>(meta + tok_a * 2 * N - (L::kKeyZero - L::kKeyScale));
-                            const uint32_t kb = *reinterpret_cast<const uint32_t*>(meta + tok_b * 2 * N - (L::kKeyZero - L::kKeyScale));
-                            if constexpr (N == 4) {
-                                mma(z, za, zb, ka, kb, qz[0], qz[1], 0.0f, 0.0f, 0.0f, 0.0f);
-                            } else {
-                                mma(z, za, zb, za, zb, qz[0], qz[1], 0.0f, 0.0f, 0.0f, 0.0f);
-                                mma(z, ka, kb, ka, kb, qz[2], qz[3]);
-                            }
-                        }
+                        if constexpr (N == 8) mma(z, za, zb, za, zb, qz[0], qz[1], 0.0f, 0.0f, 0.0f, 0.0f);
+                        else mma(z, za, zb, 0u, 0u, qz[0], 0u, 0.0f, 0.0f, 0.0f, 0.0f);
                     }
 #pragma unroll
                     for (int n = 0; n < N; ++n) {
                         float acc[4];
-                        mma(acc, wa[n] * 16u & kNibble, wb[n] * 16u & kNibble, wa[n] & kNibble, wb[n] & kNibble, qf[n][0], qf[n][1],
-                            start0[n], start1[n], start0[n], start1[n]);
+                        const uint4 qn = sm.query[n][lane];
+                        mma(acc, wa[n] * 16u & kNibble, wb[n] * 16u & kNibble, wa[n] & kNibble, wb[n] & kNibble, qn.x, qn.y,
+                            0.0f, 0.0f, 0.0f, 0.0f);
                         const uint32_t xa = wa[n] >> 8, xb = wb[n] >> 8;
-                        mma(acc, xa * 16u & kNibble, xb * 16u & kNibble, xa & kNibble, xb & kNibble, qf[n][2], qf[n][3]);
+                        mma(acc, xa * 16u & kNibble, xb * 16u & kNibble, xa & kNibble, xb & kNibble, qn.z, qn.w);
                         const float2 pa = __half22float2(half2_of(sa[n / 2])), pb = __half22float2(half2_of(sb[n / 2]));
                         const float fa = n & 1 ? pa.y : pa.x, fb = n & 1 ? pb.y : pb.x;
                         sum[0] = fmaf(fa, acc[0], sum[0]);
@@ -918,9 +904,10 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttendK p)
     const uint32_t b = p.heads.of(bh), h = bh - b * p.heads.d;
     const uint32_t entry0 = p.units ? bh : b;
     uint32_t entry = entry0;
-    wait_for_previous();
+    if (p.units) wait_for_previous();                              // for the rows' counts; lengths were there before
     const Line line = find_in_line(p, ~0u, entry, sm);
     const uint32_t count = line.count;
+    if (!p.units) wait_for_previous();
     // the CTAs that worked on segment seg: first and last
     auto first_cta = [&](uint32_t seg) { return (line.before + (seg - entry0 * per) * (count + kFixed) + kFixed) / line.chunk; };
     auto last_cta = [&](uint32_t seg) { return (line.before + (seg - entry0 * per + 1) * (count + kFixed) - 1) / line.chunk; };
