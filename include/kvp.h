@@ -391,8 +391,9 @@ int kvp_trace_generate(const kvp_trace_params* params, uint32_t* access_bitmaps,
  * device: keys and values go into a cache held in 4 bits (kvp_cache_append), attention reads it and notes what weight every
  * unit received (kvp_attend), recorded weights become access bitmaps (kvp_trace_weights) for kvp_create, and they drive
  * eviction, as one step of a serving loop (kvp_evict) or as a placement schedule (kvp_policy_accumulated). They are
- * asynchronous on `stream`, keep nothing between calls, allocate nothing and work on the current device; all of them can be
- * captured into a graph (lengths, tables, slots and bitmaps are read on the device).
+ * asynchronous on `stream`, keep nothing between calls and work on the current device; all of them can be captured into a
+ * graph (lengths, tables, slots and bitmaps are read on the device). kvp_evict and kvp_policy_accumulated over several steps of few groups
+ * take up to 1 GiB of stream-ordered scratch, freed on return, as kvp_trace_generate does; the others allocate nothing.
  *
  * A cache held in 4 bits. [pages][kv_heads][kvp_cache_page_bytes(head_dim, page_tokens)] bytes, 16-byte aligned: a page holds
  * page_tokens (a multiple of 16) tokens of one kv-head as page_tokens / 16 tiles of 16 tokens, so that a unit of the placement
@@ -495,7 +496,8 @@ typedef struct {
 /*
  * kvp_evict -- `steps` steps: add the step's weights, then choose.
  *   weights  (device) [steps][groups * units_per_group], as kvp_attend gives them
- *   acc_in   (device) [groups * units_per_group] int64 or NULL (= 0);  acc_out (device) the same, may be acc_in itself
+ *   acc_in   (device) [groups * units_per_group] int64 or NULL (= 0);  acc_out (device) the same, may be acc_in itself (another overlap
+ *            is KVP_ERR_ARG)
  *   kept_in  (device) [W32] bitmap or NULL (= every unit): the units that may be kept besides the protected ones; in a serving
  *            loop the row the call before gave, so that what was evicted stays evicted
  *   exist    (device) [groups] int32 or NULL (= units_per_group): units the group has by now (cut to 0..units_per_group)

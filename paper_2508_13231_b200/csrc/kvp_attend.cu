@@ -92,7 +92,8 @@ __device__ __forceinline__ uint32_t length_of(const AttendK& p, uint32_t b)
 __device__ __forceinline__ uint32_t tiles_of(uint32_t tokens) { return (tokens + kTileTokens - 1) / kTileTokens; }
 
 // The kernels of a call follow each other closely: the next one's CTAs come up while the last ones of this one work, and wait
-// here until all of it is done and visible.
+// here until all of it is done and visible. No CTA ends without having waited: what comes after a call in its stream starts when the last
+// kernel has ended, and that must not be before the one in front of it.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -935,11 +936,12 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttendK p)
         if (!count) {
             if (tid < kQuads) reinterpret_cast<uint2*>(p.out)[at * kQuads + tid] = make_uint2(0u, 0u);
             if (tid == 0 && p.lse) p.lse[at] = -INFINITY;
+            if (!p.units) wait_for_previous();
             return;
         }
         const uint32_t c0 = first_cta(seg), c1 = last_cta(seg);
-        if (c0 == c1) return;                                      // written by its one CTA
         if (!p.units) wait_for_previous();
+        if (c0 == c1) return;                                      // written by its one CTA
         const uint32_t piece = lane % kQuads, own = c0 + warp * kOver + lane / kQuads;
         auto part = [&](uint32_t c, uint32_t j) {
             return reinterpret_cast<const float4*>(p.part)[(((uint64_t)c + seg) * kRows + r) * kQuads + piece + 32 * j];
@@ -1004,6 +1006,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttendK p)
     if (read && p.units) read = bits_at(p, (uint64_t)bh * p.row_units + unit) & 1u;
     if (!__syncthreads_or(read)) {                                 // none of these units is read
         if (unit < p.row_units) p.weights[(uint64_t)bh * p.row_units + unit] = 0.0f;
+        if (!p.units) wait_for_previous();
         return;
     }
     if (!p.units) wait_for_previous();

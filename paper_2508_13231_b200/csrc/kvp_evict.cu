@@ -329,6 +329,8 @@ extern "C" int kvp_evict(const kvp_evict_params* a, const float* weights, const 
     if (!weights || !acc_out || !kept_out) return KVP_ERR_ARG;
     const uint64_t words = ((uint64_t)a->groups * a->units_per_group + 31) / 32;
     if (kept_in && kept_in < kept_out + words * a->steps && kept_out < kept_in + words) return KVP_ERR_ARG;
+    const uint64_t units = (uint64_t)a->groups * a->units_per_group;
+    if (acc_in && acc_in != acc_out && acc_in < acc_out + units && acc_out < acc_in + units) return KVP_ERR_ARG;
     return launch_evict(a, weights, acc_in, acc_out, kept_in, exist, kept_out, false, static_cast<cudaStream_t>(stream));
 }
 
@@ -339,8 +341,5 @@ extern "C" int kvp_policy_accumulated(kvp_problem* p, const kvp_evict_params* a,
     if (rc) return rc;
     if (a->steps != p->S || (uint64_t)a->groups * a->units_per_group != p->U) return KVP_ERR_ARG;
     if ((uint64_t)a->groups * a->budget > p->cap) return KVP_ERR_CAPACITY;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int rs = ensure_scratch(p, (size_t)p->U * 8, st);
-    if (rs) return rs;
-    return launch_evict(a, weights, nullptr, static_cast<int64_t*>(p->d_scratch), nullptr, nullptr, schedule, true, st);
+    return launch_evict(a, weights, nullptr, nullptr, nullptr, nullptr, schedule, true, static_cast<cudaStream_t>(stream));
 }

@@ -73,6 +73,16 @@ GROWING = {
                        chains=1024, moves=100_000, p0=1e-6),
 }
 
+# Traces recorded from attention over a cache held in 4 bits: one layer, `queries` query heads over `kv_heads`, units of `unit_tokens` tokens,
+# `steps` tokens decoded after a prompt. rho: how much of a query stays from one token to the next.
+RECORDED = {
+    "recorded_small": dict(kv_heads=2, queries=8, head_dim=64, unit_tokens=16, prompt=400, steps=48, topk=6, share=0.3, rho=0.9,
+                           bw=(8 * TB, 9 * TB // 10, 9 * TB // 10)),
+    # one layer of an 8B-class model: 8 kv-heads, 2048 units of 16 tokens at the end
+    "recorded_8b": dict(kv_heads=8, queries=32, head_dim=128, unit_tokens=16, prompt=32512, steps=256, topk=205, share=0.25, rho=0.9,
+                        bw=(8 * TB, 9 * TB // 10, 9 * TB // 10)),
+}
+
 
 def growing_shape(cfg):
     """-> (groups, units, steps) of a GROWING configuration."""

@@ -141,9 +141,9 @@ def attend(q, cache, table, lens, unit, scale, units=None):
 
 def most_of(key, many, allowed):
     """The `many` allowed entries with the largest key, ties to the lower index."""
-    order = [i for i in sorted(range(len(key)), key=lambda i: (-key[i], i)) if allowed[i]]
-    out = np.zeros(len(key), bool)
-    out[order[:many]] = True
+    order = np.argsort(-np.asarray(key, np.float64 if np.asarray(key).dtype.kind == "f" else np.int64), kind="stable")
+    out = np.zeros(len(order), bool)
+    out[order[np.asarray(allowed)[order]][:many]] = True
     return out
 
 
@@ -169,9 +169,10 @@ def select(weights, groups, topk):
 def evict(weights, groups, budget, sink, recent, decay_q, acc=None, kept=None, exist=None, before=False):
     s, u = weights.shape
     n = u // groups
-    a = [0] * u if acc is None else [min(max(int(x), 0), 2 ** 48 - 1) for x in acc]
+    most = np.uint64(2 ** 48 - 1)
+    a = np.zeros(u, np.uint64) if acc is None else np.minimum(np.maximum(np.asarray(acc, np.int64), 0).astype(np.uint64), most)
     old = np.ones(u, bool) if kept is None else bit(kept, np.arange(u)).astype(bool)
-    fixed = np.rint(np.clip(np.nan_to_num(weights.astype(np.float64), nan=0.0, posinf=128.0), 0, 128) * 2.0 ** 24).astype(np.int64)
+    fixed = np.rint(np.clip(np.nan_to_num(weights.astype(np.float64), nan=0.0, posinf=128.0), 0, 128) * 2.0 ** 24).astype(np.uint64)
     out = np.zeros((s, u), bool)
 
     def choose(row):
@@ -180,12 +181,14 @@ def evict(weights, groups, budget, sink, recent, decay_q, acc=None, kept=None, e
             i = np.arange(n)
             safe = ((i < sink) | (i >= e - recent)) & (i < e)
             allowed = old[g * n:(g + 1) * n] & ~safe & (i < e)
-            row[g * n:(g + 1) * n] = safe | most_of(a[g * n:(g + 1) * n], max(0, budget - int(safe.sum())), allowed)
+            row[g * n:(g + 1) * n] = safe | most_of(a[g * n:(g + 1) * n].astype(np.int64), max(0, budget - int(safe.sum())), allowed)
 
     for t in range(s):
         if before:
             choose(out[t])
-        a = [min(((x * decay_q) >> 16) + int(w), 2 ** 48 - 1) for x, w in zip(a, fixed[t])]
+        if decay_q != 65536:                                  # below 2^48 * 65536: 64 bits hold the product
+            a = (a * np.uint64(decay_q)) >> np.uint64(16)
+        a = np.minimum(a + fixed[t], most)
         if not before:
             choose(out[t])
-    return pack(out), np.array(a, np.int64)
+    return pack(out), a.astype(np.int64)

@@ -131,6 +131,8 @@ def test_evict_refuses_rows_that_overlap(lib):
     w, acc, out = C.c_void_p(1 << 20), C.c_void_p(1 << 21), 1 << 22
     for kept in (out, out + 32, out - 12):
         assert lib.kvp_evict(C.byref(p), w, None, acc, C.c_void_p(kept), None, C.c_void_p(out), None) == ARG
+    for old in ((1 << 21) + 8, (1 << 21) - 8 * 127):                         # neither acc_out nor apart from it (128 units of 8 bytes)
+        assert lib.kvp_evict(C.byref(p), w, C.c_void_p(old), acc, None, None, C.c_void_p(out), None) == ARG
     for i in (0, 2, 5):
         args = [w, None, acc, None, None, C.c_void_p(out)]
         args[i] = None

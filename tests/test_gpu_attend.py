@@ -195,6 +195,52 @@ def test_attend_values_whose_size_changes_along_the_sequence(kvp):
         check(kvp, q, cache, table, np.array([n], np.int32), None, 16)
 
 
+def test_attend_a_large_batch(kvp):
+    """More sequences than a warp goes through by itself."""
+    lens = [int(x) for x in np.random.default_rng(2).integers(0, 60, 300)]
+    check(kvp, *problem(kvp, 300, 1, 1, 3, 64, 16, 16, lens), 16)
+
+
+def test_attend_lists_longer_than_a_chunk(kvp):
+    """So many tiles that a CTA's list of them comes in several pieces: a bitmap of ones reads what no bitmap reads, in the same order."""
+    heads, d, page, tokens = 8, 64, 64, 64 * 9600                        # 307,200 tiles: more than 1024 for each of 296 CTAs
+    pages = tokens // page
+    cache = torch.empty((pages, heads, kvp.cache_page_bytes(d, page)), dtype=torch.uint8, device="cuda")
+    torch.manual_seed(0)
+    for at in range(0, tokens, 1 << 16):
+        n = min(1 << 16, tokens - at)
+        kvp.cache_append(cache, torch.randn(n, heads, d, device="cuda"), torch.randn(n, heads, d, device="cuda"), torch.arange(at, at + n, device="cuda"))
+    table = torch.randperm(pages, device="cuda").int()[None]
+    lens = torch.tensor([tokens - 5], dtype=torch.int32, device="cuda")
+    q = torch.randn(1, 2 * heads, d, device="cuda").to(BF16)
+    for unit in (1, 16, 64):
+        ones = torch.full((heads * tokens // unit // 32,), -1, dtype=torch.int32, device="cuda")
+        a, b = (kvp.attend(q, cache, table, lens, unit_tokens=unit, units=u, want_lse=True, want_weights=True) for u in (None, ones))
+        assert all(torch.equal(a[k], b[k]) for k in a)
+        assert abs(float(a["weights"].sum()) - 2 * heads) < 1e-3
+
+
+def test_a_cache_beyond_four_gigabytes(kvp):
+    """Tokens in the last pages of a cache of 4.9 GB, against the same tokens in a small one."""
+    heads, d, page, tokens = 8, 256, 64, 150
+    size = kvp.cache_page_bytes(d, page)
+    pages = 30000
+    big = torch.zeros((pages, heads, size), dtype=torch.uint8, device="cuda")
+    small = torch.zeros((3, heads, size), dtype=torch.uint8, device="cuda")
+    k, v = torch.randn(2, tokens, heads, d, device="cuda").to(BF16)
+    slots = torch.arange(tokens, device="cuda")
+    kvp.cache_append(small, k, v, slots)
+    kvp.cache_append(big, k, v, slots + (pages - 3) * page)
+    assert torch.equal(big[-3:], small) and not bool(big[:-3].any())
+    for x, y in zip(kvp.cache_read(big, slots + (pages - 3) * page, d), kvp.cache_read(small, slots, d)):
+        assert torch.equal(x, y)
+    q = torch.randn(1, 2 * heads, d, device="cuda").to(BF16)
+    lens = torch.tensor([tokens], dtype=torch.int32, device="cuda")
+    table = torch.arange(3, dtype=torch.int32, device="cuda")[None]
+    a, b = kvp.attend(q, small, table, lens, want_weights=True), kvp.attend(q, big, table + pages - 3, lens, want_weights=True)
+    assert torch.equal(a["out"], b["out"]) and torch.equal(a["weights"], b["weights"])
+
+
 @pytest.mark.parametrize("keep", [1.0, 0.1])
 def test_attend_long_and_many(kvp, keep):
     check(kvp, *problem(kvp, 2, 1, 2, 2, 128, 32, 32, [20011, 40], keep=keep), 32)                       # many CTAs for one row
@@ -353,6 +399,66 @@ def test_evict(kvp, groups, n, steps, budget, sink, recent, decay):
     assert again["acc"].data_ptr() == a.data_ptr() and torch.equal(a, got["acc"]) and torch.equal(again["kept"], got["kept"])
 
 
+def test_choices_in_graphs_and_on_streams(kvp):
+    """Captured and replayed with other weights, on a stream of their own, in both forms of eviction (many steps of few groups, and one step)."""
+    rng = np.random.default_rng(8)
+    for groups, n, steps in ((2, 96, 40), (6, 2048, 1), (3, 4096, 12)):
+        sets = [weights_of(rng, steps, groups, n) for _ in range(2)]
+        w = cuda(sets[0])
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        run = lambda **kw: (kvp.evict(w, groups, 30, sink=1, recent=2, decay_q=60000, **kw), kvp.trace_weights(w, groups, 20, **kw))  # noqa: E731
+        first = run(stream=side)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            caught = run()
+        for i in (0, 1, 0):
+            w.copy_(cuda(sets[i]))
+            graph.replay()
+            torch.cuda.synchronize()
+            rows, acc = plain.evict(sets[i], groups, 30, 1, 2, 60000)
+            assert np.array_equal(host_bits(caught[0]["kept"]), rows) and np.array_equal(caught[0]["acc"].cpu().numpy(), acc)
+            assert np.array_equal(host_bits(caught[1]), plain.select(sets[i], groups, 20))
+            if i == 0:
+                assert torch.equal(first[0]["kept"], caught[0]["kept"]) and torch.equal(first[1], caught[1])
+
+
+def test_choices_among_equal_weights(kvp):
+    """Many units with the same sum, few above them: the lowest indices are chosen, in every size of row and both forms."""
+    for n in (5, 200, 4096, 7000, 32768):
+        for steps in (1, 3):
+            w = np.full((steps, n), 0.25, np.float32)
+            w[:, n // 2:: 97] = 0.5
+            w[:, 1:: 131] = 0
+            many = max(1, n // 3)
+            assert np.array_equal(host_bits(kvp.trace_weights(cuda(w), 1, many)), plain.select(w, 1, many))
+            rows, acc = plain.evict(w, 1, many, 0, 0, 65536)
+            got = kvp.evict(cuda(w), 1, many)
+            assert np.array_equal(host_bits(got["kept"]), rows) and np.array_equal(got["acc"].cpu().numpy(), acc)
+
+
+def test_choices_over_a_long_drift(kvp):
+    """Rows whose thresholds move slowly, jump, and come back, sums that share their upper bits, weights that differ in the last bit only."""
+    rng = np.random.default_rng(12)
+    n, steps = 1500, 60
+    w = np.exp(rng.standard_normal(n)[None] + 0.1 * np.cumsum(rng.standard_normal((steps, n)), 0)).astype(np.float32)
+    w[20] *= 1000
+    w[30] = 1 + rng.integers(0, 40, n).astype(np.float32) * np.float32(2.0 ** -23)
+    w[40:45] = 0
+    w = np.minimum(w, 120).astype(np.float32)
+    assert np.array_equal(host_bits(kvp.trace_weights(cuda(w), 1, 100)), plain.select(w, 1, 100))
+    start = (2 ** 47 + rng.integers(0, 5000, n)).astype(np.int64)
+    for acc, decay in ((None, 65536), (None, 60000), (start, 65536)):
+        rows, sums = plain.evict(w, 1, 200, 1, 3, decay, acc)
+        got = kvp.evict(cuda(w), 1, 200, sink=1, recent=3, decay_q=decay, acc=None if acc is None else cuda(acc))
+        assert np.array_equal(host_bits(got["kept"]), rows) and np.array_equal(got["acc"].cpu().numpy(), sums)
+        many = np.tile(w, (1, 3))                             # three groups alike: the other form for as many steps
+        got = kvp.evict(cuda(many), 3, 200, sink=1, recent=3, decay_q=decay, acc=None if acc is None else cuda(np.tile(acc, 3)))
+        bits = np.stack([plain.bit(r, np.arange(n)) for r in rows]).astype(bool)
+        assert np.array_equal(host_bits(got["kept"]), plain.pack(np.tile(bits, (1, 3))))
+
+
 def test_evict_step_by_step_is_the_whole_walk(kvp):
     w = weights_of(np.random.default_rng(4), 9, 4, 96)
     whole = kvp.evict(cuda(w), 4, 20, sink=1, recent=2, decay_q=60000)
@@ -364,8 +470,17 @@ def test_evict_step_by_step_is_the_whole_walk(kvp):
     assert torch.equal(acc, whole["acc"])
 
 
-def test_policy_accumulated(kvp):
-    groups, n, steps = 3, 96, 12
+@pytest.mark.parametrize("groups,n,steps,decay", [(110, 4096, 9, 65536), (150, 3000, 7, 61000), (60, 8192, 4, 65536), (20, 16384, 4, 65536), (14, 30000, 3, 65000)])
+def test_evict_many_groups(kvp, groups, n, steps, decay):
+    """Enough units for the form that walks the steps of a group in one CTA."""
+    w = weights_of(np.random.default_rng(n), steps, groups, n) * 4
+    rows, acc = plain.evict(w, groups, n // 10, 1, 4, decay)
+    got = kvp.evict(cuda(w), groups, n // 10, sink=1, recent=4, decay_q=decay)
+    assert np.array_equal(host_bits(got["kept"]), rows) and np.array_equal(got["acc"].cpu().numpy(), acc)
+
+
+@pytest.mark.parametrize("groups,n,steps", [(3, 96, 12), (3, 96, 5), (3, 96, 1)])
+def test_policy_accumulated(kvp, groups, n, steps):
     w = weights_of(np.random.default_rng(6), steps, groups, n)
     access = kvp.trace_weights(cuda(w), groups, 10)
     prob = kvp.Problem(groups * n, 8192, steps, access, 80, 8 * 10 ** 12, 9 * 10 ** 11, 9 * 10 ** 11)
@@ -381,7 +496,7 @@ def test_policy_accumulated(kvp):
             prob.policy_accumulated(cuda(w), **kw)
         assert e.value.code == code
     with pytest.raises(ValueError):
-        prob.policy_accumulated(cuda(w[1:]), groups)
+        prob.policy_accumulated(cuda(w[:, 1:]), groups)
 
 
 def test_a_decode_loop_from_attention_to_the_bound(kvp):
