@@ -18,7 +18,21 @@
 
 #include "../../include/kvp.h"
 
+// A library without these still serves the scoring calls; the calls that need them say so.
+#pragma weak kvp_cache_append
+#pragma weak kvp_cache_read
+#pragma weak kvp_attend
+#pragma weak kvp_attend_workspace
+#pragma weak kvp_trace_weights
+#pragma weak kvp_evict
+
 namespace {
+
+PyObject* missing(const char* name)
+{
+    PyErr_Format(PyExc_ImportError, "libkvp.so has no %s: build it with `python -m paper_2508_13231_b200.build`", name);
+    return nullptr;
+}
 
 PyObject* value_error(const char* what)
 {
@@ -255,6 +269,7 @@ bool rows_of(PyObject* o, const char* what, const kvp_cache_shape& c, c10::Devic
 PyObject* cache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
+    if (!kvp_cache_append) return missing("kvp_cache_append");
     if (nargs != 5) return value_error("cache_append takes 5 arguments");
     kvp_cache_shape c;
     const at::Tensor *k = tensor_of(args[1], "k"), *v, *slots, *cache;
@@ -285,6 +300,7 @@ PyObject* cache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
+    if (!kvp_cache_read) return missing("kvp_cache_read");
     if (nargs != 5) return value_error("cache_read takes 5 arguments");
     kvp_cache_shape c;
     const at::Tensor *cache, *slots;
@@ -320,6 +336,7 @@ PyObject* k_out; PyObject* k_lse; PyObject* k_weights; PyObject* k_kept; PyObjec
 PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
+    if (!kvp_attend) return missing("kvp_attend");
     if (nargs != 10) return value_error("attend takes 10 arguments");
     const at::Tensor *q = tensor_of(args[0], "q"), *cache, *table, *lens, *units, *weights = nullptr;
     if (!q) return nullptr;
@@ -400,6 +417,7 @@ bool weights_of(PyObject* o, uint32_t groups, uint32_t* n, uint32_t* steps, cons
 PyObject* trace_weights(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
+    if (!kvp_trace_weights) return missing("kvp_trace_weights");
     if (nargs != 5) return value_error("trace_weights takes 5 arguments");
     const at::Tensor *w, *given;
     uint32_t groups, n, steps, topk;
@@ -427,6 +445,7 @@ PyObject* trace_weights(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 PyObject* evict(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
+    if (!kvp_evict) return missing("kvp_evict");
     if (nargs != 11) return value_error("evict takes 11 arguments");
     const at::Tensor *w, *acc, *kept, *exist, *acc_out;
     kvp_evict_params p;
