@@ -291,11 +291,13 @@ int launch_evict(const kvp_evict_params* a, const float* weights, const int64_t*
     k.groups = a->groups;
     if (!k.aligned) KVP_CUDA(cudaMemsetAsync(rows, 0, (size_t)a->steps * k.W32 * 4, st));
     const uint32_t n = k.n;
-    // A step of the one-pass form takes about 1.5 us as long as the groups fit the SMs' registers at once; the other form moves 24 bytes
-    // per unit and step, for which 4 ps are about right, in kernels that take 10 us at least.
-    const uint64_t waves = (k.groups + 1035) / 1036, all = k.U * a->steps;
+    // Which form is the faster one, in seconds as measured. One pass: a step takes 2.5 us and more with the units of a group (0.3 ns each, 0.8 where a
+    // CTA fills an SM), and with the groups (640 instead of 64: 5.8 instead of 3.8 us). Two passes: 14 us and 5.8 ps per unit and step.
+    // 8 groups x 2048 units x 16 steps 51 and 15 us, x 256 steps 668 and 35; 64 x 4096 x 64 244 and 90; 200 x 4096 x 64 281 and 311.
+    const uint64_t all = k.U * a->steps;
     const size_t bytes = all * 8;
-    const bool two = a->steps > 1 && bytes <= ((size_t)1 << 30) && 1.5e-6 * (double)(waves * a->steps) > 4e-12 * (double)all + 10e-6;
+    const double step = (2.5e-6 + n * (n > 16384 ? 0.8e-9 : 0.3e-9)) * (1 + k.groups / 1000.0);
+    const bool two = a->steps > 1 && bytes <= ((size_t)1 << 30) && a->steps * step > 14e-6 + 5.8e-12 * (double)all;
     if (two) {
         int dev = 0;
         KVP_CUDA(cudaGetDevice(&dev));
@@ -303,10 +305,10 @@ int launch_evict(const kvp_evict_params* a, const float* weights, const int64_t*
         if (prc) return prc;
         KVP_CUDA(cudaMallocAsync(&k.sums, bytes, st));
         sums_kernel<<<(uint32_t)((k.U + 127) / 128), 128, 0, st>>>(k);
-        k.chunk = std::max(1u, (uint32_t)std::min<uint64_t>(16, (uint64_t)k.groups * a->steps / (148 * 16)));
+        k.chunk = select_chunk((uint64_t)k.groups * a->steps);
     }
     const uint32_t threads = select_threads(n);
-    const int rc = threads == 128 ? launch_choice<128>(k, two, st) : threads == 256 ? launch_choice<256>(k, two, st)
+    const int rc = threads == 32 ? launch_choice<32>(k, two, st) : threads == 128 ? launch_choice<128>(k, two, st) : threads == 256 ? launch_choice<256>(k, two, st)
                  : threads == 512 ? launch_choice<512>(k, two, st) : launch_choice<1024>(k, two, st);
     const cudaError_t le = cudaGetLastError();
     if (two) KVP_CUDA(cudaFreeAsync(k.sums, st));

@@ -424,7 +424,11 @@ __device__ __forceinline__ void put_words(uint32_t* row, uint64_t first, uint32_
     }
 }
 
-// Threads of a CTA for rows of n units (at most 32768): 32 rounds at most, and 128 threads where that is enough.
-inline uint32_t select_threads(uint32_t n) { return n <= 4096 ? 128 : n <= 8192 ? 256 : n <= 16384 ? 512 : 1024; }
+// Threads of a CTA for rows of n units (at most 32768): 32 rounds at most, 128 threads where that is enough, and a warp (whose barriers
+// cost nothing) up to eight rounds.
+inline uint32_t select_threads(uint32_t n) { return n <= 256 ? 32 : n <= 4096 ? 128 : n <= 8192 ? 256 : n <= 16384 ? 512 : 1024; }
+
+// Consecutive rows of a CTA: it begins with the search for a band, so some rows together are cheaper once there are CTAs enough for all SMs (ten an SM).
+inline uint32_t select_chunk(uint64_t rows) { return rows <= 148 * 10 ? 1 : rows >= 148 * 10 * 7 ? 8 : (uint32_t)(rows / (148 * 10)) + 1; }
 
 }  // namespace kvp

@@ -450,7 +450,7 @@ struct WeightsRow {
 };
 
 template <int T, bool FULL>
-__global__ void __launch_bounds__(T, T == 1024 ? 1 : 1280 / T) weights_select_kernel(const TraceK k, uint32_t chunk, uint64_t U, const float* __restrict__ weights)
+__global__ void __launch_bounds__(T, T == 1024 ? 1 : T == 32 ? 16 : 1280 / T) weights_select_kernel(const TraceK k, uint32_t chunk, uint64_t U, const float* __restrict__ weights)
 {
     __shared__ SelectShared<uint32_t, T> sm;
     const uint32_t g = blockIdx.x % k.groups, t0 = blockIdx.x / k.groups * chunk, t1 = min(t0 + chunk, k.steps);
@@ -485,8 +485,7 @@ extern "C" int kvp_trace_weights(uint32_t groups, uint32_t units_per_group, uint
     k.out = access_bitmaps;
     k.aligned = units_per_group % 32 == 0;
     if (!k.aligned) KVP_CUDA(cudaMemsetAsync(access_bitmaps, 0, (size_t)steps * k.W32 * 4, st));
-    // Consecutive steps to a CTA once there are enough CTAs: a CTA begins with the search for a band, but many short ones fill the SMs better
-    // (640 groups of 4096 units x 64 steps: 8 steps to a CTA 208 us, 4 steps 224, 16 steps 213, all 64 349; with ten CTAs an SM, 224 with 16).
+    // 640 groups of 4096 units x 64 steps: 8 steps to a CTA 208 us, 4 steps 224, 16 steps 213, all 64 349; with ten CTAs an SM, 224 with 16
     const uint32_t chunk = std::max(1u, std::min(8u, groups * steps / (148u * 16u)));
     const uint32_t grid = groups * ((steps + chunk - 1) / chunk);
 #define KVP_SELECT(T)                                                                                     \
@@ -495,6 +494,7 @@ extern "C" int kvp_trace_weights(uint32_t groups, uint32_t units_per_group, uint
         else weights_select_kernel<T, true><<<grid, T, 0, st>>>(k, chunk, U, weights);                         \
     } while (0)
     switch (select_threads(k.n)) {
+        case 32: KVP_SELECT(32); break;
         case 128: KVP_SELECT(128); break;
         case 256: KVP_SELECT(256); break;
         case 512: KVP_SELECT(512); break;
