@@ -66,8 +66,10 @@ __device__ __forceinline__ Members members_of(const EvictK& p, uint32_t g)
     return m;
 }
 
-// One pass. The sums of a group, 48 bits each, are in shared memory as lower words and upper half-words (24 KB for 4096 units: seven CTAs an SM,
-// so that 1036 groups of that size are worked on at once); a step's first pass adds its weights.
+// One pass. The sums of a group, 48 bits each, are in shared memory as lower words and upper half-words (24 KB for 4096 units: five CTAs an SM,
+// so that 740 groups of that size are worked on at once); a step's first pass adds its weights. In registers they spill at five CTAs an SM. What
+// bounds it is the latency of a step (two barriers, the search of the band's bins by one warp) with 17 warps an SM, and 5100 warp instructions
+// for 4096 units: 640 groups x 64 steps in 374 us, 114 of them for the bytes. Twice the warps without the step ahead are no faster (387 us).
 // FULL: n = 32 T, so that every slot of 32 rounds holds a unit; the weights of a step are then on their way while the step before is chosen for.
 template <int T, bool FULL>
 struct SumsRow {

@@ -479,24 +479,34 @@ def test_evict_many_groups(kvp, groups, n, steps, decay):
     assert np.array_equal(host_bits(got["kept"]), rows) and np.array_equal(got["acc"].cpu().numpy(), acc)
 
 
-@pytest.mark.parametrize("groups,n,steps", [(3, 96, 12), (3, 96, 5), (3, 96, 1)])
+@pytest.mark.parametrize("groups,n,steps", [(3, 96, 12), (3, 96, 5), (3, 96, 1), (2, 4096, 3), (1, 8192, 2), (2, 4096, 20)])
 def test_policy_accumulated(kvp, groups, n, steps):
     w = weights_of(np.random.default_rng(6), steps, groups, n)
     access = kvp.trace_weights(cuda(w), groups, 10)
     prob = kvp.Problem(groups * n, 8192, steps, access, 80, 8 * 10 ** 12, 9 * 10 ** 11, 9 * 10 ** 11)
-    for kw, budget in ((dict(), 26), (dict(budget=20, sink=1, recent=3, decay_q=62000), 20)):
+    for kw, budget in ((dict(), 80 // groups), (dict(budget=20, sink=1, recent=3, decay_q=62000), 20)):
         got = prob.policy_accumulated(cuda(w), groups, **kw)
         want, _ = plain.evict(w, groups, budget, kw.get("sink", 0), kw.get("recent", 0), kw.get("decay_q", 65536), before=True)
         assert np.array_equal(host_bits(got), want)
         ev = prob.eval(got)
         assert int(ev["bad_step"][0]) == -1
+
+
+def test_policy_accumulated_refuses(kvp):
+    w = cuda(weights_of(np.random.default_rng(6), 4, 3, 96))
+    prob = kvp.Problem(3 * 96, 8192, 4, kvp.trace_weights(w, 3, 10), 80, 8 * 10 ** 12, 9 * 10 ** 11, 9 * 10 ** 11)
     for kw, code in ((dict(groups=3, budget=27), kvp.ERR_CAPACITY), (dict(groups=3, budget=97), kvp.ERR_ARG), (dict(groups=5), kvp.ERR_ARG),
                      (dict(groups=0), kvp.ERR_ARG), (dict(groups=3, budget=5, sink=4, recent=2), kvp.ERR_ARG)):
         with pytest.raises(kvp.KvpError) as e:
-            prob.policy_accumulated(cuda(w), **kw)
+            prob.policy_accumulated(w, **kw)
         assert e.value.code == code
     with pytest.raises(ValueError):
-        prob.policy_accumulated(cuda(w[:, 1:]), groups)
+        prob.policy_accumulated(w[1:], 3)
+    birth = torch.zeros(3 * 96, dtype=torch.int32, device="cuda")
+    growing = kvp.Problem(3 * 96, 8192, 4, kvp.trace_weights(w, 3, 10), 80, 8 * 10 ** 12, 9 * 10 ** 11, 9 * 10 ** 11, birth=birth)
+    with pytest.raises(kvp.KvpError) as e:
+        growing.policy_accumulated(w, 3)
+    assert e.value.code == kvp.ERR_ARG
 
 
 def test_a_decode_loop_from_attention_to_the_bound(kvp):
