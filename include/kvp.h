@@ -392,8 +392,9 @@ int kvp_trace_generate(const kvp_trace_params* params, uint32_t* access_bitmaps,
  * unit received (kvp_attend), recorded weights become access bitmaps (kvp_trace_weights) for kvp_create, and they drive
  * eviction, as one step of a serving loop (kvp_evict) or as a placement schedule (kvp_policy_accumulated). They are
  * asynchronous on `stream`, keep nothing between calls and work on the current device; all of them can be captured into a
- * graph (lengths, tables, slots and bitmaps are read on the device). kvp_evict and kvp_policy_accumulated over several steps of few groups
- * take up to 1 GiB of stream-ordered scratch, freed on return, as kvp_trace_generate does; the others allocate nothing.
+ * graph (lengths, tables, slots and bitmaps are read on the device). What a call writes overlaps nothing that it reads, but where it
+ * says so. kvp_evict and kvp_policy_accumulated over several steps of few groups take up to 1 GiB of stream-ordered scratch,
+ * freed on return, as kvp_trace_generate does; the others allocate nothing.
  *
  * A cache held in 4 bits. [pages][kv_heads][kvp_cache_page_bytes(head_dim, page_tokens)] bytes, 16-byte aligned: a page holds
  * page_tokens (a multiple of 16) tokens of one kv-head as page_tokens / 16 tiles of 16 tokens, so that a unit of the placement
@@ -422,10 +423,11 @@ uint64_t kvp_cache_page_bytes(uint32_t head_dim, uint32_t page_tokens);
 /*
  * kvp_cache_append -- quantise the keys and values of `tokens` tokens into the cache.
  *   k, v   (device) [tokens][kv_heads][head_dim] of `dtype` (KVP_BF16, KVP_F16, KVP_F32); strides in elements, dims contiguous.
- *          Any alignment; 16-byte aligned rows are read faster.
+ *          At the alignment of their type; 16-byte aligned rows are read faster.
  *   slots  (device) [tokens]: page * page_tokens + place in the page. A token whose slot lies outside the cache is not written
  *          (use -1 for padding). Two tokens of one call with the same slot leave a mixture of both there.
- * Errors: KVP_ERR_ARG (null, zero sizes, unknown dtype, page_tokens no multiple of 16), KVP_ERR_RANGE (head_dim, kv_heads > 65535).
+ * Errors: KVP_ERR_ARG (null, zero sizes, unknown dtype, page_tokens no multiple of 16, a cache that is not 16-byte aligned),
+ * KVP_ERR_RANGE (head_dim, kv_heads > 65535).
  */
 int kvp_cache_append(const kvp_cache_shape* c, void* cache, uint32_t dtype, uint32_t tokens, const void* k,
                      int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
@@ -464,7 +466,8 @@ typedef struct {
  *           share the kv-head; 0 for units that were not read
  *   workspace (device) 256-byte aligned, kvp_attend_workspace(...) bytes, used by this call alone until its work has finished
  * A query that sees no token gives out 0 and lse -infinity. Errors: KVP_ERR_ARG (null, zero sizes, unit_tokens, dtype, a scale that is
- * not finite, a workspace too small), KVP_ERR_RANGE (head_dim, sizes above).
+ * not finite, a workspace too small, a cache that is not 16-byte aligned, a workspace that is not 256-byte
+ * aligned, out not 8-byte aligned), KVP_ERR_RANGE (head_dim, sizes above).
  */
 int kvp_attend_workspace(const kvp_attend_params* params, int want_weights, int has_units, uint64_t* bytes);
 int kvp_attend(const kvp_attend_params* params, const void* q, const void* cache, const int32_t* table, const int32_t* lens,

@@ -1187,6 +1187,8 @@ extern "C" int kvp_attend(const kvp_attend_params* a, const void* q, const void*
     if (!q || !cache || !table || !lens || !out || !workspace) return KVP_ERR_ARG;
     const Work w = workspace_of(a, weights != nullptr, units != nullptr);
     if (workspace_bytes < w.total) return KVP_ERR_ARG;
+    if (off_by(q, 2) || off_by(cache, 16) || off_by(table, 4) || off_by(lens, 4) || off_by(units, 4) || off_by(out, 8) || off_by(lse, 4) || off_by(weights, 4) ||
+        off_by(workspace, 256)) return KVP_ERR_ARG;
     AttendK k;
     k.q = q; k.out = out; k.lse = lse; k.weights = weights;
     k.cache = static_cast<const uint8_t*>(cache); k.table = table; k.lens = lens; k.units = units;

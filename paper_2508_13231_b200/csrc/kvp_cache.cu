@@ -229,12 +229,13 @@ int launch_read(const RowsK& p, void* k, void* v, cudaStream_t st)
     return KVP_OK;
 }
 
-int check_rows(const kvp_cache_shape* c, const void* cache, uint32_t tokens, const void* a, const void* b, const int64_t* slots, uint32_t dtype)
+int check_rows(const kvp_cache_shape* c, const void* cache, uint32_t tokens, const void* a, const void* b, uint32_t rows_align, const int64_t* slots, uint32_t dtype)
 {
     if (!c || c->reserved || !c->pages || !c->kv_heads || dtype > KVP_F32) return KVP_ERR_ARG;
     if (!c->page_tokens || c->page_tokens % kTileTokens) return KVP_ERR_ARG;
     if (!head_dim_served(c->head_dim)) return KVP_ERR_RANGE;
     if (tokens && (!cache || !a || !b || !slots)) return KVP_ERR_ARG;
+    if (off_by(cache, 16) || off_by(a, rows_align) || off_by(b, rows_align) || off_by(slots, 8)) return KVP_ERR_ARG;
     if (c->kv_heads > 65535 || tokens >= (1u << 31)) return KVP_ERR_RANGE;
     return KVP_OK;
 }
@@ -269,7 +270,7 @@ extern "C" int kvp_cache_append(const kvp_cache_shape* c, void* cache, uint32_t 
                                 int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
                                 int64_t v_head_stride, const int64_t* slots, void* stream)
 {
-    const int rc = check_rows(c, cache, tokens, k, v, slots, dtype);
+    const int rc = check_rows(c, cache, tokens, k, v, dtype == KVP_F32 ? 4 : 2, slots, dtype);
     if (rc || !tokens) return rc;
     RowsK p;
     p.k = k; p.v = v;
@@ -290,7 +291,7 @@ extern "C" int kvp_cache_append(const kvp_cache_shape* c, void* cache, uint32_t 
 extern "C" int kvp_cache_read(const kvp_cache_shape* c, const void* cache, uint32_t dtype, uint32_t tokens, const int64_t* slots,
                               void* k, void* v, void* stream)
 {
-    const int rc = check_rows(c, cache, tokens, k, v, slots, dtype);
+    const int rc = check_rows(c, cache, tokens, k, v, 16, slots, dtype);
     if (rc || !tokens) return rc;
     RowsK p = {};
     p.slots = slots; p.cache = static_cast<uint8_t*>(const_cast<void*>(cache));

@@ -154,3 +154,19 @@ def test_plain_forms_agree_with_hand_worked_cases():
     assert rows[0, 0] == 0b100011 and acc.tolist() == [1 << 23, 1 << 22, 1 << 22, 0, 0, 0]
     rows, acc = plain.evict(np.zeros((1, 6), np.float32), 1, 2, 0, 0, 32768, acc=[3, 8, 8, 9, 0, 0], kept=np.array([0b110111], np.uint32))
     assert rows[0, 0] == 0b000110 and acc.tolist() == [1, 4, 4, 4, 0, 0]
+
+
+def test_calls_refuse_addresses_that_are_not_aligned(lib):
+    """Checked on the host: the kernels move 16 bytes at a time."""
+    some, st, off = C.c_void_p(256), C.c_int64(256), lambda n: C.c_void_p(256 + n)
+    p, need = attend_params(), C.c_uint64(1 << 40)
+    for i, by in ((0, 1), (1, 8), (2, 2), (3, 2), (4, 2), (5, 4), (6, 2), (7, 2), (8, 16)):     # q, cache, table, lens, units, out, lse, weights, workspace
+        args = [some] * 9
+        args[i] = off(by)
+        assert lib.kvp_attend(C.byref(p), *args, need, None) == ARG, i
+    shape = Shape(4, 2, 128, 16, 0)
+    for dtype, by in ((0, 1), (1, 1), (2, 2)):
+        for cache, k, v, slots in ((off(8), some, some, some), (some, off(by), some, some), (some, some, off(by), some), (some, some, some, off(4))):
+            assert lib.kvp_cache_append(C.byref(shape), cache, C.c_uint32(dtype), C.c_uint32(4), k, st, st, v, st, st, slots, None) == ARG
+    for cache, slots, k, v in ((off(8), some, some, some), (some, off(4), some, some), (some, some, off(8), some), (some, some, some, off(8))):
+        assert lib.kvp_cache_read(C.byref(shape), cache, 0, 4, slots, k, v, None) == ARG
