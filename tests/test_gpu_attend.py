@@ -492,6 +492,12 @@ def test_policy_accumulated(kvp, groups, n, steps):
         assert int(ev["bad_step"][0]) == -1
 
 
+def test_policy_accumulated_where_everything_fits(kvp):
+    w = cuda(weights_of(np.random.default_rng(6), 4, 3, 96))
+    prob = kvp.Problem(3 * 96, 8192, 4, kvp.trace_weights(w, 3, 10), 3 * 96, 8 * 10 ** 12, 9 * 10 ** 11, 9 * 10 ** 11)
+    assert bool((prob.policy_accumulated(w, 3) == -1).all())
+
+
 def test_policy_accumulated_refuses(kvp):
     w = cuda(weights_of(np.random.default_rng(6), 4, 3, 96))
     prob = kvp.Problem(3 * 96, 8192, 4, kvp.trace_weights(w, 3, 10), 80, 8 * 10 ** 12, 9 * 10 ** 11, 9 * 10 ** 11)
