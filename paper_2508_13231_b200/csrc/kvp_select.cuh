@@ -280,8 +280,8 @@ __device__ uint32_t choose_ties(Row& row, uint32_t rounds, uint32_t cand, uint32
     return word;
 }
 
-// -> lane j's word of round j: the chosen units. turn: a number that changes by one from call to call. Every thread of the CTA calls it; the
-// row's keys have all been loaded when it returns.
+// -> lane j's word of round j: the chosen units. turn: a number that changes by one from call to call. Every thread of the CTA calls it; when it
+// returns, no lane of the warp looks at the warp's keys any more (other warps' keys are never looked at).
 template <typename Key, int T, typename Row>
 __device__ __forceinline__ uint32_t choose(Row& row, uint32_t rounds, uint32_t cand, uint32_t left, Band<Key>& band, SelectShared<Key, T>& sm,
                                            uint32_t turn)
@@ -337,6 +337,7 @@ __device__ __forceinline__ uint32_t choose(Row& row, uint32_t rounds, uint32_t c
         if (need == 0 || wanted == equal) {
             for (uint32_t x = need ? inside : 0u; x; x &= x - 1u)
                 if (row.key(first + __ffs(x) - 1u) >= edge) word |= x & (0u - x);
+            __syncwarp();                                          // these are other lanes' keys, which those may change once `choose` returns
         } else if (equal <= kListed) {
             // the threshold splits its bin: its keys are ranked
             if (tid == 0) sm.listed = 0;
