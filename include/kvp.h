@@ -603,7 +603,7 @@ void kvp_philox4x32_10(const uint32_t ctr[4], const uint32_t key[2], uint32_t ou
 /*
  * ---- test only ----
  * Switches of the test-suite (and of tuning runs); process-wide, read at the start of every kvp_anneal /
- * kvp_anneal_chain_state. No production caller needs them. All zero = the library's normal behaviour; NULL resets.
+ * kvp_anneal_chain_state / kvp_evict / kvp_policy_accumulated. No production caller needs them. All zero = the library's normal behaviour; NULL resets.
  */
 typedef struct {
     uint32_t warps_per_chain;   /* 1, 2 or 32 + w: the narrow chain kernel with 1, 2 or w (up to 4) warps per
@@ -617,6 +617,8 @@ typedef struct {
                                    that a small job comes in several waves                                       */
     uint32_t overlay;           /* 2: the copy-on-write slices of schedules in global memory come in buckets of 8
                                    units at least, as those of large problems do                                 */
+    uint32_t evict_form;        /* kvp_evict, kvp_policy_accumulated: 1: in one pass, 2: in two (as far as the
+                                   scratch for them may go), whichever would be the faster one                   */
 } kvp_test_hooks;
 void kvp_set_test_hooks(const kvp_test_hooks* hooks);
 

@@ -26,9 +26,9 @@
 
 namespace kvp {
 
-namespace {
+kvp_test_hooks g_hooks = {0u, 0u, 0u, 0u, 0u, 0u};   // kvp_set_test_hooks; read once per call
 
-kvp_test_hooks g_hooks = {0u, 0u, 0u, 0u, 0u};   // kvp_set_test_hooks; read once per call
+namespace {
 
 // What an exchange round of neighbouring rungs needs (by pair of rungs).
 struct ExchangeArgs {

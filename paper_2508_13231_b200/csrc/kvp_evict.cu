@@ -299,7 +299,9 @@ int launch_evict(const kvp_evict_params* a, const float* weights, const int64_t*
     const uint64_t all = k.U * a->steps;
     const size_t bytes = all * 8;
     const double step = (2.5e-6 + n * (n > 16384 ? 0.8e-9 : 0.3e-9)) * (1 + k.groups / 1000.0);
-    const bool two = a->steps > 1 && bytes <= ((size_t)1 << 30) && a->steps * step > 14e-6 + 5.8e-12 * (double)all;
+    const bool faster = a->steps > 1 && a->steps * step > 14e-6 + 5.8e-12 * (double)all;
+    const uint32_t form = g_hooks.evict_form;                      // test hook
+    const bool two = bytes <= ((size_t)1 << 30) && (form ? form == 2 : faster);
     if (two) {
         int dev = 0;
         KVP_CUDA(cudaGetDevice(&dev));

@@ -120,7 +120,7 @@ class EvictParams(C.Structure):
 
 class TestHooks(C.Structure):
     _fields_ = [("warps_per_chain", C.c_uint32), ("drop_turn", C.c_uint32), ("split_queue_plus1", C.c_uint32),
-                ("resident", C.c_uint32), ("overlay", C.c_uint32)]
+                ("resident", C.c_uint32), ("overlay", C.c_uint32), ("evict_form", C.c_uint32)]
 
 
 _handle = None
@@ -180,10 +180,10 @@ def _stream(stream=None):
     return C.c_void_p(_native().current_stream() if stream is None else stream.cuda_stream)
 
 
-def set_test_hooks(warps_per_chain=0, drop_turn=0, split_queue=None, resident=0, overlay=0):
+def set_test_hooks(warps_per_chain=0, drop_turn=0, split_queue=None, resident=0, overlay=0, evict_form=0):
     """kvp_set_test_hooks (test-suite and tuning only; process-wide). Called without arguments it resets everything."""
     h = TestHooks(int(warps_per_chain), int(drop_turn), 0 if split_queue is None else int(split_queue) + 1, int(resident),
-                  int(overlay))
+                  int(overlay), int(evict_form))
     _lib().kvp_set_test_hooks(C.byref(h))
 
 
