@@ -486,14 +486,24 @@ int kvp_trace_weights(uint32_t groups, uint32_t units_per_group, uint32_t steps,
 /*
  * Eviction from a cache by accumulated attention weight. Per unit acc = floor(acc * decay_q / 65536) + round(min(max(w, 0), 128) * 2^24)
  * (ties to even, NaN counts as 0, acc is cut to 0..2^48 - 1). Of the units 0 .. exist-1 of a group the first `sink` and the last `recent` are always
- * kept; the rest of the `budget` goes to those with the largest acc among the others that kept_in still holds, ties to the lower index.
+ * kept; the rest of the `budget` goes to those with the largest acc among the candidates, ties to the lower index.
+ *
+ * With KVP_EVICT_CARRY, as a cache has it: what a step leaves out is gone. The candidates of a step are the units that the row before holds (kept_in
+ * before the first step), `exist` has an entry per step and group, and a unit that is not there yet is not evicted: the bits of units from
+ * exist on are set in every row (they do not count against the budget), so that a unit is a candidate when it comes, and kvp_attend with that row as
+ * `units` reads the token that opens it. Where a unit holds several tokens, `recent` should be 1 at least: a unit may be evicted before it is
+ * full, and the tokens that come to it later are not read then. A group that starts over, with another sequence, needs its bits set by the caller.
+ * Without it every step is a choice by itself, from kept_in: the heaviest units of each step. A unit left out at one step may be in the next row, the bits of
+ * units from exist on are clear, and a unit that came since kept_in was made is a candidate only if the caller sets its bit there.
  */
+#define KVP_EVICT_CARRY 2u
+
 typedef struct {
     uint32_t groups, units_per_group, steps;
     uint32_t budget;            /* units kept per group, sink + recent <= budget <= units_per_group */
     uint32_t sink, recent;
     uint32_t decay_q;           /* decay per step * 2^16, 0..65536 (65536 = none)                   */
-    uint32_t reserved;          /* must be 0 */
+    uint32_t flags;             /* 0 or KVP_EVICT_CARRY                                             */
 } kvp_evict_params;
 
 /*
@@ -502,8 +512,9 @@ typedef struct {
  *   acc_in   (device) [groups * units_per_group] int64 or NULL (= 0);  acc_out (device) the same, may be acc_in itself (another overlap
  *            is KVP_ERR_ARG)
  *   kept_in  (device) [W32] bitmap or NULL (= every unit): the units that may be kept besides the protected ones; in a serving
- *            loop the row the call before gave, so that what was evicted stays evicted
- *   exist    (device) [groups] int32 or NULL (= units_per_group): units the group has by now (cut to 0..units_per_group)
+ *            loop, with KVP_EVICT_CARRY, the row the call before gave
+ *   exist    (device) int32 [groups], with KVP_EVICT_CARRY [steps][groups], or NULL (= units_per_group): units the group has by then (cut to
+ *            0..units_per_group)
  *   kept_out (device) [steps][W32]: the units kept after each step; overlap with kept_in is KVP_ERR_ARG
  * Limit: units_per_group <= 32768 (KVP_ERR_RANGE).
  */
@@ -511,7 +522,7 @@ int kvp_evict(const kvp_evict_params* params, const float* weights, const int64_
               const uint32_t* kept_in, const int32_t* exist, uint32_t* kept_out, void* stream);
 
 /*
- * kvp_policy_accumulated -- the same rule as a schedule generator beside the other strategies: before each step s the units with the
+ * kvp_policy_accumulated -- the same ranking (flags 0) as a schedule generator beside the other strategies: before each step s the units with the
  * largest weight accumulated over steps 0 .. s-1 are in HBM (`budget` per group; a unit that was moved out is still read from off-package
  * DRAM, receives weight and may return). Step 0 starts from the protected units and the lowest indices.
  *   params: steps and groups * units_per_group as in the problem; groups * budget <= hbm_capacity_units (KVP_ERR_CAPACITY otherwise)

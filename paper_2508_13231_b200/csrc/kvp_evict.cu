@@ -30,6 +30,7 @@ struct EvictK {
     uint32_t chunk;           // steps of a CTA of the second pass
     bool aligned;             // n % 32 == 0: no word is shared by two groups
     bool before;              // a step's row is chosen before its weights are added
+    bool carry;               // what a step leaves out is gone for the later ones; exist is [steps][groups] then
 };
 
 // NaN and negative weights convert to 0 (fminf would make 128 of NaN)
@@ -46,24 +47,28 @@ __device__ __forceinline__ uint64_t first_sum(const EvictK& p, uint64_t u)
     return a < 0 ? 0u : min((uint64_t)a, kAccMost);
 }
 
-// Lane j's words of round j: who may be chosen, and who is protected
+// Lane j's words of round j: the units there are, those that are protected, and those that may be chosen
 struct Members {
-    uint32_t cand, safe, left;
+    uint32_t there, safe, cand, left;
 };
-__device__ __forceinline__ Members members_of(const EvictK& p, uint32_t g)
+__device__ __forceinline__ Members members_of(const EvictK& p, uint32_t g, uint32_t step, uint32_t kept)
 {
-    const uint32_t T = blockDim.x, tid = threadIdx.x, lane = tid & 31;
-    const uint64_t first = (uint64_t)g * p.n;
-    const uint32_t e = p.exist ? (uint32_t)min(max(p.exist[g], 0), (int32_t)p.n) : p.n;
-    Members m = {0, 0, p.budget - min(min(e, p.sink + p.recent), p.budget)};
-    for (uint32_t j = 0; j * T < p.n; ++j) {
-        const uint32_t i = j * T + tid;
-        const bool in = i < e, safe = in && (i < p.sink || i + p.recent >= e);
-        const bool old = in && !safe && (!p.kept || (p.kept[(first + i) >> 5] >> ((first + i) & 31) & 1u));
-        const uint32_t c = __ballot_sync(0xFFFFFFFFu, old), s = __ballot_sync(0xFFFFFFFFu, safe);
-        if (lane == j) { m.cand = c; m.safe = s; }
-    }
+    const uint32_t e = p.exist ? (uint32_t)min(max(p.exist[(uint64_t)step * p.groups + g], 0), (int32_t)p.n) : p.n;
+    Members m;
+    m.there = units_there(e);
+    m.safe = m.there & (units_there(p.sink) | ~units_there(e - min(e, p.recent)));
+    m.cand = kept & m.there & ~m.safe;
+    m.left = p.budget - min(min(e, p.sink + p.recent), p.budget);
     return m;
+}
+// Lane j's word of round j of kept_in; bits behind the group's last unit may be anything
+__device__ __forceinline__ uint32_t kept_before(const EvictK& p, uint32_t g)
+{
+    const uint32_t unit = ((threadIdx.x & 31) * (blockDim.x / 32) + threadIdx.x / 32) * 32;
+    if (!p.kept || unit >= p.n) return ~0u;
+    const uint64_t at = (uint64_t)g * p.n + unit, w = at >> 5;
+    const uint32_t sh = (uint32_t)at & 31u;
+    return __funnelshift_r(p.kept[w], sh && w + 1 < p.W32 ? p.kept[w + 1] : 0u, sh);
 }
 
 // One pass. The sums of a group, 48 bits each, are in shared memory as lower words and upper half-words (24 KB for 4096 units: five CTAs an SM,
@@ -151,7 +156,7 @@ __global__ void __launch_bounds__(T, T == 128 ? 5 : 1) evict_kernel(const EvictK
     const uint64_t first = (uint64_t)g * p.n;
     if (tid == 0) upper = 0;
     clear(sm);
-    const Members m = members_of(p, g);
+    Members m = members_of(p, g, 0, kept_before(p, g));
     SumsRow<T, FULL> row = {p, sums, reinterpret_cast<uint16_t*>(sums + p.n), nullptr, false, p.w + first, {}};
     row.done();
     uint32_t most = 0;
@@ -172,8 +177,12 @@ __global__ void __launch_bounds__(T, T == 128 ? 5 : 1) evict_kernel(const EvictK
         const uint32_t adds = p.before ? s - 1 : s;                // the step whose weights are added; none (wraps) before the first choice
         row.w = adds < p.steps ? p.w + adds * p.U + first : nullptr;
         row.next = adds + 1 < p.steps ? p.w + (adds + 1) * p.U + first : nullptr;
-        const uint32_t word = choose<uint64_t, T>(row, rounds, m.cand, m.left, band, sm, s);
-        put_words(p.out + s * p.W32, first, p.n, p.aligned, word | m.safe);
+        uint32_t word = choose<uint64_t, T>(row, rounds, m.cand, m.left, band, sm, s) | m.safe;
+        if (p.carry) {                                             // units that are not there yet are not evicted
+            word |= units_there(p.n) & ~m.there;
+            if (s + 1 < p.steps) m = members_of(p, g, s + 1, word);
+        }
+        put_words(p.out + s * p.W32, first, p.n, p.aligned, word);
     }
     if (p.before) return;                                          // a policy: nobody asks for the sums
     for (uint32_t i = tid; i < p.n; i += T) p.acc[first + i] = (int64_t)row.key(i);           // written by this thread
@@ -246,7 +255,7 @@ __global__ void __launch_bounds__(T) choose_kernel(const EvictK p)
     const uint32_t rounds = (p.n + T - 1) / T;
     const uint64_t first = (uint64_t)g * p.n;
     clear(sm);
-    const Members m = members_of(p, g);
+    const Members m = members_of(p, g, 0, kept_before(p, g));
     Band<uint64_t> band;
     band.valid = band.moved = false;
     for (uint32_t s = s0; s < s1; ++s) {
@@ -274,7 +283,7 @@ int launch_choice(const EvictK& k, bool two, cudaStream_t st)
 
 int check_evict(const kvp_evict_params* a)
 {
-    if (!a || a->reserved || !a->groups || !a->units_per_group || !a->steps || a->decay_q > 65536) return KVP_ERR_ARG;
+    if (!a || (a->flags & ~KVP_EVICT_CARRY) || !a->groups || !a->units_per_group || !a->steps || a->decay_q > 65536) return KVP_ERR_ARG;
     if ((uint64_t)a->sink + a->recent > a->budget || a->budget > a->units_per_group) return KVP_ERR_ARG;
     if (a->units_per_group > kEvictUnits || (uint64_t)a->groups * a->units_per_group >= (1ull << 31)) return KVP_ERR_RANGE;
     return KVP_OK;
@@ -290,6 +299,7 @@ int launch_evict(const kvp_evict_params* a, const float* weights, const int64_t*
     k.W32 = (k.U + 31) / 32;
     k.aligned = k.n % 32 == 0;
     k.before = before;
+    k.carry = a->flags & KVP_EVICT_CARRY;
     k.groups = a->groups;
     if (!k.aligned) KVP_CUDA(cudaMemsetAsync(rows, 0, (size_t)a->steps * k.W32 * 4, st));
     const uint32_t n = k.n;
@@ -301,7 +311,7 @@ int launch_evict(const kvp_evict_params* a, const float* weights, const int64_t*
     const double step = (2.5e-6 + n * (n > 16384 ? 0.8e-9 : 0.3e-9)) * (1 + k.groups / 1000.0);
     const bool faster = a->steps > 1 && a->steps * step > 14e-6 + 5.8e-12 * (double)all;
     const uint32_t form = g_hooks.evict_form;                      // test hook
-    const bool two = bytes <= ((size_t)1 << 30) && (form ? form == 2 : faster);
+    const bool two = !k.carry && bytes <= ((size_t)1 << 30) && (form ? form == 2 : faster);
     if (two) {
         int dev = 0;
         KVP_CUDA(cudaGetDevice(&dev));
@@ -345,6 +355,7 @@ extern "C" int kvp_policy_accumulated(kvp_problem* p, const kvp_evict_params* a,
     if (!p || !weights || !schedule || p->d_birth) return KVP_ERR_ARG;
     const int rc = check_evict(a);
     if (rc) return rc;
+    if (a->flags) return KVP_ERR_ARG;
     if (a->steps != p->S || (uint64_t)a->groups * a->units_per_group != p->U) return KVP_ERR_ARG;
     if ((uint64_t)a->groups * a->budget > p->cap) return KVP_ERR_CAPACITY;
     return launch_evict(a, weights, nullptr, nullptr, nullptr, nullptr, schedule, true, static_cast<cudaStream_t>(stream));

@@ -440,16 +440,18 @@ PyObject* trace_weights(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
-// evict(weights, groups, budget, sink, recent, decay_q, acc or None, kept or None, exist or None, acc_out or None, stream or None)
+// evict(weights, groups, budget, sink, recent, decay_q, acc or None, kept or None, exist or None, acc_out or None, stream or None, carry)
 // -> dict, or an error code
 PyObject* evict(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
     if (!kvp_evict) return missing("kvp_evict");
-    if (nargs != 11) return value_error("evict takes 11 arguments");
+    if (nargs != 12) return value_error("evict takes 12 arguments");
     const at::Tensor *w, *acc, *kept, *exist, *acc_out;
     kvp_evict_params p;
-    p.reserved = 0;
+    const int carry = PyObject_IsTrue(args[11]);
+    if (carry < 0) return nullptr;
+    p.flags = carry ? KVP_EVICT_CARRY : 0;
     if (!u32_of(args[1], "groups", &p.groups) || !u32_of(args[2], "budget", &p.budget) || !u32_of(args[3], "sink", &p.sink) ||
         !u32_of(args[4], "recent", &p.recent) || !u32_of(args[5], "decay_q", &p.decay_q) ||
         !weights_of(args[0], p.groups, &p.units_per_group, &p.steps, &w)) return nullptr;
@@ -459,7 +461,8 @@ PyObject* evict(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     const int64_t units = (int64_t)p.groups * p.units_per_group, words = (units + 31) / 32;
     if ((acc && acc->numel() != units) || (acc_out && acc_out->numel() != units)) return value_error("acc must have one entry per unit");
     if (kept && kept->numel() != words) return value_error("kept must be a row of the bitmap");
-    if (exist && exist->numel() != (int64_t)p.groups) return value_error("exist must have one entry per group");
+    if (exist && exist->numel() != (carry ? (int64_t)p.steps : 1) * p.groups)
+        return value_error(carry ? "exist must have one entry per step and group" : "exist must have one entry per group");
     c10::cuda::CUDAStream st = c10::cuda::getDefaultCUDAStream(dev.index());
     if (!cuda_stream_of(args[10], dev, &st)) return nullptr;
     at::Tensor rows, sums;

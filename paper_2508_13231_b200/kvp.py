@@ -115,7 +115,7 @@ class TraceParams(C.Structure):
 
 class EvictParams(C.Structure):
     _fields_ = [(n, C.c_uint32) for n in (
-        "groups", "units_per_group", "steps", "budget", "sink", "recent", "decay_q", "reserved")]
+        "groups", "units_per_group", "steps", "budget", "sink", "recent", "decay_q", "flags")]
 
 
 class TestHooks(C.Structure):
@@ -290,12 +290,17 @@ def trace_weights(weights, groups, topk, out=None, stream=None):
     return out
 
 
-def evict(weights, groups, budget, sink=0, recent=0, decay_q=65536, acc=None, kept=None, exist=None, acc_out=None, stream=None):
+def evict(weights, groups, budget, sink=0, recent=0, decay_q=65536, acc=None, kept=None, exist=None, acc_out=None, stream=None, carry=False):
     """kvp_evict -> dict(kept, acc): eviction by accumulated weight. weights [steps][U] (or [U]) are added to acc (int64 [U], weight 1 =
     2^24; None = 0) step by step, decaying by decay_q / 65536; kept (int32 [steps][ceil(U/32)]) are the `budget` units of each
-    group left after each step: the first `sink`, the last `recent` of the `exist` (int32 [groups]) units there are, and those with
-    most weight among the ones in the bitmap `kept`. acc_out: a tensor for the new sums, may be acc itself."""
-    out = _native().evict(weights, groups, budget, sink, recent, decay_q, acc, kept, exist, acc_out, _cuda_stream(stream))
+    group left after each step: the first `sink`, the last `recent` of the `exist` units there are, and those with
+    most weight among the ones in the bitmap `kept`. acc_out: a tensor for the new sums, may be acc itself.
+
+    carry=True is eviction as a cache has it, in a serving loop (kept: the row the call before gave) and over a recording: what a
+    step leaves out stays out, exist is int32 [steps][groups], and units that are not there yet have their bits set, so that they are
+    candidates when they come and attend(units=kept) sees the token that opens one. Without it every step is a choice by itself from
+    `kept`, with exist int32 [groups]: the heaviest units of each step."""
+    out = _native().evict(weights, groups, budget, sink, recent, decay_q, acc, kept, exist, acc_out, _cuda_stream(stream), carry)
     if out.__class__ is int:
         _chk(out, "kvp_evict")
     return out
