@@ -9,9 +9,10 @@ not the paper's values. Strategies (Section IV-A): Unlimited HBM, Static Placeme
 Page granularity (16 tokens), SA-guided = the paper's annealer over the look-ahead policy's (W, R), followed by
 direct annealing of the schedule it found. Everything runs in the library's kernels; this file only calls them.
 
---recorded: the strategies on a trace that is recorded as the paper's are (Section IV-A): random keys, values and drifting queries stand in for a
-model, tokens are decoded with attention over a cache held in 4 bits, and each step reads the units that received most
-weight. Beside them the placement by accumulated weight, and what eviction by it leaves of the attention weight.
+--recorded: the strategies on a trace of recorded attention weights, as the paper's are (Section IV-A): random keys, values and drifting queries
+stand in for a model, tokens are decoded with attention over a cache held in 4 bits (the paper records a model with an unquantised one, so
+these weights contain the error of 4 bits), and each step reads the units that received most weight. Beside them the placement by accumulated
+weight, and what eviction by it leaves of the attention weight: the units evicted after a step are gone for all later ones.
 """
 import argparse
 
@@ -79,6 +80,16 @@ def record(cfg, seed=0):
     return weights, n
 
 
+def weight_kept(weights, cfg, n, share):
+    """Eviction to `share` of a head's units after every step -> share of the next steps' attention weight on the units kept."""
+    h = cfg["kv_heads"]
+    tokens = cfg["prompt"] + 1 + torch.arange(cfg["steps"], device="cuda")
+    exist = ((tokens + cfg["unit_tokens"] - 1) // cfg["unit_tokens"]).int()[:, None].expand(-1, h).contiguous()
+    rows = kvp.evict(weights, h, max(4, int(share * n)), sink=1, recent=2, exist=exist, carry=True)["kept"]
+    bits = torch.from_numpy(wl.unpack_bits(rows.cpu().numpy().view(np.uint32), h * n)).cuda()
+    return float((weights[1:] * bits[:-1]).sum() / weights[1:].sum())
+
+
 def recorded(name, quick=False, seed=0):
     """-> dict strategy -> (total ticks, HBM hit rate), dict share of the units kept -> share of the attention weight they receive."""
     cfg = wl.RECORDED[name]
@@ -94,18 +105,13 @@ def recorded(name, quick=False, seed=0):
 
     accessed = int(np.unpackbits(access.cpu().numpy().view(np.uint8)).sum())
     out = {"static": score(prob.policy_lookahead([1], [0])[0].contiguous()), "reactive": score(prob.policy_reactive())}
-    held = prob.policy_accumulated(weights, h, sink=1, recent=2, decay_q=61440)
+    held = prob.policy_accumulated(weights, h, sink=1, decay_q=61440)
     out["accumulated"] = score(held)
     res = prob.anneal(prob.make_params(chains=64 if quick else 256, moves=20_000 if quick else 200_000, seed=seed, p0=1e-3,
                                        init_mode=kvp.INIT_USER, init_schedule=held))
     out["sa_guided"] = score(res["best_schedule"])
     prob.close()
-    kept = {}
-    for share in (0.5, 0.25, 0.125):
-        rows = kvp.evict(weights, h, max(4, int(share * n)), sink=1, recent=2)["kept"]
-        bits = torch.from_numpy(wl.unpack_bits(rows.cpu().numpy().view(np.uint32), units)).cuda()
-        kept[share] = float((weights[1:] * bits[:-1]).sum() / weights[1:].sum())
-    return out, kept
+    return out, {share: weight_kept(weights, cfg, n, share) for share in (0.5, 0.25, 0.125)}
 
 
 def main():
@@ -119,7 +125,7 @@ def main():
         print(f"Recorded attention weights ({name}): tokens/s normalised to Static Placement, HBM hit rate\n")
         print("| " + " | ".join(out) + " |\n|" + "---|" * len(out))
         print("| " + " | ".join(f"{out['static'][0] / t:.2f}, {r:.3f}" for t, r in out.values()) + " |\n")
-        print("Eviction by accumulated weight: share of the next step's attention weight on the units kept\n")
+        print("Eviction by accumulated weight: share of the later steps' attention weight on the units kept\n")
         print("| " + " | ".join(f"{s:.3f} of the units" for s in kept) + " |\n|" + "---|" * len(kept))
         print("| " + " | ".join(f"{w:.3f}" for w in kept.values()) + " |")
         return
