@@ -391,7 +391,7 @@ int kvp_trace_generate(const kvp_trace_params* params, uint32_t* access_bitmaps,
  * device: keys and values go into a cache held in 4 bits (kvp_cache_append), attention reads it and notes what weight every
  * unit received (kvp_attend), recorded weights become access bitmaps (kvp_trace_weights) for kvp_create, and they drive
  * eviction, as one step of a serving loop (kvp_evict) or as a placement schedule (kvp_policy_accumulated). They are
- * asynchronous on `stream`, keep nothing between calls and work on the current device; all of them can be captured into a
+ * asynchronous on `stream`, keep nothing between calls and work on the current device (kvp_policy_accumulated on its problem's); all of them can be captured into a
  * graph (lengths, tables, slots and bitmaps are read on the device). What a call writes overlaps nothing that it reads, but where it
  * says so. kvp_evict and kvp_policy_accumulated over several steps of few groups take up to 1 GiB of stream-ordered scratch,
  * freed on return, as kvp_trace_generate does; the others allocate nothing.

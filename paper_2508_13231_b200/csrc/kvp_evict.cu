@@ -358,5 +358,6 @@ extern "C" int kvp_policy_accumulated(kvp_problem* p, const kvp_evict_params* a,
     if (a->flags) return KVP_ERR_ARG;
     if (a->steps != p->S || (uint64_t)a->groups * a->units_per_group != p->U) return KVP_ERR_ARG;
     if ((uint64_t)a->groups * a->budget > p->cap) return KVP_ERR_CAPACITY;
+    KVP_CUDA(cudaSetDevice(p->device));
     return launch_evict(a, weights, nullptr, nullptr, nullptr, nullptr, schedule, true, static_cast<cudaStream_t>(stream));
 }
