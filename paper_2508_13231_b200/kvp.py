@@ -462,7 +462,8 @@ class Problem:
             raise ValueError("weights must be [steps][units]")
         ep = EvictParams(groups, self.units // groups if groups else 0, self.steps,
                          self.cap // groups if budget is None and groups else budget or 0, sink, recent, decay_q, 0)
-        out = torch.empty((self.steps, self.w32), dtype=torch.int32, device="cuda")
+        with torch.cuda.stream(stream):                  # memory of the stream it is written on: another's may still be read by work under way there
+            out = torch.empty((self.steps, self.w32), dtype=torch.int32, device="cuda")
         _chk(_lib().kvp_policy_accumulated(self._h, C.byref(ep), _ptr(weights, torch.float32), _ptr(out), _stream(stream)),
              "kvp_policy_accumulated")
         return out

@@ -105,3 +105,20 @@ def test_both_forms_as_a_policy(kvp, hooks, form):
         for decay in (65536, 62000):
             rows, _ = plain.evict(w, groups, 40, 1, 2, decay, before=True)
             assert np.array_equal(host_bits(prob.policy_accumulated(cuda(w), groups, sink=1, recent=2, decay_q=decay)), rows)
+
+
+def test_a_policys_schedule_is_memory_of_its_own_stream(kvp):
+    """A block that the current stream has just given back may still be read there; a schedule written on another stream must not lie in it."""
+    groups, n, steps = 2, 2048, 600                                  # 307,200 bytes: a block of its own
+    w = cuda(np.random.default_rng(0).random((steps, groups * n)).astype(np.float32))
+    prob = kvp.Problem(groups * n, 8192, steps, kvp.trace_weights(w, groups, 5), 80, 8 * 10 ** 12, 9 * 10 ** 11, 9 * 10 ** 11)
+    want = prob.policy_accumulated(w, groups)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    last = torch.empty_like(want)
+    at = last.data_ptr()
+    del last
+    got = prob.policy_accumulated(w, groups, stream=side)
+    assert got.data_ptr() != at
+    side.synchronize()
+    assert torch.equal(got, want)
