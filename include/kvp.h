@@ -393,7 +393,7 @@ int kvp_trace_generate(const kvp_trace_params* params, uint32_t* access_bitmaps,
  * eviction, as one step of a serving loop (kvp_evict) or as a placement schedule (kvp_policy_accumulated). They are
  * asynchronous on `stream`, keep nothing between calls and work on the current device (kvp_policy_accumulated on its problem's); all of them can be captured into a
  * graph (lengths, tables, slots and bitmaps are read on the device). What a call writes overlaps nothing that it reads, but where it
- * says so. kvp_evict and kvp_policy_accumulated over several steps of few groups take up to 1 GiB of stream-ordered scratch,
+ * says so. An array that does not lie at the alignment of its type is KVP_ERR_ARG. kvp_evict and kvp_policy_accumulated over several steps of few groups take up to 1 GiB of stream-ordered scratch,
  * freed on return, as kvp_trace_generate does; the others allocate nothing.
  *
  * A cache held in 4 bits. [pages][kv_heads][kvp_cache_page_bytes(head_dim, page_tokens)] bytes, 16-byte aligned: a page holds

@@ -147,6 +147,8 @@ int set_cuda_error(cudaError_t e, const char* what);
 
 extern kvp_test_hooks g_hooks;       // kvp_anneal.cu
 
+inline bool off_by(const void* p, uint32_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }       // null is not
+
 // keep freed blocks of up to `bytes` (+ 1 GiB) in the device's default memory pool
 int retain_in_pool(int device, size_t bytes);
 int ensure_scratch(kvp_problem* p, size_t bytes, cudaStream_t st);

@@ -343,6 +343,7 @@ extern "C" int kvp_evict(const kvp_evict_params* a, const float* weights, const 
     const int rc = check_evict(a);
     if (rc) return rc;
     if (!weights || !acc_out || !kept_out) return KVP_ERR_ARG;
+    if (off_by(weights, 4) || off_by(acc_in, 8) || off_by(acc_out, 8) || off_by(kept_in, 4) || off_by(exist, 4) || off_by(kept_out, 4)) return KVP_ERR_ARG;
     const uint64_t words = ((uint64_t)a->groups * a->units_per_group + 31) / 32;
     if (kept_in && kept_in < kept_out + words * a->steps && kept_out < kept_in + words) return KVP_ERR_ARG;
     const uint64_t units = (uint64_t)a->groups * a->units_per_group;
@@ -352,7 +353,7 @@ extern "C" int kvp_evict(const kvp_evict_params* a, const float* weights, const 
 
 extern "C" int kvp_policy_accumulated(kvp_problem* p, const kvp_evict_params* a, const float* weights, uint32_t* schedule, void* stream)
 {
-    if (!p || !weights || !schedule || p->d_birth) return KVP_ERR_ARG;
+    if (!p || !weights || !schedule || p->d_birth || off_by(weights, 4) || off_by(schedule, 4)) return KVP_ERR_ARG;
     const int rc = check_evict(a);
     if (rc) return rc;
     if (a->flags) return KVP_ERR_ARG;

@@ -35,8 +35,6 @@ struct Tile {
     static __host__ __device__ constexpr uint32_t value_meta(uint32_t i, uint32_t n) { return kValueScale + (((i >> 2) * N + n) * 4 + (i & 3)) * 2; }
 };
 
-inline bool off_by(const void* p, uint32_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }       // null is not
-
 inline bool head_dim_served(uint32_t d) { return d == 64 || d == 128 || d == 256; }
 
 }  // namespace kvp

@@ -476,6 +476,7 @@ extern "C" int kvp_trace_weights(uint32_t groups, uint32_t units_per_group, uint
                                  uint32_t* access_bitmaps, void* stream)
 {
     if (!groups || !units_per_group || !steps || !topk || topk > units_per_group || !weights || !access_bitmaps) return KVP_ERR_ARG;
+    if (off_by(weights, 4) || off_by(access_bitmaps, 4)) return KVP_ERR_ARG;
     const uint64_t U = (uint64_t)groups * units_per_group;
     if (units_per_group > 32768 || U >= (1ull << 31) || (uint64_t)groups * steps >= (1ull << 31)) return KVP_ERR_RANGE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
