@@ -465,7 +465,9 @@ typedef struct {
  *   weights (device) [batch][kv_heads][n] float or NULL: softmax weight of the unit's tokens, summed over the queries and heads that
  *           share the kv-head; 0 for units that were not read
  *   workspace (device) 256-byte aligned, kvp_attend_workspace(...) bytes, used by this call alone until its work has finished
- * A query that sees no token gives out 0 and lse -infinity. Errors: KVP_ERR_ARG (null, zero sizes, unit_tokens, dtype, a scale that is
+ * A query that sees no token gives out 0 and lse -infinity. Scores, maxima and sums are fp32; a weight, and its product with a value's scale, is rounded
+ * to fp16 (bf16 outputs: one term, 2^-11 each) or to two fp16 terms (fp16 outputs), with the largest weight at 2^13 and the values' scales raised where
+ * they are below 2^-7, so that weights down to 2^-20 of the largest keep those bits whatever the values' size. Errors: KVP_ERR_ARG (null, zero sizes, unit_tokens, dtype, a scale that is
  * not finite, a workspace too small, a cache that is not 16-byte aligned, a workspace that is not 256-byte
  * aligned, out not 8-byte aligned), KVP_ERR_RANGE (head_dim, sizes above).
  */

@@ -13,8 +13,9 @@
 // 32 dims in fp32, the zeros on the sums of the query's dims, which enter as two fp16 terms (22 bits). A row's queries are divided by a power
 // of two first, so that bf16 ones fit fp16 whatever their size.
 // exp runs in fp32 against a running maximum that moves only when a score passes it by 2^8 (rare), sums are fp32. The weights p
-// times the scales of the values are the second product's right operand, in fp16 (11 bits, half a step is 2^-12 of a weight; the
-// output has 8 or 11 bits); the scales are divided by a running power of two so that small values lose nothing.
+// times the scales of the values are the second product's right operand, in fp16 (11 bits, half a step is 2^-11 of a weight at most; the
+// output has 8 or 11 bits). So that the product keeps them, a weight enters as up to 2^13 .. 2^15, and scales of which none so far
+// reached 2^-7 are multiplied by a power of two that brings the largest to 1 .. 2; larger ones than 2 take as much off the weights.
 //
 // Split. The tiles (16 tokens) of all segments stand in one line that is cut into equal parts, one for each CTA, on the device,
 // where the lengths are known: any mix of lengths, and rows of a bitmap with any number of units, keep all SMs busy alike. A CTA
@@ -41,6 +42,9 @@ constexpr uint32_t kListCap = 1024;           // tiles of a bitmap row that are 
 constexpr uint32_t kNibble = 0x00F000F0u;     // bits 4 .. 7 of two fp16 significands
 constexpr float kNone = -3e38f;               // maximum of nothing
 constexpr float kLift = 13.0f, kSlack = 2.0f; // weights are at most 2^(kLift + kSlack), 2^kLift right after the maximum moved
+constexpr float kRaise = 15.0f;               // scales of values are multiplied by at most 2^15, which fp16 holds
+constexpr int kSmall = -7;                    // and only if none of them reached 2^-7
+constexpr uint32_t kFrom2 = 0x40004000u, kFromSmall = 0x60006000u;   // bits that one of two fp16 numbers has from 2 on, and from 2^-7 on
 
 // Division by a number known at the launch: n / d = (n * mul) >> (32 + shift) for n < 2^31 (d = 1: mul = 0)
 struct Divisor {
@@ -554,17 +558,14 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
         float* const mass = p.mass + (uint64_t)seg * p.row_subs * kRows + 2 * t;
 
         float o[2 * N][4], zsum[4] = {0, 0, 0, 0}, m0 = kNone, m1 = kNone, l0 = 0.0f, l1 = 0.0f;
-        float lift = kLift, d0 = kNone, d1 = kNone;                // weights are 2^(s - d), d = m - lift
+        // weights are 2^(s - d), d = m - min(lift, kLift); scales of values are multiplied by 2^(lift - kLift) where that is more than 1
+        float lift = kLift, d0 = kNone, d1 = kNone;
 #pragma unroll
         for (int i = 0; i < 2 * N; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
 
-        auto rescale = [&](float c0, float c1) {
-            l0 *= c0;
-            l1 *= c1;
-            zsum[0] *= c0;
-            zsum[1] *= c1;
+        auto rescale_sums = [&](float c0, float c1) {
 #pragma unroll
             for (int i = 0; i < 2 * N; ++i) {
                 o[i][0] *= c0;
@@ -572,6 +573,12 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                 o[i][2] *= c0;
                 o[i][3] *= c1;
             }
+        };
+        auto rescale_weights = [&](float c0, float c1) {
+            l0 *= c0;
+            l1 *= c1;
+            zsum[0] *= c0;
+            zsum[1] *= c1;
         };
 
         while (true) {
@@ -670,11 +677,13 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                     }
                     n0 = fmaxf(m0, n0);
                     n1 = fmaxf(m1, n1);
-                    rescale(exp2_fast(m0 - n0), exp2_fast(m1 - n1));
+                    const float c0 = exp2_fast(m0 - n0), c1 = exp2_fast(m1 - n1);
+                    rescale_sums(c0, c1);
+                    rescale_weights(c0, c1);
                     m0 = n0;
                     m1 = n1;
-                    d0 = m0 - lift;
-                    d1 = m1 - lift;
+                    d0 = m0 - fminf(lift, kLift);
+                    d1 = m1 - fminf(lift, kLift);
                 }
                 float e[2][4];
 #pragma unroll
@@ -756,26 +765,35 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
                         vz1 &= k1;
                     }
                     // A weight times a scale has to stay below 2^16. Up to scales of 2 the lift sees to that; larger ones (values
-                    // that span more than 30) take as much off the lift, for good.
+                    // that span more than 30) take as much off the lift, for good. Nor should it sink below fp16's normal numbers: where the
+                    // first tile has small scales only (or none), scales are raised until larger ones come.
                     uint32_t large = vs[0][0] | vs[0][1];
 #pragma unroll
                     for (int n = 1; n < N; ++n) large |= vs[n][0] | vs[n][1];
-                    if (__any_sync(0xFFFFFFFFu, large & 0x40004000u)) {
+                    if (u == 0 && k + done == 0 && !__any_sync(0xFFFFFFFFu, large & kFromSmall)) lift = kLift + kRaise;
+                    if (__any_sync(0xFFFFFFFFu, lift > kLift ? large : large & kFrom2)) {
                         __half2 v = __hmax2(half2_of(vs[0][0]), half2_of(vs[0][1]));
 #pragma unroll
                         for (int n = 1; n < N; ++n) v = __hmax2(v, __hmax2(half2_of(vs[n][0]), half2_of(vs[n][1])));
                         float most = __half2float(__hmax(__low2half(v), __high2half(v)));
                         most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
                         most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-                        const float room = kLift - (float)(most < INFINITY ? ilogbf(most) : 15);
+                        const int size = most < INFINITY ? ilogbf(most) : 15;
+                        const float room = size > 0 || size < kSmall ? fminf(kLift - (float)size, kLift + kRaise) : kLift;
                         if (room < lift) {
-                            const float c = exp2f(room - lift);
-                            rescale(c, c);
+                            const float all = exp2f(room - lift), c = exp2f(fminf(room, kLift) - fminf(lift, kLift));
+                            rescale_sums(all, all);
+                            rescale_weights(c, c);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) { e[0][i] *= c; e[1][i] *= c; }
                             lift = room;
-                            d0 = m0 - lift;
-                            d1 = m1 - lift;
+                            d0 = m0 - fminf(lift, kLift);
+                            d1 = m1 - fminf(lift, kLift);
+                        }
+                        if (lift > kLift) {                        // exact: fp16 holds a scale below 2 times the power of two
+                            const uint32_t by = bits_of(__float2half2_rn(exp2f(lift - kLift)));
+#pragma unroll
+                            for (int n = 0; n < N; ++n) { vs[n][0] = times(vs[n][0], by); vs[n][1] = times(vs[n][1], by); }
                         }
                     }
                     const uint32_t h0 = pack(e[u][0], e[u][1]), h1 = pack(e[u][2], e[u][3]), p0 = transposed(h0), p1 = transposed(h1);
@@ -828,7 +846,7 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 1 : 2) attend_kernel(const 
         l0 = over_rows(l0);
         l1 = over_rows(l1);
         __syncthreads();                                           // every warp is done with its ring
-        constexpr float up = 0x1p24f, up16 = 0x1p20f;
+        const float up = 0x1p24f * exp2f(fminf(kLift - lift, 0.0f)), up16 = up * 0x1p-4f;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const float z0 = __shfl_sync(0xFFFFFFFFu, zsum[0], n * 4 + t), z1 = __shfl_sync(0xFFFFFFFFu, zsum[1], n * 4 + t);
