@@ -72,81 +72,77 @@ __device__ __forceinline__ uint32_t kept_before(const EvictK& p, uint32_t g)
 }
 
 // One pass. The sums of a group, 48 bits each, are in shared memory as lower words and upper half-words (24 KB for 4096 units: five CTAs an SM,
-// so that 740 groups of that size are worked on at once); a step's first pass adds its weights. In registers they spill at five CTAs an SM. What
-// bounds it is the latency of a step (two barriers, the search of the band's bins by one warp) with 17 warps an SM, and 5100 warp instructions
-// for 4096 units: 640 groups x 64 steps in 374 us, 114 of them for the bytes. Twice the warps without the step ahead are no faster (387 us).
-// FULL: n = 32 T, so that every slot of 32 rounds holds a unit; the weights of a step are then on their way while the step before is chosen for.
-template <int T, bool FULL>
+// so that 740 groups of that size are worked on at once); a step's first pass adds its weights. What bounds it is the latency of a step (two barriers,
+// the search of the band's bins by one warp) with 17 warps an SM. Walks of 32 steps over 2.6 million units, us, by the units of a group: 2048 240, 2080 314,
+// 4064 217, 4096 205, 7000 416, 8192 391, 16384 533, 32768 763; 53 would move the bytes. The weights of the next step in registers meanwhile: 198 at 4096, the
+// one length for which they fit without spills (326 otherwise). Twice the threads a group are no faster.
+template <int T>
 struct SumsRow {
     typedef float Raw;
-    static constexpr int kFetch = FULL ? 32 : kBatch;
+    static constexpr int kFetch = kBatch;
+    static constexpr uint32_t kThreads = T;
+    static constexpr bool kWhole = false, kPeeled = true;
     const EvictK& p;
     uint32_t* lo;
     uint16_t* hi;
+    uint32_t n;
     const float* w;           // the weights to be added, or null
     bool plain;               // no decay, and no sum can reach 2^48
-    const float* next;        // the weights after those, or null
-    float ahead[FULL ? 32 : 1];
     __device__ __forceinline__ uint64_t key(uint32_t unit) const { return (uint64_t)hi[unit] << 32 | lo[unit]; }
-    __device__ __forceinline__ uint32_t unit_of(uint32_t j) const { return FULL ? j * T + threadIdx.x : min(j * T + threadIdx.x, p.n - 1); }
-    __device__ __forceinline__ void again(uint32_t j0, uint64_t (&k)[kBatch]) const
+    __device__ __forceinline__ uint32_t unit_of(uint32_t j) const { return min(j * T + threadIdx.x, n - 1); }
+    template <bool WHOLE>
+    __device__ __forceinline__ void keys(uint32_t j0, uint64_t (&k)[kBatch]) const
     {
         const uint32_t* l = lo + j0 * T + threadIdx.x;            // the offsets from them are constants
         const uint16_t* h = hi + j0 * T + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) k[i] = FULL ? (uint64_t)h[i * T] << 32 | l[i * T] : key(unit_of(j0 + i));
+        for (int i = 0; i < kBatch; ++i) k[i] = WHOLE ? (uint64_t)h[i * T] << 32 | l[i * T] : key(unit_of(j0 + i));
     }
-    template <bool FIRST>
+    __device__ __forceinline__ void again(uint32_t j0, uint64_t (&k)[kBatch]) const { keys<false>(j0, k); }
+    template <bool FIRST, bool WHOLE>
     __device__ __forceinline__ void fetch(uint32_t j0, float (&x)[kFetch]) const
     {
         if (FIRST && w) {
+            const float* at = w + j0 * T + threadIdx.x;
 #pragma unroll
-            for (int i = 0; i < kFetch; ++i) x[i] = FULL ? ahead[FULL ? i : 0] : __ldcs(w + unit_of(j0 + i));
+            for (int i = 0; i < kBatch; ++i) x[i] = __ldcs(WHOLE ? at + i * T : w + unit_of(j0 + i));
         }
     }
-    __device__ __forceinline__ void done()
-    {
-        if (FULL && next) {
-#pragma unroll
-            for (int i = 0; i < kFetch; ++i) ahead[FULL ? i : 0] = __ldcs(next + i * T + threadIdx.x);
-        }
-    }
-    template <bool FIRST>
+    __device__ __forceinline__ void done() const {}
+    template <bool FIRST, bool WHOLE>
     __device__ __forceinline__ void split(uint32_t j0, const float* x, uint64_t least, uint64_t most, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
     {
         uint64_t k[kBatch];
         if (FIRST && w) {
-            if (plain) {
+            uint32_t* const l0 = lo + j0 * T + threadIdx.x;
+            uint16_t* const h0 = hi + j0 * T + threadIdx.x;
+            if (plain && WHOLE) {
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i) {
-                    const uint32_t unit = FULL ? 0 : unit_of(j0 + i), add = fixed_weight(x[i]);
-                    uint32_t* const lower = FULL ? lo + j0 * T + threadIdx.x + i * T : lo + unit;
-                    uint16_t* const upper = FULL ? hi + j0 * T + threadIdx.x + i * T : hi + unit;
-                    const bool there = FULL || (j0 + i) * T + threadIdx.x < p.n;
-                    const uint32_t l = *lower + add, h = *upper + (l < add);
-                    if (there) *lower = l;
-                    if (there && l < add) *upper = (uint16_t)h;
+                    const uint32_t add = fixed_weight(x[i]), l = l0[i * T] + add, h = h0[i * T] + (l < add);
+                    l0[i * T] = l;
+                    if (l < add) h0[i * T] = (uint16_t)h;
                     k[i] = (uint64_t)h << 32 | l;
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i) {
-                    const uint32_t unit = unit_of(j0 + i);
+                    const uint32_t unit = WHOLE ? (j0 + i) * T + threadIdx.x : unit_of(j0 + i);
                     k[i] = accumulated(key(unit), p.decay, x[i]);
-                    if (FULL || (j0 + i) * T + threadIdx.x < p.n) {
+                    if (WHOLE || (j0 + i) * T + threadIdx.x < n) {
                         lo[unit] = (uint32_t)k[i];
                         hi[unit] = (uint16_t)(k[i] >> 32);
                     }
                 }
             }
         } else {
-            again(j0, k);
+            keys<WHOLE>(j0, k);
         }
         ballots(k, least, most, a, b);
     }
 };
 
-template <int T, bool FULL>
+template <int T>
 __global__ void __launch_bounds__(T, T == 128 ? 5 : 1) evict_kernel(const EvictK p)
 {
     extern __shared__ uint32_t sums[];
@@ -157,8 +153,7 @@ __global__ void __launch_bounds__(T, T == 128 ? 5 : 1) evict_kernel(const EvictK
     if (tid == 0) upper = 0;
     clear(sm);
     Members m = members_of(p, g, 0, kept_before(p, g));
-    SumsRow<T, FULL> row = {p, sums, reinterpret_cast<uint16_t*>(sums + p.n), nullptr, false, p.w + first, {}};
-    row.done();
+    SumsRow<T> row = {p, sums, reinterpret_cast<uint16_t*>(sums + p.n), p.n, nullptr, false};
     uint32_t most = 0;
     for (uint32_t i = tid; i < p.n; i += T) {
         const uint64_t x = first_sum(p, first + i);
@@ -176,7 +171,6 @@ __global__ void __launch_bounds__(T, T == 128 ? 5 : 1) evict_kernel(const EvictK
     for (uint32_t s = 0; s < p.steps; ++s) {
         const uint32_t adds = p.before ? s - 1 : s;                // the step whose weights are added; none (wraps) before the first choice
         row.w = adds < p.steps ? p.w + adds * p.U + first : nullptr;
-        row.next = adds + 1 < p.steps ? p.w + (adds + 1) * p.U + first : nullptr;
         uint32_t word = choose<uint64_t, T>(row, rounds, m.cand, m.left, band, sm, s) | m.safe;
         if (p.carry) {                                             // units that are not there yet are not evicted
             word |= units_there(p.n) & ~m.there;
@@ -221,6 +215,8 @@ template <int T>
 struct StoredRow {
     typedef uint64_t Raw;
     static constexpr int kFetch = 2 * kBatch;
+    static constexpr uint32_t kThreads = T;
+    static constexpr bool kWhole = false, kPeeled = true;
     const uint64_t* from;
     uint32_t n;
     __device__ __forceinline__ void done() const {}
@@ -230,13 +226,14 @@ struct StoredRow {
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) k[i] = from[min((j0 + i) * T + threadIdx.x, n - 1)];
     }
-    template <bool FIRST>
+    template <bool FIRST, bool WHOLE>
     __device__ __forceinline__ void fetch(uint32_t j0, uint64_t (&x)[kFetch]) const
     {
+        const uint64_t* at = from + j0 * T + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < kFetch; ++i) x[i] = from[min((j0 + i) * T + threadIdx.x, n - 1)];
+        for (int i = 0; i < kFetch; ++i) x[i] = WHOLE ? at[i * T] : from[min((j0 + i) * T + threadIdx.x, n - 1)];
     }
-    template <bool FIRST>
+    template <bool FIRST, bool WHOLE>
     __device__ __forceinline__ void split(uint32_t, const uint64_t* k, uint64_t least, uint64_t most, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
     {
 #pragma unroll
@@ -272,12 +269,9 @@ int launch_choice(const EvictK& k, bool two, cudaStream_t st)
         choose_kernel<T><<<k.groups * ((k.steps + k.chunk - 1) / k.chunk), T, 0, st>>>(k);
         return KVP_OK;
     }
-    const bool full = k.n == 32 * T;
     const uint32_t smem = (k.n * 6 + 15) / 16 * 16;
-    const void* f = full ? (const void*)evict_kernel<T, true> : (const void*)evict_kernel<T, false>;
-    if (smem > 40 * 1024) KVP_CUDA(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    if (full) evict_kernel<T, true><<<k.groups, T, smem, st>>>(k);
-    else evict_kernel<T, false><<<k.groups, T, smem, st>>>(k);
+    if (smem > 40 * 1024) KVP_CUDA(cudaFuncSetAttribute(evict_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    evict_kernel<T><<<k.groups, T, smem, st>>>(k);
     return KVP_OK;
 }
 

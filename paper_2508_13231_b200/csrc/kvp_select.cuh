@@ -8,6 +8,8 @@
 // against each other; many equal keys are taken in the order of their words.
 #pragma once
 
+#include <type_traits>
+
 #include "kvp_common.cuh"
 
 namespace kvp {
@@ -91,9 +93,10 @@ __device__ __forceinline__ void find_bin(SelectShared<Key, T>& sm, uint32_t need
     }
 }
 
-// `Row` gives the keys: again(j0, k) those of this thread in rounds j0 .. j0 + 7, key(unit) any unit's, fetch<..>(j0, x) gets
+// `Row` gives the keys of n units: again(j0, k) those of this thread in rounds j0 .. j0 + 7, key(unit) any unit's, fetch<..>(j0, x) gets
 // what kFetch rounds need from memory, done() is called when all rounds of FIRST were, and split<..>(j0, x, lo, hi, a, b) gives the ballots of >= lo and > hi over eight of them, with FIRST for
-// the first time (which may change the keys: the weights of a step are added then). Rounds behind the last unit give any key at all: `cand`, lane j's word of the
+// the first time (which may change the keys: the weights of a step are added then), WHOLE where all of these rounds hold units, so that nothing is
+// looked at and offsets are constants. kWhole: all rounds of the row do; kPeeled: the rounds that do go first, in a loop of their own. Rounds behind the last unit give any key at all: `cand`, lane j's word of the
 // candidates in round j, says which count. 32-bit keys: of the units in it, those with key 0 are no candidates either.
 
 // One digit of the search for a band: of the candidates at a distance of at most `span` from its base, counted by distance >> sh.
@@ -220,20 +223,25 @@ __device__ __forceinline__ void split(Row& row, uint32_t rounds, uint32_t cand, 
 {
     const uint32_t lane = threadIdx.x & 31;
     from = above = 0;
-    for (uint32_t j0 = 0; j0 < rounds; j0 += Row::kFetch) {
+    auto some = [&](uint32_t j0, auto whole) {
+        constexpr bool kWhole = decltype(whole)::value;
         typename Row::Raw x[Row::kFetch];
-        row.template fetch<FIRST>(j0, x);
+        row.template fetch<FIRST, kWhole>(j0, x);
 #pragma unroll
         for (int i = 0; i < Row::kFetch; i += kBatch) {
             uint32_t a[kBatch], b[kBatch];
-            row.template split<FIRST>(j0 + i, x + i, lo, hi, a, b);
+            row.template split<FIRST, kWhole>(j0 + i, x + i, lo, hi, a, b);
             const uint32_t c = own_of(a, lane), d = own_of(b, lane);
             if ((lane & ~7u) == j0 + i) {
                 from = c;
                 above = d;
             }
         }
-    }
+    };
+    uint32_t j0 = 0;
+    if constexpr (Row::kPeeled)
+        for (; (j0 + Row::kFetch) * Row::kThreads <= row.n; j0 += Row::kFetch) some(j0, std::true_type());
+    for (; j0 < rounds; j0 += Row::kFetch) some(j0, std::bool_constant<Row::kWhole>());
     from &= cand;
     above &= cand;
 }

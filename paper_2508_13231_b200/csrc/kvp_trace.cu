@@ -408,35 +408,38 @@ trace_select_kernel(const TraceK k, uint32_t want, uint32_t U, const int32_t* __
 
 // Access bitmaps of recorded weights, on the bits of positive floats, which order as whole numbers do (a unit that received nothing, or NaN, has key
 // 0 and is never picked). A CTA takes some consecutive steps of a group, in which the threshold moves little.
-// FULL: n = 32 T, so that every slot of 32 rounds holds a unit.
-template <int T, bool FULL>
+// WHOLE_ROW: n is a multiple of eight rounds of the CTA, so that no load needs a look at the row's end. 32 steps of 2.6 million units, us, in groups of 2048
+// with it 138 (that look costs 149), 2080 182, 4064 135, 4096 with it 121 (135), 7000 155, 8192 with it 132 (146), 32736 293, 32768 with it 269 (299).
+template <int T, bool WHOLE_ROW>
 struct WeightsRow {
     typedef float Raw;
     // Loads under way at once: none depends on a condition. More of them, or a step ahead as kvp_evict.cu has it, cost CTAs an SM, and were slower:
     // 640 groups of 4096 units x 64 steps 215 us with 8, 225 with 16, 298 with 32 a step ahead.
     static constexpr int kFetch = kBatch;
+    static constexpr uint32_t kThreads = T;
+    static constexpr bool kWhole = WHOLE_ROW, kPeeled = false;
     const float* from;
     uint32_t n;
     static __device__ __forceinline__ uint32_t key_of(float w) { return w > 0.0f ? __float_as_uint(w) : 0u; }
-    __device__ __forceinline__ void weights(uint32_t j0, float (&w)[kBatch]) const
-    {
-        const float* at = from + j0 * T + threadIdx.x;       // the offsets from it are constants
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) w[i] = FULL ? at[i * T] : from[min((j0 + i) * T + threadIdx.x, n - 1)];
-    }
     __device__ __forceinline__ void again(uint32_t j0, uint32_t (&k)[kBatch]) const
     {
         float w[kBatch];
-        weights(j0, w);
+        if (WHOLE_ROW || (j0 + kBatch) * T <= n) fetch<false, true>(j0, w);
+        else fetch<false, false>(j0, w);
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) k[i] = key_of(w[i]);
     }
-    template <bool FIRST>
-    __device__ __forceinline__ void fetch(uint32_t j0, float (&w)[kFetch]) const { weights(j0, w); }
+    template <bool FIRST, bool WHOLE>
+    __device__ __forceinline__ void fetch(uint32_t j0, float (&w)[kFetch]) const
+    {
+        const float* at = from + j0 * T + threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) w[i] = WHOLE || (j0 + i) * T + threadIdx.x < n ? at[i * T] : 0.0f;
+    }
     __device__ __forceinline__ void done() const {}
     // 0 < lo <= the bits of infinity, so a comparison of floats says the same as one of keys, and NaN or a negative weight fails it; hi may lie
     // behind infinity, even where the bits are those of negative numbers, and is cut to it
-    template <bool FIRST>
+    template <bool FIRST, bool WHOLE>
     __device__ __forceinline__ void split(uint32_t, const float* w, uint32_t lo, uint32_t hi, uint32_t (&a)[kBatch], uint32_t (&b)[kBatch]) const
     {
         const float least = __uint_as_float(lo), most = __uint_as_float(min(hi, 0x7F800000u));
@@ -449,7 +452,7 @@ struct WeightsRow {
     __device__ __forceinline__ uint32_t key(uint32_t unit) const { return key_of(from[unit]); }
 };
 
-template <int T, bool FULL>
+template <int T, bool WHOLE_ROW>
 __global__ void __launch_bounds__(T, T == 1024 ? 1 : T == 32 ? 16 : 1280 / T) weights_select_kernel(const TraceK k, uint32_t chunk, uint64_t U, const float* __restrict__ weights)
 {
     __shared__ SelectShared<uint32_t, T> sm;
@@ -460,7 +463,7 @@ __global__ void __launch_bounds__(T, T == 1024 ? 1 : T == 32 ? 16 : 1280 / T) we
     Band<uint32_t> band;
     band.valid = band.moved = false;
     for (uint32_t t = t0; t < t1; ++t) {
-        WeightsRow<T, FULL> row = {weights + t * U + first, k.n};
+        WeightsRow<T, WHOLE_ROW> row = {weights + t * U + first, k.n};
         const uint32_t word = choose<uint32_t, T>(row, rounds, cand, k.topk, band, sm, t);
         put_words(k.out + (size_t)t * k.W32, first, k.n, k.aligned, word);
     }
@@ -491,8 +494,8 @@ extern "C" int kvp_trace_weights(uint32_t groups, uint32_t units_per_group, uint
     const uint32_t grid = groups * ((steps + chunk - 1) / chunk);
 #define KVP_SELECT(T)                                                                                     \
     do {                                                                                                  \
-        if (k.n != 32 * T) weights_select_kernel<T, false><<<grid, T, 0, st>>>(k, chunk, U, weights);     \
-        else weights_select_kernel<T, true><<<grid, T, 0, st>>>(k, chunk, U, weights);                         \
+        if (k.n % (kBatch * T)) weights_select_kernel<T, false><<<grid, T, 0, st>>>(k, chunk, U, weights); \
+        else weights_select_kernel<T, true><<<grid, T, 0, st>>>(k, chunk, U, weights);                    \
     } while (0)
     switch (select_threads(k.n)) {
         case 32: KVP_SELECT(32); break;
