@@ -197,8 +197,10 @@ __global__ void __launch_bounds__(128) sums_kernel(const EvictK p)
         float x[kAhead];
 #pragma unroll
         for (uint32_t i = 0; i < kAhead; ++i) x[i] = next[i];
+        if (s0 + kAhead < p.steps) {
 #pragma unroll
-        for (uint32_t i = 0; i < kAhead; ++i) next[i] = __ldcs(p.w + min(s0 + kAhead + i, last) * p.U + u);
+            for (uint32_t i = 0; i < kAhead; ++i) next[i] = __ldcs(p.w + min(s0 + kAhead + i, last) * p.U + u);
+        }
 #pragma unroll
         for (uint32_t i = 0; i < kAhead; ++i) {
             if (s0 + i >= p.steps) break;
