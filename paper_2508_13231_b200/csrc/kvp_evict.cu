@@ -299,13 +299,14 @@ int launch_evict(const kvp_evict_params* a, const float* weights, const int64_t*
     k.groups = a->groups;
     if (!k.aligned) KVP_CUDA(cudaMemsetAsync(rows, 0, (size_t)a->steps * k.W32 * 4, st));
     const uint32_t n = k.n;
-    // Which form is the faster one, in seconds as measured. One pass: a step takes 2.5 us and more with the units of a group (0.3 ns each, 0.8 where a
-    // CTA fills an SM), and with the groups (640 instead of 64: 5.8 instead of 3.8 us). Two passes: 14 us and 5.8 ps per unit and step.
-    // 8 groups x 2048 units x 16 steps 51 and 15 us, x 256 steps 668 and 35; 64 x 4096 x 64 244 and 90; 200 x 4096 x 64 281 and 311.
+    // Which form is the faster one, in seconds. One pass: a step's latency grows with the units of a group, and with many groups the SMs are full. Two
+    // passes: by the bytes. Measured on 461 shapes (128 .. 32768 units, 1 .. 1280 groups, 2 .. 256 steps): the form taken is 1% slower than the other at the
+    // mean, 35% at most (1280 groups x 128 units x 4 steps, 36 and 27 us). 8 groups x 2048 units x 256 steps 37 and 754 us in two passes and one, 64 x 4096
+    // x 64 107 and 407, 300 x 4096 x 64 354 and 420, 148 x 32768 x 4 188 and 106. One step, or more than 1 GiB of sums: one pass.
     const uint64_t all = k.U * a->steps;
     const size_t bytes = all * 8;
-    const double step = (2.5e-6 + n * (n > 16384 ? 0.8e-9 : 0.3e-9)) * (1 + k.groups / 1000.0);
-    const bool faster = a->steps > 1 && a->steps * step > 14e-6 + 5.8e-12 * (double)all;
+    const double one = std::max(a->steps * (3.5e-6 + n * 0.5e-9), (double)all * (n > 4096 ? 3.2e-12 : 2.0e-12));
+    const bool faster = a->steps > 1 && one > 9e-6 + 4.3e-12 * (double)all;
     const uint32_t form = g_hooks.evict_form;                      // test hook
     const bool two = !k.carry && bytes <= ((size_t)1 << 30) && (form ? form == 2 : faster);
     if (two) {

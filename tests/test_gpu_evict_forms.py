@@ -27,7 +27,7 @@ def host_bits(t):
 
 
 @pytest.mark.parametrize("n", [4096, 4000])
-def test_sums_are_not_added_to_while_a_row_is_still_chosen(kvp, n):
+def test_sums_are_not_added_to_while_a_row_is_still_chosen(kvp, hooks, n):
     """Many groups walk their steps in one CTA each, with the sums in shared memory: the weights of a step are added only when every lane of a
     warp has finished looking at the sums of the step before. Bands around the thresholds of sums without ties end in that branch at most steps."""
     groups, steps, budget = 300, 20, n // 10
@@ -36,6 +36,7 @@ def test_sums_are_not_added_to_while_a_row_is_still_chosen(kvp, n):
     w = (base * rng.uniform(0.5, 1.5, (steps, groups, n))).astype(np.float32).reshape(steps, groups * n)
     rows, acc = plain.evict(w, groups, budget, 1, 4, 65536)
     dev = cuda(w)
+    hooks(evict_form=1)
     for _ in range(5):
         got = kvp.evict(dev, groups, budget, sink=1, recent=4)
         assert np.array_equal(host_bits(got["kept"]), rows) and np.array_equal(got["acc"].cpu().numpy(), acc)
