@@ -159,7 +159,8 @@ __global__ void __launch_bounds__(kThreads) count_kernel(const AttendK p)
 // the same number of tiles. A segment with tiles takes kFixed places before its first one: what a CTA spends on a segment whatever
 // its length (queries, the first tiles' way from memory, the join) is that of kFixed tiles about. CTA c works on the tiles at places
 // c * chunk .. c * chunk + chunk - 1.
-// (kFixed 16, 32, 48, 64: 49.7, 47.5, 47.3, 48.0 us for 32 sequences of up to 8192 tokens x 8 heads).
+// Us with kFixed 16, 32, 48, 64, 96: 32 sequences of up to 8192 tokens x 8 heads of 128 dims 56, 53, 53, 54, 57, of 64 dims 39, 37, 37, 39, 41, of 256 105, 98,
+// 95, 97, 100; 64 of up to 2048 43, 39, 39, 41, 42 (64 dims 31, 29, 30, 31, 32); one of 131072 45, 44, 43, 43, 43; four of up to 8192 14.5 to 15.1.
 constexpr uint32_t kFixed = 48;
 
 struct Line {
@@ -1229,8 +1230,10 @@ extern "C" int kvp_attend(const kvp_attend_params* a, const void* q, const void*
     k.least = kWarps;
     k.unit_log2 = k.unit == 1 ? 0 : k.unit == 2 ? 1 : k.unit == 4 ? 2 : k.unit == 8 ? 3 : 4;
     k.scale = a->scale;
-    // 32 sequences x 8 heads in 296 parts: 46.1 us with a warp to a row, 47.7 with a CTA; 8 segments in 296 parts want the CTA
-    k.warp_rows = (uint64_t)k.batch * k.heads.d * k.segs.d >= k.ctas / 8;
+    // Segments of few parts are joined by a warp a row, others by a CTA. Us by warps and by CTAs in 296 parts, head dim 128: 1 sequence x 8 heads 47.5, 43.2; 2 x 8
+    // 31.0, 28.9; 4 x 8 20.7, 20.7; 40 x 1 20.4, 18.6; 8 x 8 18.6, 18.6; 16 x 8 31.6, 31.9; 32 x 8 52.7, 55.3; 128 x 4 30.9, 36.0. In 148, head dim 256: 4 x 8
+    // 32.9, 31.0; 40 x 1 29.0, 28.9; 8 x 8 24.8, 24.5; 16 x 8 60.1, 61.6; 128 x 4 54.3, 59.2.
+    k.warp_rows = (uint64_t)k.batch * k.heads.d * k.segs.d >= k.ctas / 4;
     k.q_aligned = ((uint64_t)(uintptr_t)q | (uint64_t)(a->q_batch_stride * 2) | (uint64_t)(a->q_query_stride * 2) | (uint64_t)(a->q_head_stride * 2)) % 16 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (a->dtype == KVP_F16) {
