@@ -462,10 +462,11 @@ class Problem:
             raise ValueError("weights must be [steps][units]")
         ep = EvictParams(groups, self.units // groups if groups else 0, self.steps,
                          self.cap // groups if budget is None and groups else budget or 0, sink, recent, decay_q, 0)
-        with torch.cuda.stream(stream):                  # memory of the stream it is written on: another's may still be read by work under way there
-            out = torch.empty((self.steps, self.w32), dtype=torch.int32, device="cuda")
-        _chk(_lib().kvp_policy_accumulated(self._h, C.byref(ep), _ptr(weights, torch.float32), _ptr(out), _stream(stream)),
-             "kvp_policy_accumulated")
+        # memory of the device and the stream it is written on: another stream's may still be read by work under way there
+        with torch.cuda.device(weights.device), torch.cuda.stream(stream):
+            out = torch.empty((self.steps, self.w32), dtype=torch.int32, device=weights.device)
+            _chk(_lib().kvp_policy_accumulated(self._h, C.byref(ep), _ptr(weights, torch.float32), _ptr(out), _stream(stream)),
+                 "kvp_policy_accumulated")
         return out
 
     def wr_grid(self, w_max, n_ratio=11, init_mode=INIT_STATIC_FIRST, stream=None):
