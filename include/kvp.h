@@ -393,8 +393,8 @@ int kvp_trace_generate(const kvp_trace_params* params, uint32_t* access_bitmaps,
  * eviction, as one step of a serving loop (kvp_evict) or as a placement schedule (kvp_policy_accumulated). They are
  * asynchronous on `stream`, keep nothing between calls and work on the current device (kvp_policy_accumulated on its problem's); all of them can be captured into a
  * graph (lengths, tables, slots and bitmaps are read on the device). What a call writes overlaps nothing that it reads, but where it
- * says so. An array that does not lie at the alignment of its type is KVP_ERR_ARG. kvp_evict and kvp_policy_accumulated over several steps of few groups take up to 1 GiB of stream-ordered scratch,
- * freed on return, as kvp_trace_generate does; the others allocate nothing.
+ * says so. An array that does not lie at the alignment of its type is KVP_ERR_ARG. kvp_evict and kvp_policy_accumulated over several steps of
+ * few groups take up to 1 GiB of stream-ordered scratch, freed on return, as kvp_trace_generate does; the others allocate nothing.
  *
  * A cache held in 4 bits. [pages][kv_heads][kvp_cache_page_bytes(head_dim, page_tokens)] bytes, 16-byte aligned: a page holds
  * page_tokens (a multiple of 16) tokens of one kv-head as page_tokens / 16 tiles of 16 tokens, so that a unit of the placement
@@ -467,7 +467,8 @@ typedef struct {
  *   workspace (device) 256-byte aligned, kvp_attend_workspace(...) bytes, used by this call alone until its work has finished
  * A query that sees no token gives out 0 and lse -infinity. Scores, maxima and sums are fp32; a weight, and its product with a value's scale, is rounded
  * to fp16 (bf16 outputs: one term, 2^-11 each) or to two fp16 terms (fp16 outputs), with the largest weight at 2^13 and the values' scales raised where
- * they are below 2^-7, so that weights down to 2^-20 of the largest keep those bits whatever the values' size. Errors: KVP_ERR_ARG (null, zero sizes, unit_tokens, dtype, a scale that is
+ * they are below 2^-7, so that weights down to 2^-20 of the largest keep the first term's bits however small the values are (values that span 2^k * 30 take k
+ * of those 20). Errors: KVP_ERR_ARG (null, zero sizes, unit_tokens, dtype, a scale that is
  * not finite, a workspace too small, a cache that is not 16-byte aligned, a workspace that is not 256-byte
  * aligned, out not 8-byte aligned), KVP_ERR_RANGE (head_dim, sizes above).
  */

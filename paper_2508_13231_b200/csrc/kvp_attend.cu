@@ -7,12 +7,13 @@
 //
 // Products. Up to eight rows that share a kv-head are one segment; the matrix instruction m16n8k16 takes 16 tokens x 16 dims of
 // keys as its left operand and the rows as its right one, so that no row is padding where eight heads share a kv-head.
-// (tcgen05.mma wants 64 or 128 rows of the left operand and 8 columns would use it no better; what bounds this kernel is memory.)
-// The 4-bit whole numbers enter as fp16 subnormals (bits 0-3 of a half-word are q 2^-24, bits 4-7 are q 2^-20), which costs one
-// AND for two numbers and no conversion; their products with fp16 queries are exact and summed in fp32. Scales act on the sums of
+// (tcgen05.mma takes 64 or 128 rows of tokens and eight columns at least, as far as decoding goes: its operands would have to be unpacked to shared memory first,
+// and the tensor pipe is 23% busy as it is. A chunk of a prompt, with hundreds of rows a kv-head, would fill it; here it reads the cache once for every eight rows.)
+// The 4-bit whole numbers enter as fp16 subnormals, two by one AND and no conversion (values as they lie, q 2^-24 and q 2^-20; keys shifted to bits 4 .. 7
+// of a significand, q 2^-20, because leading zeros cost bits of the sum); products with fp16 queries are exact and summed in fp32. Scales act on the sums of
 // 32 dims in fp32, the zeros on the sums of the query's dims, which enter as two fp16 terms (22 bits). A row's queries are divided by a power
 // of two first, so that bf16 ones fit fp16 whatever their size.
-// exp runs in fp32 against a running maximum that moves only when a score passes it by 2^8 (rare), sums are fp32. The weights p
+// exp runs in fp32 against a running maximum that moves only when a score passes it by 2^2 (kSlack; seldom behind the first tiles), sums are fp32. The weights p
 // times the scales of the values are the second product's right operand, in fp16 (11 bits, half a step is 2^-11 of a weight at most; the
 // output has 8 or 11 bits). So that the product keeps them, a weight enters as up to 2^13 .. 2^15, and scales of which none so far
 // reached 2^-7 are multiplied by a power of two that brings the largest to 1 .. 2; larger ones than 2 take as much off the weights.
@@ -23,10 +24,11 @@
 // CTA worked on are joined by the second kernel, which also turns what was noted per unit into weights. The order of every sum is
 // fixed, so results do not change from run to run.
 //
-// What bounds it. A warp works on two tiles at a time (a tile costs 300 instructions; two share the exchange of maxima, the loads of queries and the
-// loop), with two more on their way through cp.async, 16 warps an SM at 128 registers. 8 x 131072 tokens x 8 heads of 128 dims x 8 queries, 1.34 GB, take
-// 259 us (5.2 TB/s), one such sequence 44 us where 26 would move its bytes: 6 us until the first tiles are there, 3 for the join of the warps, and CTAs
-// that end at different times. Fewer registers and more warps spill; 4 warps a CTA were faster on batches (45 instead of 48 us) and slower here (51).
+// What bounds it. A warp works on two tiles at a time (346 instructions a tile, all of a call's counted; two share the exchange of maxima, the loads of queries
+// and the loop), with two more on their way through cp.async, 16 warps an SM at 128 registers: latency at that number of warps, with issue slots 55% and DRAM
+// half busy. 8 x 131072 tokens x 8 heads of 128 dims x 8 queries, 1.34 GB, take 251 us (5.3 TB/s; 274 with weights), one such sequence 45 us where 26 would move
+// its bytes: 6 us until the first tiles are there, 3 for the join of the warps, and CTAs that end at different times. Fewer registers and more
+// warps spill; 4 warps a CTA were faster on batches (45 instead of 48 us) and slower here (51).
 #include <cuda_bf16.h>
 
 #include "kvp_tile.cuh"

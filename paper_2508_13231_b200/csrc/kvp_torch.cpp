@@ -18,7 +18,8 @@
 
 #include "../../include/kvp.h"
 
-// A library without these still serves the scoring calls; the calls that need them say so.
+// A library without these still serves the scoring calls (Python loads this module with all references bound, and the tests put a stand-in with the scoring
+// calls alone in the library's place); the calls that need them say so.
 #pragma weak kvp_cache_append
 #pragma weak kvp_cache_read
 #pragma weak kvp_attend
