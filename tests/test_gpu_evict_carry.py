@@ -1,5 +1,6 @@
 """Eviction as a cache has it (carry): what a step leaves out stays out, units that come are candidates, and attention over the units kept sees the
 token that opens a new one. The form it is compared with goes by sets of units, one at a time; nothing of it comes from the other plain forms."""
+import ctypes
 import os
 import sys
 
@@ -178,3 +179,11 @@ def test_carry_refuses(kvp):
             kvp.evict(w, 1, 4, exist=exist, carry=True)
     with pytest.raises(ValueError):
         kvp.evict(w, 1, 4, exist=torch.zeros(3, dtype=torch.int32, device="cuda"))
+    # a placement policy's units return
+    prob = kvp.Problem(32, 8192, 3, torch.ones(3, 1, dtype=torch.int32, device="cuda"), 8, 8 * 10 ** 12, 9 * 10 ** 11, 9 * 10 ** 11)
+    out = torch.full((3, 1), -1, dtype=torch.int32, device="cuda")
+    for flags, code in ((2, kvp.ERR_ARG), (0, 0)):
+        ep = kvp.EvictParams(1, 32, 3, 4, 0, 0, 65536, flags)
+        rc = kvp._lib().kvp_policy_accumulated(prob._h, ctypes.byref(ep), ctypes.c_void_p(w.data_ptr()), ctypes.c_void_p(out.data_ptr()), None)
+        torch.cuda.synchronize()
+        assert rc == code and bool((out == (-1 if flags else 15)).all())
