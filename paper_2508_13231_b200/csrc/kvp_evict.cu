@@ -73,8 +73,8 @@ __device__ __forceinline__ uint32_t kept_before(const EvictK& p, uint32_t g)
 
 // One pass. The sums of a group, 48 bits each, are in shared memory as lower words and upper half-words (24 KB for 4096 units: five CTAs an SM,
 // so that 740 groups of that size are worked on at once); a step's first pass adds its weights. What bounds it is the latency of a step (two barriers,
-// the search of the band's bins by one warp) with 17 warps an SM. Walks of 32 steps over 2.6 million units, us, by the units of a group: 2048 240, 2080 314,
-// 4064 217, 4096 205, 7000 416, 8192 391, 16384 533, 32768 763; 53 would move the bytes. The weights of the next step in registers meanwhile: 198 at 4096, the
+// the search of the band's bins by one warp) with 17 warps an SM. Walks of 32 steps over 2.6 million units, us, by the units of a group: 2048 246, 2080 308,
+// 4064 221, 4096 209, 7000 410, 8192 393, 16384 536, 32768 772; 53 would move the bytes. The weights of the next step in registers meanwhile: 198 at 4096, the
 // one length for which they fit without spills (326 otherwise). Twice the threads a group are no faster.
 template <int T>
 struct SumsRow {
@@ -89,14 +89,15 @@ struct SumsRow {
     const float* w;           // the weights to be added, or null
     bool plain;               // no decay, and no sum can reach 2^48
     __device__ __forceinline__ uint64_t key(uint32_t unit) const { return (uint64_t)hi[unit] << 32 | lo[unit]; }
-    __device__ __forceinline__ uint32_t unit_of(uint32_t j) const { return min(j * T + threadIdx.x, n - 1); }
+    // Slots behind the row's end are not looked at: clamped to its last unit, they would read a sum that another warp is adding to.
+    __device__ __forceinline__ bool there(uint32_t j) const { return j * T + threadIdx.x < n; }
     template <bool WHOLE>
     __device__ __forceinline__ void keys(uint32_t j0, uint64_t (&k)[kBatch]) const
     {
         const uint32_t* l = lo + j0 * T + threadIdx.x;            // the offsets from them are constants
         const uint16_t* h = hi + j0 * T + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) k[i] = WHOLE ? (uint64_t)h[i * T] << 32 | l[i * T] : key(unit_of(j0 + i));
+        for (int i = 0; i < kBatch; ++i) k[i] = WHOLE || there(j0 + i) ? (uint64_t)h[i * T] << 32 | l[i * T] : 0u;
     }
     __device__ __forceinline__ void again(uint32_t j0, uint64_t (&k)[kBatch]) const { keys<false>(j0, k); }
     template <bool FIRST, bool WHOLE>
@@ -105,7 +106,7 @@ struct SumsRow {
         if (FIRST && w) {
             const float* at = w + j0 * T + threadIdx.x;
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) x[i] = __ldcs(WHOLE ? at + i * T : w + unit_of(j0 + i));
+            for (int i = 0; i < kBatch; ++i) x[i] = WHOLE || there(j0 + i) ? __ldcs(at + i * T) : 0.0f;
         }
     }
     __device__ __forceinline__ void done() const {}
@@ -127,11 +128,11 @@ struct SumsRow {
             } else {
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i) {
-                    const uint32_t unit = WHOLE ? (j0 + i) * T + threadIdx.x : unit_of(j0 + i);
-                    k[i] = accumulated(key(unit), p.decay, x[i]);
-                    if (WHOLE || (j0 + i) * T + threadIdx.x < n) {
-                        lo[unit] = (uint32_t)k[i];
-                        hi[unit] = (uint16_t)(k[i] >> 32);
+                    k[i] = 0;
+                    if (WHOLE || there(j0 + i)) {
+                        k[i] = accumulated((uint64_t)h0[i * T] << 32 | l0[i * T], p.decay, x[i]);
+                        l0[i * T] = (uint32_t)k[i];
+                        h0[i * T] = (uint16_t)(k[i] >> 32);
                     }
                 }
             }
