@@ -477,6 +477,156 @@ int kvp_attend(const kvp_attend_params* params, const void* q, const void* cache
                const uint32_t* units, void* out, float* lse, float* weights, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /*
+ * ---- a cache held in 8 bits, and what a step of decoding does around it ----
+ * The same path with less error in the recorded weights (4 bits are a fifteenth of a group's range, 8 bits here a sixteenth of a value), with scores
+ * as models have them, and the calls that make its inputs on the device: kvp_block_tables (pages, slots, positions and lengths of the requests of a
+ * step), kvp_rope (rotary positions), kvp_cache8_append, kvp_attend8. They are asynchronous, keep nothing between calls, can be captured, work on the current
+ * device and allocate nothing; what a call writes overlaps nothing that it reads, but where it says so.
+ *
+ * A cache held in 8 bits. [pages][kv_heads][kvp_cache8_page_bytes(head_dim, page_tokens)] bytes, 16-byte aligned: a page holds page_tokens (a
+ * multiple of 16) tokens of one kv-head as page_tokens / 16 blocks of 16 tokens, so that a unit of the placement problem lies in one piece. head_dim is
+ * 64, 128 or 256. The keys of a block are kept as scale * q, its values with a scale of their own: q in e4m3 (four significant bits, to the nearest, ties to
+ * even; no NaN), scale = 2^e, fp32, the smallest for which every |x| of the block's keys (or values) is at most 448 * 2^e, e >= -100; 0 where all of
+ * them are 0. Inputs beyond +-2^100 count as that, NaN as 0.
+ * Tokens come to a block one after the other. The token of its first place begins the block anew; with every other token the scale stays
+ * or grows (it never shrinks), and when it grows what the block holds is rounded to e4m3 again, which changes it only below the
+ * smallest normal number (2^-6 * scale). A cache begins as zeros: a block whose scales are 0 holds nothing.
+ * A block is 32 * head_dim + 16 bytes; with i the token of the block and d the dim, in this order:
+ *   keys [i/8][d/16][i%8][d%16] and values [d][i], 8 bits each; scale of the keys, scale of the values, fp32; 8 bytes that are not used.
+ * 257 bytes for a token's key and value at head_dim 128.
+ */
+
+/* Bytes of a page of one kv-head; 0 for a head_dim or page_tokens that is not served. */
+uint64_t kvp_cache8_page_bytes(uint32_t head_dim, uint32_t page_tokens);
+
+/*
+ * kvp_cache8_append -- the keys and values of `tokens` tokens into the cache. Arguments and errors as of kvp_cache_append (the shape's head_dim and
+ * page_tokens are those of kvp_cache8_page_bytes). The tokens of one block stand within 16 tokens of the call, in any order, as the tokens of a
+ * sequence do; where they stand further apart, or two have the same slot, what that block holds afterwards is not specified.
+ */
+int kvp_cache8_append(const kvp_cache_shape* c, void* cache, uint32_t dtype, uint32_t tokens, const void* k,
+                      int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                      const int64_t* slots, void* stream);
+
+/* kvp_cache8_read -- the inverse: k, v (device) [tokens][kv_heads][head_dim], contiguous, 16-byte aligned: scale * q rounded to `dtype`. A token whose
+ * slot lies outside the cache reads as 0. */
+int kvp_cache8_read(const kvp_cache_shape* c, const void* cache, uint32_t dtype, uint32_t tokens, const int64_t* slots, void* k,
+                    void* v, void* stream);
+
+typedef struct {
+    kvp_cache_shape cache;
+    uint32_t batch;             /* sequences                                                                 */
+    uint32_t queries;           /* query tokens per sequence, the last ones of it: 1..1024                   */
+    uint32_t group;             /* query heads per kv-head; queries * group <= 4096                          */
+    uint32_t table_pages;       /* pages per row of the table; table_pages * page_tokens < 2^30              */
+    uint32_t unit_tokens;       /* tokens per unit: 1, 2, 4, 8 or a multiple of 16; divides page_tokens      */
+    uint32_t dtype;             /* of q and out: KVP_BF16 or KVP_F16                                         */
+    float    scale;             /* of the scores, usually 1 / sqrt(head_dim)                                 */
+    float    cap;               /* scores x become cap * tanh(x / cap); 0: as they are                       */
+    uint32_t window;            /* a query sees the last `window` tokens up to its own; 0 (or >= 2^30): all  */
+    uint32_t sink;              /* with a window: and the first `sink` tokens of the sequence                */
+    uint32_t reserved;          /* must be 0 */
+    int64_t  q_batch_stride, q_query_stride, q_head_stride; /* in elements; dims contiguous                  */
+} kvp_attend8_params;
+
+/*
+ * kvp_attend8 -- attention of the last `queries` tokens of each sequence over its cache, and the weight every unit received.
+ *   q, table, lens, units, out, lse, weights, workspace: as of kvp_attend (kvp_attend8_workspace(...) bytes)
+ *   slopes  (device) [kv_heads * group] float or NULL: a score gets slope * (position of the token - position of the query) added, behind the cap
+ * The scores of a query that sees a token are cap(scale * q . k) + bias in fp32. A query that sees no token gives out 0 and lse -infinity; a row of q
+ * with a value that is not finite gives NaN. The products run in e4m3 with fp32 sums: a bf16 value of q enters exactly as two terms and an fp16 one as three (values
+ * below 2^-14 of the row's largest to within 2^-22 of that), a weight as three terms, 2^-12 of itself, in units of 2^-26 of the largest weight times
+ * the largest scale of the values: tokens whose weights are below that add nothing. A chunk of a prompt (many queries) reads the cache once for every 64 rows.
+ * A wait inside the kernel that takes two seconds, which only a fault can cause, ends it with NaN in out.
+ * Errors: as of kvp_attend, and a cap that is negative or not finite (KVP_ERR_ARG).
+ */
+int kvp_attend8_workspace(const kvp_attend8_params* params, int want_weights, int has_units, uint64_t* bytes);
+int kvp_attend8(const kvp_attend8_params* params, const void* q, const void* cache, const int32_t* table, const int32_t* lens,
+                const uint32_t* units, const float* slopes, void* out, float* lse, float* weights, void* workspace, uint64_t workspace_bytes,
+                void* stream);
+
+/*
+ * Rotary positions. Dims come in pairs (a, b), pair j = 0 .. rotary_dim / 2 - 1 of a head: dims j and j + rotary_dim / 2, or with KVP_ROPE_INTERLEAVED
+ * 2 j and 2 j + 1. With angle = position * frequencies[j]:  a' = scale * (a cos - b sin),  b' = scale * (a sin + b cos).  KVP_ROPE_INVERSE turns by
+ * -angle, which is the gradient of the call without it (and undoes it where scale is 1). The dims from rotary_dim on stay as they are.
+ */
+#define KVP_ROPE_INTERLEAVED 1u
+#define KVP_ROPE_INVERSE     2u
+
+typedef struct {
+    uint32_t tokens, heads, kv_heads; /* of q and of k; one of them may be 0 (its pointers are not used)              */
+    uint32_t head_dim;                /* at most 65536                                                                */
+    uint32_t rotary_dim;              /* even, 2..head_dim                                                            */
+    uint32_t dtype;                   /* KVP_BF16, KVP_F16, KVP_F32                                                   */
+    uint32_t flags;                   /* KVP_ROPE_*                                                                   */
+    float    scale;                   /* of the turned dims; 1 unless the frequencies come with one                   */
+    uint32_t reserved;                /* must be 0 */
+    int64_t  q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride;     /* in elements; dims contiguous */
+    int64_t  k_token_stride, k_head_stride, k_out_token_stride, k_out_head_stride;
+} kvp_rope_params;
+
+/*
+ * kvp_rope -- queries and keys of `tokens` tokens in one launch.
+ *   q, k (device) [tokens][heads or kv_heads][head_dim];  q_out, k_out (device) the same, may be q or k themselves with the same strides (another
+ *        overlap is not allowed)
+ *   positions (device) [tokens] int32, also negative;  frequencies (device) [rotary_dim / 2] double, radians a token, finite
+ * Sums and products in fp32, rounded once. An angle is reduced in 64-bit whole numbers, so sines and cosines are good to 2^-24 at any position.
+ * Errors: KVP_ERR_ARG (null, sizes, dtype, flags, a scale that is not finite, alignment), KVP_ERR_RANGE (sizes). 16-byte aligned rows with
+ * rotary_dim / 2 (interleaved: rotary_dim) and the rest of the head multiples of 16 bytes are moved 16 bytes at a time.
+ */
+int kvp_rope(const kvp_rope_params* params, const void* q, void* q_out, const void* k, void* k_out, const int32_t* positions,
+             const double* frequencies, void* stream);
+
+/* Frequencies base^(-2 j / rotary_dim), scaled for contexts `factor` times as long as the model was trained on. */
+#define KVP_ROPE_PLAIN  0u
+#define KVP_ROPE_LINEAR 1u   /* all divided by factor                                                                  */
+#define KVP_ROPE_BASE   2u   /* base * factor^(rotary_dim / (rotary_dim - 2)): the highest stays, the lowest is divided */
+#define KVP_ROPE_PARTS  3u   /* by the turns t = original_tokens * frequency / 2 pi: t >= high stays, t <= low is divided, between linear in t */
+#define KVP_ROPE_RAMP   4u   /* the same borders, between them linear in j (their dims rounded outwards); scale = 0.1 ln(factor) + 1 */
+
+typedef struct {
+    uint32_t kind;              /* KVP_ROPE_PLAIN .. KVP_ROPE_RAMP                              */
+    uint32_t reserved;          /* must be 0 */
+    double   base;              /* usually 10000                                                */
+    double   factor;            /* >= 1                                                         */
+    double   original_tokens;   /* PARTS, RAMP: the context that the model was trained on       */
+    double   low, high;         /* PARTS, RAMP: turns, 0 <= low < high (often 1 and 4, 1 and 32) */
+} kvp_rope_scaling;
+
+/* frequencies (host) [rotary_dim / 2];  scale (host) or NULL: what kvp_rope's `scale` is to be. Errors: KVP_ERR_ARG. */
+int kvp_rope_frequencies(const kvp_rope_scaling* scaling, uint32_t rotary_dim, double* frequencies, float* scale);
+
+typedef struct {
+    uint32_t batch;             /* requests, below 2^24                                                       */
+    uint32_t table_pages;       /* pages per row of the table; table_pages * page_tokens < 2^30               */
+    uint32_t pages;             /* of the cache, below 2^30; also the size of the ring                        */
+    uint32_t page_tokens;
+    uint32_t tokens;            /* room for new tokens (slots, positions, rows), below 2^30                   */
+    uint32_t reserved;          /* must be 0 */
+} kvp_tables_params;
+
+/*
+ * kvp_block_tables -- the tables of a step: pages for the new tokens of every request, their slots and positions; pages of finished requests are given back.
+ *   new_tokens (device) int32 [batch]: tokens that come (a prompt, 1 while decoding, 0 for an idle row); < 0: the request is finished
+ *   lens       (device) int32 [batch]: tokens that each request has (cut to 0..table_pages * page_tokens);  lens_out the same afterwards, may be lens
+ *   table      (device) int32 [batch][table_pages]: pages of each request, of which the first ceil(len / page_tokens) count; entries of new pages are written
+ *   ring       (device) int32 [pages]: the free pages are ring[(head + i) % pages], i = 0 .. count-1;  state (device) int32 [2] = head, count;
+ *              state_out the same afterwards, may be state
+ *   slots      (device) int64 [tokens], positions, rows int32 [tokens]: of the new tokens, request by request: page * page_tokens + place, position in
+ *              the request, the request. Behind the last one slot -1, position 0, row -1; slot -1 also where the table names no page
+ *   starts     (device) int32 [batch + 1]: the first of a request's tokens, and how many there are in all;  page_starts the same of pages given
+ *   granted    (device) int32 [batch]: 1, or 0 for a request that did not get what it asked for: it stays as it is, with no token in this step
+ * A request asks for ceil((len + new) / page_tokens) - ceil(len / page_tokens) pages. It is granted if it fits its table's row and, counted over the requests up to
+ * it that fit theirs, the pages asked for are at most `count` and the tokens at most `tokens` (one that asks for no page, or no token, does
+ * not mind the respective sum). Pages are taken from the ring's head in order; pages given back, those of the row that are 0..pages-1, go to its tail in order and
+ * are free from the next call on. The table's row of a finished request is not cleared. Without lens_out == lens and state_out == state
+ * a call repeated gives the same. All numbers are exact and do not depend on any order. Errors: KVP_ERR_ARG (null, zero sizes, alignment), KVP_ERR_RANGE.
+ */
+int kvp_block_tables(const kvp_tables_params* params, const int32_t* new_tokens, const int32_t* lens, int32_t* lens_out, int32_t* table, int32_t* ring,
+                     const int32_t* state, int32_t* state_out, int64_t* slots, int32_t* positions, int32_t* rows, int32_t* starts,
+                     int32_t* page_starts, int32_t* granted, void* stream);
+
+/*
  * kvp_trace_weights -- access bitmaps of recorded weights: every step each group reads the `topk` units that received most.
  *   weights        (device) [steps][groups * units_per_group]; a unit without a positive weight (0, negative, NaN) is not read,
  *                  so a group can read fewer than topk, or nothing at the steps of other layers

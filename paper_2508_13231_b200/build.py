@@ -9,8 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvp.so")
 BINDING = os.path.join(HERE, "_kvp_torch.so")
 SOURCES = ["kvp_api.cu", "kvp_cost.cu", "kvp_layout.cu", "kvp_anneal.cu", "kvp_trace.cu", "kvp_policy.cu", "kvp_cache.cu", "kvp_attend.cu",
-           "kvp_evict.cu", "kvp_table.cpp"]
-HEADERS = ["kvp_common.cuh", "kvp_chain.cuh", "kvp_narrow.cuh", "kvp_tile.cuh", "kvp_line.cuh", "kvp_select.cuh"]
+           "kvp_evict.cu", "kvp_cache8.cu", "kvp_attend8.cu", "kvp_rope.cu", "kvp_tables.cu", "kvp_table.cpp"]
+HEADERS = ["kvp_common.cuh", "kvp_chain.cuh", "kvp_narrow.cuh", "kvp_tile.cuh", "kvp_line.cuh", "kvp_select.cuh", "kvp_tile8.cuh", "kvp_mma.cuh"]
 
 
 def _nvcc():

@@ -137,13 +137,13 @@ __device__ __forceinline__ uint32_t sum_upto(uint32_t x, uint32_t lane)       //
 }
 
 struct LineSmem {
-    uint32_t warp[kWarps], before, entry;
+    uint32_t warp[20], before, entry;
 };
 
 // Every thread of the CTA calls it. With a CTA's number: the entry in which its part begins (`entry`; only if it has a part) and the places
 // before that entry. With cta = ~0: the places before `entry`. Up to 128 entries every warp goes through them by itself (one load's
 // latency, no barrier), more of them are split over the CTA.
-template <class P>
+template <uint32_t THREADS = kThreads, class P>
 __device__ __forceinline__ Line find_in_line(const P& p, uint32_t cta, uint32_t& entry, LineSmem& sm)
 {
     const uint32_t E = line_entries(p), per = line_per(p), tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
@@ -181,7 +181,7 @@ __device__ __forceinline__ Line find_in_line(const P& p, uint32_t cta, uint32_t&
             }
         return line;
     }
-    const uint32_t each = (E + kThreads - 1) / kThreads, first = min(tid * each, E), last = min(first + each, E);
+    const uint32_t each = (E + THREADS - 1) / THREADS, first = min(tid * each, E), last = min(first + each, E);
     uint32_t mine = 0;
     for (uint32_t e = first; e < last; ++e) mine += entry_places(p, e, per);
     const uint32_t upto = sum_upto(mine, lane);
@@ -189,7 +189,7 @@ __device__ __forceinline__ Line find_in_line(const P& p, uint32_t cta, uint32_t&
     __syncthreads();
     uint32_t base = 0, total = 0;
 #pragma unroll
-    for (uint32_t w = 0; w < (uint32_t)kWarps; ++w) {
+    for (uint32_t w = 0; w < THREADS / 32; ++w) {
         if (w < warp) base += sm.warp[w];
         total += sm.warp[w];
     }

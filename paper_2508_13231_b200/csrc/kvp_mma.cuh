@@ -68,6 +68,11 @@ __device__ __forceinline__ void tensor_after_sync() { asm volatile("tcgen05.fenc
 __device__ __forceinline__ void tensor_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tensor_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// the numbers of a load are not used before here (the compiler knows no other order between a load's registers and the wait)
+__device__ __forceinline__ void tensor_hold8(float* x)
+{
+    asm volatile("" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]));
+}
 // eight columns of this thread's lane (warp w of a group of four has lanes 32 w .. 32 w + 31)
 __device__ __forceinline__ void tensor_load8(uint32_t at, float* x)
 {

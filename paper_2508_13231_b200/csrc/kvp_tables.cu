@@ -1,0 +1,212 @@
+// Block tables and slot maps from the lengths of requests (include/kvp.h, kvp_block_tables).
+//
+// Whole numbers and prefix sums over the requests. One CTA goes through the requests (a chunk of its threads at a time): who is granted
+// its pages is decided by one pair of running sums, what it gets by a second. Tokens then find their request by a binary search in `starts`: in the same
+// CTA where there are few of them (a decode step is one launch), else in a second kernel over all tokens, which writes 16 bytes each.
+#include "kvp_line.cuh"
+
+namespace kvp {
+
+namespace {
+
+struct TablesK {
+    const int32_t *new_tokens, *lens, *state;
+    int32_t *table, *ring, *lens_out, *state_out, *granted, *starts, *page_starts, *positions, *rows;
+    int64_t* slots;
+    uint32_t batch, table_pages, tokens;
+    Divisor page;            // tokens of a page
+    uint32_t pages;
+};
+
+constexpr uint32_t kScanThreads = 1024, kScanWarps = 32;
+constexpr uint32_t kAlone = 4096;                  // tokens that the CTA of the sums still serves by itself: four a thread
+constexpr uint32_t kSharedStarts = 2048;           // requests whose `starts` a CTA of the second kernel takes to shared memory
+constexpr uint32_t kFull = 0x7FFFFFFFu;            // running sums of what is asked for stay here
+
+__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return min(a + b, kFull); }       // of two that are at most kFull
+
+struct Pair {
+    uint32_t a, b;
+};
+// running sums over the CTA's threads, this one's included, and of all; every thread calls it
+template <bool SATURATE>
+__device__ __forceinline__ Pair sum_over(Pair x, Pair& all, Pair* sm)
+{
+    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
+    auto add = [](uint32_t u, uint32_t v) { return SATURATE ? sat_add(u, v) : u + v; };
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t a = __shfl_up_sync(0xFFFFFFFFu, x.a, o), b = __shfl_up_sync(0xFFFFFFFFu, x.b, o);
+        if (lane >= (uint32_t)o) {
+            x.a = add(x.a, a);
+            x.b = add(x.b, b);
+        }
+    }
+    __syncthreads();                                            // sm is free
+    if (lane == 31) sm[warp] = x;
+    __syncthreads();
+    Pair w = lane < warps ? sm[lane] : Pair{0, 0};
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t a = __shfl_up_sync(0xFFFFFFFFu, w.a, o), b = __shfl_up_sync(0xFFFFFFFFu, w.b, o);
+        if (lane >= (uint32_t)o) {
+            w.a = add(w.a, a);
+            w.b = add(w.b, b);
+        }
+    }
+    all.a = __shfl_sync(0xFFFFFFFFu, w.a, 31);
+    all.b = __shfl_sync(0xFFFFFFFFu, w.b, 31);
+    const uint32_t before = warp ? warp - 1 : 0;
+    const uint32_t a = __shfl_sync(0xFFFFFFFFu, w.a, before), b = __shfl_sync(0xFFFFFFFFu, w.b, before);
+    if (warp) {
+        x.a = add(x.a, a);
+        x.b = add(x.b, b);
+    }
+    return x;
+}
+
+__device__ __forceinline__ uint32_t pages_of(const TablesK& p, uint32_t tokens) { return p.page.of(tokens + p.page.d - 1); }
+__device__ __forceinline__ uint32_t around(uint32_t at, uint32_t pages) { return at >= pages ? at - pages : at; }       // at < 2 pages
+
+// Token t of the call: its request, position and slot; a page that begins with it goes into the table. `head`: of the ring, before the call.
+__device__ __forceinline__ void place_token(const TablesK& p, uint32_t t, const int32_t* starts, uint32_t head)
+{
+    if (t >= (uint32_t)starts[p.batch]) {
+        p.slots[t] = -1;
+        p.positions[t] = 0;
+        p.rows[t] = -1;
+        return;
+    }
+    uint32_t low = 0, high = p.batch;                           // starts[low] <= t < starts[high]
+    while (high - low > 1) {
+        const uint32_t mid = (low + high) / 2;
+        if ((uint32_t)starts[mid] <= t) low = mid;
+        else high = mid;
+    }
+    const uint32_t row = low, first = starts[row], before = (uint32_t)p.lens_out[row] - (starts[row + 1] - first), pos = before + t - first;
+    const uint32_t j = p.page.of(pos), had = pages_of(p, before);
+    int32_t* entry = p.table + (uint64_t)row * p.table_pages + j;
+    int32_t page;
+    if (j >= had) {
+        page = p.ring[around(head + around(p.page_starts[row] + j - had, p.pages), p.pages)];
+        if (pos == j * p.page.d) *entry = page;                 // no other token reads it: the entry is new
+    } else {
+        page = *entry;
+    }
+    p.slots[t] = page >= 0 && (uint32_t)page < p.pages ? (int64_t)page * p.page.d + (pos - j * p.page.d) : -1;
+    p.positions[t] = (int32_t)pos;
+    p.rows[t] = (int32_t)row;
+}
+
+__global__ void __launch_bounds__(kScanThreads) tables_kernel(const TablesK p, bool alone)
+{
+    __shared__ Pair sm[kScanWarps];
+    let_next_start();
+    const uint32_t tid = threadIdx.x, lane = tid % 32;
+    const uint32_t head = (uint32_t)p.state[0] % p.pages, count = min((uint32_t)max(p.state[1], 0), p.pages);
+    const uint32_t most = p.table_pages * p.page.d;
+    Pair asked = {0, 0}, given = {0, 0};                        // pages and tokens so far: asked for, given
+    uint32_t back = 0;                                          // pages given back so far
+    for (uint32_t base = 0; base < p.batch; base += blockDim.x) {
+        const uint32_t i = base + tid;
+        const bool in = i < p.batch;
+        const int32_t n = in ? p.new_tokens[i] : 0;
+        const uint32_t len = in ? min((uint32_t)max(p.lens[i], 0), most) : 0, had = pages_of(p, len);
+        const bool leaves = n < 0, fits = in && !leaves && (uint32_t)n <= most - len;
+        const uint32_t need = fits ? pages_of(p, len + n) - had : 0;
+        uint32_t own = 0;                                       // pages it gives back
+        for (uint32_t left = __ballot_sync(0xFFFFFFFFu, in && leaves && had); left; left &= left - 1) {        // a warp counts one request's pages
+            const uint32_t l = __ffs(left) - 1, many = __shfl_sync(0xFFFFFFFFu, had, l);
+            const int32_t* row = p.table + (uint64_t)(base + tid - lane + l) * p.table_pages;
+            uint32_t good = 0;
+            for (uint32_t j = lane; j < many; j += 32) good += (uint32_t)row[j] < p.pages;
+            good = __reduce_add_sync(0xFFFFFFFFu, good);
+            if (lane == l) own = good;
+        }
+        Pair all;
+        Pair sum = sum_over<true>(Pair{need, fits ? (uint32_t)n : 0u}, all, sm);
+        const bool yes = fits && (!need || sat_add(asked.a, sum.a) <= count) && (!n || sat_add(asked.b, sum.b) <= p.tokens);
+        asked.a = sat_add(asked.a, all.a);
+        asked.b = sat_add(asked.b, all.b);
+        const Pair mine = {yes ? need : 0u, yes ? (uint32_t)n : 0u};
+        sum = sum_over<false>(mine, all, sm);
+        if (in) {
+            p.starts[i] = (int32_t)(given.b + sum.b - mine.b);
+            p.page_starts[i] = (int32_t)(given.a + sum.a - mine.a);
+            p.granted[i] = yes || leaves;
+            p.lens_out[i] = leaves ? 0 : (int32_t)(len + mine.b);
+        }
+        given.a += all.a;
+        given.b += all.b;
+        if (__syncthreads_or(leaves)) {
+            sum = sum_over<false>(Pair{own, 0}, all, sm);
+            for (uint32_t left = __ballot_sync(0xFFFFFFFFu, own != 0); left; left &= left - 1) {
+                const uint32_t l = __ffs(left) - 1, many = __shfl_sync(0xFFFFFFFFu, had, l);
+                const int32_t* row = p.table + (uint64_t)(base + tid - lane + l) * p.table_pages;
+                uint32_t to = head + count + back + __shfl_sync(0xFFFFFFFFu, sum.a - own, l);
+                for (uint32_t j0 = 0; j0 < many; j0 += 32) {
+                    const int32_t page = j0 + lane < many ? row[j0 + lane] : -1;
+                    const uint32_t good = __ballot_sync(0xFFFFFFFFu, (uint32_t)page < p.pages);
+                    if (good >> lane & 1u) p.ring[(to + __popc(good & ((1u << lane) - 1u))) % p.pages] = page;
+                    to += __popc(good);
+                }
+            }
+            back += all.a;
+        }
+    }
+    if (tid == 0) {
+        p.starts[p.batch] = (int32_t)given.b;
+        p.page_starts[p.batch] = (int32_t)given.a;
+        p.state_out[0] = (int32_t)around(head + given.a, p.pages);
+        p.state_out[1] = (int32_t)min(count - given.a + back, p.pages);
+    }
+    if (!alone) return;
+    __syncthreads();
+    for (uint32_t t = tid; t < p.tokens; t += blockDim.x) place_token(p, t, p.starts, head);
+}
+
+__global__ void __launch_bounds__(256) tokens_kernel(const TablesK p)
+{
+    __shared__ int32_t near[kSharedStarts + 1];
+    const uint32_t tid = threadIdx.x;
+    wait_for_previous();
+    const int32_t* starts = p.starts;
+    if (p.batch <= kSharedStarts) {
+        for (uint32_t i = tid; i <= p.batch; i += 256) near[i] = p.starts[i];
+        __syncthreads();
+        starts = near;
+    }
+    const uint32_t head = around((uint32_t)p.state_out[0] + p.pages - p.page_starts[p.batch], p.pages);
+    for (uint32_t t = blockIdx.x * 256 + tid; t < p.tokens; t += gridDim.x * 256) place_token(p, t, starts, head);
+}
+
+}  // namespace
+
+}  // namespace kvp
+
+using namespace kvp;
+
+extern "C" int kvp_block_tables(const kvp_tables_params* a, const int32_t* new_tokens, const int32_t* lens, int32_t* lens_out, int32_t* table, int32_t* ring,
+                                const int32_t* state, int32_t* state_out, int64_t* slots, int32_t* positions, int32_t* rows, int32_t* starts,
+                                int32_t* page_starts, int32_t* granted, void* stream)
+{
+    if (!a || a->reserved || !a->batch || !a->table_pages || !a->pages || !a->page_tokens) return KVP_ERR_ARG;
+    if (!new_tokens || !lens || !lens_out || !table || !ring || !state || !state_out || !starts || !page_starts || !granted) return KVP_ERR_ARG;
+    if (a->tokens && (!slots || !positions || !rows)) return KVP_ERR_ARG;
+    if (off_by(new_tokens, 4) || off_by(lens, 4) || off_by(lens_out, 4) || off_by(table, 4) || off_by(ring, 4) || off_by(state, 4) || off_by(state_out, 4) ||
+        off_by(slots, 8) || off_by(positions, 4) || off_by(rows, 4) || off_by(starts, 4) || off_by(page_starts, 4) || off_by(granted, 4)) return KVP_ERR_ARG;
+    // a length and a page more, pages given and a ring's index twice around are counted in 31 bits
+    if ((uint64_t)a->table_pages * a->page_tokens >= (1ull << 30) || a->page_tokens >= (1u << 30) || a->pages >= (1u << 30) || a->tokens >= (1u << 30) ||
+        a->batch >= (1u << 24)) return KVP_ERR_RANGE;
+    TablesK k;
+    k.new_tokens = new_tokens; k.lens = lens; k.state = state;
+    k.table = table; k.ring = ring; k.lens_out = lens_out; k.state_out = state_out; k.granted = granted; k.starts = starts; k.page_starts = page_starts;
+    k.positions = positions; k.rows = rows; k.slots = slots;
+    k.batch = a->batch; k.table_pages = a->table_pages; k.tokens = a->tokens; k.page = divisor(a->page_tokens); k.pages = a->pages;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool alone = a->tokens <= kAlone;
+    const uint32_t wide = a->batch > a->tokens ? a->batch : a->tokens, threads = wide >= kScanThreads ? kScanThreads : (wide + 31) / 32 * 32;
+    int rc = launch(tables_kernel, 1, alone ? threads : kScanThreads, 0, false, st, k, alone);
+    if (!rc && !alone) rc = launch(tokens_kernel, (a->tokens + 1023) / 1024, 256, 0, true, st, k);
+    return rc;
+}

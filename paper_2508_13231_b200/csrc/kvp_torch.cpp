@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
@@ -26,6 +27,12 @@
 #pragma weak kvp_attend_workspace
 #pragma weak kvp_trace_weights
 #pragma weak kvp_evict
+#pragma weak kvp_cache8_append
+#pragma weak kvp_cache8_read
+#pragma weak kvp_attend8
+#pragma weak kvp_attend8_workspace
+#pragma weak kvp_rope
+#pragma weak kvp_block_tables
 
 namespace {
 
@@ -206,7 +213,7 @@ bool dense(PyObject* o, const char* what, at::ScalarType dtype, c10::Device dev,
     if (!t) return false;
     if (t->device() != dev) { PyErr_Format(PyExc_ValueError, "%s: on another device", what); return false; }
     if (!t->is_contiguous()) { PyErr_Format(PyExc_ValueError, "%s: expected a contiguous CUDA tensor", what); return false; }
-    if (t->scalar_type() != dtype) { PyErr_Format(PyExc_ValueError, "%s: expected dtype torch.%s", what, dtype == at::kInt ? "int32" : dtype == at::kLong ? "int64" : dtype == at::kByte ? "uint8" : "float32"); return false; }
+    if (t->scalar_type() != dtype) { PyErr_Format(PyExc_ValueError, "%s: expected dtype torch.%s", what, dtype == at::kInt ? "int32" : dtype == at::kLong ? "int64" : dtype == at::kByte ? "uint8" : dtype == at::kDouble ? "float64" : "float32"); return false; }
     *out = t;
     return true;
 }
@@ -231,18 +238,21 @@ bool size_fits(int64_t n, const char* what, uint32_t* v)
     return true;
 }
 
+// bytes of 16 tokens of a kv-head, of a cache held in 4 or 8 bits
+int64_t block_bytes(int64_t head_dim, bool eight) { return eight ? 32 * head_dim + 16 : 20 * head_dim; }
+
 // [pages][kv_heads][bytes of a page] uint8
-bool cache_of(PyObject* o, int64_t head_dim, kvp_cache_shape* c, const at::Tensor** out)
+bool cache_of(PyObject* o, int64_t head_dim, bool eight, kvp_cache_shape* c, const at::Tensor** out)
 {
     const at::Tensor* t = tensor_of(o, "cache");
     if (!t || !dense(o, "cache", at::kByte, t->device(), false, out)) return false;
     if (t->dim() != 3) { value_error("cache must be [pages][kv_heads][page bytes]"); return false; }
     if (reinterpret_cast<uintptr_t>(t->data_ptr()) % 16) { value_error("cache must be 16-byte aligned"); return false; }
     const int64_t bytes = t->size(2);
-    if (head_dim <= 0 || bytes <= 0 || bytes % (20 * head_dim)) { value_error("cache: the bytes of a page do not belong to this head_dim"); return false; }
+    if (head_dim <= 0 || bytes <= 0 || bytes % block_bytes(head_dim, eight)) { value_error("cache: the bytes of a page do not belong to this head_dim"); return false; }
     c->reserved = 0;
     return size_fits(t->size(0), "pages", &c->pages) && size_fits(t->size(1), "kv_heads", &c->kv_heads) &&
-           size_fits(head_dim, "head_dim", &c->head_dim) && size_fits(bytes / (20 * head_dim) * 16, "page_tokens", &c->page_tokens);
+           size_fits(head_dim, "head_dim", &c->head_dim) && size_fits(bytes / block_bytes(head_dim, eight) * 16, "page_tokens", &c->page_tokens);
 }
 
 bool cuda_stream_of(PyObject* o, c10::Device dev, c10::cuda::CUDAStream* out)
@@ -266,17 +276,19 @@ bool rows_of(PyObject* o, const char* what, const kvp_cache_shape& c, c10::Devic
     return true;
 }
 
-// cache_append(cache, k, v, slots, stream or None) -> error code
+// cache_append(cache, k, v, slots, stream or None) -> error code; cache8_append the same
+template <bool EIGHT>
 PyObject* cache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
-    if (!kvp_cache_append) return missing("kvp_cache_append");
+    const auto call = EIGHT ? &kvp_cache8_append : &kvp_cache_append;
+    if (!call) return missing(EIGHT ? "kvp_cache8_append" : "kvp_cache_append");
     if (nargs != 5) return value_error("cache_append takes 5 arguments");
     kvp_cache_shape c;
     const at::Tensor *k = tensor_of(args[1], "k"), *v, *slots, *cache;
     if (!k) return nullptr;
     if (k->dim() != 3) return value_error("k must be [tokens][kv_heads][head_dim]");
-    if (!cache_of(args[0], k->size(2), &c, &cache)) return nullptr;
+    if (!cache_of(args[0], k->size(2), EIGHT, &c, &cache)) return nullptr;
     const c10::Device dev = cache->device();
     if (!rows_of(args[1], "k", c, dev, &k) || !rows_of(args[2], "v", c, dev, &v) || !dense(args[3], "slots", at::kLong, dev, false, &slots)) return nullptr;
     uint32_t tokens;
@@ -290,23 +302,25 @@ PyObject* cache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     {
         Unlocked unlocked;
         c10::cuda::CUDAStreamGuard guard(st);
-        rc = kvp_cache_append(&c, cache->data_ptr(), (uint32_t)code, tokens, k->data_ptr(), k->stride(0), k->stride(1), v->data_ptr(),
-                              v->stride(0), v->stride(1), static_cast<const int64_t*>(slots->data_ptr()), st.stream());
+        rc = call(&c, cache->data_ptr(), (uint32_t)code, tokens, k->data_ptr(), k->stride(0), k->stride(1), v->data_ptr(),
+                  v->stride(0), v->stride(1), static_cast<const int64_t*>(slots->data_ptr()), st.stream());
     }
     return PyLong_FromLong(rc);
     END_HANDLE_TH_ERRORS
 }
 
-// cache_read(cache, slots, head_dim, a tensor of the dtype or its code, stream or None) -> (k, v), or an error code
+// cache_read(cache, slots, head_dim, a tensor of the dtype or its code, stream or None) -> (k, v), or an error code; cache8_read the same
+template <bool EIGHT>
 PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
-    if (!kvp_cache_read) return missing("kvp_cache_read");
+    const auto call = EIGHT ? &kvp_cache8_read : &kvp_cache_read;
+    if (!call) return missing(EIGHT ? "kvp_cache8_read" : "kvp_cache_read");
     if (nargs != 5) return value_error("cache_read takes 5 arguments");
     kvp_cache_shape c;
     const at::Tensor *cache, *slots;
     uint32_t head_dim, code, tokens;
-    if (!u32_of(args[2], "head_dim", &head_dim) || !u32_of(args[3], "dtype", &code) || !cache_of(args[0], head_dim, &c, &cache)) return nullptr;
+    if (!u32_of(args[2], "head_dim", &head_dim) || !u32_of(args[3], "dtype", &code) || !cache_of(args[0], head_dim, EIGHT, &c, &cache)) return nullptr;
     const c10::Device dev = cache->device();
     if (!dense(args[1], "slots", at::kLong, dev, false, &slots) || !size_fits(slots->numel(), "tokens", &tokens)) return nullptr;
     if (code > KVP_F32) return value_error("dtype must be bfloat16, float16 or float32");
@@ -321,7 +335,7 @@ PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         const int64_t shape[3] = {(int64_t)tokens, (int64_t)c.kv_heads, (int64_t)head_dim};
         k = make(shape, t, dev);
         v = make(shape, t, dev);
-        rc = kvp_cache_read(&c, cache->data_ptr(), code, tokens, static_cast<const int64_t*>(slots->data_ptr()), k.data_ptr(), v.data_ptr(), st.stream());
+        rc = call(&c, cache->data_ptr(), code, tokens, static_cast<const int64_t*>(slots->data_ptr()), k.data_ptr(), v.data_ptr(), st.stream());
     }
     if (rc) return PyLong_FromLong(rc);
     PyObject *a = THPVariable_Wrap(k), *b = THPVariable_Wrap(v);
@@ -332,19 +346,31 @@ PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 
 PyObject* k_out; PyObject* k_lse; PyObject* k_weights; PyObject* k_kept; PyObject* k_acc;
 
-// attend(q, cache, table, lens, unit_tokens or 0, scale or None, units or None, want_lse, weights: bool or a tensor to write to,
-// stream or None) -> dict, or an error code
-PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t nargs)
+// kvp_attend and kvp_attend8 under one name each; `slopes` is the second's
+int workspace_bytes(const kvp_attend_params* p, bool weights, bool units, uint64_t* bytes) { return kvp_attend_workspace(p, weights, units, bytes); }
+int workspace_bytes(const kvp_attend8_params* p, bool weights, bool units, uint64_t* bytes) { return kvp_attend8_workspace(p, weights, units, bytes); }
+template <typename... A>
+int run_attend(const kvp_attend_params* p, const void* q, const void* cache, const int32_t* table, const int32_t* lens, const uint32_t* units, const float*, A... rest)
 {
-    HANDLE_TH_ERRORS
-    if (!kvp_attend) return missing("kvp_attend");
-    if (nargs != 10) return value_error("attend takes 10 arguments");
-    const at::Tensor *q = tensor_of(args[0], "q"), *cache, *table, *lens, *units, *weights = nullptr;
+    return kvp_attend(p, q, cache, table, lens, units, rest...);
+}
+template <typename... A>
+int run_attend(const kvp_attend8_params* p, const void* q, const void* cache, const int32_t* table, const int32_t* lens, const uint32_t* units, const float* slopes, A... rest)
+{
+    return kvp_attend8(p, q, cache, table, lens, units, slopes, rest...);
+}
+
+// args: q, cache, table, lens, unit_tokens or 0, scale or None, units or None, want_lse, weights: bool or a tensor to write to,
+// stream or None. Fills what both kinds of `p` have.
+template <typename P>
+PyObject* attend_over(P& p, PyObject* const* args, PyObject* slopes_arg)
+{
+    constexpr bool EIGHT = std::is_same<P, kvp_attend8_params>::value;
+    const at::Tensor *q = tensor_of(args[0], "q"), *cache, *table, *lens, *units, *weights = nullptr, *slopes = nullptr;
     if (!q) return nullptr;
     if (q->dim() != 3 && q->dim() != 4) return value_error("q must be [batch][heads][head_dim] or [batch][queries][heads][head_dim]");
     const int64_t d = q->dim(), head_dim = q->size(d - 1), heads = q->size(d - 2), queries = d == 4 ? q->size(1) : 1;
-    kvp_attend_params p;
-    if (!cache_of(args[1], head_dim, &p.cache, &cache)) return nullptr;
+    if (!cache_of(args[1], head_dim, EIGHT, &p.cache, &cache)) return nullptr;
     const c10::Device dev = cache->device();
     if (q->device() != dev) return value_error("q: on another device");
     if (q->stride(d - 1) != 1) return value_error("q: dims must be contiguous");
@@ -371,8 +397,10 @@ PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         if (!dense(args[8], "weights", at::kFloat, dev, false, &weights)) return nullptr;
         want_weights = true;
     }
+    if (slopes_arg && !dense(slopes_arg, "slopes", at::kFloat, dev, true, &slopes)) return nullptr;
+    if (slopes && slopes->numel() != heads) return value_error("slopes must have one entry per head of q");
     uint64_t bytes = 0;
-    int rc = kvp_attend_workspace(&p, want_weights, units != nullptr, &bytes);
+    int rc = workspace_bytes(&p, want_weights, units != nullptr, &bytes);
     if (rc) return PyLong_FromLong(rc);
     const int64_t n = (int64_t)p.table_pages * p.cache.page_tokens / p.unit_tokens, all = (int64_t)p.batch * p.cache.kv_heads * n;
     if (weights && weights->numel() != all) return value_error("weights must be [batch][kv_heads][units]");
@@ -388,10 +416,10 @@ PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         const int64_t shape[3] = {(int64_t)p.batch, (int64_t)p.cache.kv_heads, n}, room[1] = {(int64_t)bytes};
         if (want_weights) made = weights ? *weights : make(shape, at::kFloat, dev);
         const at::Tensor workspace = make(room, at::kByte, dev);
-        rc = kvp_attend(&p, q->data_ptr(), cache->data_ptr(), static_cast<const int32_t*>(table->data_ptr()),
-                        static_cast<const int32_t*>(lens->data_ptr()), static_cast<const uint32_t*>(data_of(units)), out.data_ptr(),
-                        want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, want_weights ? static_cast<float*>(made.data_ptr()) : nullptr,
-                        workspace.data_ptr(), bytes, st.stream());
+        rc = run_attend(&p, q->data_ptr(), cache->data_ptr(), static_cast<const int32_t*>(table->data_ptr()),
+                        static_cast<const int32_t*>(lens->data_ptr()), static_cast<const uint32_t*>(data_of(units)), static_cast<const float*>(data_of(slopes)),
+                        out.data_ptr(), want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr,
+                        want_weights ? static_cast<float*>(made.data_ptr()) : nullptr, workspace.data_ptr(), bytes, st.stream());
     }
     if (rc) return PyLong_FromLong(rc);
     PyObject* r = PyDict_New();
@@ -399,6 +427,148 @@ PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         Py_XDECREF(r);
         return nullptr;
     }
+    return r;
+}
+
+// attend(q, cache, table, lens, unit_tokens or 0, scale or None, units or None, want_lse, weights: bool or a tensor to write to,
+// stream or None) -> dict, or an error code
+PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (!kvp_attend) return missing("kvp_attend");
+    if (nargs != 10) return value_error("attend takes 10 arguments");
+    kvp_attend_params p;
+    return attend_over(p, args, nullptr);
+    END_HANDLE_TH_ERRORS
+}
+
+// attend8(the same, cap, slopes or None, window, sink) -> dict, or an error code
+PyObject* attend8(PyObject*, PyObject* const* args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (!kvp_attend8) return missing("kvp_attend8");
+    if (nargs != 14) return value_error("attend8 takes 14 arguments");
+    kvp_attend8_params p;
+    const double cap = PyFloat_AsDouble(args[10]);
+    if (PyErr_Occurred() || !u32_of(args[12], "window", &p.window) || !u32_of(args[13], "sink", &p.sink)) return nullptr;
+    p.cap = (float)cap;
+    return attend_over(p, args, args[11]);
+    END_HANDLE_TH_ERRORS
+}
+
+// queries or keys of kvp_rope: [tokens][heads][head_dim], dims contiguous; None: no such rows
+bool turned_rows(PyObject* o, const char* what, int64_t tokens, int64_t head_dim, at::ScalarType dtype, c10::Device dev, const at::Tensor** out)
+{
+    *out = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t = tensor_of(o, what);
+    if (!t) return false;
+    if (t->dim() != 3 || t->size(0) != tokens || t->size(2) != head_dim) { PyErr_Format(PyExc_ValueError, "%s must be [tokens][heads][head_dim]", what); return false; }
+    if (t->device() != dev) { PyErr_Format(PyExc_ValueError, "%s: on another device", what); return false; }
+    if (t->scalar_type() != dtype) { PyErr_Format(PyExc_ValueError, "%s: of another dtype", what); return false; }
+    if (t->stride(2) != 1) { PyErr_Format(PyExc_ValueError, "%s: dims must be contiguous", what); return false; }
+    *out = t;
+    return true;
+}
+
+// rope(q, k or None, positions, frequencies, flags, scale, in place, stream or None) -> (q, k or None), or an error code
+PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (!kvp_rope) return missing("kvp_rope");
+    if (nargs != 8) return value_error("rope takes 8 arguments");
+    const at::Tensor *q = tensor_of(args[0], "q"), *k, *positions, *frequencies;
+    if (!q) return nullptr;
+    if (q->dim() != 3) return value_error("q must be [tokens][heads][head_dim]");
+    const c10::Device dev = q->device();
+    const int code = dtype_code(q->scalar_type());
+    if (code < 0) return value_error("q and k must both be bfloat16, float16 or float32");
+    kvp_rope_params p = {};
+    if (!turned_rows(args[0], "q", q->size(0), q->size(2), q->scalar_type(), dev, &q) || !turned_rows(args[1], "k", q->size(0), q->size(2), q->scalar_type(), dev, &k) ||
+        !dense(args[2], "positions", at::kInt, dev, false, &positions) || !dense(args[3], "frequencies", at::kDouble, dev, false, &frequencies) ||
+        !u32_of(args[4], "flags", &p.flags)) return nullptr;
+    if (positions->numel() != q->size(0)) return value_error("positions must have one entry per token");
+    const double scale = PyFloat_AsDouble(args[5]);
+    if (PyErr_Occurred()) return nullptr;
+    const int in_place = PyObject_IsTrue(args[6]);
+    if (in_place < 0) return nullptr;
+    if (!size_fits(q->size(0), "tokens", &p.tokens) || !size_fits(q->size(1), "heads", &p.heads) || !size_fits(k ? k->size(1) : 0, "kv_heads", &p.kv_heads) ||
+        !size_fits(q->size(2), "head_dim", &p.head_dim) || !size_fits(2 * frequencies->numel(), "frequencies", &p.rotary_dim)) return nullptr;
+    p.dtype = (uint32_t)code;
+    p.scale = (float)scale;
+    c10::cuda::CUDAStream st = c10::cuda::getDefaultCUDAStream(dev.index());
+    if (!cuda_stream_of(args[7], dev, &st)) return nullptr;
+    at::Tensor q_out, k_out;
+    int rc;
+    {
+        Unlocked unlocked;
+        c10::cuda::CUDAStreamGuard guard(st);
+        q_out = in_place ? *q : make(q->sizes(), q->scalar_type(), dev);
+        if (k) k_out = in_place ? *k : make(k->sizes(), k->scalar_type(), dev);
+        p.q_token_stride = q->stride(0); p.q_head_stride = q->stride(1);
+        p.q_out_token_stride = q_out.stride(0); p.q_out_head_stride = q_out.stride(1);
+        if (k) {
+            p.k_token_stride = k->stride(0); p.k_head_stride = k->stride(1);
+            p.k_out_token_stride = k_out.stride(0); p.k_out_head_stride = k_out.stride(1);
+        }
+        rc = kvp_rope(&p, q->data_ptr(), q_out.data_ptr(), k ? k->data_ptr() : nullptr, k ? k_out.data_ptr() : nullptr,
+                      static_cast<const int32_t*>(positions->data_ptr()), static_cast<const double*>(frequencies->data_ptr()), st.stream());
+    }
+    if (rc) return PyLong_FromLong(rc);
+    PyObject *a = THPVariable_Wrap(q_out), *b = k ? THPVariable_Wrap(k_out) : (Py_INCREF(Py_None), Py_None);
+    if (!a || !b) { Py_XDECREF(a); Py_XDECREF(b); return nullptr; }
+    return Py_BuildValue("(NN)", a, b);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* k_lens; PyObject* k_state; PyObject* k_slots; PyObject* k_positions; PyObject* k_rows; PyObject* k_starts; PyObject* k_page_starts; PyObject* k_granted;
+
+// block_tables(new_tokens, lens, table, ring, state, page_tokens, tokens, lens_out or None, state_out or None, stream or None) -> dict, or an error code
+PyObject* block_tables(PyObject*, PyObject* const* args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (!kvp_block_tables) return missing("kvp_block_tables");
+    if (nargs != 10) return value_error("block_tables takes 10 arguments");
+    const at::Tensor *table = tensor_of(args[2], "table"), *fresh, *lens, *ring, *state, *lens_given, *state_given;
+    if (!table) return nullptr;
+    const c10::Device dev = table->device();
+    kvp_tables_params p = {};
+    if (!dense(args[0], "new_tokens", at::kInt, dev, false, &fresh) || !dense(args[1], "lens", at::kInt, dev, false, &lens) ||
+        !dense(args[2], "table", at::kInt, dev, false, &table) || !dense(args[3], "ring", at::kInt, dev, false, &ring) ||
+        !dense(args[4], "state", at::kInt, dev, false, &state) || !u32_of(args[5], "page_tokens", &p.page_tokens) || !u32_of(args[6], "tokens", &p.tokens) ||
+        !dense(args[7], "lens_out", at::kInt, dev, true, &lens_given) || !dense(args[8], "state_out", at::kInt, dev, true, &state_given)) return nullptr;
+    if (table->dim() != 2) return value_error("table must be [batch][pages]");
+    const int64_t batch = table->size(0);
+    if (fresh->numel() != batch || lens->numel() != batch || (lens_given && lens_given->numel() != batch)) return value_error("new_tokens and lens must have one entry per row of the table");
+    if (state->numel() != 2 || (state_given && state_given->numel() != 2)) return value_error("state must be the ring's head and count");
+    if (!size_fits(batch, "batch", &p.batch) || !size_fits(table->size(1), "table", &p.table_pages) || !size_fits(ring->numel(), "ring", &p.pages)) return nullptr;
+    c10::cuda::CUDAStream st = c10::cuda::getDefaultCUDAStream(dev.index());
+    if (!cuda_stream_of(args[9], dev, &st)) return nullptr;
+    at::Tensor t[8];
+    int rc;
+    {
+        Unlocked unlocked;
+        c10::cuda::CUDAStreamGuard guard(st);
+        const int64_t n[1] = {batch}, more[1] = {batch + 1}, two[1] = {2}, many[1] = {(int64_t)p.tokens};
+        t[0] = lens_given ? *lens_given : make(n, at::kInt, dev);
+        t[1] = state_given ? *state_given : make(two, at::kInt, dev);
+        t[2] = make(many, at::kLong, dev);
+        t[3] = make(many, at::kInt, dev);
+        t[4] = make(many, at::kInt, dev);
+        t[5] = make(more, at::kInt, dev);
+        t[6] = make(more, at::kInt, dev);
+        t[7] = make(n, at::kInt, dev);
+        int32_t* at[8];
+        for (int i = 0; i < 8; ++i) at[i] = i == 2 ? nullptr : static_cast<int32_t*>(t[i].data_ptr());
+        rc = kvp_block_tables(&p, static_cast<const int32_t*>(fresh->data_ptr()), static_cast<const int32_t*>(lens->data_ptr()), at[0], static_cast<int32_t*>(table->data_ptr()),
+                              static_cast<int32_t*>(ring->data_ptr()), static_cast<const int32_t*>(state->data_ptr()), at[1], static_cast<int64_t*>(t[2].data_ptr()), at[3], at[4],
+                              at[5], at[6], at[7], st.stream());
+    }
+    if (rc) return PyLong_FromLong(rc);
+    PyObject* const keys[8] = {k_lens, k_state, k_slots, k_positions, k_rows, k_starts, k_page_starts, k_granted};
+    PyObject* r = PyDict_New();
+    for (int i = 0; r && i < 8; ++i)
+        if (!put(r, keys[i], t[i])) Py_CLEAR(r);
     return r;
     END_HANDLE_TH_ERRORS
 }
@@ -501,8 +671,13 @@ PyMethodDef methods[] = {
     {"eval", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(eval)), METH_FASTCALL, nullptr},
     {"eval_noalloc", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(eval_noalloc)), METH_FASTCALL, nullptr},
     {"eval_counts", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(eval_counts)), METH_FASTCALL, nullptr},
-    {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cache_append)), METH_FASTCALL, nullptr},
-    {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cache_read)), METH_FASTCALL, nullptr},
+    {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cache_append<false>)), METH_FASTCALL, nullptr},
+    {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cache_read<false>)), METH_FASTCALL, nullptr},
+    {"cache8_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cache_append<true>)), METH_FASTCALL, nullptr},
+    {"cache8_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cache_read<true>)), METH_FASTCALL, nullptr},
+    {"attend8", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attend8)), METH_FASTCALL, nullptr},
+    {"rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rope)), METH_FASTCALL, nullptr},
+    {"block_tables", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(block_tables)), METH_FASTCALL, nullptr},
     {"attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attend)), METH_FASTCALL, nullptr},
     {"trace_weights", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(trace_weights)), METH_FASTCALL, nullptr},
     {"evict", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(evict)), METH_FASTCALL, nullptr},
@@ -523,5 +698,13 @@ PyMODINIT_FUNC PyInit__kvp_torch()
     k_weights = PyUnicode_InternFromString("weights");
     k_kept = PyUnicode_InternFromString("kept");
     k_acc = PyUnicode_InternFromString("acc");
+    k_lens = PyUnicode_InternFromString("lens");
+    k_state = PyUnicode_InternFromString("state");
+    k_slots = PyUnicode_InternFromString("slots");
+    k_positions = PyUnicode_InternFromString("positions");
+    k_rows = PyUnicode_InternFromString("rows");
+    k_starts = PyUnicode_InternFromString("starts");
+    k_page_starts = PyUnicode_InternFromString("page_starts");
+    k_granted = PyUnicode_InternFromString("granted");
     return PyModule_Create(&module);
 }

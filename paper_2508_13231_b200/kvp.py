@@ -28,7 +28,8 @@ EXPORTS = [
     "kvp_policy_lookahead", "kvp_policy_reactive", "kvp_policy_page", "kvp_wr_grid", "kvp_wr_anneal", "kvp_set_births",
     "kvp_set_test_hooks", "kvp_anneal_exchange", "kvp_exchange_temps",
     "kvp_cache_page_bytes", "kvp_cache_append", "kvp_cache_read", "kvp_attend", "kvp_attend_workspace", "kvp_trace_weights",
-    "kvp_evict", "kvp_policy_accumulated",
+    "kvp_evict", "kvp_policy_accumulated", "kvp_cache8_page_bytes", "kvp_cache8_append", "kvp_cache8_read", "kvp_attend8", "kvp_attend8_workspace",
+    "kvp_rope", "kvp_rope_frequencies", "kvp_block_tables",
 ]
 
 
@@ -118,6 +119,10 @@ class EvictParams(C.Structure):
         "groups", "units_per_group", "steps", "budget", "sink", "recent", "decay_q", "flags")]
 
 
+class RopeScaling(C.Structure):
+    _fields_ = [("kind", C.c_uint32), ("reserved", C.c_uint32)] + [(n, C.c_double) for n in ("base", "factor", "original_tokens", "low", "high")]
+
+
 class TestHooks(C.Structure):
     _fields_ = [("warps_per_chain", C.c_uint32), ("drop_turn", C.c_uint32), ("split_queue_plus1", C.c_uint32),
                 ("resident", C.c_uint32), ("overlay", C.c_uint32), ("evict_form", C.c_uint32)]
@@ -139,6 +144,8 @@ def _lib():
         h.kvp_philox4x32_10.restype = None
         h.kvp_set_test_hooks.restype = None
         h.kvp_cache_page_bytes.restype = C.c_uint64
+        if hasattr(h, "kvp_cache8_page_bytes"):
+            h.kvp_cache8_page_bytes.restype = C.c_uint64
         _handle = h
     return _handle
 
@@ -278,6 +285,88 @@ def attend(q, cache, table, lens, unit_tokens=0, scale=None, units=None, want_ls
                            _cuda_stream(stream))
     if out.__class__ is int:
         _chk(out, "kvp_attend")
+    return out
+
+
+def cache8_page_bytes(head_dim, page_tokens):
+    """Bytes of a page of one kv-head of a cache held in 8 bits (2 * head_dim + 1 a token): a cache is a uint8 CUDA tensor
+    [pages][kv_heads][cache8_page_bytes], zeros to begin with. head_dim 64, 128 or 256; page_tokens a multiple of 16."""
+    n = int(_lib().kvp_cache8_page_bytes(C.c_uint32(head_dim), C.c_uint32(page_tokens)))
+    if not n:
+        raise ValueError("head_dim must be 64, 128 or 256 and page_tokens a multiple of 16")
+    return n
+
+
+def cache8_append(cache, k, v, slots, stream=None):
+    """kvp_cache8_append: keys and values [tokens][kv_heads][head_dim] into the cache at slots (int64 [tokens], page * page_tokens +
+    place; a slot outside the cache, such as -1, writes nothing). The tokens of a block of 16 stand within 16 tokens of the call."""
+    rc = _native().cache8_append(cache, k, v, slots, _cuda_stream(stream))
+    if rc:
+        _chk(rc, "kvp_cache8_append")
+
+
+def cache8_read(cache, slots, head_dim, dtype=torch.bfloat16, stream=None):
+    """kvp_cache8_read -> (k, v) [tokens][kv_heads][head_dim]: what the cache holds at slots (0 outside it)."""
+    if dtype not in _DTYPES:
+        raise ValueError("dtype must be bfloat16, float16 or float32")
+    out = _native().cache8_read(cache, slots, head_dim, _DTYPES[dtype], _cuda_stream(stream))
+    if out.__class__ is int:
+        _chk(out, "kvp_cache8_read")
+    return out
+
+
+def attend8(q, cache, table, lens, unit_tokens=0, scale=None, units=None, cap=0.0, slopes=None, window=0, sink=0, want_lse=False,
+            want_weights=False, weights=None, stream=None):
+    """kvp_attend8 -> dict(out, lse, weights): attend() over a cache held in 8 bits; the arguments it has too mean the same.
+
+    cap: scores x become cap * tanh(x / cap), 0 leaves them; slopes: float32 [heads], a score gets slope * (position of the token -
+    position of the query) added; window: a query sees the last `window` tokens up to its own (0: all) and the first `sink` of the sequence."""
+    out = _native().attend8(q, cache, table, lens, unit_tokens, scale, units, want_lse, bool(want_weights) if weights is None else weights,
+                            _cuda_stream(stream), cap, slopes, window, sink)
+    if out.__class__ is int:
+        _chk(out, "kvp_attend8")
+    return out
+
+
+_ROPE_SCALINGS = {None: 0, "linear": 1, "base": 2, "parts": 3, "ramp": 4}
+
+
+def rope_frequencies(rotary_dim, base=10000.0, scaling=None, factor=1.0, original_tokens=8192, low=1.0, high=None):
+    """kvp_rope_frequencies -> (frequencies float64 [rotary_dim / 2] on the CPU, scale): radians a token for rope(), and its scale.
+
+    scaling, for contexts `factor` times as long: "linear" (all divided), "base" (a larger base), "parts" (by the turns within
+    original_tokens: from `high` on as they are, up to `low` divided, linear between; high 4 unless given), "ramp" (the same borders, linear
+    in the dim, with a scale; high 32 unless given)."""
+    if scaling not in _ROPE_SCALINGS:
+        raise ValueError("scaling must be None, 'linear', 'base', 'parts' or 'ramp'")
+    if rotary_dim < 2 or rotary_dim % 2:
+        raise ValueError("rotary_dim must be even")
+    out = torch.empty(rotary_dim // 2, dtype=torch.float64)
+    scale = C.c_float()
+    p = RopeScaling(_ROPE_SCALINGS[scaling], 0, base, factor, original_tokens, low, (4.0 if scaling == "parts" else 32.0) if high is None else high)
+    _chk(_lib().kvp_rope_frequencies(C.byref(p), C.c_uint32(rotary_dim), C.c_void_p(out.data_ptr()), C.byref(scale)), "kvp_rope_frequencies")
+    return out, float(scale.value)
+
+
+def rope(q, k, positions, frequencies, interleaved=False, inverse=False, scale=1.0, in_place=False, stream=None):
+    """kvp_rope -> (q, k): rotary positions of queries and keys [tokens][heads][head_dim] (k may be None), any strides but the last;
+    positions int32 [tokens], frequencies float64 [rotary_dim / 2] on the device. inverse turns back: the gradient of the call
+    without it. in_place writes to q and k themselves, else the results are new."""
+    out = _native().rope(q, k, positions, frequencies, (1 if interleaved else 0) | (2 if inverse else 0), scale, in_place, _cuda_stream(stream))
+    if out.__class__ is int:
+        _chk(out, "kvp_rope")
+    return out
+
+
+def block_tables(new_tokens, lens, table, ring, state, page_tokens, tokens, lens_out=None, state_out=None, stream=None):
+    """kvp_block_tables -> dict(slots, positions, rows, starts, page_starts, granted, lens, state): pages for the new tokens of each request
+    (int32 [batch]: a prompt, 1, 0, or < 0 for a finished request), their slots (int64 [tokens], -1 behind the last) and positions.
+
+    table (int32 [batch][pages]) and ring (int32 [pages of the cache], the free ones from state[0] on, state[1] of them) are updated in
+    place; lens and state come back new, or in lens_out and state_out, which may be lens and state themselves."""
+    out = _native().block_tables(new_tokens, lens, table, ring, state, page_tokens, tokens, lens_out, state_out, _cuda_stream(stream))
+    if out.__class__ is int:
+        _chk(out, "kvp_block_tables")
     return out
 
 
