@@ -7,8 +7,8 @@
 // Products. Both run on the matrix unit (tcgen05.mma, e4m3) with the cache's bytes as they lie as the left operand: 128 tokens x D dims of keys, then
 // D dims x 128 tokens of values. The right operand has a column for each row, or rather for each term of a row: a number with more bits than
 // e4m3's four is split into x = t0 + t1 / 32 + t2 / 1024, each the nearest e4m3 to what the ones before leave. A bf16 query is two terms and an fp16 query three,
-// exactly (down to 2^-14 of the row's largest, below that to within 2^-22 of it); a weight is three terms, 12 bits (2^-12 of itself), down to 2^-26 of
-// the largest. Products of e4m3 numbers are exact and the unit keeps 25 bits of their sums; terms have sums of their own, joined in fp32.
+// exactly (down to 2^-14 of the row's largest, below that to within 2^-22 of it); a weight is rounded to fp16 (2^-11 of itself)
+// and that is three terms, exactly, down to 2^-26 of the largest. Products of e4m3 numbers are exact and the unit keeps 25 bits of their sums; terms have sums of their own, joined in fp32.
 // No byte of the cache goes through a register, and a chunk of a prompt runs at the matrix unit's rate for 16 bits.
 //
 // exp runs in fp32 against a running maximum that moves only when a score passes it by 2^2 (kSlack). A weight times 2^6 and the scale of its block's values over the
@@ -17,7 +17,7 @@
 // Split over CTAs as in kvp_attend: one line of all tiles (16 tokens), cut into equal parts on the device; the join is its join.
 //
 // A CTA: warp 0 sends for tiles (bulk copies; a stage is eight tiles, keys and values), one thread of warp 1 issues the products with keys, one of
-// warp 2 those with values, four (or eight) warps turn scores into weights, a token a thread. Every hand-over is a barrier in
+// warp 2 those with values, teams of four warps turn scores into weights, a token a thread. Every hand-over is a barrier in
 // shared memory whose wait ends after two seconds; a CTA that gave up writes NaN.
 #include <type_traits>
 
@@ -31,9 +31,9 @@ namespace {
 
 constexpr uint32_t kFixed8 = 48;              // what a CTA spends on a segment whatever its length, in tiles
 constexpr uint32_t kGroup = 8;                // tiles of a stage
+constexpr uint32_t kOthers = 3;               // warps that are in no team
 constexpr uint32_t kListCap8 = 1024;          // units of a bitmap row that are listed at a time: 32 words
 constexpr float kSlack = 2.0f;
-constexpr float kLift = 6.0f;                 // weights are split after a multiplication by 2^kLift
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Attend8K : LineK<kFixed8> {
@@ -105,58 +105,82 @@ __global__ void __launch_bounds__(kThreads) count8_kernel(const Attend8K p)
     }
 }
 
-// D: dims of a head; ROWS: rows of a segment, 8, 16, 32 or 64, worked on by teams of four warps for 16 rows at most
+// D: dims of a head; ROWS: rows of a segment, 8, 16, 32 or 64. A team is four warps that turn the scores of a group (eight tiles, 128 tokens) into
+// weights, a token a thread, for 16 rows at most. Teams share a group's rows (kRowTeams) and take groups in turn (kTurns): one group takes a warp 2000 cycles, most of them
+// latency, so two groups under way a CTA and two CTAs an SM where they fit. Each turn has scores, weights and sums of its own.
 template <int D_, bool HALF_, uint32_t ROWS_>
 struct Shape8 {
     static constexpr int D = D_;
     static constexpr bool HALF = HALF_;
     static constexpr uint32_t ROWS = ROWS_;
     using L = Tile8<D>;
-    static constexpr uint32_t kTeams = ROWS > 16 ? ROWS / 16 : 1;      // of four warps
-    static constexpr uint32_t kRowsEach = ROWS / kTeams;
-    static constexpr uint32_t kBlock = 128 + 128 * kTeams;
     static constexpr uint32_t kQTerms = HALF ? 3 : 2;
     static constexpr uint32_t kQCols = (kQTerms * ROWS + 15) / 16 * 16;
     static constexpr uint32_t kPCols = (3 * ROWS + 15) / 16 * 16;
     static constexpr uint32_t kHalves = D == 256 ? 2 : 1;              // 128 dims of values a product
     static constexpr uint32_t kSumCols = kHalves * kPCols;
-    static constexpr uint32_t kScoreBufs = 2 * kQCols + kSumCols <= 512 ? 2 : 1;
-    static constexpr uint32_t kColsUsed = kScoreBufs * kQCols + kSumCols;
+    static constexpr uint32_t kRowTeams = ROWS > 16 ? ROWS / 16 : 1;
+    static constexpr uint32_t kTurns = ROWS <= 32 && 2 * (kQCols + kSumCols) <= 512 ? 2 : 1;
+    static constexpr uint32_t kTeams = kRowTeams * kTurns;
+    static constexpr uint32_t kRowsEach = ROWS / kRowTeams;
+    static constexpr uint32_t kBlock = 32 * kOthers + 128 * kTeams;
+    static constexpr uint32_t kScoreBufs = kTurns == 2 || 2 * kQCols + kSumCols <= 512 ? 2 : 1;
+    static constexpr uint32_t kColsUsed = kScoreBufs * kQCols + kTurns * kSumCols;
     static constexpr uint32_t kCols = kColsUsed <= 64 ? 64 : kColsUsed <= 128 ? 128 : kColsUsed <= 256 ? 256 : 512;
-    static constexpr uint32_t kStage = kGroup * (L::kKeyBytes + L::kValueBytes);
+    static constexpr uint32_t kCtas = D <= 128 && ROWS <= 16 ? 2 : 1;  // of an SM
+    // shared memory: a stage of keys is free when the scores are there, one of values when the sums are
+    static constexpr uint32_t kKeyStage = kGroup * L::kKeyBytes, kValueStage = kGroup * L::kValueBytes;
     static constexpr uint32_t kQBytes = kQCols * D;
     static constexpr uint32_t kPBytes = kPCols * 128;
-    static constexpr uint32_t kPad = 2048;                             // D == 64: rows 64 .. 127 of the values' operand are what lies behind
-    static constexpr uint32_t kCtas = D <= 128 && ROWS <= 16 ? 2 : 1;  // of an SM
-    static constexpr uint32_t kRoom = kCtas == 2 ? 115712 - 2944 : 232448 - 4608;            // less what is declared statically
-    static constexpr uint32_t kPBufs = ROWS == 16 && D == 128 ? 1 : 2;
-    static constexpr uint32_t kOther = kQBytes + kPBufs * kPBytes + (D == 64 ? kPad : 0);
-    static constexpr uint32_t kStagesFit = (kRoom - kOther) / kStage;
-    static constexpr uint32_t kStages = kStagesFit < 8 ? kStagesFit : 8;
-    static constexpr uint32_t kSmem = kStages * kStage + kOther;
-    static_assert(kStages >= 2 && kColsUsed <= 512 && kQCols <= 256 && kPCols <= 256, "does not fit");
+    static constexpr uint32_t kPad = D == 64 ? 2048 : 0;               // rows 64 .. 127 of the values' operand are what lies behind
+    static constexpr uint32_t kStatic = kCtas == 2 ? 4096 : 6144;      // declared statically, at most
+    static constexpr uint32_t kRoom = (kCtas == 2 ? 115712 : 232448) - kStatic - kQBytes - 2 * kPBytes - kPad;
+    static constexpr uint32_t kKeyStages = 2;
+    static constexpr uint32_t kValueFit = (kRoom - kKeyStages * kKeyStage) / kValueStage;
+    static constexpr uint32_t kValueStages = kValueFit < 6 ? kValueFit : 6;
+    static constexpr uint32_t kSmem = kKeyStages * kKeyStage + kValueStages * kValueStage + kQBytes + 2 * kPBytes + kPad;
+    static_assert(kValueStages >= 2 && kColsUsed <= 512 && kQCols <= 256 && kPCols <= 256, "does not fit");
 };
 
 template <class S>
 struct Smem8 {
-    uint64_t full[S::kStages], empty[S::kStages];      // a stage has come; its products are done
+    uint64_t keys[S::kKeyStages], keys_free[S::kKeyStages];            // a stage has come; its products are done
+    uint64_t values[S::kValueStages], values_free[S::kValueStages];
     uint64_t scored[2], taken[2];                      // scores are in tensor memory; they are in registers
     uint64_t weighed[2], summed[2];                    // weights are in shared memory; the products with values are done
     uint64_t query;                                    // a segment's queries are in shared memory
     uint32_t tensor, gave_up;
     LineSmem line;
-    uint32_t tile[S::kStages][kGroup];                 // numbers of a stage's tiles; ~0: not there
-    float factor[S::ROWS], slope[S::ROWS];             // per row: what scores are multiplied by, and its bias a token
-    int32_t see[S::ROWS];                              // tokens before this one
-    float top[S::kTeams][4][S::kRowsEach];             // of the four warps of a team
-    float most[S::kTeams][4];
+    uint32_t tile[S::kValueStages][kGroup];            // numbers of a stage's tiles; ~0: not there
+    alignas(16) float factor[S::ROWS];                 // per row: what scores are multiplied by,
+    float slope[S::ROWS];                              // its bias a token,
+    int32_t see[S::ROWS];                              // the tokens that it sees are before this one
+    alignas(16) float top[S::kTeams][S::kRowsEach];    // what scores are taken less: the running maximum, 0 before a row has seen a token
+    alignas(16) float by[S::kTeams][S::kRowsEach];     // what sums are multiplied by when it moves; at the end of a segment see `last`
+    float peak[S::kTeams][4][S::kRowsEach];            // of each warp: how far its scores pass it; at the end its sum of weights
+    float scale[S::kTeams][4];                         // of each warp: the largest scale of its values
+    float2 last[S::kTeams][S::kRowsEach];              // of each turn's row: its factor, and the reciprocal of the row's sum
     uint16_t list[kListCap8];                          // units of 32 words of a bitmap's row
+};
+
+// Number of a ring's place and the parity of its turn.
+template <uint32_t N>
+struct Ring {
+    uint32_t at = 0, parity = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++at == N) {
+            at = 0;
+            parity ^= 1u;
+        }
+    }
 };
 
 // The segments of this CTA's part, one after the other; each warp goes through them by itself.
 struct Walk {
     uint32_t todo, per, entries, entry, inner, at_place, count;
-    uint32_t seg, bh, rt, b, h, len, off, take;
+    uint32_t seg, bh, rt, b, h, len, off, take, tiles;
+    template <uint32_t ROWS>
     __device__ __forceinline__ bool next(const Attend8K& p)
     {
         while (todo) {
@@ -178,6 +202,14 @@ struct Walk {
             b = p.heads.of(bh);
             h = bh - b * p.heads.d;
             len = length_of(p, b);
+            tiles = take;                                          // of these, those that some row sees
+            if (!p.units && !p.sub && p.queries > 1) {
+                const int32_t see = (int32_t)len - (int32_t)p.queries + 1 + (int32_t)p.group.of(min(rt * ROWS + ROWS, p.rows) - 1);
+                const Visible v = visible_tiles(p, len);
+                uint32_t last = see > 0 ? tiles_of((uint32_t)see) : 0;
+                if (last > v.head) last = max(v.head, last - min(last, v.skip));
+                tiles = last > off ? min(take, last - off) : 0u;
+            }
             return true;
         }
         return false;
@@ -206,7 +238,17 @@ __device__ __forceinline__ void floats_of8(uint32_t x, float* to)
     }
 }
 
-// the next term of two numbers, and what it leaves, 32 times as large
+// the next term of two fp16 numbers, and what it leaves, 32 times as large; both are exact
+__device__ __forceinline__ uint32_t next_term(uint32_t& h)
+{
+    uint16_t t;
+    uint32_t f;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(t) : "r"(h));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f) : "h"(t));
+    h = bits_of(__hfma2(half2_of(f), __float2half2_rn(-32.0f), __hmul2(half2_of(h), __float2half2_rn(32.0f))));
+    return t;
+}
+// the same of two fp32 numbers
 __device__ __forceinline__ uint32_t next_term(float& a, float& b)
 {
     const uint32_t t = e4m3_pair(a, b);
@@ -216,6 +258,17 @@ __device__ __forceinline__ uint32_t next_term(float& a, float& b)
     return t;
 }
 
+// two fp32 numbers at a time
+struct F2 {
+    uint64_t v;
+    __device__ __forceinline__ F2() {}
+    __device__ __forceinline__ F2(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi)); }
+    __device__ __forceinline__ void get(float& lo, float& hi) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+};
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+
 __device__ __forceinline__ bool team_any(bool x, uint32_t team)    // over the four warps of a team
 {
     uint32_t r;
@@ -223,18 +276,14 @@ __device__ __forceinline__ bool team_any(bool x, uint32_t team)    // over the f
     return r != 0;
 }
 __device__ __forceinline__ void team_sync(uint32_t team) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(team + 1) : "memory"); }
-__device__ __forceinline__ float warp_sum(float x)
-{
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
-    return x;
-}
 __device__ __forceinline__ float warp_max(float x)
 {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
-    return x;
+    float y;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(y) : "f"(x));
+    return y;
 }
+template <uint32_t TEAMS>
+__device__ __forceinline__ void teams_sync() { asm volatile("barrier.cta.sync 15, %0;" ::"n"(128 * TEAMS) : "memory"); }
 
 // sums over 2^LOG neighbouring lanes of R numbers each; lane l of them is left with those of rows from(l) on, R >> LOG (one at least) of them
 template <int R, int LOG>
@@ -269,187 +318,216 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
     constexpr uint32_t ROWS = S::ROWS, R = S::kRowsEach;
     extern __shared__ __align__(128) uint8_t room[];
     __shared__ Smem8<S> sm;
-    static_assert(S::kSmem + sizeof(Smem8<S>) <= (S::kCtas == 2 ? 115712 : 232448), "does not fit");
+    static_assert(sizeof(Smem8<S>) <= S::kStatic, "does not fit");
     let_next_start();
     const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
-    wait_for_previous();
-    Walk walk;
-    {
-        uint32_t entry = 0;
-        const Line line = find_in_line<S::kBlock>(p, blockIdx.x, entry, sm.line);
-        const uint64_t begin = (uint64_t)line.chunk * blockIdx.x;
-        if (begin >= line.total) return;
-        walk.todo = min(line.chunk, line.total - (uint32_t)begin);     // places
-        walk.per = line_per(p);
-        walk.entries = line_entries(p);
-        walk.entry = entry;
-        walk.count = line.count;
-        walk.inner = ((uint32_t)begin - line.before) / (line.count + kFixed8);
-        walk.at_place = ((uint32_t)begin - line.before) - walk.inner * (line.count + kFixed8);
-    }
-    uint8_t* const queries = room + S::kStages * S::kStage;
-    uint8_t* const weights = queries + S::kQBytes;
-    auto keys_of = [&](uint32_t st) { return room + st * S::kStage; };
-    auto values_of = [&](uint32_t st) { return room + st * S::kStage + kGroup * L::kKeyBytes; };
     const auto bar = [](uint64_t& b) { return smem_at(&b); };
+    if (warp == 1) tensor_alloc<S::kCols>(smem_at(&sm.tensor));
     if (tid == 0) {
-        for (uint32_t i = 0; i < S::kStages; ++i) {
-            barrier_init(bar(sm.full[i]), 1);
-            barrier_init(bar(sm.empty[i]), 1);
+        for (uint32_t i = 0; i < S::kKeyStages; ++i) {
+            barrier_init(bar(sm.keys[i]), 1);
+            barrier_init(bar(sm.keys_free[i]), 1);
+        }
+        for (uint32_t i = 0; i < S::kValueStages; ++i) {
+            barrier_init(bar(sm.values[i]), 1);
+            barrier_init(bar(sm.values_free[i]), 1);
         }
         for (uint32_t i = 0; i < 2; ++i) {
             barrier_init(bar(sm.scored[i]), 1);
-            barrier_init(bar(sm.taken[i]), 4 * S::kTeams);
-            barrier_init(bar(sm.weighed[i]), 4 * S::kTeams);
+            barrier_init(bar(sm.taken[i]), 4 * S::kRowTeams);
+            barrier_init(bar(sm.weighed[i]), 4 * S::kRowTeams);
             barrier_init(bar(sm.summed[i]), 1);
         }
         barrier_init(bar(sm.query), 4 * S::kTeams);
         sm.gave_up = 0;
         show_to_async();
     }
-    if (warp == 1) tensor_alloc<S::kCols>(smem_at(&sm.tensor));
+    wait_for_previous();
+    Walk walk;
+    {
+        uint32_t entry = 0;
+        const Line line = find_in_line<S::kBlock>(p, blockIdx.x, entry, sm.line);
+        const uint64_t begin = (uint64_t)line.chunk * blockIdx.x;
+        walk.todo = begin < line.total ? min(line.chunk, line.total - (uint32_t)begin) : 0u;       // places
+        walk.per = line_per(p);
+        walk.entries = line_entries(p);
+        walk.entry = entry;
+        walk.count = line.count;
+        if (walk.todo) {
+            walk.inner = ((uint32_t)begin - line.before) / (line.count + kFixed8);
+            walk.at_place = ((uint32_t)begin - line.before) - walk.inner * (line.count + kFixed8);
+        }
+    }
+    uint8_t* const value_room = room + S::kKeyStages * S::kKeyStage;
+    uint8_t* const queries = value_room + S::kValueStages * S::kValueStage;
+    uint8_t* const weights = queries + S::kQBytes;
     tensor_before_sync();
     __syncthreads();
     tensor_after_sync();
     const uint32_t scores_at = sm.tensor, sums_at = sm.tensor + S::kScoreBufs * S::kQCols;
     volatile uint32_t* const gave_up = &sm.gave_up;
-    uint32_t it = 0;                                                   // groups so far, over all segments
 
-    if (warp == 0) {
-        // ---- sends for tiles ----
-        bool ok = true;
-        while (ok && walk.next(p)) {
-            const int32_t* table = p.table + (uint64_t)walk.b * p.table_pages;
-            const Visible seen = p.units ? Visible{0, 0} : visible_tiles(p, walk.len);
-            // a bitmap's row: `chunk` of 32 words is listed, before it stand `base` tiles of the row, in it `here`
-            const uint32_t units = units_of(p, walk.len), k = p.unit > kTileTokens ? p.unit / kTileTokens : 1, fold = p.unit < kTileTokens ? kTileTokens / p.unit : 1;
-            uint32_t chunk = 0, base = 0, here = 0;
-            const auto list_chunk = [&]() {
-                const uint32_t w = 32 * chunk + lane;
-                uint32_t bits = 32u * w < units ? unit_word(p, walk.bh, w, units) : 0u;
-                const uint32_t mine = __popc(bits), upto = sum_upto(mine, lane);
-                __syncwarp();
-                for (uint32_t at = upto - mine; bits; bits &= bits - 1u, ++at) sm.list[at] = (uint16_t)(32u * lane + __ffs(bits) - 1u);
-                __syncwarp();
-                here = p.marks[(uint64_t)walk.bh * p.mark_row + chunk];
-            };
-            if (p.units) {
-                // the chunk with tile `off`
-                const uint32_t chunks = (units + 1023) / 1024;
-                for (uint32_t c0 = 0;; c0 += 32) {
-                    const uint32_t n = c0 + lane < chunks ? p.marks[(uint64_t)walk.bh * p.mark_row + c0 + lane] : 0u, upto = sum_upto(n, lane);
-                    const uint32_t found = __ballot_sync(0xFFFFFFFFu, base + upto > walk.off);
-                    if (found || c0 + 32 >= chunks) {
-                        const int l = found ? __ffs(found) - 1 : 31;
-                        chunk = c0 + l;
-                        base += __shfl_sync(0xFFFFFFFFu, upto - n, l);
-                        break;
-                    }
-                    base += __shfl_sync(0xFFFFFFFFu, upto, 31);
-                }
-                list_chunk();
-            }
-            for (uint32_t g = 0; g < walk.take; g += kGroup, ++it) {
-                const uint32_t st = it % S::kStages;
-                // which tiles, and where they lie; lanes 8 .. 15 do as 0 .. 7, for the values
-                const uint32_t i = walk.off + g + lane % kGroup;
-                const bool mine = lane < 2 * kGroup && g + lane % kGroup < walk.take;
-                uint32_t tile = 0;
-                if (p.units) {
-                    bool left = mine;
-                    while (true) {
-                        if (left && i < base + here) {
-                            tile = (1024 * chunk + sm.list[(i - base) / k]) / fold * k + (i - base) % k;
-                            left = false;
-                        }
-                        if (!__any_sync(0xFFFFFFFFu, left)) break;
-                        base += here;
-                        ++chunk;
-                        list_chunk();
-                    }
-                } else {
-                    tile = i < seen.head ? i : i + seen.skip;
-                }
-                const uint8_t* from = nullptr;
-                if (mine) {
-                    const uint32_t page = p.page_tiles.of(tile), pg = (uint32_t)__ldg(table + page);
-                    if (pg < p.pages) from = p.cache + (((uint64_t)pg * p.heads.d + walk.h) * p.page_tiles.d + (tile - page * p.page_tiles.d)) * L::kBytes;
-                }
-                if (it >= S::kStages) ok = __all_sync(0xFFFFFFFFu, barrier_wait(bar(sm.empty[st]), (it / S::kStages - 1) & 1, gave_up));
-                if (!ok) break;
-                const uint32_t many = __popc(__ballot_sync(0xFFFFFFFFu, from != nullptr) & 0xFFu);
-                if (lane < kGroup) sm.tile[st][lane] = from ? tile : ~0u;
-                __syncwarp();
-                if (lane == 0) barrier_arrive_expect(bar(sm.full[st]), many * (L::kKeyBytes + L::kValueBytes));
-                __syncwarp();
-                if (from) {
-                    if (lane < kGroup) copy_bulk(smem_at(keys_of(st)) + lane * L::kKeyBytes, from, L::kKeyBytes, bar(sm.full[st]));
-                    else copy_bulk(smem_at(values_of(st)) + (lane - kGroup) * L::kValueBytes, from + L::kValues, L::kValueBytes, bar(sm.full[st]));
-                }
-            }
-        }
-        // copies under way end before the CTA does
-        for (uint32_t j = it > S::kStages ? it - S::kStages : 0; !ok && j < it; ++j)
-            for (uint32_t tries = 0; tries < 1u << 16 && !barrier_try(bar(sm.full[j % S::kStages]), (j / S::kStages) & 1); ++tries) {}
-    } else if (warp == 1) {
-        // ---- products with keys ----
-        if (lane == 0) {
-            uint32_t segment = 0;
+    if (warp < kOthers) {
+        if (warp == 0) {
+            // ---- sends for tiles ----
             bool ok = true;
-            for (; ok && walk.next(p); ++segment) {
-                ok = barrier_wait(bar(sm.query), segment & 1, gave_up);
-                for (uint32_t g = 0; ok && g < walk.take; g += kGroup, ++it) {
-                    const uint32_t st = it % S::kStages, sb = it % S::kScoreBufs;
-                    ok = barrier_wait(bar(sm.full[st]), (it / S::kStages) & 1, gave_up) &&
-                         (it < S::kScoreBufs || barrier_wait(bar(sm.taken[sb]), (it / S::kScoreBufs - 1) & 1, gave_up));
+            uint32_t it = 0;
+            Ring<S::kKeyStages> ks;
+            Ring<S::kValueStages> vs;
+            while (ok && walk.next<ROWS>(p)) {
+                const int32_t* table = p.table + (uint64_t)walk.b * p.table_pages;
+                const Visible seen = p.units ? Visible{0, 0} : visible_tiles(p, walk.len);
+                // a bitmap's row: `chunk` of 32 words is listed, before it stand `base` tiles of the row, in it `here`
+                const uint32_t units = units_of(p, walk.len), k = p.unit > kTileTokens ? p.unit / kTileTokens : 1, fold = p.unit < kTileTokens ? kTileTokens / p.unit : 1;
+                uint32_t chunk = 0, base = 0, here = 0;
+                const auto list_chunk = [&]() {
+                    const uint32_t w = 32 * chunk + lane;
+                    uint32_t bits = 32u * w < units ? unit_word(p, walk.bh, w, units) : 0u;
+                    const uint32_t mine = __popc(bits), upto = sum_upto(mine, lane);
+                    __syncwarp();
+                    for (uint32_t at = upto - mine; bits; bits &= bits - 1u, ++at) sm.list[at] = (uint16_t)(32u * lane + __ffs(bits) - 1u);
+                    __syncwarp();
+                    here = p.marks[(uint64_t)walk.bh * p.mark_row + chunk];
+                };
+                if (p.units && walk.tiles) {
+                    // the chunk with the last tile of this part
+                    const uint32_t chunks = (units + 1023) / 1024;
+                    for (uint32_t c0 = 0;; c0 += 32) {
+                        const uint32_t n = c0 + lane < chunks ? p.marks[(uint64_t)walk.bh * p.mark_row + c0 + lane] : 0u, upto = sum_upto(n, lane);
+                        const uint32_t found = __ballot_sync(0xFFFFFFFFu, base + upto > walk.off + walk.tiles - 1);
+                        if (found || c0 + 32 >= chunks) {
+                            const int l = found ? __ffs(found) - 1 : 31;
+                            chunk = c0 + l;
+                            base += __shfl_sync(0xFFFFFFFFu, upto - n, l);
+                            break;
+                        }
+                        base += __shfl_sync(0xFFFFFFFFu, upto, 31);
+                    }
+                    list_chunk();
+                }
+                for (uint32_t g = 0; g < walk.tiles; g += kGroup, ++it) {
+                    // which tiles, and where they lie; lanes 8 .. 15 do as 0 .. 7, for the values. The last ones come first: a bias by distance favours them, and
+                    // the maximum then seldom moves.
+                    const uint32_t n = g + lane % kGroup;
+                    const bool mine = lane < 2 * kGroup && n < walk.tiles;
+                    const uint32_t i = walk.off + walk.tiles - 1 - n;
+                    uint32_t tile = 0;
+                    if (p.units) {
+                        bool left = mine;
+                        while (true) {
+                            if (left && i >= base) {
+                                tile = (1024 * chunk + sm.list[(i - base) / k]) / fold * k + (i - base) % k;
+                                left = false;
+                            }
+                            if (!__any_sync(0xFFFFFFFFu, left)) break;
+                            --chunk;
+                            list_chunk();
+                            base -= here;
+                        }
+                    } else {
+                        tile = i < seen.head ? i : i + seen.skip;
+                    }
+                    const uint8_t* from = nullptr;
+                    if (mine) {
+                        const uint32_t page = p.page_tiles.of(tile), pg = (uint32_t)__ldg(table + page);
+                        if (pg < p.pages) from = p.cache + (((uint64_t)pg * p.heads.d + walk.h) * p.page_tiles.d + (tile - page * p.page_tiles.d)) * L::kBytes;
+                    }
+                    const uint32_t many = __popc(__ballot_sync(0xFFFFFFFFu, from != nullptr) & 0xFFu);
+                    if (it >= S::kKeyStages) ok = __all_sync(0xFFFFFFFFu, barrier_wait(bar(sm.keys_free[ks.at]), ks.parity ^ 1u, gave_up));
+                    if (!ok) break;
+                    if (lane == 0) barrier_arrive_expect(bar(sm.keys[ks.at]), many * L::kKeyBytes);
+                    __syncwarp();
+                    if (from && lane < kGroup) copy_bulk(smem_at(room + ks.at * S::kKeyStage) + lane * L::kKeyBytes, from, L::kKeyBytes, bar(sm.keys[ks.at]));
+                    ks.next();
+                    if (it >= S::kValueStages) ok = __all_sync(0xFFFFFFFFu, barrier_wait(bar(sm.values_free[vs.at]), vs.parity ^ 1u, gave_up));
+                    if (!ok) break;
+                    if (lane < kGroup) sm.tile[vs.at][lane] = from ? tile : ~0u;
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive_expect(bar(sm.values[vs.at]), many * L::kValueBytes);
+                    __syncwarp();
+                    if (from && lane >= kGroup)
+                        copy_bulk(smem_at(value_room + vs.at * S::kValueStage) + (lane - kGroup) * L::kValueBytes, from + L::kValues, L::kValueBytes, bar(sm.values[vs.at]));
+                    vs.next();
+                }
+            }
+            // copies under way end before the CTA does: the phase that a stage is in, or the one before, ends
+            if (!ok) {
+                for (uint32_t i = 0; i < S::kKeyStages; ++i, ks.next())
+                    for (uint32_t tries = 0; tries < 1u << 14 && !barrier_try(bar(sm.keys[ks.at]), ks.parity ^ 1u); ++tries) {}
+                for (uint32_t i = 0; i < S::kValueStages; ++i, vs.next())
+                    for (uint32_t tries = 0; tries < 1u << 14 && !barrier_try(bar(sm.values[vs.at]), vs.parity ^ 1u); ++tries) {}
+            }
+        } else if (warp == 1 && lane == 0) {
+            // ---- products with keys ----
+            uint32_t segment = 0, it = 0;
+            bool ok = true;
+            Ring<S::kKeyStages> ks;
+            Ring<S::kScoreBufs> sb;
+            for (; ok && walk.next<ROWS>(p); ++segment) {
+                ok = barrier_wait(bar(sm.query), segment & 1u, gave_up);
+                for (uint32_t g = 0; ok && g < walk.tiles; g += kGroup, ++it) {
+                    ok = barrier_wait(bar(sm.keys[ks.at]), ks.parity, gave_up) && (it < S::kScoreBufs || barrier_wait(bar(sm.taken[sb.at]), sb.parity ^ 1u, gave_up));
                     if (!ok) break;
                     tensor_after_sync();
-                    const uint32_t a = smem_at(keys_of(st)), b = smem_at(queries);
+                    const uint32_t a = smem_at(room + ks.at * S::kKeyStage), b = smem_at(queries);
 #pragma unroll
                     for (uint32_t k = 0; k < D / 32; ++k)
-                        multiply_e4m3(scores_at + sb * S::kQCols, operand(a + 256 * k, 128, 8 * D), operand(b + 256 * k, 128, 8 * D), shape_e4m3(S::kQCols), k > 0);
-                    products_arrive(bar(sm.scored[sb]));
+                        multiply_e4m3(scores_at + sb.at * S::kQCols, operand(a + 256 * k, 128, 8 * D), operand(b + 256 * k, 128, 8 * D), shape_e4m3(S::kQCols), k > 0);
+                    products_arrive(bar(sm.scored[sb.at]));
+                    products_arrive(bar(sm.keys_free[ks.at]));
+                    ks.next();
+                    sb.next();
                 }
             }
-        }
-    } else if (warp == 2) {
-        // ---- products with values ----
-        if (lane == 0) {
+        } else if (warp == 2 && lane == 0) {
+            // ---- products with values ----
             bool ok = true;
-            while (ok && walk.next(p)) {
-                for (uint32_t g = 0; g < walk.take; g += kGroup, ++it) {
-                    const uint32_t st = it % S::kStages, pb = it % S::kPBufs, pairs = (min(walk.take - g, kGroup) + 1) / 2;
-                    ok = barrier_wait(bar(sm.full[st]), (it / S::kStages) & 1, gave_up) && barrier_wait(bar(sm.weighed[pb]), (it / S::kPBufs) & 1, gave_up);
+            Ring<S::kValueStages> vs;
+            Ring<2> pb;
+            while (ok && walk.next<ROWS>(p)) {
+                for (uint32_t g = 0; g < walk.tiles; g += kGroup) {
+                    const uint32_t pairs = (min(walk.tiles - g, kGroup) + 1) / 2;
+                    ok = barrier_wait(bar(sm.values[vs.at]), vs.parity, gave_up) && barrier_wait(bar(sm.weighed[pb.at]), pb.parity, gave_up);
                     if (!ok) break;
                     tensor_after_sync();
-                    const uint32_t a = smem_at(values_of(st)), b = smem_at(weights + pb * S::kPBytes);
+                    const uint32_t a = smem_at(value_room + vs.at * S::kValueStage), b = smem_at(weights + pb.at * S::kPBytes);
+                    const uint32_t sums = sums_at + (S::kTurns == 2 ? pb.at * S::kSumCols : 0u);
                     for (uint32_t k = 0; k < pairs; ++k)
 #pragma unroll
                         for (uint32_t half = 0; half < S::kHalves; ++half)
-                            multiply_e4m3(sums_at + half * S::kPCols, operand(a + half * 2048 + 2 * k * L::kValueBytes, L::kValueBytes, 128), operand(b + 256 * k, 128, 1024),
-                                          shape_e4m3(S::kPCols), g + k > 0);
-                    products_arrive(bar(sm.empty[st]));
-                    products_arrive(bar(sm.summed[pb]));
+                            multiply_e4m3(sums + half * S::kPCols, operand(a + half * 2048 + 2 * k * L::kValueBytes, L::kValueBytes, 128), operand(b + 512 * k, 128, 2048),
+                                          shape_e4m3(S::kPCols) | kColumnsContiguous, g >= S::kTurns * kGroup || k > 0);
+                    products_arrive(bar(sm.values_free[vs.at]));
+                    products_arrive(bar(sm.summed[pb.at]));
+                    vs.next();
+                    pb.next();
                 }
             }
         }
-    } else if (warp >= 4) {
+        __syncwarp();
+    } else {
         // ---- scores to weights: thread `me` of a team has token `me` of a group and rows row0 .. row0 + R - 1 ----
-        const uint32_t team = (warp - 4) / 4, part = warp % 4, me = tid % 128, row0 = team * R;
+        const uint32_t team = (warp - kOthers) / 4, turn = team % S::kTurns, row0 = team / S::kTurns * R, part = warp % 4, me = part * 32 + lane;
         const uint32_t lanes = part * 32 << 16;                        // of tensor memory
+        const uint32_t scores = scores_at + lanes + row0, sums = sums_at + lanes + turn * S::kSumCols + row0;
+        float* const top = sm.top[team];
         bool ok = true;
-        while (walk.next(p)) {
+        uint32_t it = 0;                                               // groups so far, all teams'
+        Ring<S::kValueStages> vs;
+        Ring<S::kScoreBufs> sb;
+        Ring<2> pb;
+        while (walk.next<ROWS>(p)) {
             // the queries: kEach threads a row
             {
                 constexpr uint32_t kFew = 128 * S::kTeams / ROWS, kEach = kFew < D / 8 ? kFew : D / 8, kVecs = D / 8 / kEach;
-                const uint32_t t = tid - 128, row = t / kEach, j = t % kEach, r = walk.rt * ROWS + row, query = p.group.of(r);
-                const bool mine = row < ROWS;                          // a team's rows are its own
+                const uint32_t t = tid - 32 * kOthers, row = t / kEach, j = t % kEach, r = walk.rt * ROWS + row, query = p.group.of(min(r, p.rows - 1));     // rows that are none see what the last one does
+                const bool mine = row < ROWS;
                 uint4 raw[kVecs];
 #pragma unroll
                 for (uint32_t v = 0; v < kVecs; ++v)
                     raw[v] = mine && r < p.rows ? load_q8(p, walk.b * p.q_batch + (int64_t)query * p.q_query +
-                                                         (int64_t)(walk.h * p.group.d + (r - query * p.group.d)) * p.q_head + (v * kEach + j) * 8)
-                                        : make_uint4(0, 0, 0, 0);
+                                                                 (int64_t)(walk.h * p.group.d + (r - query * p.group.d)) * p.q_head + (v * kEach + j) * 8)
+                                                : make_uint4(0, 0, 0, 0);
                 float most = 0.0f, odd = 0.0f;
 #pragma unroll
                 for (uint32_t v = 0; v < kVecs; ++v) {
@@ -492,53 +570,66 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     const float unit = p.cap > 0.0f ? p.scale / p.cap : p.scale * kLog2e;      // scores in units of the cap, or to the base 2
                     sm.factor[row] = scalbnf(unit, e) + odd;
                     sm.slope[row] = p.slopes && r < p.rows ? __ldg(p.slopes + walk.h * p.group.d + (r - query * p.group.d)) * kLog2e : 0.0f;
-                    const int32_t see = (int32_t)walk.len - (int32_t)p.queries + 1 + (int32_t)query;
-                    sm.see[row] = r < p.rows ? see : INT32_MIN / 2;
+                    sm.see[row] = (int32_t)walk.len - (int32_t)p.queries + 1 + (int32_t)query;
                 }
                 show_to_async();
                 __syncwarp();
                 if (lane == 0) barrier_arrive(bar(sm.query));
-                team_sync(team);
+                if (me < R) top[me] = 0.0f;
+                teams_sync<S::kTeams>();
             }
-            float m[R], l[R];                                          // running maximum of the team, sums of this thread's weights
-            float most_scale = 0.0f;                                   // largest scale of values so far
+            float l[R];                                                // sums of this thread's weights
+            float most_scale = 0.0f, lift_by = 0.0f;                   // largest scale of values so far, 2^6 over it
+            bool any = false;                                          // has this team had a group of the segment?
+            bool first = true, unset = true;                           // row `me` has not seen a token; some row has not
+            const int32_t see_least = sm.see[row0], see_most = sm.see[row0 + R - 1];       // later rows are those of later queries
+            const int32_t window = p.window ? (int32_t)p.window : INT32_MAX / 2, sink = (int32_t)p.sink;
 #pragma unroll
-            for (uint32_t r = 0; r < R; ++r) {
-                m[r] = kNone;
-                l[r] = 0.0f;
-            }
+            for (uint32_t r = 0; r < R; ++r) l[r] = 0.0f;
             float* const mass = p.mass + (uint64_t)walk.seg * p.row_subs * ROWS + row0;
 
-            for (uint32_t g = 0; g < walk.take; g += kGroup, ++it) {
-                const uint32_t st = it % S::kStages, sb = it % S::kScoreBufs, pb = it % S::kPBufs, j = me / 16, many = min(walk.take - g, kGroup);
-                ok = ok && barrier_wait(bar(sm.scored[sb]), (it / S::kScoreBufs) & 1, gave_up) && barrier_wait(bar(sm.full[st]), (it / S::kStages) & 1, gave_up);
-                __syncwarp();
-                tensor_after_sync();
-                uint8_t* const block = values_of(st) + j * L::kValueBytes;
-                const uint32_t tile = j < many ? sm.tile[st][j] : ~0u;
+            for (uint32_t g = 0; g < walk.tiles; g += kGroup, ++it, vs.next(), sb.next(), pb.next()) {
+                if (S::kTurns == 2 && it % 2 != turn) continue;
+                const uint32_t j = me / 16, many = min(walk.tiles - g, kGroup);
+                ok = ok && barrier_wait(bar(sm.values[vs.at]), vs.parity, gave_up);
+                uint8_t* const block = value_room + vs.at * S::kValueStage + j * L::kValueBytes;
+                const uint32_t tile = j < many ? sm.tile[vs.at][j] : ~0u;
                 const int32_t pos = (int32_t)(tile * kTileTokens + me % 16);
+                const float2 scales = *reinterpret_cast<const float2*>(block + 16 * D);        // of keys, of values
                 bool live = tile != ~0u && pos < (int32_t)walk.len;
                 if (live && p.units && p.unit < kTileTokens) live = bits_at(p, (uint64_t)walk.bh * p.row_units + ((uint32_t)pos >> p.unit_log2)) & 1u;
-                const float2 scales = *reinterpret_cast<const float2*>(block + 16 * D);        // of keys, of values
-                float s[R];
+                const float scale = live ? scales.y : 0.0f;
+                // does every row see every token of the warp?
+                const bool all_seen = __all_sync(0xFFFFFFFFu, live && pos < see_least && (pos >= see_most - window || pos < sink));
+                ok = ok && barrier_wait(bar(sm.scored[sb.at]), sb.parity, gave_up);
+                __syncwarp();
+                tensor_after_sync();
+                float s[R];                                            // scores, less the maximum, then weights
 #pragma unroll
                 for (uint32_t r = 0; r < R; r += 8) {
                     float x[S::kQTerms][8];
 #pragma unroll
-                    for (uint32_t term = 0; term < S::kQTerms; ++term) tensor_load8(scores_at + lanes + sb * S::kQCols + term * ROWS + row0 + r, x[term]);
+                    for (uint32_t term = 0; term < S::kQTerms; ++term) tensor_load(scores + sb.at * S::kQCols + term * ROWS + r, x[term]);
                     tensor_wait_load();
 #pragma unroll
-                    for (uint32_t term = 0; term < S::kQTerms; ++term) tensor_hold8(x[term]);
+                    for (uint32_t term = 0; term < S::kQTerms; ++term) tensor_hold(x[term]);
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) {
-                        float y = fmaf(x[1][i], 0x1p-5f, x[0][i]);
-                        if (S::kQTerms == 3) y = fmaf(x[S::kQTerms - 1][i], 0x1p-10f, y);
-                        s[r + i] = y * (sm.factor[row0 + r + i] * scales.x);
+                    for (uint32_t i = 0; i < 8; i += 4) {
+                        const float4 f = *reinterpret_cast<const float4*>(sm.factor + row0 + r + i);
+                        const F2 scale2(scales.x, scales.x), by[2] = {F2(f.x, f.y) * scale2, F2(f.z, f.w) * scale2};
+#pragma unroll
+                        for (uint32_t k = 0; k < 2; ++k) {
+                            const uint32_t n = i + 2 * k;
+                            F2 y = fma2(F2(x[1][n], x[1][n + 1]), F2(0x1p-5f, 0x1p-5f), F2(x[0][n], x[0][n + 1]));
+                            if (S::kQTerms == 3) y = fma2(F2(x[S::kQTerms - 1][n], x[S::kQTerms - 1][n + 1]), F2(0x1p-10f, 0x1p-10f), y);
+                            y = y * by[k];
+                            y.get(s[r + n], s[r + n + 1]);
+                        }
                     }
                 }
                 tensor_before_sync();
                 __syncwarp();
-                if (lane == 0) barrier_arrive(bar(sm.taken[sb]));
+                if (lane == 0) barrier_arrive(bar(sm.taken[sb.at]));
                 if (p.cap > 0.0f) {
 #pragma unroll
                     for (uint32_t r = 0; r < R; ++r) s[r] = tanhf(s[r]) * (p.cap * kLog2e);
@@ -547,64 +638,81 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
 #pragma unroll
                     for (uint32_t r = 0; r < R; ++r) s[r] = fmaf(sm.slope[row0 + r], (float)(pos - sm.see[row0 + r] + 1), s[r]);
                 }
-                bool up = false;                                       // has a score passed the maximum by more than the slack?
-#pragma unroll
-                for (uint32_t r = 0; r < R; ++r) {
-                    const int32_t see = sm.see[row0 + r];
-                    const bool seen = live && pos < see && (!p.window || pos >= see - (int32_t)p.window || pos < (int32_t)p.sink);
-                    s[r] = seen ? s[r] : -INFINITY;
-                    up = up || s[r] > m[r] + kSlack;
-                }
-                const float scale = live ? scales.y : 0.0f;
-                up = up || scale > most_scale;
-                if (team_any(up || !ok, team)) {
+                if (!all_seen) {
 #pragma unroll
                     for (uint32_t r = 0; r < R; ++r) {
-                        const float x = warp_max(s[r]);
-                        if (lane == 0) sm.top[team][part][r] = x;
+                        const int32_t see = sm.see[row0 + r];
+                        s[r] = live && pos < see && (pos >= see - window || pos < sink) ? s[r] : -INFINITY;
                     }
-                    const float x = warp_max(scale);
-                    if (lane == 0) sm.most[team][part] = x;
-                    // sums of the group before are to be there, all of them
-                    if (g) ok = ok && barrier_wait(bar(sm.summed[(it - 1) % S::kPBufs]), ((it - 1) / S::kPBufs) & 1, gave_up);
+                }
+                float over = -INFINITY;                                // how far scores pass the maximum
+#pragma unroll
+                for (uint32_t r = 0; r < R; r += 4) {
+                    const float4 m = *reinterpret_cast<const float4*>(top + r);
+                    s[r] -= m.x;
+                    s[r + 1] -= m.y;
+                    s[r + 2] -= m.z;
+                    s[r + 3] -= m.w;
+                    over = fmaxf(over, fmaxf(fmaxf(s[r], s[r + 1]), fmaxf(s[r + 2], s[r + 3])));
+                }
+                if (team_any(over > kSlack || scale > most_scale || unset || !ok, team)) {
+                    float x = warp_max(scale);
+                    if (lane == 0) sm.scale[team][part] = x;
+#pragma unroll
+                    for (uint32_t r = 0; r < R; ++r) {
+                        const float y = warp_max(s[r]);
+                        if (lane == r) x = y;
+                    }
+                    if (lane < R) sm.peak[team][part][lane] = x;
+                    // the sums of the team's group before are to be there, all of them
+                    if (any) ok = ok && barrier_wait(bar(sm.summed[S::kTurns == 2 ? pb.at : pb.at ^ 1u]), S::kTurns == 2 || pb.at == 0 ? pb.parity ^ 1u : pb.parity, gave_up);
                     __syncwarp();
                     if (team_any(!ok, team)) { ok = false; break; }    // also: the maxima are there
                     tensor_after_sync();
-                    const float new_scale = fmaxf(most_scale, fmaxf(fmaxf(sm.most[team][0], sm.most[team][1]), fmaxf(sm.most[team][2], sm.most[team][3])));
+                    const float new_scale = fmaxf(most_scale, fmaxf(fmaxf(sm.scale[team][0], sm.scale[team][1]), fmaxf(sm.scale[team][2], sm.scale[team][3])));
                     const float by_scale = most_scale > 0.0f ? most_scale / new_scale : 1.0f;
                     most_scale = new_scale;
-#pragma unroll
-                    for (uint32_t r = 0; r < R; r += 8) {
-                        float by[8];
-#pragma unroll
-                        for (uint32_t i = 0; i < 8; ++i) {
-                            const float top = fmaxf(m[r + i], fmaxf(fmaxf(sm.top[team][0][r + i], sm.top[team][1][r + i]), fmaxf(sm.top[team][2][r + i], sm.top[team][3][r + i])));
-                            by[i] = exp2_fast(m[r + i] - top);
-                            l[r + i] *= by[i];
-                            by[i] *= by_scale;
-                            m[r + i] = top;
-                        }
-                        if (g) {
-#pragma unroll
-                            for (uint32_t c = 0; c < 3 * S::kHalves; ++c) {
-                                const uint32_t at = sums_at + lanes + c / 3 * S::kPCols + c % 3 * ROWS + row0 + r;
-                                float y[8];
-                                tensor_load8(at, y);
-                                tensor_wait_load();
-                                tensor_hold8(y);
-#pragma unroll
-                                for (uint32_t i = 0; i < 8; ++i) y[i] *= by[i];
-                                tensor_store8(at, y);
-                            }
-                        }
+                    lift_by = new_scale > 0.0f ? 64.0f / new_scale : 0.0f;
+                    bool none = false;                                 // has row `me` not seen a token?
+                    if (me < R) {
+                        float up = fmaxf(fmaxf(sm.peak[team][0][me], sm.peak[team][1][me]), fmaxf(sm.peak[team][2][me], sm.peak[team][3][me]));
+                        if (first) up = fmaxf(up, kNone);              // the first maximum, whatever its sign
+                        else up = fmaxf(up, 0.0f);
+                        none = up == kNone;
+                        first = none;
+                        if (none) up = 0.0f;
+                        sm.by[team][me] = up;
+                        top[me] += up;
                     }
-                    tensor_wait_store();
-                    tensor_before_sync();
-                    team_sync(team);                                   // the maxima's room is free again
+                    unset = team_any(none, team);                      // also: the new maxima are there
+                    if (any) {
+#pragma unroll 1
+                        for (uint32_t c = 0; c < 3 * S::kHalves; ++c)
+#pragma unroll
+                            for (uint32_t r = 0; r < R; r += 8) {
+                                const uint32_t at = sums + c / 3 * S::kPCols + c % 3 * ROWS + r;
+                                float y[8];
+                                tensor_load(at, y);
+                                tensor_wait_load();
+                                tensor_hold(y);
+#pragma unroll
+                                for (uint32_t i = 0; i < 8; ++i) y[i] *= exp2_fast(fminf(-sm.by[team][r + i], 0.0f)) * by_scale;
+                                tensor_store(at, y);
+                            }
+                        tensor_wait_store();
+                        tensor_before_sync();
+                    }
+#pragma unroll
+                    for (uint32_t r = 0; r < R; ++r) {
+                        const float up = sm.by[team][r];
+                        s[r] -= up;
+                        l[r] *= exp2_fast(fminf(-up, 0.0f));           // a first maximum may be below 0; the sums are 0 then
+                    }
                 }
+                any = true;
 #pragma unroll
                 for (uint32_t r = 0; r < R; ++r) {
-                    s[r] = exp2_fast(s[r] - m[r]);
+                    s[r] = exp2_fast(s[r]);
                     l[r] += s[r];
                 }
                 if (p.sub) {                                           // what each block of `sub` tokens received, as log2
@@ -618,12 +726,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                         if (tile == ~0u) return;
                         float* to = mass + ((uint64_t)(uint32_t)pos >> LOG) * ROWS + from;
 #pragma unroll
-                        for (int i = 0; i < LEFT; ++i) {
-                            float mx = m[i];
-#pragma unroll
-                            for (uint32_t r = LEFT; r < R; r += LEFT) mx = from == r ? m[r + i] : mx;
-                            to[i] = mx + log2_fast(x[i]);
-                        }
+                        for (int i = 0; i < LEFT; ++i) to[i] = top[from + i] + log2_fast(x[i]);
                     };
 #define KVP_INT(X) std::integral_constant<int, (X)>{}
 #define KVP_LEFT(LOG) KVP_INT((R >> LOG) ? (R >> LOG) : 1)
@@ -636,22 +739,34 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     }
                 }
                 // the weights as the right operand; the buffer is free when the products with what it held are done
-                if (it >= S::kPBufs) ok = ok && barrier_wait(bar(sm.summed[pb]), (it / S::kPBufs - 1) & 1, gave_up);
-                const float by = scale > 0.0f ? scale / most_scale * 64.0f : 0.0f;             // 2^kLift
-                uint8_t* const to = weights + pb * S::kPBytes + me / 16 * 128 + me % 16;
+                if (it >= 2) ok = ok && barrier_wait(bar(sm.summed[pb.at]), pb.parity ^ 1u, gave_up);
+                const float by = scale * lift_by;
+                uint8_t* const to = weights + pb.at * S::kPBytes + me * 16;
+                uint32_t term[3][R / 4];
 #pragma unroll
-                for (uint32_t r = 0; r < R; r += 2) {
-                    float a = s[r] * by, b = s[r + 1] * by;
+                for (uint32_t r = 0; r < R; r += 4) {
+                    const F2 both(by, by), lo = F2(s[r], s[r + 1]) * both, hi = F2(s[r + 2], s[r + 3]) * both;
+                    float x[4];
+                    lo.get(x[0], x[1]);
+                    hi.get(x[2], x[3]);
+                    uint32_t a = pack(x[0], x[1]), b = pack(x[2], x[3]);
 #pragma unroll
-                    for (uint32_t term = 0; term < 3; ++term) {
-                        const uint32_t t = next_term(a, b), col = term * ROWS + row0 + r;
-                        to[col / 8 * 1024 + col % 8 * 16] = (uint8_t)t;
-                        to[col / 8 * 1024 + col % 8 * 16 + 16] = (uint8_t)(t >> 8);
+                    for (uint32_t i = 0; i < 3; ++i) {
+                        const uint32_t y = next_term(a);
+                        term[i][r / 4] = __byte_perm(y, next_term(b), 0x5410);
                     }
+                }
+                if constexpr (R == 8) {
+                    *reinterpret_cast<uint4*>(to) = make_uint4(term[0][0], term[0][1], term[1][0], term[1][1]);
+                    *reinterpret_cast<uint2*>(to + 2048) = make_uint2(term[2][0], term[2][1]);
+                } else {
+#pragma unroll
+                    for (uint32_t i = 0; i < 3; ++i)
+                        *reinterpret_cast<uint4*>(to + (i * ROWS + row0) / 16 * 2048) = make_uint4(term[i][0], term[i][1], term[i][2], term[i][3]);
                 }
                 // What lies in the cache where no token is may be anything, also NaN, and so may a tile that did not come: its values are cleared.
                 const uint32_t lives = __ballot_sync(0xFFFFFFFFu, live) >> (lane & 16u) & 0xFFFFu;
-                if (team == 0 && lives != 0xFFFFu && j < (many + 1) / 2 * 2) {
+                if (row0 == 0 && !all_seen && lives != 0xFFFFu && j < (many + 1) / 2 * 2) {
                     uint4 keep;
                     uint32_t* word = &keep.x;
 #pragma unroll
@@ -666,70 +781,87 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 }
                 show_to_async();
                 __syncwarp();
-                if (lane == 0) barrier_arrive(bar(sm.weighed[pb]));
+                if (lane == 0) barrier_arrive(bar(sm.weighed[pb.at]));
             }
 
-            // ---- the end of a segment ----
-            const uint32_t last = it - 1;
-            ok = ok && barrier_wait(bar(sm.summed[last % S::kPBufs]), (last / S::kPBufs) & 1, gave_up);
-#pragma unroll
-            for (uint32_t r = 0; r < R; ++r) {
-                const float x = warp_sum(l[r]);
-                if (lane == 0) sm.top[team][part][r] = x;
+            // ---- the end of a segment: the turns' sums are joined, each team writes some of the rows ----
+            if (any) {
+                // the last group of this team: pb stands behind the segment's last group
+                const bool mine_last = S::kTurns == 1 || (it - 1) % 2 == turn;
+                const uint32_t behind = S::kTurns == 1 || mine_last ? 1u : 2u;             // groups since
+                const uint32_t at = (pb.at + 2 - behind) % 2, parity = behind > pb.at ? pb.parity ^ 1u : pb.parity;
+                ok = ok && barrier_wait(bar(sm.summed[at]), parity, gave_up);
             }
-            if (team_any(!ok, team)) ok = false;
+            __syncwarp();
+            {
+                uint32_t from;
+                sum_neighbours<R, 5>(l, lane, from);                   // R <= 16: one row a lane is left
+                sm.peak[team][part][from] = l[0];                      // the same from lanes of the same row
+            }
+            if (lane == 0) sm.scale[team][part] = ok ? 0.0f : NAN;
+            teams_sync<S::kTeams>();
             tensor_after_sync();
             const bool whole = walk.take == walk.count;
             const uint64_t slot = (uint64_t)blockIdx.x + walk.seg;
-#pragma unroll
-            for (uint32_t r = 0; r < R; ++r) {
-                l[r] = (sm.top[team][0][r] + sm.top[team][1][r]) + (sm.top[team][2][r] + sm.top[team][3][r]);
-                if (!ok) l[r] = NAN;
-            }
+            constexpr uint32_t F = R / S::kTurns;                      // rows of a team now
+            const uint32_t mine = turn * F, team0 = team - turn, row_at = walk.rt * ROWS + row0 + mine;
             const auto place = [&](uint32_t row) {
                 const uint32_t query = p.group.of(row);
                 return ((uint64_t)walk.b * p.queries + query) * (p.heads.d * p.group.d) + walk.h * p.group.d + (row - query * p.group.d);
             };
+            if (me < F) {
+                // row mine + me: its maximum and sum over the turns
+                float m = kNone, sum = 0.0f, one[S::kTurns];
 #pragma unroll
-            for (uint32_t r = 0; r < R; ++r)
-                if (me == r) {
-                    const uint32_t row = walk.rt * ROWS + row0 + r;
-                    p.ml[slot * ROWS + row0 + r] = make_float2(m[r], l[r]);
-                    if (whole && p.lse && row < p.rows) p.lse[place(row)] = l[r] == 0.0f ? -INFINITY : (m[r] + log2f(l[r])) * 0.6931471805599453f;
+                for (uint32_t u = 0; u < S::kTurns; ++u) {
+                    const float* x = &sm.peak[team0 + u][0][mine + me];
+                    const float* gone = sm.scale[team0 + u];
+                    one[u] = ((x[0] + x[R]) + (x[2 * R] + x[3 * R])) + ((gone[0] + gone[1]) + (gone[2] + gone[3]));
+                    if (one[u] != 0.0f) m = fmaxf(m, sm.top[team0 + u][mine + me]);
                 }
-            const float up = most_scale * 0x1p-6f;
 #pragma unroll
-            for (uint32_t half = 0; half < S::kHalves; ++half) {
-                const uint32_t d = half * 128 + me;
+                for (uint32_t u = 0; u < S::kTurns; ++u) {
+                    const float k = one[u] != 0.0f ? exp2_fast(sm.top[team0 + u][mine + me] - m) : 0.0f;
+                    sum = fmaf(one[u], k, sum);
+                    sm.last[team0 + u][mine + me].x = k;
+                }
+                const float by = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
+                sm.last[team0][mine + me].y = by;
+                p.ml[slot * ROWS + row0 + mine + me] = make_float2(m, sum);
+                if (whole && p.lse && row_at + me < p.rows) p.lse[place(row_at + me)] = sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
+            }
+            if (me == 0) sm.by[team][0] = any ? most_scale * 0x1p-6f : -1.0f;          // a turn's units; below 0: it had no group
+            teams_sync<S::kTeams>();
+#pragma unroll 1
+            for (uint32_t i = 0; i < S::kHalves * F / 4; ++i) {
+                const uint32_t half = i / (F / 4), r = mine + i % (F / 4) * 4, d = half * 128 + me;
+                float y[4] = {0, 0, 0, 0};
 #pragma unroll
-                for (uint32_t r = 0; r < R; r += 8) {
-                    float x[3][8];
+                for (uint32_t u = 0; u < S::kTurns; ++u) {
+                    const float units = sm.by[team0 + u][0];
+                    if (units < 0.0f) continue;                        // uniform: nothing was written there
+                    float x[3][4];
 #pragma unroll
-                    for (uint32_t c = 0; c < 3; ++c) tensor_load8(sums_at + lanes + half * S::kPCols + c * ROWS + row0 + r, x[c]);
+                    for (uint32_t c = 0; c < 3; ++c) tensor_load(sums_at + lanes + u * S::kSumCols + half * S::kPCols + c * ROWS + row0 + r, x[c]);
                     tensor_wait_load();
 #pragma unroll
-                    for (uint32_t c = 0; c < 3; ++c) tensor_hold8(x[c]);
-                    if (d < D) {
+                    for (uint32_t c = 0; c < 3; ++c) tensor_hold(x[c]);
 #pragma unroll
-                        for (uint32_t i = 0; i < 8; ++i) {
-                            const uint32_t row = walk.rt * ROWS + row0 + r + i;
-                            float y = fmaf(fmaf(x[2][i], 0x1p-5f, x[1][i]), 0x1p-5f, x[0][i]) * up;
-                            if (row >= p.rows) continue;
-                            if (whole) {
-                                y = l[r + i] == 0.0f ? 0.0f : y / l[r + i];
-                                uint16_t bits;
-                                if (S::HALF) bits = __half_as_ushort(__float2half_rn(y));
-                                else bits = __bfloat16_as_ushort(__float2bfloat16_rn(y));
-                                static_cast<uint16_t*>(p.out)[place(row) * D + d] = bits;
-                            } else {
-                                p.part[(slot * ROWS + row0 + r + i) * D + d] = y;
-                            }
-                        }
+                    for (uint32_t k = 0; k < 4; ++k)
+                        y[k] = fmaf(fmaf(fmaf(x[2][k], 0x1p-5f, x[1][k]), 0x1p-5f, x[0][k]), units * sm.last[team0 + u][r + k].x, y[k]);
+                }
+                if (d < D) {
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) {
+                        const uint32_t row = walk.rt * ROWS + row0 + r + k;
+                        const float x = y[k] * sm.last[team0][r + k].y;
+                        if (!whole) p.part[(slot * ROWS + row0 + r + k) * D + d] = x;
+                        else if (row < p.rows) static_cast<uint16_t*>(p.out)[place(row) * D + d] = S::HALF ? __half_as_ushort(__float2half_rn(x)) : __bfloat16_as_ushort(__float2bfloat16_rn(x));
                     }
                 }
             }
             tensor_before_sync();
-            team_sync(team);
+            teams_sync<S::kTeams>();
         }
     }
     tensor_before_sync();

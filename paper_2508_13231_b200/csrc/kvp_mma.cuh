@@ -15,11 +15,11 @@ __device__ __forceinline__ void barrier_arrive_expect(uint32_t bar, uint32_t byt
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// the phase of `parity` has ended?
+// Has the phase of `parity` ended? The hardware may hold the thread back for up to 10 us before it says no.
 __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity), "r"(10000u) : "memory");
     return ok != 0;
 }
 // Waits for the end of the phase of `parity`, two seconds at most; false if it did not come, or if another waiter of the CTA gave up before.
@@ -28,7 +28,7 @@ static __device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t par
     uint64_t from, now;
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(from));
     while (true) {
-        for (int i = 0; i < 256; ++i)
+        for (int i = 0; i < 16; ++i)
             if (barrier_try(bar, parity)) return true;
         if (*gave_up) return false;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
@@ -69,24 +69,26 @@ __device__ __forceinline__ void tensor_wait_load() { asm volatile("tcgen05.wait:
 __device__ __forceinline__ void tensor_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // the numbers of a load are not used before here (the compiler knows no other order between a load's registers and the wait)
-__device__ __forceinline__ void tensor_hold8(float* x)
+template <int N>
+__device__ __forceinline__ void tensor_hold(float (&x)[N])
 {
-    asm volatile("" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]));
-}
-// eight columns of this thread's lane (warp w of a group of four has lanes 32 w .. 32 w + 31)
-__device__ __forceinline__ void tensor_load8(uint32_t at, float* x)
-{
-    uint32_t r[8];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(at));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < N; ++i) asm volatile("" : "+f"(x[i]));
 }
-__device__ __forceinline__ void tensor_store8(uint32_t at, const float* x)
+// four or eight columns of this thread's lane (warp w of a team of four has lanes 32 w .. 32 w + 31)
+__device__ __forceinline__ void tensor_load(uint32_t at, float (&x)[4])
 {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "r"(__float_as_uint(x[0])),
-                 "r"(__float_as_uint(x[1])), "r"(__float_as_uint(x[2])), "r"(__float_as_uint(x[3])), "r"(__float_as_uint(x[4])), "r"(__float_as_uint(x[5])),
-                 "r"(__float_as_uint(x[6])), "r"(__float_as_uint(x[7])) : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "r"(at));
+}
+__device__ __forceinline__ void tensor_load(uint32_t at, float (&x)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "r"(at));
+}
+__device__ __forceinline__ void tensor_store(uint32_t at, const float (&x)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]),
+                 "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
 }
 
 // ---- products ----
@@ -96,6 +98,8 @@ __device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t along_k, uint3
 {
     return (uint64_t)(at >> 4) | (uint64_t)(along_k >> 4) << 16 | (uint64_t)(along_rows >> 4) << 32 | 1ull << 46;
 }
+// The right operand may have its columns contiguous instead: cores of 16 columns x 8 in k, `along_k` to the next eight in k, `along_rows` to the next 16 columns.
+constexpr uint32_t kColumnsContiguous = 1u << 16;
 // sums in fp32 of e4m3 times e4m3, 128 rows x `columns` (a multiple of 16, at most 256)
 __host__ __device__ constexpr uint32_t shape_e4m3(uint32_t columns) { return 1u << 4 | (columns / 8) << 17 | (128u / 16) << 24; }
 // sums [128 lanes][columns] (+)= a [128][32 in k] b [columns][32 in k]^T; one thread
