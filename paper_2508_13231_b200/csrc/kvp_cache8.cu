@@ -6,6 +6,7 @@
 // the block holds is divided by a power of two, which rounds only what falls below e4m3's normal numbers (2^-15 of the block's largest).
 #include <cuda_bf16.h>
 
+#include "kvp_line.cuh"
 #include "kvp_tile8.cuh"
 
 namespace kvp {
@@ -19,6 +20,7 @@ struct Rows8K {
     uint8_t* cache;
     uint64_t slots_in_cache;                      // pages * page_tokens
     uint32_t tokens, heads, page_tokens;
+    Divisor by_heads;                             // of a CTA's number: heads of the same tokens stand next to each other, as in memory
 };
 
 constexpr float kMost = 0x1p100f;                 // larger magnitudes count as this
@@ -31,20 +33,46 @@ __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(__half* p, float x) { *p = __float2half_rn(x); }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
+// eight neighbouring elements as they lie; `aligned`: at a 16-byte boundary
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, bool aligned, float* x)
-{
-    if (aligned) {
-        alignas(16) T e[8];
+struct Eight {
+    alignas(16) T e[8];
+    __device__ __forceinline__ void load(const T* p, bool aligned)
+    {
+        if (aligned) {
 #pragma unroll
-        for (uint32_t i = 0; i < sizeof(e) / 16; ++i) reinterpret_cast<uint4*>(e)[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+            for (uint32_t i = 0; i < sizeof(e) / 16; ++i) reinterpret_cast<uint4*>(e)[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = to_float(e[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = to_float(p[i]);
+            for (int i = 0; i < 8; ++i) e[i] = p[i];
+        }
     }
-}
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(e) / 16; ++i) reinterpret_cast<uint4*>(e)[i] = make_uint4(0, 0, 0, 0);
+    }
+    // as fp32, NaN as 0, cut to what is held; returns the largest magnitude
+    __device__ __forceinline__ float floats(float* x) const
+    {
+        float m = 0.0f, odd = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = to_float(e[i]);
+            m = fmaxf(m, fabsf(x[i]));
+            odd = fmaf(x[i], 0.0f, odd);                               // NaN if one is not finite
+        }
+        if (odd != 0.0f || m > kMost) {                                // rare
+            m = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] = x[i] != x[i] ? 0.0f : fminf(fmaxf(x[i], -kMost), kMost);
+                m = fmaxf(m, fabsf(x[i]));
+            }
+        }
+        return m;
+    }
+};
 
 // the block of a slot, for one head; slot < slots_in_cache
 template <int D>
@@ -76,124 +104,171 @@ __device__ __forceinline__ uint32_t rounded_again(uint32_t four, float by)
     return e4m3_pair(a.x * by, a.y * by) | e4m3_pair(b.x * by, b.y * by) << 16;
 }
 
-struct Run {
-    uint64_t block;          // where it lies in the cache
-    float old, now;          // scales
-    bool begins;             // the block's first token is among them: nothing is held
-    uint32_t many;           // places that are written
-    uint8_t token[16];       // of each place, counted from the CTA's first; kNobody: not written
-};
+// eight numbers over a power of two, or 0 where that is 0
+__device__ __forceinline__ uint2 rounded(const float* x, float scale)
+{
+    if (!(scale > 0.0f)) return make_uint2(0, 0);
+    const float by = __int_as_float((254 << 23) - __float_as_int(scale));              // 1 / scale
+    return make_uint2(e4m3_pair(x[0] * by, x[1] * by) | e4m3_pair(x[2] * by, x[3] * by) << 16, e4m3_pair(x[4] * by, x[5] * by) | e4m3_pair(x[6] * by, x[7] * by) << 16);
+}
+
 constexpr uint8_t kNobody = 0xFF;
 
-// A run is the tokens of one block in the call, which stand within 16 tokens of it. A CTA takes the runs that begin among 16 tokens; the last ones may go
-// on behind them, so a thread has eight dims of two tokens. blockIdx.y is the head, blockIdx.z 0 for keys and 1 for values. One CTA thus knows the largest magnitude
-// of a block's new tokens, and the block's bytes are written by nobody else.
-// A run's bytes are gathered in shared memory and written 16 at a time: a token's 16 dims, or a dim of 16 tokens; single values (one byte each) where the
-// run does not fill the block and its scale stays.
+// The runs that begin in a CTA; a run is the tokens of one block in the call, which stand within 16 tokens of it. [2]: keys, values
+struct Runs {
+    uint64_t block[16];              // where it lies in the cache
+    float old[2][16], now[2][16];    // scales
+    alignas(16) uint8_t token[16][16];       // of each place, counted from the CTA's first; kNobody: not written
+    uint32_t many;
+};
+
+// A CTA takes the runs that begin among 16 tokens, of one head, keys and values; the last runs may go on behind the 16, so a thread has eight dims of two
+// tokens. One CTA thus knows the largest magnitude of a block's new tokens, and the block's bytes are written by nobody else.
+// Where the 16 tokens are a block from its first place to its last, as most of a prompt's are, nothing else is looked at: keys are written as a thread has them
+// (two tokens of a warp fill whole sectors), values by way of shared memory, 8 tokens of a dim a thread. 32768 tokens x 8 heads of 128 dims, bf16:
+// see launch_append. Elsewhere a run's bytes are gathered in shared memory and written 16 at a time, or one by one where the run does not fill the block and its scale stays.
 template <int D, typename T>
-__global__ void __launch_bounds__(2 * D) append8_kernel(const Rows8K p, bool aligned)
+__global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Rows8K p, uint32_t rounds, bool aligned)
 {
     using L = Tile8<D>;
-    constexpr uint32_t kThreads = 2 * D, kPerRow = D / 8;
-    __shared__ int64_t slot[48];                                       // of the tokens from 16 before the CTA's first on
-    __shared__ uint32_t leads[64];                                     // by the same numbers: the first token of its run; 0: no token
-    __shared__ float most[32];
-    __shared__ Run runs[16];
-    __shared__ uint32_t many_runs;
-    __shared__ alignas(16) uint8_t held[32][D];
-    const uint32_t tid = threadIdx.x, row = tid / kPerRow, part = tid % kPerRow, head = blockIdx.y, base = blockIdx.x * 16;
-    const bool is_value = blockIdx.z;
-    const T* const from = is_value ? static_cast<const T*>(p.v) + head * p.v_head + 8 * part : static_cast<const T*>(p.k) + head * p.k_head + 8 * part;
-    const int64_t stride = is_value ? p.v_token : p.k_token;
+    constexpr uint32_t kThreads = 2 * D, kPerRow = D / 8, kStride = D + 8;             // rows eight apart lie in other banks
+    __shared__ int64_t slot[48];                                       // of the tokens from 16 before the CTA's first on; -1: none
+    __shared__ uint8_t run_of[32];                                     // of the tokens from the CTA's first on
+    __shared__ float most[2][32];
+    __shared__ Runs runs;
+    __shared__ bool whole;
+    __shared__ alignas(16) uint8_t held[2][32][kStride];
+    const uint32_t tid = threadIdx.x, lane = tid % 32, row = tid / kPerRow, part = tid % kPerRow;
+    // what a round needs from memory is sent for a round ahead: the eight dims of a token, keys and values, and the slots
+    Eight<T> raw[2];
+    int64_t my_slot = -1;
+    const auto from = [&](int u, uint32_t token, uint32_t head) {
+        return u ? static_cast<const T*>(p.v) + token * p.v_token + head * p.v_head + 8 * part : static_cast<const T*>(p.k) + token * p.k_token + head * p.k_head + 8 * part;
+    };
+    const auto fetch = [&](uint32_t round) {
+        const uint32_t group = p.by_heads.of(round), head = round - group * p.heads, base = group * 16;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            raw[u].clear();
+            if (base + row < p.tokens) raw[u].load(from(u, base + row, head), aligned);
+        }
+        if (tid < 48) {
+            const int64_t t = (int64_t)base - 16 + tid;
+            my_slot = t >= 0 && t < p.tokens ? __ldg(p.slots + t) : -1;
+        }
+    };
+    fetch(blockIdx.x);
+    for (uint32_t round = blockIdx.x; round < rounds; round += gridDim.x) {
+    const uint32_t group = p.by_heads.of(round), head = round - group * p.heads, base = group * 16;
+    if (tid < 48) slot[tid] = my_slot < 0 || (uint64_t)my_slot >= p.slots_in_cache ? -1 : my_slot;
+    else if (tid < 64) reinterpret_cast<uint4*>(runs.token)[tid - 48] = make_uint4(~0u, ~0u, ~0u, ~0u);
+    __syncthreads();
+    if (tid < 32) {
+        const int64_t s = slot[16 + (lane & 15)], s0 = slot[16];
+        const bool all = __all_sync(0xFFFFFFFFu, s0 >= 0 && s0 % kTileTokens == 0 && s == s0 + (lane & 15));
+        if (lane == 0) whole = all;
+        if (all) {
+            if (lane == 0) runs.block[0] = block_at<D>((uint64_t)s0, head, p);
+        } else {
+            // token 16 + lane: the first of the 15 before it in the same block leads
+            const int64_t mine = lane < 31 ? slot[16 + lane] : -1;
+            uint32_t first = 16 + lane;
+#pragma unroll
+            for (uint32_t j = 15; j > 0; --j)
+                if (slot[1 + lane + (15 - j)] >= 0 && slot[1 + lane + (15 - j)] / kTileTokens == mine / kTileTokens) first = min(first, 1 + lane + (15 - j));
+            const bool here = mine >= 0 && first >= 16 && first < 32, leader = here && first == 16 + lane;
+            const uint32_t leaders = __ballot_sync(0xFFFFFFFFu, leader), run = here ? __popc(leaders & ((1u << (first - 16)) - 1u)) : kNobody;
+            run_of[lane] = (uint8_t)run;
+            if (here) runs.token[run][mine % kTileTokens] = (uint8_t)lane;
+            if (lane == 0) runs.many = __popc(leaders);
+            if (leader) {
+                const uint64_t at = block_at<D>((uint64_t)mine, head, p);
+                const float2 old = *reinterpret_cast<const float2*>(p.cache + at + L::kScale);
+                runs.block[run] = at;
+                // a scale that is no power of two is none: nothing is held
+                runs.old[0][run] = old.x >= 0x1p-126f && old.x < INFINITY && !(__float_as_int(old.x) & 0x7FFFFF) ? old.x : 0.0f;
+                runs.old[1][run] = old.y >= 0x1p-126f && old.y < INFINITY && !(__float_as_int(old.y) & 0x7FFFFF) ? old.y : 0.0f;
+            }
+        }
+    }
     float x[2][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[0][i] = x[1][i] = 0.0f;
-    if (base + row < p.tokens) load8(from + (base + row) * stride, aligned, x[0]);
-    if (tid < 48) {
-        const int64_t t = (int64_t)base - 16 + tid;
-        int64_t s = -1;
-        if (t >= 0 && t < p.tokens) s = __ldg(p.slots + t);
-        slot[tid] = s < 0 || (uint64_t)s >= p.slots_in_cache ? -1 : s;
-    }
-    __syncthreads();
-    if (tid < 64) {                                                    // two whole warps
-        const int64_t s = tid < 48 ? slot[tid] : -1;
-        uint32_t first = tid;
-        for (uint32_t j = tid < 16 ? 0 : tid - 15; s >= 0 && j < first; ++j)
-            if (slot[j] >= 0 && slot[j] / kTileTokens == s / kTileTokens) first = j;
-        leads[tid] = s >= 0 ? first : 0;
-    }
-    __syncthreads();
-    // in a run that begins here?
-    const bool in0 = leads[16 + row] >= 16, in1 = leads[32 + row] >= 16 && leads[32 + row] < 32;
-    if (in1 && base + 16 + row < p.tokens) load8(from + (base + 16 + row) * stride, aligned, x[1]);
-    if (tid < 32) {
-        const bool leader = tid < 16 && leads[16 + tid] == 16 + tid;
-        const uint32_t all = __ballot_sync(0xFFFFFFFFu, leader), at = __popc(all & ((1u << tid) - 1u));
-        if (tid == 0) many_runs = __popc(all);
-        if (leader) {
-            Run& r = runs[at];
-            r.block = block_at<D>((uint64_t)slot[16 + tid], head, p);
-            const float old = *reinterpret_cast<const float*>(p.cache + r.block + L::kScale + (is_value ? 4 : 0));
-            for (uint32_t i = 0; i < 16; ++i) r.token[i] = kNobody;
-            r.many = 0;
-            for (uint32_t t = tid; t < tid + 16; ++t)
-                if (leads[16 + t] == 16 + tid) {
-                    const uint32_t place = (uint32_t)(slot[16 + t] % kTileTokens);
-                    r.many += r.token[place] == kNobody;
-                    r.token[place] = (uint8_t)t;
-                }
-            r.begins = r.token[0] != kNobody;
-            // a scale that is no power of two is none: nothing is held
-            r.old = !r.begins && old >= 0x1p-126f && old < INFINITY && !(__float_as_int(old) & 0x7FFFFF) ? old : 0.0f;
-        }
-    }
-#pragma unroll
     for (int u = 0; u < 2; ++u) {
-        float m = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[u][i] = x[u][i] != x[u][i] ? 0.0f : fminf(fmaxf(x[u][i], -kMost), kMost);
-            m = fmaxf(m, fabsf(x[u][i]));
-        }
+        float m = raw[u].floats(x[u]);
 #pragma unroll
         for (uint32_t o = 1; o < kPerRow; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-        if (part == 0) most[16 * u + row] = m;
+        if (part == 0) most[u][row] = m;
     }
     __syncthreads();
-    if (tid < many_runs) {
-        Run& r = runs[tid];
+    if (whole) {
+        if (round + gridDim.x < rounds) fetch(round + gridDim.x);
+        uint8_t* const block = p.cache + runs.block[0];
+        float scale[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float m = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m = fmaxf(m, most[u][i]);
+            scale[u] = scale_for(m);
+        }
+        *reinterpret_cast<uint2*>(block + L::key(row, part / 2) + 8 * (part % 2)) = rounded(x[0], scale[0]);
+        *reinterpret_cast<uint2*>(&held[1][row][8 * part]) = rounded(x[1], scale[1]);
+        if (tid == 0) *reinterpret_cast<float2*>(block + L::kScale) = make_float2(scale[0], scale[1]);
+        __syncthreads();
+        const uint32_t d = tid / 2, first = tid % 2 * 8;
+        uint32_t q[2] = {0, 0};
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) q[j / 4] |= (uint32_t)held[1][first + j][d] << (8 * (j % 4));
+        *reinterpret_cast<uint2*>(block + L::value(d) + first) = make_uint2(q[0], q[1]);
+        continue;                                                      // what the next round writes before its first barrier nobody reads any more
+    }
+    const bool in0 = run_of[row] != kNobody, in1 = row < 15 && run_of[16 + row] != kNobody;
+    float y[2][8];                                                     // of the token 16 further on
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        raw[u].clear();
+        if (in1) raw[u].load(from(u, base + 16 + row, head), aligned);
+        float m = raw[u].floats(y[u]);
+#pragma unroll
+        for (uint32_t o = 1; o < kPerRow; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        if (part == 0) most[u][16 + row] = m;
+    }
+    __syncthreads();
+    if (tid < 2 * runs.many) {
+        const uint32_t run = tid / 2, u = tid % 2;
+        const bool begins = runs.token[run][0] != kNobody;             // the block's first token is among them: nothing is held
+        const float old = begins ? 0.0f : runs.old[u][run];
         float m = 0.0f;
-        for (uint32_t i = 0; i < 16; ++i)
-            if (r.token[i] != kNobody) m = fmaxf(m, most[r.token[i]]);
-        r.now = fmaxf(r.old, scale_for(m));
-        for (uint32_t i = 0; i < 16; ++i)
-            if (r.token[i] != kNobody) most[r.token[i]] = r.now;
-        if (r.now != r.old || r.begins) *reinterpret_cast<float*>(p.cache + r.block + L::kScale + (is_value ? 4 : 0)) = r.now;
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i) {
+            const uint32_t t = runs.token[run][i];
+            m = fmaxf(m, t != kNobody ? most[u][t] : 0.0f);
+        }
+        const float now = fmaxf(old, scale_for(m));
+        runs.old[u][run] = old;
+        runs.now[u][run] = now;
+        if (now != old || begins) *reinterpret_cast<float*>(p.cache + runs.block[run] + L::kScale + 4 * u) = now;
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-        if (u ? in1 : in0) {
-            const float scale = most[16 * u + row];
-            const float by = scale > 0.0f ? __int_as_float((254 << 23) - __float_as_int(scale)) : 0.0f;      // 1 / scale
-            uint2 q;
-            q.x = e4m3_pair(x[u][0] * by, x[u][1] * by) | e4m3_pair(x[u][2] * by, x[u][3] * by) << 16;
-            q.y = e4m3_pair(x[u][4] * by, x[u][5] * by) | e4m3_pair(x[u][6] * by, x[u][7] * by) << 16;
-            if (!(scale > 0.0f)) q = make_uint2(0, 0);                 // -0 among them
-            *reinterpret_cast<uint2*>(&held[16 * u + row][8 * part]) = q;
-        }
+    for (int u = 0; u < 2; ++u) {
+        if (in0) *reinterpret_cast<uint2*>(&held[u][row][8 * part]) = rounded(x[u], runs.now[u][run_of[row]]);
+        if (in1) *reinterpret_cast<uint2*>(&held[u][16 + row][8 * part]) = rounded(y[u], runs.now[u][run_of[16 + row]]);
+    }
     __syncthreads();
-    for (uint32_t i = tid; i < many_runs * D; i += kThreads) {
-        const Run& r = runs[i / D];
-        const uint32_t at = i % D;
-        const bool again = !r.begins && r.now != r.old;                // what is there is rounded again
-        const float by = r.old > 0.0f ? r.old / r.now : 0.0f;
-        if (!is_value) {
-            const uint32_t place = at % 16, c = at / 16;
-            uint4* to = reinterpret_cast<uint4*>(p.cache + r.block + L::key(place, c));
-            if (r.token[place] != kNobody) {
-                *to = *reinterpret_cast<const uint4*>(&held[r.token[place]][16 * c]);
+    // 2 D pieces of 16 bytes a run: its keys (place, 16 dims), then its values (dim, 16 places)
+    for (uint32_t i = tid; i < runs.many * 2 * D; i += kThreads) {
+        const uint32_t run = i / (2 * D), u = i / D % 2, at = i % D;
+        const uint8_t* token = runs.token[run];
+        const float old = runs.old[u][run], now = runs.now[u][run], by = old > 0.0f ? old / now : 0.0f;
+        const bool again = token[0] == kNobody && now != old;          // what is there is rounded again
+        uint8_t* const block = p.cache + runs.block[run];
+        if (u == 0) {
+            const uint32_t place = at % 16, c = at / 16, t = token[place];
+            uint4* to = reinterpret_cast<uint4*>(block + L::key(place, c));
+            if (t != kNobody) {
+                const uint2* q = reinterpret_cast<const uint2*>(&held[0][t][16 * c]);
+                *to = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
             } else if (again) {
                 uint4 q = make_uint4(0, 0, 0, 0);
                 if (by > 0.0f) {
@@ -203,10 +278,13 @@ __global__ void __launch_bounds__(2 * D) append8_kernel(const Rows8K p, bool ali
                 *to = q;
             }
         } else {
-            uint8_t* to = p.cache + r.block + L::value(at);
-            if (again || r.many == kTileTokens) {
+            uint8_t* to = block + L::value(at);
+            bool full = true;
+#pragma unroll
+            for (uint32_t j = 0; j < 16; ++j) full = full && token[j] != kNobody;
+            if (again || full) {
                 uint32_t q[4] = {0, 0, 0, 0};
-                if (r.many < kTileTokens && by > 0.0f) {
+                if (!full && by > 0.0f) {
                     const uint4 x = *reinterpret_cast<const uint4*>(to);
                     q[0] = rounded_again(x.x, by);
                     q[1] = rounded_again(x.y, by);
@@ -215,88 +293,88 @@ __global__ void __launch_bounds__(2 * D) append8_kernel(const Rows8K p, bool ali
                 }
 #pragma unroll
                 for (uint32_t j = 0; j < 16; ++j)
-                    if (r.token[j] != kNobody) q[j / 4] = q[j / 4] & ~(0xFFu << (8 * (j % 4))) | (uint32_t)held[r.token[j]][at] << (8 * (j % 4));
+                    if (token[j] != kNobody) q[j / 4] = q[j / 4] & ~(0xFFu << (8 * (j % 4))) | (uint32_t)held[1][token[j]][at] << (8 * (j % 4));
                 *reinterpret_cast<uint4*>(to) = make_uint4(q[0], q[1], q[2], q[3]);
             } else {
                 for (uint32_t j = 0; j < 16; ++j)
-                    if (r.token[j] != kNobody) to[j] = held[r.token[j]][at];
+                    if (token[j] != kNobody) to[j] = held[1][token[j]][at];
             }
         }
     }
+    if (round + gridDim.x < rounds) fetch(round + gridDim.x);
+    __syncthreads();
+    }
 }
 
-// The inverse. A CTA reads 16 tokens of the call, one head, keys or values; values by way of shared memory, 16 bytes (a dim of 16 tokens) at a
-// time where the tokens are a whole block in order.
+// The inverse. A CTA reads 16 tokens of the call, one head; values by way of shared memory, 8 bytes (a dim of 8 tokens) at a time where the tokens are a whole
+// block in order.
 template <int D, typename T>
 __global__ void __launch_bounds__(2 * D) read8_kernel(const Rows8K p, T* __restrict__ k, T* __restrict__ v)
 {
     using L = Tile8<D>;
-    constexpr uint32_t kThreads = 2 * D, kPerRow = D / 8;
+    constexpr uint32_t kThreads = 2 * D, kPerRow = D / 8, kStride = D + 8;
     __shared__ uint64_t block[16];
-    __shared__ uint32_t place[16];
-    __shared__ float scale[16];                                        // -1: no such token
-    __shared__ alignas(16) uint8_t held[16][D + 16];
-    __shared__ uint32_t whole;
-    const uint32_t tid = threadIdx.x, row = tid / kPerRow, part = tid % kPerRow, head = blockIdx.y, base = blockIdx.x * 16;
-    const bool is_value = blockIdx.z;
+    __shared__ uint32_t place[16];                                     // ~0: no such token
+    __shared__ alignas(16) uint8_t held[16][kStride];
+    __shared__ bool whole;
+    const uint32_t tid = threadIdx.x, row = tid / kPerRow, part = tid % kPerRow, group = p.by_heads.of(blockIdx.x), head = blockIdx.x - group * p.heads, base = group * 16;
     if (tid < 32) {
         const uint32_t t = base + tid;
         const int64_t s = tid < 16 && t < p.tokens ? __ldg(p.slots + t) : -1;
         const bool there = s >= 0 && (uint64_t)s < p.slots_in_cache;
         if (tid < 16) {
-            float f = -1.0f;
-            if (there) {
-                block[tid] = block_at<D>((uint64_t)s, head, p);
-                place[tid] = (uint32_t)(s % kTileTokens);
-                f = *reinterpret_cast<const float*>(p.cache + block[tid] + L::kScale + (is_value ? 4 : 0));
-            }
-            scale[tid] = f;
+            block[tid] = there ? block_at<D>((uint64_t)s, head, p) : 0;
+            place[tid] = there ? (uint32_t)(s % kTileTokens) : ~0u;
         }
         const int64_t first = __shfl_sync(0xFFFFFFFFu, s, 0);
         const bool in_order = __all_sync(0xFFFFFFFFu, tid >= 16 || (there && s == first + tid && first % kTileTokens == 0));
         if (tid == 0) whole = in_order;
     }
     __syncthreads();
-    if (is_value) {
-        if (whole) {
-            for (uint32_t d = tid; d < D; d += kThreads) {
-                const uint4 q = __ldg(reinterpret_cast<const uint4*>(p.cache + block[0] + L::value(d)));
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    const bool there = place[row] != ~0u;
+    const uint8_t* const mine = p.cache + block[row];
+    uint2 q[2] = {make_uint2(0, 0), make_uint2(0, 0)};
+    float2 scale = make_float2(0.0f, 0.0f);
+    if (there) {
+        q[0] = __ldg(reinterpret_cast<const uint2*>(mine + L::key(place[row], part / 2) + 8 * (part % 2)));
+        scale = __ldg(reinterpret_cast<const float2*>(mine + L::kScale));
+    }
+    if (whole) {
+        const uint32_t d = tid / 2, first = tid % 2 * 8;
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(p.cache + block[0] + L::value(d) + first));
 #pragma unroll
-                for (uint32_t i = 0; i < 16; ++i) held[i][d] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
-            }
-        } else {
-            for (uint32_t i = tid; i < 16 * D; i += kThreads) {
-                const uint32_t t = i / D, d = i % D;
-                if (scale[t] >= 0.0f) held[t][d] = p.cache[block[t] + L::value(d) + place[t]];
-            }
+        for (uint32_t j = 0; j < 8; ++j) held[first + j][d] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j % 4)));
+    } else {
+        for (uint32_t i = tid; i < 16 * D; i += kThreads) {
+            const uint32_t t = i / D, d = i % D;
+            if (place[t] != ~0u) held[t][d] = p.cache[block[t] + L::value(d) + place[t]];
         }
-        __syncthreads();
     }
+    __syncthreads();
     if (base + row >= p.tokens) return;
-    const float s = scale[row];
-    uint2 q = make_uint2(0, 0);
-    if (s >= 0.0f) {
-        if (is_value) q = *reinterpret_cast<const uint2*>(&held[row][8 * part]);
-        else q = __ldg(reinterpret_cast<const uint2*>(p.cache + block[row] + L::key(place[row], part / 2) + 8 * (part % 2)));
-    }
-    const float by = fmaxf(s, 0.0f);
-    alignas(16) T e[8];
+    if (there) q[1] = *reinterpret_cast<const uint2*>(&held[row][8 * part]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = floats_of_e4m3((i < 2 ? q.x : q.y) >> (16 * (i % 2)) & 0xFFFFu);
-        put(e + 2 * i, f.x * by);
-        put(e + 2 * i + 1, f.y * by);
-    }
-    uint4* to = reinterpret_cast<uint4*>((is_value ? v : k) + ((uint64_t)(base + row) * p.heads + head) * D + 8 * part);
+    for (int u = 0; u < 2; ++u) {
+        const float by = u ? scale.y : scale.x;
+        alignas(16) T e[8];
 #pragma unroll
-    for (uint32_t i = 0; i < sizeof(e) / 16; ++i) to[i] = reinterpret_cast<uint4*>(e)[i];
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = floats_of_e4m3((i < 2 ? q[u].x : q[u].y) >> (16 * (i % 2)) & 0xFFFFu);
+            put(e + 2 * i, f.x * by);
+            put(e + 2 * i + 1, f.y * by);
+        }
+        uint4* to = reinterpret_cast<uint4*>((u ? v : k) + ((uint64_t)(base + row) * p.heads + head) * D + 8 * part);
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(e) / 16; ++i) to[i] = reinterpret_cast<uint4*>(e)[i];
+    }
 }
 
 template <int D, typename T>
 int launch_append(const Rows8K& p, bool aligned, cudaStream_t st)
 {
-    append8_kernel<D, T><<<dim3((p.tokens + 15) / 16, p.heads, 2), 2 * D, 0, st>>>(p, aligned);
+    // as many CTAs as are resident, each with the next round's loads under way
+    const uint32_t rounds = (p.tokens + 15) / 16 * p.heads, resident = 148 * (1024 / (2 * D));
+    append8_kernel<D, T><<<rounds < resident ? rounds : resident, 2 * D, 0, st>>>(p, rounds, aligned);
     KVP_CUDA(cudaGetLastError());
     return KVP_OK;
 }
@@ -304,7 +382,7 @@ int launch_append(const Rows8K& p, bool aligned, cudaStream_t st)
 template <int D, typename T>
 int launch_read(const Rows8K& p, void* k, void* v, cudaStream_t st)
 {
-    read8_kernel<D, T><<<dim3((p.tokens + 15) / 16, p.heads, 2), 2 * D, 0, st>>>(p, static_cast<T*>(k), static_cast<T*>(v));
+    read8_kernel<D, T><<<(p.tokens + 15) / 16 * p.heads, 2 * D, 0, st>>>(p, static_cast<T*>(k), static_cast<T*>(v));
     KVP_CUDA(cudaGetLastError());
     return KVP_OK;
 }
@@ -316,7 +394,7 @@ int check_rows(const kvp_cache_shape* c, const void* cache, uint32_t tokens, con
     if (!head_dim_served(c->head_dim)) return KVP_ERR_RANGE;
     if (tokens && (!cache || !a || !b || !slots)) return KVP_ERR_ARG;
     if (off_by(cache, 16) || off_by(a, rows_align) || off_by(b, rows_align) || off_by(slots, 8)) return KVP_ERR_ARG;
-    if (c->kv_heads > 65535 || tokens >= (1u << 31)) return KVP_ERR_RANGE;
+    if (c->kv_heads > 65535 || tokens >= (1u << 31) || (uint64_t)(tokens / 16 + 1) * c->kv_heads >= (1u << 31)) return KVP_ERR_RANGE;
     return KVP_OK;
 }
 
@@ -357,7 +435,7 @@ extern "C" int kvp_cache8_append(const kvp_cache_shape* c, void* cache, uint32_t
     p.k_token = k_token_stride; p.k_head = k_head_stride; p.v_token = v_token_stride; p.v_head = v_head_stride;
     p.slots = slots; p.cache = static_cast<uint8_t*>(cache);
     p.slots_in_cache = (uint64_t)c->pages * c->page_tokens;
-    p.tokens = tokens; p.heads = c->kv_heads; p.page_tokens = c->page_tokens;
+    p.tokens = tokens; p.heads = c->kv_heads; p.page_tokens = c->page_tokens; p.by_heads = divisor(c->kv_heads);
     const uint64_t e = dtype == KVP_F32 ? 4 : 2;
     const uint64_t low = (uint64_t)(uintptr_t)k | (uint64_t)(uintptr_t)v | (uint64_t)k_token_stride * e | (uint64_t)k_head_stride * e |
                          (uint64_t)v_token_stride * e | (uint64_t)v_head_stride * e;
@@ -376,7 +454,7 @@ extern "C" int kvp_cache8_read(const kvp_cache_shape* c, const void* cache, uint
     Rows8K p = {};
     p.slots = slots; p.cache = static_cast<uint8_t*>(const_cast<void*>(cache));
     p.slots_in_cache = (uint64_t)c->pages * c->page_tokens;
-    p.tokens = tokens; p.heads = c->kv_heads; p.page_tokens = c->page_tokens;
+    p.tokens = tokens; p.heads = c->kv_heads; p.page_tokens = c->page_tokens; p.by_heads = divisor(c->kv_heads);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
 #define KVP_READ(D, T) launch_read<D, T>(p, k, v, st)
     KVP_BY_SHAPE(KVP_READ)

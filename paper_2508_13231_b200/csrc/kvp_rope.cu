@@ -10,6 +10,7 @@
 #include <cuda_fp16.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "kvp_line.cuh"
 
@@ -26,7 +27,7 @@ struct RopeK {
     uint32_t tokens, heads, all_heads, per;       // per: heads of a thread
     uint32_t half;                                // pairs of a head
     uint32_t turned;                              // chunks of a head that are turned; those behind are copied
-    Divisor chunks;
+    Divisor chunks, groups;                       // of a thread's number, of a CTA's
     float scale;
     bool inverse;
 };
@@ -38,9 +39,46 @@ __device__ __forceinline__ void round_to(float* p, float x) { *p = x; }
 __device__ __forceinline__ void round_to(__half* p, float x) { *p = __float2half_rn(x); }
 __device__ __forceinline__ void round_to(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
+// V elements of a load, kept as they lie: 16 bytes, or one element
 template <typename T, int V>
-struct alignas(V * sizeof(T)) Vec {
-    T e[V];
+struct Vec {
+    uint4 w;
+    __device__ __forceinline__ void load(const T* p) { w = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = w; }
+    __device__ __forceinline__ uint32_t& word(int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; }
+    __device__ __forceinline__ void get(float* x)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t u = word(i);
+            if constexpr (sizeof(T) == 4) {
+                x[i] = __uint_as_float(u);
+            } else if constexpr (std::is_same<T, __half>::value) {
+                const float2 f = __half22float2(half2_of(u));
+                x[2 * i] = f.x;
+                x[2 * i + 1] = f.y;
+            } else {
+                x[2 * i] = __uint_as_float(u << 16);
+                x[2 * i + 1] = __uint_as_float(u & 0xFFFF0000u);
+            }
+        }
+    }
+    __device__ __forceinline__ void put(const float* x)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) word(i) = __float_as_uint(x[i]);
+            else word(i) = out_pair<std::is_same<T, __half>::value>(x[2 * i], x[2 * i + 1]);
+        }
+    }
+};
+template <typename T>
+struct Vec<T, 1> {
+    T e;
+    __device__ __forceinline__ void load(const T* p) { e = *p; }
+    __device__ __forceinline__ void store(T* p) const { *p = e; }
+    __device__ __forceinline__ void get(float* x) { x[0] = float_of(e); }
+    __device__ __forceinline__ void put(const float* x) { round_to(&e, x[0]); }
 };
 
 __device__ __forceinline__ void turn_of(int32_t position, double frequency, float scale, bool inverse, float& c, float& s)
@@ -60,17 +98,19 @@ __device__ __forceinline__ void turn_of(int32_t position, double frequency, floa
     s *= inverse ? -scale : scale;
 }
 
-// V: elements of a load (1: any alignment and sizes). A chunk is V pairs (halves) or V elements, V / 2 pairs, side by side (interleaved); blockIdx.y takes
-// `per` heads, queries before keys.
+// V: elements of a load (1: any alignment and sizes). A chunk is V pairs (halves) or V elements, V / 2 pairs, side by side (interleaved); a CTA takes
+// `per` heads of 256 chunks, queries before keys.
 template <typename T, int V, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) rope_kernel(const RopeK p)
 {
     constexpr int kPairs = INTERLEAVED && V > 1 ? V / 2 : V;
     constexpr bool kTwo = !(INTERLEAVED && V > 1);                     // two loads for a chunk
+    constexpr uint32_t kBatch = 4;
     using W = Vec<T, V>;
-    const uint32_t i = blockIdx.x * 256 + threadIdx.x, t = p.chunks.of(i), chunk = i - t * p.chunks.d;
+    const uint32_t block = p.groups.of(blockIdx.x), group = blockIdx.x - block * p.groups.d;       // heads of the same tokens at the same time, as they lie in memory
+    const uint32_t i = block * 256 + threadIdx.x, t = p.chunks.of(i), chunk = i - t * p.chunks.d;
     if (t >= p.tokens) return;
-    const uint32_t first = blockIdx.y * p.per, last = min(first + p.per, p.all_heads);
+    const uint32_t first = group * p.per, last = min(first + p.per, p.all_heads);
     const bool turned = chunk < p.turned;
     uint32_t at0, at1 = 0;
     float c[kPairs], s[kPairs];
@@ -83,32 +123,42 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeK p)
     } else {
         at0 = 2 * p.half + (chunk - p.turned) * V;
     }
-#pragma unroll 4
-    for (uint32_t h = first; h < last; ++h) {
-        const bool is_q = h < p.heads;
-        const T* from = is_q ? static_cast<const T*>(p.q) + t * p.q_token + h * p.q_head : static_cast<const T*>(p.k) + t * p.k_token + (h - p.heads) * p.k_head;
-        T* to = is_q ? static_cast<T*>(p.q_out) + t * p.qo_token + h * p.qo_head : static_cast<T*>(p.k_out) + t * p.ko_token + (h - p.heads) * p.ko_head;
-        W x = *reinterpret_cast<const W*>(from + at0);
-        if (turned) {
-            if (kTwo) {
-                W y = *reinterpret_cast<const W*>(from + at1);
+    // Loads of four heads before the first store: results may lie over what is read, so the compiler keeps their order.
+    for (uint32_t h0 = first; h0 < last; h0 += kBatch) {
+        W x[kBatch], y[kBatch];
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float a = float_of(x.e[j]), b = float_of(y.e[j]);
-                    round_to(&x.e[j], a * c[j] - b * s[j]);
-                    round_to(&y.e[j], a * s[j] + b * c[j]);
-                }
-                *reinterpret_cast<W*>(to + at1) = y;
-            } else {
-#pragma unroll
-                for (int j = 0; j < kPairs; ++j) {
-                    const float a = float_of(x.e[2 * j]), b = float_of(x.e[2 * j + 1]);
-                    round_to(&x.e[2 * j], a * c[j] - b * s[j]);
-                    round_to(&x.e[2 * j + 1], a * s[j] + b * c[j]);
-                }
+        for (uint32_t k = 0; k < kBatch; ++k)
+            if (h0 + k < last) {
+                const uint32_t h = h0 + k;
+                const T* from = h < p.heads ? static_cast<const T*>(p.q) + t * p.q_token + h * p.q_head : static_cast<const T*>(p.k) + t * p.k_token + (h - p.heads) * p.k_head;
+                x[k].load(from + at0);
+                if (kTwo && turned) y[k].load(from + at1);
             }
-        }
-        *reinterpret_cast<W*>(to + at0) = x;
+#pragma unroll
+        for (uint32_t k = 0; k < kBatch; ++k)
+            if (h0 + k < last) {
+                const uint32_t h = h0 + k;
+                T* to = h < p.heads ? static_cast<T*>(p.q_out) + t * p.qo_token + h * p.qo_head : static_cast<T*>(p.k_out) + t * p.ko_token + (h - p.heads) * p.ko_head;
+                if (turned) {
+                    float u[V], v[V];
+                    x[k].get(u);
+                    if (kTwo) y[k].get(v);
+#pragma unroll
+                    for (int j = 0; j < kPairs; ++j) {
+                        float& a = u[kTwo ? j : 2 * j];
+                        float& b = kTwo ? v[j] : u[kTwo ? 0 : 2 * j + 1];
+                        const float new_a = a * c[j] - b * s[j], new_b = a * s[j] + b * c[j];
+                        a = new_a;
+                        b = new_b;
+                    }
+                    x[k].put(u);
+                    if (kTwo) {
+                        y[k].put(v);
+                        y[k].store(to + at1);
+                    }
+                }
+                x[k].store(to + at0);
+            }
     }
 }
 
@@ -121,16 +171,16 @@ int launch_rope(RopeK k, const kvp_rope_params* a, bool copies, cudaStream_t st)
     k.chunks = divisor(chunks);
     if ((uint64_t)k.tokens * chunks >= (1ull << 31) - 256) return KVP_ERR_RANGE;
     // As many heads a thread as leave about eight warps for each of an SM's four schedulers: few tokens spread over the GPU (a decode step is latency), many share
-    // the sines and cosines of ten heads.
+    // the sines and cosines of eight heads, two batches of loads.
     const uint64_t threads = (uint64_t)k.tokens * chunks;
     uint64_t per = threads * k.all_heads / (148 * 1024);
-    per = per < 1 ? 1 : per > 10 ? 10 : per;
-    uint64_t groups = (k.all_heads + per - 1) / per;
-    if (groups > 65535) groups = 65535;
-    k.per = (uint32_t)((k.all_heads + groups - 1) / groups);
-    const dim3 grid((uint32_t)((threads + 255) / 256), (k.all_heads + k.per - 1) / k.per);
-    if (interleaved) rope_kernel<T, V, true><<<grid, 256, 0, st>>>(k);
-    else rope_kernel<T, V, false><<<grid, 256, 0, st>>>(k);
+    per = per < 1 ? 1 : per < 4 ? per : per < 8 ? 4 : 8;
+    k.per = (uint32_t)per;
+    k.groups = divisor((k.all_heads + k.per - 1) / k.per);
+    const uint64_t grid = (threads + 255) / 256 * k.groups.d;
+    if (grid >= (1ull << 31)) return KVP_ERR_RANGE;
+    if (interleaved) rope_kernel<T, V, true><<<(uint32_t)grid, 256, 0, st>>>(k);
+    else rope_kernel<T, V, false><<<(uint32_t)grid, 256, 0, st>>>(k);
     KVP_CUDA(cudaGetLastError());
     return KVP_OK;
 }

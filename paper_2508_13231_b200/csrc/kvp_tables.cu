@@ -119,6 +119,7 @@ __global__ void __launch_bounds__(kScanThreads) tables_kernel(const TablesK p, b
             const uint32_t l = __ffs(left) - 1, many = __shfl_sync(0xFFFFFFFFu, had, l);
             const int32_t* row = p.table + (uint64_t)(base + tid - lane + l) * p.table_pages;
             uint32_t good = 0;
+#pragma unroll 8
             for (uint32_t j = lane; j < many; j += 32) good += (uint32_t)row[j] < p.pages;
             good = __reduce_add_sync(0xFFFFFFFFu, good);
             if (lane == l) own = good;
@@ -144,11 +145,16 @@ __global__ void __launch_bounds__(kScanThreads) tables_kernel(const TablesK p, b
                 const uint32_t l = __ffs(left) - 1, many = __shfl_sync(0xFFFFFFFFu, had, l);
                 const int32_t* row = p.table + (uint64_t)(base + tid - lane + l) * p.table_pages;
                 uint32_t to = head + count + back + __shfl_sync(0xFFFFFFFFu, sum.a - own, l);
-                for (uint32_t j0 = 0; j0 < many; j0 += 32) {
-                    const int32_t page = j0 + lane < many ? row[j0 + lane] : -1;
-                    const uint32_t good = __ballot_sync(0xFFFFFFFFu, (uint32_t)page < p.pages);
-                    if (good >> lane & 1u) p.ring[(to + __popc(good & ((1u << lane) - 1u))) % p.pages] = page;
-                    to += __popc(good);
+                for (uint32_t j0 = 0; j0 < many; j0 += 256) {   // eight loads under way
+                    int32_t page[8];
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; ++k) page[k] = j0 + 32 * k + lane < many ? row[j0 + 32 * k + lane] : -1;
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; ++k) {
+                        const uint32_t good = __ballot_sync(0xFFFFFFFFu, (uint32_t)page[k] < p.pages);
+                        if (good >> lane & 1u) p.ring[(to + __popc(good & ((1u << lane) - 1u))) % p.pages] = page[k];
+                        to += __popc(good);
+                    }
                 }
             }
             back += all.a;
