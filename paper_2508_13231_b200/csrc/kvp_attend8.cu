@@ -81,6 +81,7 @@ __global__ void __launch_bounds__(kThreads) count8_kernel(const Attend8K p)
 {
     __shared__ uint32_t sum[kWarps];
     let_next_start();
+    wait_for_previous();
     const uint32_t bh = blockIdx.x, tid = threadIdx.x;
     const uint32_t len = length_of(p, p.heads.of(bh)), units = units_of(p, len), tiles = tiles_of(len);
     const uint32_t k = p.unit > kTileTokens ? p.unit / kTileTokens : 1;
@@ -142,41 +143,7 @@ struct Shape8 {
     static_assert(kValueStages >= 2 && kColsUsed <= 512 && kQCols <= 256 && kPCols <= 256, "does not fit");
 };
 
-template <class S>
-struct Smem8 {
-    uint64_t keys[S::kKeyStages], keys_free[S::kKeyStages];            // a stage has come; its products are done
-    uint64_t values[S::kValueStages], values_free[S::kValueStages];
-    uint64_t scored[2], taken[2];                      // scores are in tensor memory; they are in registers
-    uint64_t weighed[2], summed[2];                    // weights are in shared memory; the products with values are done
-    uint64_t query;                                    // a segment's queries are in shared memory
-    uint32_t tensor, gave_up;
-    LineSmem line;
-    uint32_t tile[S::kValueStages][kGroup];            // numbers of a stage's tiles; ~0: not there
-    alignas(16) float factor[S::ROWS];                 // per row: what scores are multiplied by,
-    float slope[S::ROWS];                              // its bias a token,
-    int32_t see[S::ROWS];                              // the tokens that it sees are before this one
-    alignas(16) float top[S::kTeams][S::kRowsEach];    // what scores are taken less: the running maximum, 0 before a row has seen a token
-    alignas(16) float by[S::kTeams][S::kRowsEach];     // what sums are multiplied by when it moves; at the end of a segment see `last`
-    float peak[S::kTeams][4][S::kRowsEach];            // of each warp: how far its scores pass it; at the end its sum of weights
-    float scale[S::kTeams][4];                         // of each warp: the largest scale of its values
-    float2 last[S::kTeams][S::kRowsEach];              // of each turn's row: its factor, and the reciprocal of the row's sum
-    uint16_t list[kListCap8];                          // units of 32 words of a bitmap's row
-};
-
-// Number of a ring's place and the parity of its turn.
-template <uint32_t N>
-struct Ring {
-    uint32_t at = 0, parity = 0;
-    __device__ __forceinline__ void next()
-    {
-        if (++at == N) {
-            at = 0;
-            parity ^= 1u;
-        }
-    }
-};
-
-// The segments of this CTA's part, one after the other; each warp goes through them by itself.
+// The segments of this CTA's part, one after the other; each of the warps that are in no team goes through them by itself, the teams together.
 struct Walk {
     uint32_t todo, per, entries, entry, inner, at_place, count;
     uint32_t seg, bh, rt, b, h, len, off, take, tiles;
@@ -213,6 +180,42 @@ struct Walk {
             return true;
         }
         return false;
+    }
+};
+
+template <class S>
+struct Smem8 {
+    uint64_t keys[S::kKeyStages], keys_free[S::kKeyStages];            // a stage has come; its products are done
+    uint64_t values[S::kValueStages], values_free[S::kValueStages];
+    uint64_t scored[2], taken[2];                      // scores are in tensor memory; they are in registers
+    uint64_t weighed[2], summed[2];                    // weights are in shared memory; the products with values are done
+    uint64_t query;                                    // a segment's queries are in shared memory
+    uint32_t tensor, gave_up;
+    LineSmem line;
+    Walk walk[2];                                      // the teams': this segment, and the next one
+    bool more[2];
+    uint32_t tile[S::kValueStages][kGroup];            // numbers of a stage's tiles; ~0: not there
+    alignas(16) float factor[S::ROWS];                 // per row: what scores are multiplied by,
+    float slope[S::ROWS];                              // its bias a token,
+    int32_t see[S::ROWS];                              // the tokens that it sees are before this one
+    alignas(16) float top[S::kTeams][S::kRowsEach];    // what scores are taken less: the running maximum, 0 before a row has seen a token
+    alignas(16) float by[S::kTeams][S::kRowsEach];     // what sums are multiplied by when it moves; at the end of a segment see `last`
+    float peak[S::kTeams][4][S::kRowsEach];            // of each warp: how far its scores pass it; at the end its sum of weights
+    float scale[S::kTeams][4];                         // of each warp: the largest scale of its values
+    float2 last[S::kTeams][S::kRowsEach];              // of each turn's row: its factor, and the reciprocal of the row's sum
+    uint16_t list[kListCap8];                          // units of 32 words of a bitmap's row
+};
+
+// Number of a ring's place and the parity of its turn.
+template <uint32_t N>
+struct Ring {
+    uint32_t at = 0, parity = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++at == N) {
+            at = 0;
+            parity ^= 1u;
+        }
     }
 };
 
@@ -358,6 +361,11 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
             walk.at_place = ((uint32_t)begin - line.before) - walk.inner * (line.count + kFixed8);
         }
     }
+    bool more = walk.next<ROWS>(p);
+    if (tid == 0) {
+        sm.walk[0] = walk;
+        sm.more[0] = more;
+    }
     uint8_t* const value_room = room + S::kKeyStages * S::kKeyStage;
     uint8_t* const queries = value_room + S::kValueStages * S::kValueStage;
     uint8_t* const weights = queries + S::kQBytes;
@@ -374,7 +382,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
             uint32_t it = 0;
             Ring<S::kKeyStages> ks;
             Ring<S::kValueStages> vs;
-            while (ok && walk.next<ROWS>(p)) {
+            for (; ok && more; more = walk.next<ROWS>(p)) {
                 const int32_t* table = p.table + (uint64_t)walk.b * p.table_pages;
                 const Visible seen = p.units ? Visible{0, 0} : visible_tiles(p, walk.len);
                 // a bitmap's row: `chunk` of 32 words is listed, before it stand `base` tiles of the row, in it `here`
@@ -405,13 +413,12 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     }
                     list_chunk();
                 }
-                for (uint32_t g = 0; g < walk.tiles; g += kGroup, ++it) {
-                    // which tiles, and where they lie; lanes 8 .. 15 do as 0 .. 7, for the values. The last ones come first: a bias by distance favours them, and
-                    // the maximum then seldom moves.
-                    const uint32_t n = g + lane % kGroup;
-                    const bool mine = lane < 2 * kGroup && n < walk.tiles;
-                    const uint32_t i = walk.off + walk.tiles - 1 - n;
-                    uint32_t tile = 0;
+                // Which tiles, and their pages, a lane each, 32 ahead of where they are needed: under load an entry of the table takes 2 us. The last ones come first: a
+                // bias by distance favours them, and the maximum then seldom moves.
+                const auto look = [&](uint32_t n0, uint32_t& tile, uint32_t& page) {
+                    const bool mine = n0 + lane < walk.tiles;
+                    const uint32_t i = walk.off + walk.tiles - 1 - (n0 + lane);
+                    tile = 0;
                     if (p.units) {
                         bool left = mine;
                         while (true) {
@@ -427,11 +434,21 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     } else {
                         tile = i < seen.head ? i : i + seen.skip;
                     }
-                    const uint8_t* from = nullptr;
-                    if (mine) {
-                        const uint32_t page = p.page_tiles.of(tile), pg = (uint32_t)__ldg(table + page);
-                        if (pg < p.pages) from = p.cache + (((uint64_t)pg * p.heads.d + walk.h) * p.page_tiles.d + (tile - page * p.page_tiles.d)) * L::kBytes;
+                    page = mine ? (uint32_t)__ldg(table + p.page_tiles.of(tile)) : ~0u;
+                };
+                uint32_t tiles = 0, pages = 0, next_tiles = 0, next_pages = 0;
+                if (walk.tiles) look(0, next_tiles, next_pages);
+                for (uint32_t g = 0; g < walk.tiles; g += kGroup, ++it) {
+                    if (g % 32 == 0) {
+                        tiles = next_tiles;
+                        pages = next_pages;
+                        if (g + 32 < walk.tiles) look(g + 32, next_tiles, next_pages);
                     }
+                    // lanes 8 .. 15 do as 0 .. 7, for the values
+                    const uint32_t tile = __shfl_sync(0xFFFFFFFFu, tiles, g % 32 + lane % kGroup), page = __shfl_sync(0xFFFFFFFFu, pages, g % 32 + lane % kGroup);
+                    const uint8_t* from = nullptr;
+                    if (lane < 2 * kGroup && page < p.pages)
+                        from = p.cache + (((uint64_t)page * p.heads.d + walk.h) * p.page_tiles.d + (tile - p.page_tiles.of(tile) * p.page_tiles.d)) * L::kBytes;
                     const uint32_t many = __popc(__ballot_sync(0xFFFFFFFFu, from != nullptr) & 0xFFu);
                     if (it >= S::kKeyStages) ok = __all_sync(0xFFFFFFFFu, barrier_wait(bar(sm.keys_free[ks.at]), ks.parity ^ 1u, gave_up));
                     if (!ok) break;
@@ -463,7 +480,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
             bool ok = true;
             Ring<S::kKeyStages> ks;
             Ring<S::kScoreBufs> sb;
-            for (; ok && walk.next<ROWS>(p); ++segment) {
+            for (; ok && more; ++segment, more = walk.next<ROWS>(p)) {
                 ok = barrier_wait(bar(sm.query), segment & 1u, gave_up);
                 for (uint32_t g = 0; ok && g < walk.tiles; g += kGroup, ++it) {
                     ok = barrier_wait(bar(sm.keys[ks.at]), ks.parity, gave_up) && (it < S::kScoreBufs || barrier_wait(bar(sm.taken[sb.at]), sb.parity ^ 1u, gave_up));
@@ -484,7 +501,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
             bool ok = true;
             Ring<S::kValueStages> vs;
             Ring<2> pb;
-            while (ok && walk.next<ROWS>(p)) {
+            for (; ok && more; more = walk.next<ROWS>(p)) {
                 for (uint32_t g = 0; g < walk.tiles; g += kGroup) {
                     const uint32_t pairs = (min(walk.tiles - g, kGroup) + 1) / 2;
                     ok = barrier_wait(bar(sm.values[vs.at]), vs.parity, gave_up) && barrier_wait(bar(sm.weighed[pb.at]), pb.parity, gave_up);
@@ -516,7 +533,13 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
         Ring<S::kValueStages> vs;
         Ring<S::kScoreBufs> sb;
         Ring<2> pb;
-        while (walk.next<ROWS>(p)) {
+        for (uint32_t side = 0; sm.more[side]; side ^= 1u) {
+            const Walk& walk = sm.walk[side];                  // not in registers: the loop over groups needs them
+            if (tid == 32 * kOthers) {
+                Walk ahead = walk;
+                sm.more[side ^ 1u] = ahead.next<ROWS>(p);
+                sm.walk[side ^ 1u] = ahead;
+            }
             // the queries: kEach threads a row
             {
                 constexpr uint32_t kFew = 128 * S::kTeams / ROWS, kEach = kFew < D / 8 ? kFew : D / 8, kVecs = D / 8 / kEach;
@@ -545,8 +568,8 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
                     odd += __shfl_xor_sync(0xFFFFFFFFu, odd, o);
                 }
-                // largest magnitude in [2^7, 2^8); the power of two in two factors, either of them a normal number
-                const int e = most > 0.0f && most < INFINITY ? ilogbf(most) - 7 : 0, half_e = -e / 2;
+                // largest magnitude in [2^7, 2^8), or below it where it is not a normal number; the power of two in two factors, either of them a normal number
+                const int e = (__float_as_int(most) >> 23) - 127 - 7, half_e = -e / 2;
                 const float by0 = __int_as_float((half_e + 127) << 23), by1 = __int_as_float((-e - half_e + 127) << 23);
 #pragma unroll
                 for (uint32_t v = 0; v < kVecs; ++v) {
@@ -568,7 +591,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 }
                 if (mine && j == 0) {
                     const float unit = p.cap > 0.0f ? p.scale / p.cap : p.scale * kLog2e;      // scores in units of the cap, or to the base 2
-                    sm.factor[row] = scalbnf(unit, e) + odd;
+                    sm.factor[row] = unit * __int_as_float((127 - half_e) << 23) * __int_as_float((127 + e + half_e) << 23) + odd;
                     sm.slope[row] = p.slopes && r < p.rows ? __ldg(p.slopes + walk.h * p.group.d + (r - query * p.group.d)) * kLog2e : 0.0f;
                     sm.see[row] = (int32_t)walk.len - (int32_t)p.queries + 1 + (int32_t)query;
                 }
@@ -578,6 +601,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 if (me < R) top[me] = 0.0f;
                 teams_sync<S::kTeams>();
             }
+            const uint32_t tiles = walk.tiles, len = walk.len;
             float l[R];                                                // sums of this thread's weights
             float most_scale = 0.0f, lift_by = 0.0f;                   // largest scale of values so far, 2^6 over it
             bool any = false;                                          // has this team had a group of the segment?
@@ -588,15 +612,15 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
             for (uint32_t r = 0; r < R; ++r) l[r] = 0.0f;
             float* const mass = p.mass + (uint64_t)walk.seg * p.row_subs * ROWS + row0;
 
-            for (uint32_t g = 0; g < walk.tiles; g += kGroup, ++it, vs.next(), sb.next(), pb.next()) {
+            for (uint32_t g = 0; g < tiles; g += kGroup, ++it, vs.next(), sb.next(), pb.next()) {
                 if (S::kTurns == 2 && it % 2 != turn) continue;
-                const uint32_t j = me / 16, many = min(walk.tiles - g, kGroup);
+                const uint32_t j = me / 16, many = min(tiles - g, kGroup);
                 ok = ok && barrier_wait(bar(sm.values[vs.at]), vs.parity, gave_up);
                 uint8_t* const block = value_room + vs.at * S::kValueStage + j * L::kValueBytes;
                 const uint32_t tile = j < many ? sm.tile[vs.at][j] : ~0u;
                 const int32_t pos = (int32_t)(tile * kTileTokens + me % 16);
                 const float2 scales = *reinterpret_cast<const float2*>(block + 16 * D);        // of keys, of values
-                bool live = tile != ~0u && pos < (int32_t)walk.len;
+                bool live = tile != ~0u && pos < (int32_t)len;
                 if (live && p.units && p.unit < kTileTokens) live = bits_at(p, (uint64_t)walk.bh * p.row_units + ((uint32_t)pos >> p.unit_log2)) & 1u;
                 const float scale = live ? scales.y : 0.0f;
                 // does every row see every token of the warp?
@@ -926,8 +950,8 @@ int launch_attend8(const Attend8K& k, cudaStream_t st)
 {
     using S = Shape8<D, HALF, ROWS>;
     KVP_CUDA(cudaFuncSetAttribute(attend8_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem));
-    int rc = k.units ? launch(count8_kernel, k.batch * k.heads.d, kThreads, 0, false, st, k) : KVP_OK;
-    if (!rc) rc = launch(attend8_kernel<S>, k.ctas, S::kBlock, S::kSmem, k.units != nullptr, st, k);
+    int rc = k.units ? launch(count8_kernel, k.batch * k.heads.d, kThreads, 0, true, st, k) : KVP_OK;
+    if (!rc) rc = launch(attend8_kernel<S>, k.ctas, S::kBlock, S::kSmem, true, st, k);
     const uint64_t blocks = (uint64_t)k.batch * k.heads.d * ((k.warp_rows ? k.segs.d * (ROWS / kWarps) : k.rows) + (k.weights ? (k.row_units + kThreads - 1) / kThreads : 0));
     if (!rc) rc = launch(join_kernel<Attend8K, D / 32, HALF, ROWS>, (uint32_t)blocks, kThreads, 0, true, st, k);
     return rc;

@@ -4,7 +4,7 @@
 // the smallest power of two 2^e with |x| <= 448 * 2^e for all of them. A power of two costs nothing (e4m3 has the same four bits over 2^15 of its
 // range) and makes the form exact to handle: x / scale is exact, and when a token comes that asks for a larger scale, what
 // the block holds is divided by a power of two, which rounds only what falls below e4m3's normal numbers (2^-15 of the block's largest).
-#include <cuda_bf16.h>
+#include <type_traits>
 
 #include "kvp_line.cuh"
 #include "kvp_tile8.cuh"
@@ -26,31 +26,41 @@ struct Rows8K {
 constexpr float kMost = 0x1p100f;                 // larger magnitudes count as this
 constexpr int kLeastExp = -100;                   // of a scale
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ void put(float* p, float x) { *p = x; }
-__device__ __forceinline__ void put(__half* p, float x) { *p = __float2half_rn(x); }
-__device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
-
 // eight neighbouring elements as they lie; `aligned`: at a 16-byte boundary
 template <typename T>
 struct Eight {
-    alignas(16) T e[8];
+    static constexpr int kWords = 2 * sizeof(T);
+    uint32_t w[kWords];
     __device__ __forceinline__ void load(const T* p, bool aligned)
     {
         if (aligned) {
 #pragma unroll
-            for (uint32_t i = 0; i < sizeof(e) / 16; ++i) reinterpret_cast<uint4*>(e)[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
-        } else {
+            for (int i = 0; i < kWords; i += 4) {
+                const uint4 x = __ldg(reinterpret_cast<const uint4*>(p) + i / 4);
+                w[i] = x.x;
+                w[i + 1] = x.y;
+                w[i + 2] = x.z;
+                w[i + 3] = x.w;
+            }
+        } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = p[i];
+            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(p[i]);
+        } else {
+            const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = (uint32_t)q[2 * i] | (uint32_t)q[2 * i + 1] << 16;
         }
     }
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
-        for (uint32_t i = 0; i < sizeof(e) / 16; ++i) reinterpret_cast<uint4*>(e)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else if constexpr (std::is_same<T, __half>::value) return i % 2 ? __high2float(half2_of(w[i / 2])) : __low2float(half2_of(w[i / 2]));
+        else return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     }
     // as fp32, NaN as 0, cut to what is held; returns the largest magnitude
     __device__ __forceinline__ float floats(float* x) const
@@ -58,7 +68,7 @@ struct Eight {
         float m = 0.0f, odd = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[i] = to_float(e[i]);
+            x[i] = at(i);
             m = fmaxf(m, fabsf(x[i]));
             odd = fmaf(x[i], 0.0f, odd);                               // NaN if one is not finite
         }
@@ -157,6 +167,8 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
             my_slot = t >= 0 && t < p.tokens ? __ldg(p.slots + t) : -1;
         }
     };
+    let_next_start();
+    wait_for_previous();
     fetch(blockIdx.x);
     for (uint32_t round = blockIdx.x; round < rounds; round += gridDim.x) {
     const uint32_t group = p.by_heads.of(round), head = round - group * p.heads, base = group * 16;
@@ -318,6 +330,8 @@ __global__ void __launch_bounds__(2 * D) read8_kernel(const Rows8K p, T* __restr
     __shared__ alignas(16) uint8_t held[16][kStride];
     __shared__ bool whole;
     const uint32_t tid = threadIdx.x, row = tid / kPerRow, part = tid % kPerRow, group = p.by_heads.of(blockIdx.x), head = blockIdx.x - group * p.heads, base = group * 16;
+    let_next_start();
+    wait_for_previous();
     if (tid < 32) {
         const uint32_t t = base + tid;
         const int64_t s = tid < 16 && t < p.tokens ? __ldg(p.slots + t) : -1;
@@ -356,16 +370,20 @@ __global__ void __launch_bounds__(2 * D) read8_kernel(const Rows8K p, T* __restr
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const float by = u ? scale.y : scale.x;
-        alignas(16) T e[8];
+        uint32_t e[2 * sizeof(T)];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float2 f = floats_of_e4m3((i < 2 ? q[u].x : q[u].y) >> (16 * (i % 2)) & 0xFFFFu);
-            put(e + 2 * i, f.x * by);
-            put(e + 2 * i + 1, f.y * by);
+            if constexpr (sizeof(T) == 4) {
+                e[2 * i] = __float_as_uint(f.x * by);
+                e[2 * i + 1] = __float_as_uint(f.y * by);
+            } else {
+                e[i] = out_pair<std::is_same<T, __half>::value>(f.x * by, f.y * by);
+            }
         }
         uint4* to = reinterpret_cast<uint4*>((u ? v : k) + ((uint64_t)(base + row) * p.heads + head) * D + 8 * part);
 #pragma unroll
-        for (uint32_t i = 0; i < sizeof(e) / 16; ++i) to[i] = reinterpret_cast<uint4*>(e)[i];
+        for (uint32_t i = 0; i < sizeof(T) / 2; ++i) to[i] = make_uint4(e[4 * i], e[4 * i + 1], e[4 * i + 2], e[4 * i + 3]);
     }
 }
 
@@ -374,17 +392,13 @@ int launch_append(const Rows8K& p, bool aligned, cudaStream_t st)
 {
     // as many CTAs as are resident, each with the next round's loads under way
     const uint32_t rounds = (p.tokens + 15) / 16 * p.heads, resident = 148 * (1024 / (2 * D));
-    append8_kernel<D, T><<<rounds < resident ? rounds : resident, 2 * D, 0, st>>>(p, rounds, aligned);
-    KVP_CUDA(cudaGetLastError());
-    return KVP_OK;
+    return launch(append8_kernel<D, T>, rounds < resident ? rounds : resident, 2 * D, 0, true, st, p, rounds, aligned);
 }
 
 template <int D, typename T>
 int launch_read(const Rows8K& p, void* k, void* v, cudaStream_t st)
 {
-    read8_kernel<D, T><<<(p.tokens + 15) / 16 * p.heads, 2 * D, 0, st>>>(p, static_cast<T*>(k), static_cast<T*>(v));
-    KVP_CUDA(cudaGetLastError());
-    return KVP_OK;
+    return launch(read8_kernel<D, T>, (p.tokens + 15) / 16 * p.heads, 2 * D, 0, true, st, p, static_cast<T*>(k), static_cast<T*>(v));
 }
 
 int check_rows(const kvp_cache_shape* c, const void* cache, uint32_t tokens, const void* a, const void* b, uint32_t rows_align, const int64_t* slots, uint32_t dtype)

@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const P p)
 
 inline uint64_t up256(uint64_t x) { return (x + 255) & ~255ull; }
 
-// `chained`: behind another kernel of the same call, whose end it waits for by itself
+// `chained`: waits by itself for the end of the kernel before it in the stream, so that it may come up while that one works
 template <typename... A>
 int launch(void (*kernel)(A...), uint32_t grid, uint32_t threads, uint32_t smem, bool chained, cudaStream_t st, const A&... k)
 {

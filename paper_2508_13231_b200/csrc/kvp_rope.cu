@@ -107,6 +107,8 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeK p)
     constexpr bool kTwo = !(INTERLEAVED && V > 1);                     // two loads for a chunk
     constexpr uint32_t kBatch = 4;
     using W = Vec<T, V>;
+    let_next_start();
+    wait_for_previous();
     const uint32_t block = p.groups.of(blockIdx.x), group = blockIdx.x - block * p.groups.d;       // heads of the same tokens at the same time, as they lie in memory
     const uint32_t i = block * 256 + threadIdx.x, t = p.chunks.of(i), chunk = i - t * p.chunks.d;
     if (t >= p.tokens) return;
@@ -179,10 +181,7 @@ int launch_rope(RopeK k, const kvp_rope_params* a, bool copies, cudaStream_t st)
     k.groups = divisor((k.all_heads + k.per - 1) / k.per);
     const uint64_t grid = (threads + 255) / 256 * k.groups.d;
     if (grid >= (1ull << 31)) return KVP_ERR_RANGE;
-    if (interleaved) rope_kernel<T, V, true><<<(uint32_t)grid, 256, 0, st>>>(k);
-    else rope_kernel<T, V, false><<<(uint32_t)grid, 256, 0, st>>>(k);
-    KVP_CUDA(cudaGetLastError());
-    return KVP_OK;
+    return interleaved ? launch(rope_kernel<T, V, true>, (uint32_t)grid, 256, 0, true, st, k) : launch(rope_kernel<T, V, false>, (uint32_t)grid, 256, 0, true, st, k);
 }
 
 template <typename T>

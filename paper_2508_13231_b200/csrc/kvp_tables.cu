@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(kScanThreads) tables_kernel(const TablesK p, b
 {
     __shared__ Pair sm[kScanWarps];
     let_next_start();
+    wait_for_previous();
     const uint32_t tid = threadIdx.x, lane = tid % 32;
     const uint32_t head = (uint32_t)p.state[0] % p.pages, count = min((uint32_t)max(p.state[1], 0), p.pages);
     const uint32_t most = p.table_pages * p.page.d;
@@ -175,6 +176,7 @@ __global__ void __launch_bounds__(256) tokens_kernel(const TablesK p)
 {
     __shared__ int32_t near[kSharedStarts + 1];
     const uint32_t tid = threadIdx.x;
+    let_next_start();
     wait_for_previous();
     const int32_t* starts = p.starts;
     if (p.batch <= kSharedStarts) {
@@ -212,7 +214,7 @@ extern "C" int kvp_block_tables(const kvp_tables_params* a, const int32_t* new_t
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool alone = a->tokens <= kAlone;
     const uint32_t wide = a->batch > a->tokens ? a->batch : a->tokens, threads = wide >= kScanThreads ? kScanThreads : (wide + 31) / 32 * 32;
-    int rc = launch(tables_kernel, 1, alone ? threads : kScanThreads, 0, false, st, k, alone);
+    int rc = launch(tables_kernel, 1, alone ? threads : kScanThreads, 0, true, st, k, alone);
     if (!rc && !alone) rc = launch(tokens_kernel, (a->tokens + 1023) / 1024, 256, 0, true, st, k);
     return rc;
 }
