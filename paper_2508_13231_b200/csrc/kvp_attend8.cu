@@ -198,7 +198,7 @@ struct Smem8 {
     alignas(16) float factor[S::ROWS];                 // per row: what scores are multiplied by,
     float slope[S::ROWS];                              // its bias a token,
     int32_t see[S::ROWS];                              // the tokens that it sees are before this one
-    alignas(16) float top[S::kTeams][S::kRowsEach];    // what scores are taken less: the running maximum, 0 before a row has seen a token
+    alignas(16) float low[S::kTeams][S::kRowsEach];    // what is added to scores: less the running maximum, 0 before a row has seen a token
     alignas(16) float by[S::kTeams][S::kRowsEach];     // what sums are multiplied by when it moves; at the end of a segment see `last`
     float peak[S::kTeams][4][S::kRowsEach];            // of each warp: how far its scores pass it; at the end its sum of weights
     float scale[S::kTeams][4];                         // of each warp: the largest scale of its values
@@ -241,17 +241,24 @@ __device__ __forceinline__ void floats_of8(uint32_t x, float* to)
     }
 }
 
-// the next term of two fp16 numbers, and what it leaves, 32 times as large; both are exact
-__device__ __forceinline__ uint32_t next_term(uint32_t& h)
+// the next term of four fp16 numbers, and what it leaves, 32 times as large; both are exact
+__device__ __forceinline__ uint32_t next_term(uint32_t& a, uint32_t& b)
 {
-    uint16_t t;
-    uint32_t f;
-    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(t) : "r"(h));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f) : "h"(t));
-    h = bits_of(__hfma2(half2_of(f), __float2half2_rn(-32.0f), __hmul2(half2_of(h), __float2half2_rn(32.0f))));
+    uint32_t t, x, y;
+    asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f16x2 lo, %3;\n\tcvt.rn.satfinite.e4m3x2.f16x2 hi, %4;\n\tmov.b32 %0, {lo, hi};\n\t"
+        "cvt.rn.f16x2.e4m3x2 %1, lo;\n\tcvt.rn.f16x2.e4m3x2 %2, hi;\n\t}" : "=r"(t), "=r"(x), "=r"(y) : "r"(a), "r"(b));
+    const __half2 by = __float2half2_rn(32.0f), less = __float2half2_rn(-32.0f);
+    a = bits_of(__hfma2(half2_of(x), less, __hmul2(half2_of(a), by)));
+    b = bits_of(__hfma2(half2_of(y), less, __hmul2(half2_of(b), by)));
     return t;
 }
-// the same of two fp32 numbers
+__device__ __forceinline__ uint32_t last_term(uint32_t a, uint32_t b)
+{
+    uint32_t t;
+    asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f16x2 lo, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 hi, %2;\n\tmov.b32 %0, {lo, hi};\n\t}" : "=r"(t) : "r"(a), "r"(b));
+    return t;
+}
+// of two fp32 numbers
 __device__ __forceinline__ uint32_t next_term(float& a, float& b)
 {
     const uint32_t t = e4m3_pair(a, b);
@@ -527,7 +534,8 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
         const uint32_t team = (warp - kOthers) / 4, turn = team % S::kTurns, row0 = team / S::kTurns * R, part = warp % 4, me = part * 32 + lane;
         const uint32_t lanes = part * 32 << 16;                        // of tensor memory
         const uint32_t scores = scores_at + lanes + row0, sums = sums_at + lanes + turn * S::kSumCols + row0;
-        float* const top = sm.top[team];
+        float* const lows = sm.low[team];
+        const bool plain = !(p.cap > 0.0f) && !p.slopes;
         bool ok = true;
         uint32_t it = 0;                                               // groups so far, all teams'
         Ring<S::kValueStages> vs;
@@ -598,7 +606,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 show_to_async();
                 __syncwarp();
                 if (lane == 0) barrier_arrive(bar(sm.query));
-                if (me < R) top[me] = 0.0f;
+                if (me < R) lows[me] = 0.0f;
                 teams_sync<S::kTeams>();
             }
             const uint32_t tiles = walk.tiles, len = walk.len;
@@ -637,30 +645,33 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     tensor_wait_load();
 #pragma unroll
                     for (uint32_t term = 0; term < S::kQTerms; ++term) tensor_hold(x[term]);
+                    const F2 one(scales.x, scales.x), small(scales.x * 0x1p-5f, scales.x * 0x1p-5f), least(scales.x * 0x1p-10f, scales.x * 0x1p-10f);
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; i += 4) {
-                        const float4 f = *reinterpret_cast<const float4*>(sm.factor + row0 + r + i);
-                        const F2 scale2(scales.x, scales.x), by[2] = {F2(f.x, f.y) * scale2, F2(f.z, f.w) * scale2};
-#pragma unroll
-                        for (uint32_t k = 0; k < 2; ++k) {
-                            const uint32_t n = i + 2 * k;
-                            F2 y = fma2(F2(x[1][n], x[1][n + 1]), F2(0x1p-5f, 0x1p-5f), F2(x[0][n], x[0][n + 1]));
-                            if (S::kQTerms == 3) y = fma2(F2(x[S::kQTerms - 1][n], x[S::kQTerms - 1][n + 1]), F2(0x1p-10f, 0x1p-10f), y);
-                            y = y * by[k];
-                            y.get(s[r + n], s[r + n + 1]);
-                        }
+                    for (uint32_t i = 0; i < 8; i += 2) {
+                        F2 y = F2(x[0][i], x[0][i + 1]) * one;
+                        y = fma2(F2(x[1][i], x[1][i + 1]), small, y);
+                        if (S::kQTerms == 3) y = fma2(F2(x[S::kQTerms - 1][i], x[S::kQTerms - 1][i + 1]), least, y);
+                        y.get(s[r + i], s[r + i + 1]);
                     }
                 }
                 tensor_before_sync();
                 __syncwarp();
                 if (lane == 0) barrier_arrive(bar(sm.taken[sb.at]));
-                if (p.cap > 0.0f) {
+                if (plain) {
 #pragma unroll
-                    for (uint32_t r = 0; r < R; ++r) s[r] = tanhf(s[r]) * (p.cap * kLog2e);
-                }
-                if (p.slopes) {
+                    for (uint32_t r = 0; r < R; r += 4) {
+                        const float4 f = *reinterpret_cast<const float4*>(sm.factor + row0 + r), low = *reinterpret_cast<const float4*>(lows + r);
+                        fma2(F2(s[r], s[r + 1]), F2(f.x, f.y), F2(low.x, low.y)).get(s[r], s[r + 1]);
+                        fma2(F2(s[r + 2], s[r + 3]), F2(f.z, f.w), F2(low.z, low.w)).get(s[r + 2], s[r + 3]);
+                    }
+                } else {
 #pragma unroll
-                    for (uint32_t r = 0; r < R; ++r) s[r] = fmaf(sm.slope[row0 + r], (float)(pos - sm.see[row0 + r] + 1), s[r]);
+                    for (uint32_t r = 0; r < R; ++r) {
+                        s[r] *= sm.factor[row0 + r];
+                        if (p.cap > 0.0f) s[r] = tanhf(s[r]) * (p.cap * kLog2e);
+                        if (p.slopes) s[r] = fmaf(sm.slope[row0 + r], (float)(pos - sm.see[row0 + r] + 1), s[r]);
+                        s[r] += lows[r];
+                    }
                 }
                 if (!all_seen) {
 #pragma unroll
@@ -671,14 +682,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 }
                 float over = -INFINITY;                                // how far scores pass the maximum
 #pragma unroll
-                for (uint32_t r = 0; r < R; r += 4) {
-                    const float4 m = *reinterpret_cast<const float4*>(top + r);
-                    s[r] -= m.x;
-                    s[r + 1] -= m.y;
-                    s[r + 2] -= m.z;
-                    s[r + 3] -= m.w;
-                    over = fmaxf(over, fmaxf(fmaxf(s[r], s[r + 1]), fmaxf(s[r + 2], s[r + 3])));
-                }
+                for (uint32_t r = 0; r < R; r += 2) over = fmaxf(over, fmaxf(s[r], s[r + 1]));
                 if (team_any(over > kSlack || scale > most_scale || unset || !ok, team)) {
                     float x = warp_max(scale);
                     if (lane == 0) sm.scale[team][part] = x;
@@ -706,7 +710,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                         first = none;
                         if (none) up = 0.0f;
                         sm.by[team][me] = up;
-                        top[me] += up;
+                        lows[me] -= up;
                     }
                     unset = team_any(none, team);                      // also: the new maxima are there
                     if (any) {
@@ -735,9 +739,10 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 }
                 any = true;
 #pragma unroll
-                for (uint32_t r = 0; r < R; ++r) {
+                for (uint32_t r = 0; r < R; r += 2) {
                     s[r] = exp2_fast(s[r]);
-                    l[r] += s[r];
+                    s[r + 1] = exp2_fast(s[r + 1]);
+                    (F2(l[r], l[r + 1]) + F2(s[r], s[r + 1])).get(l[r], l[r + 1]);
                 }
                 if (p.sub) {                                           // what each block of `sub` tokens received, as log2
                     float x[R];
@@ -750,7 +755,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                         if (tile == ~0u) return;
                         float* to = mass + ((uint64_t)(uint32_t)pos >> LOG) * ROWS + from;
 #pragma unroll
-                        for (int i = 0; i < LEFT; ++i) to[i] = top[from + i] + log2_fast(x[i]);
+                        for (int i = 0; i < LEFT; ++i) to[i] = log2_fast(x[i]) - lows[from + i];
                     };
 #define KVP_INT(X) std::integral_constant<int, (X)>{}
 #define KVP_LEFT(LOG) KVP_INT((R >> LOG) ? (R >> LOG) : 1)
@@ -774,11 +779,9 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     lo.get(x[0], x[1]);
                     hi.get(x[2], x[3]);
                     uint32_t a = pack(x[0], x[1]), b = pack(x[2], x[3]);
-#pragma unroll
-                    for (uint32_t i = 0; i < 3; ++i) {
-                        const uint32_t y = next_term(a);
-                        term[i][r / 4] = __byte_perm(y, next_term(b), 0x5410);
-                    }
+                    term[0][r / 4] = next_term(a, b);
+                    term[1][r / 4] = next_term(a, b);
+                    term[2][r / 4] = last_term(a, b);
                 }
                 if constexpr (R == 8) {
                     *reinterpret_cast<uint4*>(to) = make_uint4(term[0][0], term[0][1], term[1][0], term[1][1]);
@@ -841,11 +844,11 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     const float* x = &sm.peak[team0 + u][0][mine + me];
                     const float* gone = sm.scale[team0 + u];
                     one[u] = ((x[0] + x[R]) + (x[2 * R] + x[3 * R])) + ((gone[0] + gone[1]) + (gone[2] + gone[3]));
-                    if (one[u] != 0.0f) m = fmaxf(m, sm.top[team0 + u][mine + me]);
+                    if (one[u] != 0.0f) m = fmaxf(m, -sm.low[team0 + u][mine + me]);
                 }
 #pragma unroll
                 for (uint32_t u = 0; u < S::kTurns; ++u) {
-                    const float k = one[u] != 0.0f ? exp2_fast(sm.top[team0 + u][mine + me] - m) : 0.0f;
+                    const float k = one[u] != 0.0f ? exp2_fast(-sm.low[team0 + u][mine + me] - m) : 0.0f;
                     sum = fmaf(one[u], k, sum);
                     sm.last[team0 + u][mine + me].x = k;
                 }

@@ -15,11 +15,11 @@ __device__ __forceinline__ void barrier_arrive_expect(uint32_t bar, uint32_t byt
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// Has the phase of `parity` ended? The hardware may hold the thread back for up to 10 us before it says no.
+// has the phase of `parity` ended?
 __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity), "r"(10000u) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
 // Waits for the end of the phase of `parity`, two seconds at most; false if it did not come, or if another waiter of the CTA gave up before.
@@ -28,8 +28,10 @@ static __device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t par
     uint64_t from, now;
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(from));
     while (true) {
-        for (int i = 0; i < 16; ++i)
+        for (int i = 0; i < 256; ++i) {
             if (barrier_try(bar, parity)) return true;
+            __nanosleep(20);                                           // others have work for the issue slots
+        }
         if (*gave_up) return false;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
         if (now - from > 2000000000ull) {
