@@ -250,6 +250,9 @@ extern "C" int kvp_rope(const kvp_rope_params* a, const void* q, void* q_out, co
     if ((a->heads && (!q || !q_out)) || (a->kv_heads && (!k || !k_out)) || !positions || !frequencies) return KVP_ERR_ARG;
     const uint32_t e = a->dtype == KVP_F32 ? 4 : 2;
     if (off_by(q, e) || off_by(k, e) || off_by(q_out, e) || off_by(k_out, e) || off_by(positions, 4) || off_by(frequencies, 8)) return KVP_ERR_ARG;
+    // over the input itself only as it lies
+    if ((a->heads && q == q_out && (a->q_token_stride != a->q_out_token_stride || a->q_head_stride != a->q_out_head_stride)) ||
+        (a->kv_heads && k == k_out && (a->k_token_stride != a->k_out_token_stride || a->k_head_stride != a->k_out_head_stride))) return KVP_ERR_ARG;
     RopeK p = {};
     p.tokens = a->tokens; p.heads = a->heads; p.all_heads = a->heads + a->kv_heads;
     p.half = a->rotary_dim / 2;

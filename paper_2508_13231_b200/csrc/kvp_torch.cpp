@@ -488,6 +488,9 @@ PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         !dense(args[2], "positions", at::kInt, dev, false, &positions) || !dense(args[3], "frequencies", at::kDouble, dev, false, &frequencies) ||
         !u32_of(args[4], "flags", &p.flags)) return nullptr;
     if (positions->numel() != q->size(0)) return value_error("positions must have one entry per token");
+    for (const at::Tensor* t : {q, k})
+        if (t && PyObject_IsTrue(args[6]) == 1 && ((t->size(0) > 1 && t->stride(0) == 0) || (t->size(1) > 1 && t->stride(1) == 0)))
+            return value_error("in place: tokens or heads share their memory");
     const double scale = PyFloat_AsDouble(args[5]);
     if (PyErr_Occurred()) return nullptr;
     const int in_place = PyObject_IsTrue(args[6]);

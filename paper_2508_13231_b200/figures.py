@@ -1,6 +1,6 @@
 """Synthetic reruns of the paper's sensitivity study (Section IV-B, Fig. 3-5) on one B200.
 
-    python -m paper_2508_13231_b200.figures [--quick] [--recorded]
+    python -m paper_2508_13231_b200.figures [--quick] [--recorded [--bits 8]]
 
 One attention head at token granularity: 4096 tokens (512 B of K+V each), 512 decode steps, HBM room for 25% of
 them, 8 TB/s HBM against 0.9 TB/s off-package, Zipf(1.1) importance with AR(1) drift. The recorded LLaMA-3.1-8B /
@@ -13,6 +13,8 @@ direct annealing of the schedule it found. Everything runs in the library's kern
 stand in for a model, tokens are decoded with attention over a cache held in 4 bits (the paper records a model with an unquantised one, so
 these weights contain the error of 4 bits), and each step reads the units that received most weight. Beside them the placement by accumulated
 weight, and what eviction by it leaves of the attention weight: the units evicted after a step are gone for all later ones.
+--bits 8 records with a cache held in 8 bits (normal values are off by 0.027 of their deviation where 4 bits leave 0.078), with rotary positions and
+with pages, slots and positions from the device's block tables.
 """
 import argparse
 
@@ -59,6 +61,38 @@ def strategies(topk, rho, quick=False, seed=0):
     return out
 
 
+def record8(cfg, seed=0):
+    """record() with a cache held in 8 bits, rotary positions and the device's block tables."""
+    h, d, page = cfg["kv_heads"], cfg["head_dim"], cfg["unit_tokens"]
+    total = cfg["prompt"] + cfg["steps"]
+    n = -(-total // page)
+    rng = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda *size: torch.randn(*size, generator=rng, device="cuda")  # noqa: E731
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    cache = torch.zeros(n, h, kvp.cache8_page_bytes(d, page), dtype=torch.uint8, device="cuda")
+    table, lens, state = torch.full((1, n), -1, dtype=torch.int32, device="cuda"), i32(0), i32(0, n)
+    ring = torch.randperm(n, generator=rng, device="cuda").int()
+    frequencies, scale = kvp.rope_frequencies(d, scaling="ramp", factor=4.0)
+    frequencies = frequencies.cuda()
+
+    def append(q, k, v):
+        """The next tokens: their pages and slots, rotary positions of queries and keys, keys and values into the cache -> the queries."""
+        r = kvp.block_tables(i32(len(q)), lens, table, ring, state, page, len(q), lens_out=lens, state_out=state)
+        q, k = kvp.rope(q, k, r["positions"], frequencies, scale=scale)
+        kvp.cache8_append(cache, k, v, r["slots"])
+        return q
+
+    k, v, q = rand(total, h, d).bfloat16(), rand(total, h, d).bfloat16(), rand(cfg["queries"], d)
+    p = cfg["prompt"]
+    append(q.bfloat16().expand(p, -1, -1), k[:p], v[:p])
+    weights = torch.empty(cfg["steps"], h * n, device="cuda")
+    for s in range(cfg["steps"]):
+        q = cfg["rho"] * q + (1 - cfg["rho"] ** 2) ** 0.5 * rand(*q.shape)
+        turned = append((2.5 * q).bfloat16()[None], k[p + s: p + s + 1], v[p + s: p + s + 1])
+        kvp.attend8(turned, cache, table, lens, weights=weights[s])
+    return weights, n
+
+
 def record(cfg, seed=0):
     """Decodes cfg["steps"] tokens of one layer -> weights [steps][kv_heads * units] (kvp.attend), units per kv-head."""
     h, d, page = cfg["kv_heads"], cfg["head_dim"], cfg["unit_tokens"]
@@ -90,14 +124,15 @@ def weight_kept(weights, cfg, n, share):
     return float((weights[1:] * bits[:-1]).sum() / weights[1:].sum())
 
 
-def recorded(name, quick=False, seed=0):
+def recorded(name, quick=False, seed=0, bits=4):
     """-> dict strategy -> (total ticks, HBM hit rate), dict share of the units kept -> share of the attention weight they receive."""
     cfg = wl.RECORDED[name]
     h, steps = cfg["kv_heads"], cfg["steps"]
-    weights, n = record(cfg, seed)
+    weights, n = record8(cfg, seed) if bits == 8 else record(cfg, seed)
     access = kvp.trace_weights(weights, h, cfg["topk"])
     units, cap = h * n, int(cfg["share"] * h * n)
-    prob = kvp.Problem(units, kvp.cache_page_bytes(cfg["head_dim"], cfg["unit_tokens"]), steps, access, cap, *cfg["bw"])
+    page_bytes = kvp.cache8_page_bytes if bits == 8 else kvp.cache_page_bytes
+    prob = kvp.Problem(units, page_bytes(cfg["head_dim"], cfg["unit_tokens"]), steps, access, cap, *cfg["bw"])
 
     def score(sched):
         counts = prob.eval_counts(sched)[0].long().sum(0)
@@ -118,11 +153,12 @@ def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--quick", action="store_true")
     ap.add_argument("--recorded", action="store_true")
+    ap.add_argument("--bits", type=int, choices=(4, 8), default=4, help="of the cache that --recorded decodes with")
     args = ap.parse_args()
     if args.recorded:
         name = "recorded_small" if args.quick else "recorded_8b"
-        out, kept = recorded(name, args.quick)
-        print(f"Recorded attention weights ({name}): tokens/s normalised to Static Placement, HBM hit rate\n")
+        out, kept = recorded(name, args.quick, bits=args.bits)
+        print(f"Recorded attention weights ({name}, cache in {args.bits} bits): tokens/s normalised to Static Placement, HBM hit rate\n")
         print("| " + " | ".join(out) + " |\n|" + "---|" * len(out))
         print("| " + " | ".join(f"{out['static'][0] / t:.2f}, {r:.3f}" for t, r in out.values()) + " |\n")
         print("Eviction by accumulated weight: share of the later steps' attention weight on the units kept\n")
