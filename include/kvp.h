@@ -538,7 +538,7 @@ typedef struct {
  * below 2^-14 of the row's largest to within 2^-22 of that), a weight as three terms, 2^-12 of itself, in units of 2^-26 of the largest weight times
  * the largest scale of the values: tokens whose weights are below that add nothing. A chunk of a prompt (many queries) reads the cache once for every 64 rows.
  * A wait inside the kernel that takes two seconds, which only a fault can cause, ends it with NaN in out.
- * Errors: as of kvp_attend, and a cap that is negative or not finite (KVP_ERR_ARG).
+ * Errors: as of kvp_attend, and a cap that is negative or not finite or so small that scale / cap is not finite (KVP_ERR_ARG).
  */
 int kvp_attend8_workspace(const kvp_attend8_params* params, int want_weights, int has_units, uint64_t* bytes);
 int kvp_attend8(const kvp_attend8_params* params, const void* q, const void* cache, const int32_t* table, const int32_t* lens,

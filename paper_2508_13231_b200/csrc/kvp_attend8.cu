@@ -332,7 +332,6 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
     let_next_start();
     const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     const auto bar = [](uint64_t& b) { return smem_at(&b); };
-    if (warp == 1) tensor_alloc<S::kCols>(smem_at(&sm.tensor));
     if (tid == 0) {
         for (uint32_t i = 0; i < S::kKeyStages; ++i) {
             barrier_init(bar(sm.keys[i]), 1);
@@ -353,6 +352,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
         show_to_async();
     }
     wait_for_previous();
+    if (warp == 1) tensor_alloc<S::kCols>(smem_at(&sm.tensor));        // not sooner: the kernel before may still have to ask for its own
     Walk walk;
     {
         uint32_t entry = 0;
@@ -937,6 +937,7 @@ int check_attend8(const kvp_attend8_params* a)
     const uint32_t u = a->unit_tokens;
     if (!u || a->cache.page_tokens % u || (u < kTileTokens ? kTileTokens % u : u % kTileTokens)) return KVP_ERR_ARG;
     if (!(a->scale > -INFINITY && a->scale < INFINITY) || !(a->cap >= 0.0f && a->cap < INFINITY)) return KVP_ERR_ARG;
+    if (a->cap > 0.0f && !(fabsf(a->scale / a->cap) < INFINITY)) return KVP_ERR_ARG;
     if (!head_dim_served(a->cache.head_dim)) return KVP_ERR_RANGE;
     const uint64_t rows = (uint64_t)a->queries * a->group, bh = (uint64_t)a->batch * a->cache.kv_heads;
     const uint64_t tokens = (uint64_t)a->table_pages * a->cache.page_tokens;

@@ -188,8 +188,11 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
 #pragma unroll
             for (uint32_t j = 15; j > 0; --j)
                 if (slot[1 + lane + (15 - j)] >= 0 && slot[1 + lane + (15 - j)] / kTileTokens == mine / kTileTokens) first = min(first, 1 + lane + (15 - j));
-            const bool here = mine >= 0 && first >= 16 && first < 32, leader = here && first == 16 + lane;
-            const uint32_t leaders = __ballot_sync(0xFFFFFFFFu, leader), run = here ? __popc(leaders & ((1u << (first - 16)) - 1u)) : kNobody;
+            const bool leader = mine >= 0 && first < 32 && first == 16 + lane;
+            const uint32_t leaders = __ballot_sync(0xFFFFFFFFu, leader);
+            // in a run that begins here; a token whose first one is led itself, from further away than allowed, is left out
+            const bool here = mine >= 0 && first >= 16 && first < 32 && (leaders >> (first - 16) & 1u);
+            const uint32_t run = here ? __popc(leaders & ((1u << (first - 16)) - 1u)) : kNobody;
             run_of[lane] = (uint8_t)run;
             if (here) runs.token[run][mine % kTileTokens] = (uint8_t)lane;
             if (lane == 0) runs.many = __popc(leaders);

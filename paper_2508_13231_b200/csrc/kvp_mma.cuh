@@ -22,11 +22,12 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Waits for the end of the phase of `parity`, two seconds at most; false if it did not come, or if another waiter of the CTA gave up before.
+// Waits for the end of the phase of `parity`, two seconds at most; false if it did not come, or if another waiter of the CTA gave up before. Of the time between two
+// looks a millisecond counts at most: a GPU that was given to another process meanwhile has not kept anyone waiting.
 static __device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up)
 {
-    uint64_t from, now;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(from));
+    uint64_t last, now, waited = 0;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(last));
     while (true) {
         for (int i = 0; i < 256; ++i) {
             if (barrier_try(bar, parity)) return true;
@@ -34,7 +35,9 @@ static __device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t par
         }
         if (*gave_up) return false;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
-        if (now - from > 2000000000ull) {
+        waited += now - last < 1000000ull ? now - last : 1000000ull;
+        last = now;
+        if (waited > 2000000000ull) {
             *gave_up = 1;
             return false;
         }

@@ -141,7 +141,7 @@ def attend_params(**change):
     (dict(table_pages=0), ARG), (dict(page_tokens=0), ARG), (dict(page_tokens=24), ARG), (dict(dtype=2), ARG), (dict(reserved=1), ARG),
     (dict(unit_tokens=0), ARG), (dict(unit_tokens=3), ARG), (dict(unit_tokens=32), ARG), (dict(page_tokens=48, unit_tokens=32), ARG),
     (dict(page_tokens=48, unit_tokens=24), ARG), (dict(scale=float("nan")), ARG), (dict(scale=float("inf")), ARG), (dict(cap=-1.0), ARG),
-    (dict(cap=float("inf")), ARG), (dict(cap=float("nan")), ARG), (dict(head_dim=96), RANGE), (dict(queries=1025), RANGE), (dict(queries=1024, group=5), RANGE),
+    (dict(cap=float("inf")), ARG), (dict(cap=1e-44), ARG), (dict(cap=float("nan")), ARG), (dict(head_dim=96), RANGE), (dict(queries=1025), RANGE), (dict(queries=1024, group=5), RANGE),
     (dict(batch=1 << 24), RANGE), (dict(table_pages=1 << 26), RANGE), (dict(batch=1 << 16, table_pages=1 << 14), RANGE)])
 def test_attend_refuses(lib, change, code):
     need, some = C.c_uint64(0), C.c_void_p(256)

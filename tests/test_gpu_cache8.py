@@ -141,6 +141,24 @@ def test_scale_that_is_none(kvp):
             assert torch.equal(a, b)
 
 
+def test_tokens_of_a_block_further_apart_than_allowed_leave_other_blocks_alone(kvp):
+    """What the block of the scattered tokens holds is not specified; the tokens between them are written as ever, and nothing else is touched."""
+    heads, d, page = 2, 64, 16
+    rng = np.random.default_rng(8)
+    for gap in (14, 15, 16, 20):
+        slots = np.arange(100, dtype=np.int64) + 5 * page                      # tokens of other blocks
+        at = np.arange(0, 100, gap)
+        slots[at] = 2 * page + (np.arange(len(at)) * 3) % 16                   # one of block 2 every `gap` tokens
+        k, v = (cuda(x).float() for x in rng.standard_normal((2, 100, heads, d)))
+        dev = torch.zeros(14, heads, plain.page_bytes(d, page), dtype=torch.uint8, device="cuda")
+        kvp.cache8_append(dev, k, v, cuda(slots))
+        want = np.zeros(dev.shape, np.uint8)
+        rest = np.where(slots // page == 2, -1, slots)
+        plain.append(want, f64(k), f64(v), rest)
+        got = dev.cpu().numpy()
+        assert np.array_equal(np.delete(got, 2, 0), np.delete(want, 2, 0)), gap
+
+
 def test_append_strided_and_unaligned_rows(kvp):
     """Keys and values as slices of one fused projection, at an odd offset too; a whole prompt in pages out of order, on another stream."""
     heads, d, page, tokens = 2, 64, 16, 50
