@@ -16,6 +16,7 @@ struct TablesK {
     uint32_t batch, table_pages, tokens;
     Divisor page;            // tokens of a page
     uint32_t pages;
+    bool fours;              // rows of the table can be read 16 bytes at a time
 };
 
 constexpr uint32_t kScanThreads = 1024, kScanWarps = 32;
@@ -66,10 +67,38 @@ __device__ __forceinline__ Pair sum_over(Pair x, Pair& all, Pair* sm)
 }
 
 __device__ __forceinline__ uint32_t pages_of(const TablesK& p, uint32_t tokens) { return p.page.of(tokens + p.page.d - 1); }
+// entries j .. j + 3 of a row (j a multiple of 4), of the first `many`: those that name no page are -1; w: how many do
+struct Four {
+    int32_t page[4];
+    uint32_t w;
+};
+__device__ __forceinline__ Four good_pages(const TablesK& p, const int32_t* row, uint32_t j, uint32_t many)
+{
+    Four x = {{-1, -1, -1, -1}, 0};
+    if (j >= many) return x;
+    int32_t e[4];
+    if (p.fours) {                                                             // the row has a multiple of four entries
+        const int4 v = *reinterpret_cast<const int4*>(row + j);
+        e[0] = v.x;
+        e[1] = v.y;
+        e[2] = v.z;
+        e[3] = v.w;
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) e[i] = j + i < many ? row[j + i] : -1;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+        const bool good = j + i < many && (uint32_t)e[i] < p.pages;
+        x.page[i] = good ? e[i] : -1;
+        x.w += good;
+    }
+    return x;
+}
 __device__ __forceinline__ uint32_t around(uint32_t at, uint32_t pages) { return at >= pages ? at - pages : at; }       // at < 2 pages
 
 // Token t of the call: its request, position and slot; a page that begins with it goes into the table. `head`: of the ring, before the call.
-__device__ __forceinline__ void place_token(const TablesK& p, uint32_t t, const int32_t* starts, uint32_t head)
+__device__ __forceinline__ void place_token(const TablesK& p, uint32_t t, const int32_t* starts, const int32_t* page_starts, const int32_t* lens_out, uint32_t head)
 {
     if (t >= (uint32_t)starts[p.batch]) {
         p.slots[t] = -1;
@@ -83,12 +112,12 @@ __device__ __forceinline__ void place_token(const TablesK& p, uint32_t t, const 
         if ((uint32_t)starts[mid] <= t) low = mid;
         else high = mid;
     }
-    const uint32_t row = low, first = starts[row], before = (uint32_t)p.lens_out[row] - (starts[row + 1] - first), pos = before + t - first;
+    const uint32_t row = low, first = starts[row], before = (uint32_t)lens_out[row] - (starts[row + 1] - first), pos = before + t - first;
     const uint32_t j = p.page.of(pos), had = pages_of(p, before);
     int32_t* entry = p.table + (uint64_t)row * p.table_pages + j;
     int32_t page;
     if (j >= had) {
-        page = p.ring[around(head + around(p.page_starts[row] + j - had, p.pages), p.pages)];
+        page = p.ring[around(head + around(page_starts[row] + j - had, p.pages), p.pages)];
         if (pos == j * p.page.d) *entry = page;                 // no other token reads it: the entry is new
     } else {
         page = *entry;
@@ -101,6 +130,8 @@ __device__ __forceinline__ void place_token(const TablesK& p, uint32_t t, const 
 __global__ void __launch_bounds__(kScanThreads) tables_kernel(const TablesK p, bool alone)
 {
     __shared__ Pair sm[kScanWarps];
+    __shared__ struct { int32_t starts[kScanThreads + 1], page_starts[kScanThreads], lens[kScanThreads]; } near;      // of the last chunk
+    __shared__ struct { uint32_t upto[kScanThreads], many[kScanThreads], warp[kScanWarps]; } gone;       // of a chunk: items up to a request, its pages
     let_next_start();
     wait_for_previous();
     const uint32_t tid = threadIdx.x, lane = tid % 32;
@@ -115,16 +146,6 @@ __global__ void __launch_bounds__(kScanThreads) tables_kernel(const TablesK p, b
         const uint32_t len = in ? min((uint32_t)max(p.lens[i], 0), most) : 0, had = pages_of(p, len);
         const bool leaves = n < 0, fits = in && !leaves && (uint32_t)n <= most - len;
         const uint32_t need = fits ? pages_of(p, len + n) - had : 0;
-        uint32_t own = 0;                                       // pages it gives back
-        for (uint32_t left = __ballot_sync(0xFFFFFFFFu, in && leaves && had); left; left &= left - 1) {        // a warp counts one request's pages
-            const uint32_t l = __ffs(left) - 1, many = __shfl_sync(0xFFFFFFFFu, had, l);
-            const int32_t* row = p.table + (uint64_t)(base + tid - lane + l) * p.table_pages;
-            uint32_t good = 0;
-#pragma unroll 8
-            for (uint32_t j = lane; j < many; j += 32) good += (uint32_t)row[j] < p.pages;
-            good = __reduce_add_sync(0xFFFFFFFFu, good);
-            if (lane == l) own = good;
-        }
         Pair all;
         Pair sum = sum_over<true>(Pair{need, fits ? (uint32_t)n : 0u}, all, sm);
         const bool yes = fits && (!need || sat_add(asked.a, sum.a) <= count) && (!n || sat_add(asked.b, sum.b) <= p.tokens);
@@ -137,39 +158,74 @@ __global__ void __launch_bounds__(kScanThreads) tables_kernel(const TablesK p, b
             p.page_starts[i] = (int32_t)(given.a + sum.a - mine.a);
             p.granted[i] = yes || leaves;
             p.lens_out[i] = leaves ? 0 : (int32_t)(len + mine.b);
+            near.starts[tid] = (int32_t)(given.b + sum.b - mine.b);
+            near.page_starts[tid] = (int32_t)(given.a + sum.a - mine.a);
+            near.lens[tid] = leaves ? 0 : (int32_t)(len + mine.b);
         }
         given.a += all.a;
         given.b += all.b;
         if (__syncthreads_or(leaves)) {
-            sum = sum_over<false>(Pair{own, 0}, all, sm);
-            for (uint32_t left = __ballot_sync(0xFFFFFFFFu, own != 0); left; left &= left - 1) {
-                const uint32_t l = __ffs(left) - 1, many = __shfl_sync(0xFFFFFFFFu, had, l);
-                const int32_t* row = p.table + (uint64_t)(base + tid - lane + l) * p.table_pages;
-                uint32_t to = head + count + back + __shfl_sync(0xFFFFFFFFu, sum.a - own, l);
-                for (uint32_t j0 = 0; j0 < many; j0 += 256) {   // eight loads under way
-                    int32_t page[8];
+            // Pages given back: entries of the rows that leave, 128 to an item, four items a warp at a time, so that the loads of 512 entries are under way together.
+            // Items are in the order of requests and entries, and a place in the ring is the number of pages before.
+            const uint32_t many = leaves ? had : 0u;
+            sum = sum_over<false>(Pair{(many + 127) / 128, 0}, all, sm);
+            gone.upto[tid] = sum.a;
+            gone.many[tid] = many;
+            __syncthreads();
+            const uint32_t warp = tid / 32, warps = blockDim.x / 32, rows = min(blockDim.x, p.batch - base);
+            for (uint32_t i0 = 0; i0 < all.a; i0 += 4 * warps) {
+                Four x[4];
+                uint32_t upto[4], mine = 0;
 #pragma unroll
-                    for (uint32_t k = 0; k < 8; ++k) page[k] = j0 + 32 * k + lane < many ? row[j0 + 32 * k + lane] : -1;
-#pragma unroll
-                    for (uint32_t k = 0; k < 8; ++k) {
-                        const uint32_t good = __ballot_sync(0xFFFFFFFFu, (uint32_t)page[k] < p.pages);
-                        if (good >> lane & 1u) p.ring[(to + __popc(good & ((1u << lane) - 1u))) % p.pages] = page[k];
-                        to += __popc(good);
+                for (uint32_t k = 0; k < 4; ++k) {
+                    const uint32_t item = i0 + 4 * warp + k;
+                    x[k] = Four{{-1, -1, -1, -1}, 0};
+                    if (item < all.a) {
+                        uint32_t low = 0, high = rows;                  // the first row with upto > item is in low .. high - 1
+                        while (high - low > 1) {
+                            const uint32_t mid = (low + high) / 2;
+                            if (gone.upto[mid - 1] > item) high = mid;
+                            else low = mid;
+                        }
+                        const uint32_t first = low ? gone.upto[low - 1] : 0u;
+                        x[k] = good_pages(p, p.table + (uint64_t)(base + low) * p.table_pages, (item - first) * 128 + 4 * lane, gone.many[low]);
                     }
                 }
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) {
+                    upto[k] = mine + sum_upto(x[k].w, lane);
+                    mine = __shfl_sync(0xFFFFFFFFu, upto[k], 31);
+                }
+                if (lane == 0) gone.warp[warp] = mine;
+                __syncthreads();
+                const uint32_t w = sum_upto(lane < warps ? gone.warp[lane] : 0u, lane), before = __shfl_sync(0xFFFFFFFFu, w, warp) - mine, total = __shfl_sync(0xFFFFFFFFu, w, 31);
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) {
+                    uint32_t at = (head + count + back + before + upto[k] - x[k].w) % p.pages;
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i)
+                        if (x[k].page[i] >= 0) {
+                            p.ring[at] = x[k].page[i];
+                            if (++at == p.pages) at = 0;
+                        }
+                }
+                back += total;
+                __syncthreads();                                        // the warps' numbers are free
             }
-            back += all.a;
         }
     }
     if (tid == 0) {
         p.starts[p.batch] = (int32_t)given.b;
+        if (p.batch <= blockDim.x) near.starts[p.batch] = (int32_t)given.b;
         p.page_starts[p.batch] = (int32_t)given.a;
         p.state_out[0] = (int32_t)around(head + given.a, p.pages);
         p.state_out[1] = (int32_t)min(count - given.a + back, p.pages);
     }
     if (!alone) return;
     __syncthreads();
-    for (uint32_t t = tid; t < p.tokens; t += blockDim.x) place_token(p, t, p.starts, head);
+    const bool here = p.batch <= blockDim.x;                    // what the tokens look up is in shared memory too
+    for (uint32_t t = tid; t < p.tokens; t += blockDim.x)
+        place_token(p, t, here ? near.starts : p.starts, here ? near.page_starts : p.page_starts, here ? near.lens : p.lens_out, head);
 }
 
 __global__ void __launch_bounds__(256) tokens_kernel(const TablesK p)
@@ -185,7 +241,7 @@ __global__ void __launch_bounds__(256) tokens_kernel(const TablesK p)
         starts = near;
     }
     const uint32_t head = around((uint32_t)p.state_out[0] + p.pages - p.page_starts[p.batch], p.pages);
-    for (uint32_t t = blockIdx.x * 256 + tid; t < p.tokens; t += gridDim.x * 256) place_token(p, t, starts, head);
+    for (uint32_t t = blockIdx.x * 256 + tid; t < p.tokens; t += gridDim.x * 256) place_token(p, t, starts, p.page_starts, p.lens_out, head);
 }
 
 }  // namespace
@@ -211,6 +267,7 @@ extern "C" int kvp_block_tables(const kvp_tables_params* a, const int32_t* new_t
     k.table = table; k.ring = ring; k.lens_out = lens_out; k.state_out = state_out; k.granted = granted; k.starts = starts; k.page_starts = page_starts;
     k.positions = positions; k.rows = rows; k.slots = slots;
     k.batch = a->batch; k.table_pages = a->table_pages; k.tokens = a->tokens; k.page = divisor(a->page_tokens); k.pages = a->pages;
+    k.fours = a->table_pages % 4 == 0 && !off_by(table, 16);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool alone = a->tokens <= kAlone;
     const uint32_t wide = a->batch > a->tokens ? a->batch : a->tokens, threads = wide >= kScanThreads ? kScanThreads : (wide + 31) / 32 * 32;
