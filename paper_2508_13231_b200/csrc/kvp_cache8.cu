@@ -129,6 +129,7 @@ struct Runs {
     uint64_t block[16];              // where it lies in the cache
     float old[2][16], now[2][16];    // scales
     alignas(16) uint8_t token[16][16];       // of each place, counted from the CTA's first; kNobody: not written
+    uint32_t mask[16];               // of the places that are written
     uint32_t many;
 };
 
@@ -254,11 +255,14 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
         const bool begins = runs.token[run][0] != kNobody;             // the block's first token is among them: nothing is held
         const float old = begins ? 0.0f : runs.old[u][run];
         float m = 0.0f;
+        uint32_t mask = 0;
 #pragma unroll
         for (uint32_t i = 0; i < 16; ++i) {
             const uint32_t t = runs.token[run][i];
             m = fmaxf(m, t != kNobody ? most[u][t] : 0.0f);
+            mask |= (t != kNobody) << i;
         }
+        if (u == 0) runs.mask[run] = mask;
         const float now = fmaxf(old, scale_for(m));
         runs.old[u][run] = old;
         runs.now[u][run] = now;
@@ -276,13 +280,14 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
         const uint32_t run = i / (2 * D), u = i / D % 2, at = i % D;
         const uint8_t* token = runs.token[run];
         const float old = runs.old[u][run], now = runs.now[u][run], by = old > 0.0f ? old / now : 0.0f;
-        const bool again = token[0] == kNobody && now != old;          // what is there is rounded again
+        const uint32_t mask = runs.mask[run];
+        const bool again = !(mask & 1u) && now != old;                 // what is there is rounded again
         uint8_t* const block = p.cache + runs.block[run];
         if (u == 0) {
-            const uint32_t place = at % 16, c = at / 16, t = token[place];
+            const uint32_t place = at % 16, c = at / 16;
             uint4* to = reinterpret_cast<uint4*>(block + L::key(place, c));
-            if (t != kNobody) {
-                const uint2* q = reinterpret_cast<const uint2*>(&held[0][t][16 * c]);
+            if (mask >> place & 1u) {
+                const uint2* q = reinterpret_cast<const uint2*>(&held[0][token[place]][16 * c]);
                 *to = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
             } else if (again) {
                 uint4 q = make_uint4(0, 0, 0, 0);
@@ -294,9 +299,7 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
             }
         } else {
             uint8_t* to = block + L::value(at);
-            bool full = true;
-#pragma unroll
-            for (uint32_t j = 0; j < 16; ++j) full = full && token[j] != kNobody;
+            const bool full = mask == 0xFFFFu;
             if (again || full) {
                 uint32_t q[4] = {0, 0, 0, 0};
                 if (!full && by > 0.0f) {
@@ -308,11 +311,13 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
                 }
 #pragma unroll
                 for (uint32_t j = 0; j < 16; ++j)
-                    if (token[j] != kNobody) q[j / 4] = q[j / 4] & ~(0xFFu << (8 * (j % 4))) | (uint32_t)held[1][token[j]][at] << (8 * (j % 4));
+                    if (mask >> j & 1u) q[j / 4] = q[j / 4] & ~(0xFFu << (8 * (j % 4))) | (uint32_t)held[1][token[j]][at] << (8 * (j % 4));
                 *reinterpret_cast<uint4*>(to) = make_uint4(q[0], q[1], q[2], q[3]);
             } else {
-                for (uint32_t j = 0; j < 16; ++j)
-                    if (token[j] != kNobody) to[j] = held[1][token[j]][at];
+                for (uint32_t left = mask; left; left &= left - 1u) {
+                    const uint32_t j = __ffs(left) - 1u;
+                    to[j] = held[1][token[j]][at];
+                }
             }
         }
     }
