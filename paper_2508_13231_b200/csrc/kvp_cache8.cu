@@ -62,26 +62,29 @@ struct Eight {
         else if constexpr (std::is_same<T, __half>::value) return i % 2 ? __high2float(half2_of(w[i / 2])) : __low2float(half2_of(w[i / 2]));
         else return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     }
-    // as fp32, NaN as 0, cut to what is held; returns the largest magnitude
-    __device__ __forceinline__ float floats(float* x) const
+    // The largest magnitude of what is held, as the bits of an fp32 number: without the signs numbers are in the order of their bits.
+    __device__ __forceinline__ uint32_t most(bool& odd) const              // odd: some number is not held as it is
     {
-        float m = 0.0f, odd = 0.0f;
+        uint32_t m;
+        if constexpr (sizeof(T) == 4) {
+            m = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[i] = at(i);
-            m = fmaxf(m, fabsf(x[i]));
-            odd = fmaf(x[i], 0.0f, odd);                               // NaN if one is not finite
+            for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
+        } else {
+            m = __vimax3_u16x2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu, w[2] & 0x7FFF7FFFu);
+            m = __vimax3_u16x2(m, w[3] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu);
+            m = max(m & 0xFFFFu, m >> 16);
+            if constexpr (std::is_same<T, __half>::value) m = m >= 0x7C00u ? 0x7F800000u : __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));
+            else m <<= 16;
         }
-        if (odd != 0.0f || m > kMost) {                                // rare
-            m = 0.0f;
+        odd = m > __float_as_uint(kMost);
+        if (!odd) return m;
+        m = 0;                                                         // rare: NaN and what is cut
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = x[i] != x[i] ? 0.0f : fminf(fmaxf(x[i], -kMost), kMost);
-                m = fmaxf(m, fabsf(x[i]));
-            }
-        }
+        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(fabsf(held(at(i)))));
         return m;
     }
+    static __device__ __forceinline__ float held(float x) { return x != x ? 0.0f : fminf(fmaxf(x, -kMost), kMost); }
 };
 
 // the block of a slot, for one head; slot < slots_in_cache
@@ -115,11 +118,20 @@ __device__ __forceinline__ uint32_t rounded_again(uint32_t four, float by)
 }
 
 // eight numbers over a power of two, or 0 where that is 0
-__device__ __forceinline__ uint2 rounded(const float* x, float scale)
+template <typename T>
+__device__ __forceinline__ uint2 rounded(const Eight<T>& x, float scale, bool odd)
 {
     if (!(scale > 0.0f)) return make_uint2(0, 0);
     const float by = __int_as_float((254 << 23) - __float_as_int(scale));              // 1 / scale
-    return make_uint2(e4m3_pair(x[0] * by, x[1] * by) | e4m3_pair(x[2] * by, x[3] * by) << 16, e4m3_pair(x[4] * by, x[5] * by) | e4m3_pair(x[6] * by, x[7] * by) << 16);
+    uint32_t q[4];
+    if (!odd) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = e4m3_pair(x.at(2 * i) * by, x.at(2 * i + 1) * by);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = e4m3_pair(Eight<T>::held(x.at(2 * i)) * by, Eight<T>::held(x.at(2 * i + 1)) * by);
+    }
+    return make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
 }
 
 constexpr uint8_t kNobody = 0xFF;
@@ -145,7 +157,7 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
     constexpr uint32_t kThreads = 2 * D, kPerRow = D / 8, kStride = D + 8;             // rows eight apart lie in other banks
     __shared__ int64_t slot[48];                                       // of the tokens from 16 before the CTA's first on; -1: none
     __shared__ uint8_t run_of[32];                                     // of the tokens from the CTA's first on
-    __shared__ float most[2][32];
+    __shared__ uint32_t most[2][32];                                   // bits of magnitudes
     __shared__ Runs runs;
     __shared__ bool whole;
     __shared__ alignas(16) uint8_t held[2][32][kStride];
@@ -207,28 +219,26 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
             }
         }
     }
-    float x[2][8];
+    const Eight<T> x[2] = {raw[0], raw[1]};
+    bool odd[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        float m = raw[u].floats(x[u]);
+        uint32_t m = x[u].most(odd[u]);
 #pragma unroll
-        for (uint32_t o = 1; o < kPerRow; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        for (uint32_t o = 1; o < kPerRow; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
         if (part == 0) most[u][row] = m;
     }
+    if (round + gridDim.x < rounds) fetch(round + gridDim.x);
     __syncthreads();
     if (whole) {
-        if (round + gridDim.x < rounds) fetch(round + gridDim.x);
         uint8_t* const block = p.cache + runs.block[0];
         float scale[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            float m = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) m = fmaxf(m, most[u][i]);
-            scale[u] = scale_for(m);
+            scale[u] = scale_for(__uint_as_float(__reduce_max_sync(0xFFFFFFFFu, most[u][lane % 16])));
         }
-        *reinterpret_cast<uint2*>(block + L::key(row, part / 2) + 8 * (part % 2)) = rounded(x[0], scale[0]);
-        *reinterpret_cast<uint2*>(&held[1][row][8 * part]) = rounded(x[1], scale[1]);
+        *reinterpret_cast<uint2*>(block + L::key(row, part / 2) + 8 * (part % 2)) = rounded(x[0], scale[0], odd[0]);
+        *reinterpret_cast<uint2*>(&held[1][row][8 * part]) = rounded(x[1], scale[1], odd[1]);
         if (tid == 0) *reinterpret_cast<float2*>(block + L::kScale) = make_float2(scale[0], scale[1]);
         __syncthreads();
         const uint32_t d = tid / 2, first = tid % 2 * 8;
@@ -239,14 +249,15 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
         continue;                                                      // what the next round writes before its first barrier nobody reads any more
     }
     const bool in0 = run_of[row] != kNobody, in1 = row < 15 && run_of[16 + row] != kNobody;
-    float y[2][8];                                                     // of the token 16 further on
+    Eight<T> y[2];                                                     // of the token 16 further on
+    bool odder[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        raw[u].clear();
-        if (in1) raw[u].load(from(u, base + 16 + row, head), aligned);
-        float m = raw[u].floats(y[u]);
+        y[u].clear();
+        if (in1) y[u].load(from(u, base + 16 + row, head), aligned);
+        uint32_t m = y[u].most(odder[u]);
 #pragma unroll
-        for (uint32_t o = 1; o < kPerRow; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        for (uint32_t o = 1; o < kPerRow; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
         if (part == 0) most[u][16 + row] = m;
     }
     __syncthreads();
@@ -254,16 +265,15 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
         const uint32_t run = tid / 2, u = tid % 2;
         const bool begins = runs.token[run][0] != kNobody;             // the block's first token is among them: nothing is held
         const float old = begins ? 0.0f : runs.old[u][run];
-        float m = 0.0f;
-        uint32_t mask = 0;
+        uint32_t m = 0, mask = 0;
 #pragma unroll
         for (uint32_t i = 0; i < 16; ++i) {
             const uint32_t t = runs.token[run][i];
-            m = fmaxf(m, t != kNobody ? most[u][t] : 0.0f);
+            m = max(m, t != kNobody ? most[u][t] : 0u);
             mask |= (t != kNobody) << i;
         }
         if (u == 0) runs.mask[run] = mask;
-        const float now = fmaxf(old, scale_for(m));
+        const float now = fmaxf(old, scale_for(__uint_as_float(m)));
         runs.old[u][run] = old;
         runs.now[u][run] = now;
         if (now != old || begins) *reinterpret_cast<float*>(p.cache + runs.block[run] + L::kScale + 4 * u) = now;
@@ -271,8 +281,8 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        if (in0) *reinterpret_cast<uint2*>(&held[u][row][8 * part]) = rounded(x[u], runs.now[u][run_of[row]]);
-        if (in1) *reinterpret_cast<uint2*>(&held[u][16 + row][8 * part]) = rounded(y[u], runs.now[u][run_of[16 + row]]);
+        if (in0) *reinterpret_cast<uint2*>(&held[u][row][8 * part]) = rounded(x[u], runs.now[u][run_of[row]], odd[u]);
+        if (in1) *reinterpret_cast<uint2*>(&held[u][16 + row][8 * part]) = rounded(y[u], runs.now[u][run_of[16 + row]], odder[u]);
     }
     __syncthreads();
     // 2 D pieces of 16 bytes a run: its keys (place, 16 dims), then its values (dim, 16 places)
@@ -321,7 +331,6 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
             }
         }
     }
-    if (round + gridDim.x < rounds) fetch(round + gridDim.x);
     __syncthreads();
     }
 }
