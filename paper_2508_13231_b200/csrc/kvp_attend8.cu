@@ -108,7 +108,10 @@ __global__ void __launch_bounds__(kThreads) count8_kernel(const Attend8K p)
 
 // D: dims of a head; ROWS: rows of a segment, 8, 16, 32 or 64. A team is four warps that turn the scores of a group (eight tiles, 128 tokens) into
 // weights, a token a thread, for 16 rows at most. Teams share a group's rows (kRowTeams) and take groups in turn (kTurns): one group takes a warp 2000 cycles, most of them
-// latency, so two groups under way a CTA and two CTAs an SM where they fit. Each turn has scores, weights and sums of its own.
+// latency, so several groups are under way, in two CTAs of an SM or in turns of one, as registers allow without spills. Each turn has scores, weights and sums of its own.
+// Us, 131072 tokens x 8 heads of 128 dims x 8 rows: two CTAs without turns 57.5, with two (spills) 60.5; 16 sequences of 8192 tokens x 4 heads of 128 x 12 rows: one CTA of two
+// row teams and two turns 48, two CTAs with turns (spills) 59; the windowed case, 64 dims x 12 rows: 29.6 and 28.3.
+__host__ __device__ constexpr bool two_ctas(uint32_t d, uint32_t rows) { return d <= 128 && (rows <= 8 || (rows == 16 && d == 64)); }
 template <int D_, bool HALF_, uint32_t ROWS_>
 struct Shape8 {
     static constexpr int D = D_;
@@ -120,15 +123,15 @@ struct Shape8 {
     static constexpr uint32_t kPCols = (3 * ROWS + 15) / 16 * 16;
     static constexpr uint32_t kHalves = D == 256 ? 2 : 1;              // 128 dims of values a product
     static constexpr uint32_t kSumCols = kHalves * kPCols;
-    static constexpr uint32_t kRowTeams = ROWS > 16 ? ROWS / 16 : 1;
-    static constexpr uint32_t kTurns = ROWS <= 32 && 2 * (kQCols + kSumCols) <= 512 ? 2 : 1;
+    static constexpr uint32_t kCtas = two_ctas(D, ROWS) ? 2 : 1;       // of an SM
+    static constexpr uint32_t kRowTeams = ROWS > 16 ? ROWS / 16 : ROWS == 16 && kCtas == 1 ? 2 : 1;
+    static constexpr uint32_t kTurns = (ROWS > 8 || kCtas == 1) && ROWS <= 32 && 2 * (kQCols + kSumCols) <= 512 ? 2 : 1;
     static constexpr uint32_t kTeams = kRowTeams * kTurns;
     static constexpr uint32_t kRowsEach = ROWS / kRowTeams;
     static constexpr uint32_t kBlock = 32 * kOthers + 128 * kTeams;
     static constexpr uint32_t kScoreBufs = kTurns == 2 || 2 * kQCols + kSumCols <= 512 ? 2 : 1;
     static constexpr uint32_t kColsUsed = kScoreBufs * kQCols + kTurns * kSumCols;
     static constexpr uint32_t kCols = kColsUsed <= 64 ? 64 : kColsUsed <= 128 ? 128 : kColsUsed <= 256 ? 256 : 512;
-    static constexpr uint32_t kCtas = D <= 128 && ROWS <= 16 ? 2 : 1;  // of an SM
     // shared memory: a stage of keys is free when the scores are there, one of values when the sums are
     static constexpr uint32_t kKeyStage = kGroup * L::kKeyBytes, kValueStage = kGroup * L::kValueBytes;
     static constexpr uint32_t kQBytes = kQCols * D;
@@ -783,9 +786,13 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     term[1][r / 4] = next_term(a, b);
                     term[2][r / 4] = last_term(a, b);
                 }
-                if constexpr (R == 8) {
+                if constexpr (ROWS == 8) {
                     *reinterpret_cast<uint4*>(to) = make_uint4(term[0][0], term[0][1], term[1][0], term[1][1]);
                     *reinterpret_cast<uint2*>(to + 2048) = make_uint2(term[2][0], term[2][1]);
+                } else if constexpr (R == 8) {
+#pragma unroll
+                    for (uint32_t i = 0; i < 3; ++i)
+                        *reinterpret_cast<uint2*>(to + (i * ROWS + row0) / 16 * 2048 + row0 % 16) = make_uint2(term[i][0], term[i][1]);
                 } else {
 #pragma unroll
                     for (uint32_t i = 0; i < 3; ++i)
@@ -918,7 +925,7 @@ Work8 workspace_of(const kvp_attend8_params* a, bool weights, bool bitmap)
     w.rows = segment_rows(a);
     const uint64_t rows = (uint64_t)a->queries * a->group, segs = (rows + w.rows - 1) / w.rows, bh = (uint64_t)a->batch * a->cache.kv_heads;
     const uint64_t tokens = (uint64_t)a->table_pages * a->cache.page_tokens, tiles = bh * segs * (tokens / kTileTokens);
-    const uint64_t most = a->cache.head_dim == 256 || w.rows > 16 ? 148 : 296;
+    const uint64_t most = two_ctas(a->cache.head_dim, w.rows) ? 296 : 148;
     w.ctas = (uint32_t)(tiles < most ? (tiles ? tiles : 1) : most);
     const uint64_t slots = w.ctas + bh * segs, sub = a->unit_tokens < kTileTokens ? a->unit_tokens : kTileTokens;
     w.ml = up256(slots * w.rows * a->cache.head_dim * 4);
