@@ -19,6 +19,10 @@
 // A CTA: warp 0 sends for tiles (bulk copies; a stage is eight tiles, keys and values), one thread of warp 1 issues the products with keys, one of
 // warp 2 those with values, teams of four warps turn scores into weights, a token a thread. Every hand-over is a barrier in
 // shared memory whose wait ends after two seconds; a CTA that gave up writes NaN.
+//
+// What bounds it. 131072 tokens x 8 heads of 128 dims x 8 queries with weights (270 MB, 42 us at the rate of a copy) take 57.8 us: 12 until the first groups are through (line,
+// queries and first tiles, and the instructions' first fetch), then memory at 5.6 TB/s, 3 for the join; issue slots 36%, matrix unit 6% busy. A chunk of 512 queries x
+// 4 heads over 32768 tokens x 8 heads: 782 us, 352 TFLOP/s, issue slots 59%, matrix unit 20%: 25 instructions of a warp a score, a third of them for the terms.
 #include <type_traits>
 
 #include "kvp_line.cuh"

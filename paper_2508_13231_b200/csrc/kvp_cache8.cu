@@ -4,6 +4,9 @@
 // the smallest power of two 2^e with |x| <= 448 * 2^e for all of them. A power of two costs nothing (e4m3 has the same four bits over 2^15 of its
 // range) and makes the form exact to handle: x / scale is exact, and when a token comes that asks for a larger scale, what
 // the block holds is divided by a power of two, which rounds only what falls below e4m3's normal numbers (2^-15 of the block's largest).
+//
+// What bounds it, 32768 tokens x 8 heads of 128 dims, bf16 (134 MB of numbers, 67 MB of blocks): writing 63 us, instructions (20 a number, issue slots 66%) and three
+// barriers a block, with the next block's loads under way; reading 44 us, the latency of loads at full occupancy. A step of 32 tokens: 6 and 3.5 us, latency.
 #include <type_traits>
 
 #include "kvp_line.cuh"
@@ -148,8 +151,7 @@ struct Runs {
 // A CTA takes the runs that begin among 16 tokens, of one head, keys and values; the last runs may go on behind the 16, so a thread has eight dims of two
 // tokens. One CTA thus knows the largest magnitude of a block's new tokens, and the block's bytes are written by nobody else.
 // Where the 16 tokens are a block from its first place to its last, as most of a prompt's are, nothing else is looked at: keys are written as a thread has them
-// (two tokens of a warp fill whole sectors), values by way of shared memory, 8 tokens of a dim a thread. 32768 tokens x 8 heads of 128 dims, bf16:
-// see launch_append. Elsewhere a run's bytes are gathered in shared memory and written 16 at a time, or one by one where the run does not fill the block and its scale stays.
+// (two tokens of a warp fill whole sectors), values by way of shared memory, 8 tokens of a dim a thread. Elsewhere a run's bytes are gathered in shared memory and written 16 at a time, or one by one where the run does not fill the block and its scale stays.
 template <int D, typename T>
 __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Rows8K p, uint32_t rounds, bool aligned)
 {

@@ -5,7 +5,8 @@
 // of a turn, whose fp32 form is off by 2^-27 turns at most.
 //
 // What bounds it is memory: a thread computes the sines and cosines of its pairs once and goes through several heads with them,
-// 16 bytes at a time.
+// 16 bytes at a time, four heads' loads under way. 32768 tokens x 40 heads of 128 dims, bf16 (671 MB): 103 us, 6.5 TB/s; one head's loads at a time 203, elements
+// unpacked as they are loaded 184 (120 registers instead of 80). 32 tokens: 2.5 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
