@@ -84,8 +84,8 @@ __device__ __forceinline__ bool tile_seen(const Attend8K& p, uint32_t len, uint3
 __global__ void __launch_bounds__(kThreads) count8_kernel(const Attend8K p)
 {
     __shared__ uint32_t sum[kWarps];
-    let_next_start();
     wait_for_previous();
+    let_next_start();
     const uint32_t bh = blockIdx.x, tid = threadIdx.x;
     const uint32_t len = length_of(p, p.heads.of(bh)), units = units_of(p, len), tiles = tiles_of(len);
     const uint32_t k = p.unit > kTileTokens ? p.unit / kTileTokens : 1;
@@ -336,7 +336,6 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
     extern __shared__ __align__(128) uint8_t room[];
     __shared__ Smem8<S> sm;
     static_assert(sizeof(Smem8<S>) <= S::kStatic, "does not fit");
-    let_next_start();
     const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     const auto bar = [](uint64_t& b) { return smem_at(&b); };
     if (tid == 0) {
@@ -359,6 +358,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
         show_to_async();
     }
     wait_for_previous();
+    let_next_start();                                                  // not sooner: the join looks at the lengths, and fills rows that see nothing, before it waits
     if (warp == 1) tensor_alloc<S::kCols>(smem_at(&sm.tensor));        // not sooner: the kernel before may still have to ask for its own
     Walk walk;
     {

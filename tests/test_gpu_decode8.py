@@ -102,6 +102,32 @@ def test_a_captured_step_replayed():
         assert torch.equal(eager.cache, graphed.cache) and torch.equal(eager.table, graphed.table) and torch.equal(eager.lens, graphed.lens)
 
 
+def test_lengths_that_a_kernel_just_before_makes():
+    """A long kernel, block tables in place and attention right behind each other: every part of attention sees the new lengths, also those that come up early."""
+    from paper_2508_13231_b200 import kvp
+    rng = torch.Generator(device="cuda").manual_seed(3)
+    batch, width, pages = 64, 40, 64 * 40
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    cache = torch.zeros(pages, H, kvp.cache8_page_bytes(D, 16), dtype=torch.uint8, device="cuda")
+    x = torch.randn(2, pages * 16, H, D, generator=rng, device="cuda").bfloat16()
+    kvp.cache8_append(cache, x[0], x[1], torch.arange(pages * 16, device="cuda"))
+    table, ring = torch.full((batch, width), -1, dtype=torch.int32, device="cuda"), torch.randperm(pages, generator=rng, device="cuda").int()
+    lens, state, new = i32(batch), torch.tensor([0, pages], dtype=torch.int32, device="cuda"), i32(batch)
+    q = torch.randn(batch, H * G, D, generator=rng, device="cuda").bfloat16()
+    big, at, f = torch.randn(16384, 8, 128, device="cuda").bfloat16(), torch.arange(16384, dtype=torch.int32, device="cuda"), kvp.rope_frequencies(128)[0].cuda()
+    for step in range(20):
+        new.copy_(torch.randint(0, 60, (batch,), generator=rng, device="cuda"))
+        new[torch.rand(batch, generator=rng, device="cuda") < 0.3] = -1                # these have no token then: their rows are zeros
+        torch.cuda.synchronize()
+        kvp.rope(big, None, at, f)
+        kvp.block_tables(new, lens, table, ring, state, 16, 64 * 64, lens_out=lens, state_out=state)
+        got = kvp.attend8(q, cache, table, lens, want_lse=True, want_weights=True)
+        torch.cuda.synchronize()
+        want = kvp.attend8(q, cache, table, lens, want_lse=True, want_weights=True)
+        assert all(torch.equal(got[k], want[k]) for k in want), step
+        assert bool(got["lse"][lens == 0].isneginf().all()) and not bool(got["out"][lens == 0].any())
+
+
 def test_the_recorded_study_in_8_bits():
     from paper_2508_13231_b200 import figures
     out, kept = figures.recorded("recorded_small", quick=True, bits=8)
