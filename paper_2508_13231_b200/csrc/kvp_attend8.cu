@@ -9,7 +9,7 @@
 // e4m3's four is split into x = t0 + t1 / 32 + t2 / 1024, each the nearest e4m3 to what the ones before leave. A bf16 query is two terms and an fp16 query three,
 // exactly (down to 2^-14 of the row's largest, below that to within 2^-22 of it); a weight is rounded to fp16 (2^-11 of itself)
 // and that is three terms, exactly, down to 2^-26 of the largest. Products of e4m3 numbers are exact and the unit keeps 25 bits of their sums; terms have sums of their own, joined in fp32.
-// No byte of the cache goes through a register, and a chunk of a prompt runs at the matrix unit's rate for 16 bits.
+// No byte of the cache goes through a register, and a chunk of a prompt reads it once for 64 rows.
 //
 // exp runs in fp32 against a running maximum that moves only when a score passes it by 2^2 (kSlack). A weight times 2^6 and the scale of its block's values over the
 // largest such scale so far is what is split: at most 256.
@@ -20,7 +20,7 @@
 // warp 2 those with values, teams of four warps turn scores into weights, a token a thread. Every hand-over is a barrier in
 // shared memory whose wait ends after two seconds; a CTA that gave up writes NaN.
 //
-// What bounds it. 131072 tokens x 8 heads of 128 dims x 8 queries with weights (270 MB, 42 us at the rate of a copy) take 57.8 us: 12 until the first groups are through (line,
+// What bounds it. 131072 tokens x 8 heads of 128 dims x 8 queries with weights (270 MB, 42 us at the rate of a copy) take 57 us: 12 until the first groups are through (line,
 // queries and first tiles, and the instructions' first fetch), then memory at 5.6 TB/s, 3 for the join; issue slots 36%, matrix unit 6% busy. A chunk of 512 queries x
 // 4 heads over 32768 tokens x 8 heads: 782 us, 352 TFLOP/s, issue slots 59%, matrix unit 20%: 25 instructions of a warp a score, a third of them for the terms.
 #include <type_traits>
@@ -33,7 +33,9 @@ namespace kvp {
 
 namespace {
 
-constexpr uint32_t kFixed8 = 48;              // what a CTA spends on a segment whatever its length, in tiles
+// What a CTA spends on a segment whatever its length, in tiles. Us with 16, 32, 48, 96, 144: 32 sequences of up to 8192 tokens x 8 heads of 128 dims 75, 71, 69, 74, 79 (capped), of
+// 64 dims 59, 56, 57, 61, 67, of 256 114, 110, 110, 113, 116; 64 of up to 2048 60, 56, 55, 57, 60; four of up to 8192 23.4 to 21.4.
+constexpr uint32_t kFixed8 = 48;
 constexpr uint32_t kGroup = 8;                // tiles of a stage
 constexpr uint32_t kOthers = 3;               // warps that are in no team
 constexpr uint32_t kListCap8 = 1024;          // units of a bitmap row that are listed at a time: 32 words
