@@ -198,7 +198,7 @@ struct Smem8 {
     uint64_t values[S::kValueStages], values_free[S::kValueStages];
     uint64_t scored[2], taken[2];                      // scores are in tensor memory; they are in registers
     uint64_t weighed[2], summed[2];                    // weights are in shared memory; the products with values are done
-    uint64_t query;                                    // a segment's queries are in shared memory
+    uint64_t query;                                    // the queries of a segment with tiles are in shared memory
     uint32_t tensor, gave_up;
     LineSmem line;
     Walk walk[2];                                      // the teams': this segment, and the next one
@@ -492,12 +492,14 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
             }
         } else if (warp == 1 && lane == 0) {
             // ---- products with keys ----
-            uint32_t segment = 0, it = 0;
+            uint32_t it = 0, turn = 0;
             bool ok = true;
             Ring<S::kKeyStages> ks;
             Ring<S::kScoreBufs> sb;
-            for (; ok && more; ++segment, more = walk.next<ROWS>(p)) {
-                ok = barrier_wait(bar(sm.query), segment & 1u, gave_up);
+            for (; ok && more; more = walk.next<ROWS>(p)) {
+                if (!walk.tiles) continue;                             // nobody arrives for it either
+                ok = barrier_wait(bar(sm.query), turn, gave_up);
+                turn ^= 1u;
                 for (uint32_t g = 0; ok && g < walk.tiles; g += kGroup, ++it) {
                     ok = barrier_wait(bar(sm.keys[ks.at]), ks.parity, gave_up) && (it < S::kScoreBufs || barrier_wait(bar(sm.taken[sb.at]), sb.parity ^ 1u, gave_up));
                     if (!ok) break;
@@ -612,9 +614,10 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     sm.slope[row] = p.slopes && r < p.rows ? __ldg(p.slopes + walk.h * p.group.d + (r - query * p.group.d)) * kLog2e : 0.0f;
                     sm.see[row] = (int32_t)walk.len - (int32_t)p.queries + 1 + (int32_t)query;
                 }
+                // Only where products follow: the teams then wait for their scores, and are never more than one such segment ahead of the thread that looks at the parity.
                 show_to_async();
                 __syncwarp();
-                if (lane == 0) barrier_arrive(bar(sm.query));
+                if (lane == 0 && walk.tiles) barrier_arrive(bar(sm.query));
                 if (me < R) lows[me] = 0.0f;
                 teams_sync<S::kTeams>();
             }
