@@ -11,8 +11,9 @@
 // and that is three terms, exactly, down to 2^-26 of the largest. Products of e4m3 numbers are exact and the unit keeps 25 bits of their sums; terms have sums of their own, joined in fp32.
 // No byte of the cache goes through a register, and a chunk of a prompt reads it once for 64 rows.
 //
-// exp runs in fp32 against a running maximum that moves only when a score passes it by 2^2 (kSlack). A weight times 2^6 and the scale of its block's values over the
-// largest such scale so far is what is split: at most 256.
+// exp runs in fp32 against a running maximum M of s_i + e_i, with 2^e_i the scale of token i's values, over the tokens that the row sees: 2^(s_i - M) times 2^6 and the scale is
+// what is split. It is at most 64, and 256 before M moves: that happens only when a token passes it by 2^2 (kSlack). So neither values behind a row's mask nor large ones that get no
+// weight take bits from the others. The weights' sum has the same M; what it holds (up to 2^92 times as many as there are tokens, 2^-94 at least) fp32 does.
 //
 // Split over CTAs as in kvp_attend: one line of all tiles (16 tokens), cut into equal parts on the device; the join is its join.
 //
@@ -40,6 +41,7 @@ constexpr uint32_t kGroup = 8;                // tiles of a stage
 constexpr uint32_t kOthers = 3;               // warps that are in no team
 constexpr uint32_t kListCap8 = 1024;          // units of a bitmap row that are listed at a time: 32 words
 constexpr float kSlack = 2.0f;
+constexpr float kLeastPower = -90.0f;         // smaller scales count as 2^this where the maximum is looked for, also 0
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Attend8K : LineK<kFixed8> {
@@ -208,9 +210,9 @@ struct Smem8 {
     float slope[S::ROWS];                              // its bias a token,
     int32_t see[S::ROWS];                              // the tokens that it sees are before this one
     alignas(16) float low[S::kTeams][S::kRowsEach];    // what is added to scores: less the running maximum, 0 before a row has seen a token
-    alignas(16) float by[S::kTeams][S::kRowsEach];     // what sums are multiplied by when it moves; at the end of a segment see `last`
+    alignas(16) float by[S::kTeams][S::kRowsEach];     // how far it moves; at the end of a segment [0] is below 0 for a team that had no group
     float peak[S::kTeams][4][S::kRowsEach];            // of each warp: how far its scores pass it; at the end its sum of weights
-    float scale[S::kTeams][4];                         // of each warp: the largest scale of its values
+    float gone[S::kTeams][4];                          // at the end of a segment: NaN from a warp that gave up
     float2 last[S::kTeams][S::kRowsEach];              // of each turn's row: its factor, and the reciprocal of the row's sum
     uint16_t list[kListCap8];                          // units of 32 words of a bitmap's row
 };
@@ -623,7 +625,6 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
             }
             const uint32_t tiles = walk.tiles, len = walk.len;
             float l[R];                                                // sums of this thread's weights
-            float most_scale = 0.0f, lift_by = 0.0f;                   // largest scale of values so far, 2^6 over it
             bool any = false;                                          // has this team had a group of the segment?
             bool first = true, unset = true;                           // row `me` has not seen a token; some row has not
             const int32_t see_least = sm.see[row0], see_most = sm.see[row0 + R - 1];       // later rows are those of later queries
@@ -642,7 +643,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 const float2 scales = *reinterpret_cast<const float2*>(block + 16 * D);        // of keys, of values
                 bool live = tile != ~0u && pos < (int32_t)len;
                 if (live && p.units && p.unit < kTileTokens) live = bits_at(p, (uint64_t)walk.bh * p.row_units + ((uint32_t)pos >> p.unit_log2)) & 1u;
-                const float scale = live ? scales.y : 0.0f;
+                const float scale = live ? scales.y : 0.0f, power = fmaxf((float)((__float_as_int(scale) >> 23) - 127), kLeastPower);
                 // does every row see every token of the warp?
                 const bool all_seen = __all_sync(0xFFFFFFFFu, live && pos < see_least && (pos >= see_most - window || pos < sink));
                 ok = ok && barrier_wait(bar(sm.scored[sb.at]), sb.parity, gave_up);
@@ -692,15 +693,14 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                         s[r] = live && pos < see && (pos >= see - window || pos < sink) ? s[r] : -INFINITY;
                     }
                 }
-                float over = -INFINITY;                                // how far scores pass the maximum
+                float over = -INFINITY;                                // with `power`: how far tokens pass the maximum
 #pragma unroll
                 for (uint32_t r = 0; r < R; r += 2) over = fmaxf(over, fmaxf(s[r], s[r + 1]));
-                if (team_any(over > kSlack || scale > most_scale || unset || !ok, team)) {
-                    float x = warp_max(scale);
-                    if (lane == 0) sm.scale[team][part] = x;
+                if (team_any(over + power > kSlack || unset || !ok, team)) {
+                    float x = 0.0f;
 #pragma unroll
                     for (uint32_t r = 0; r < R; ++r) {
-                        const float y = warp_max(s[r]);
+                        const float y = warp_max(__fadd_ru(s[r], power));              // never less than it is, however large scores are
                         if (lane == r) x = y;
                     }
                     if (lane < R) sm.peak[team][part][lane] = x;
@@ -709,10 +709,6 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     __syncwarp();
                     if (team_any(!ok, team)) { ok = false; break; }    // also: the maxima are there
                     tensor_after_sync();
-                    const float new_scale = fmaxf(most_scale, fmaxf(fmaxf(sm.scale[team][0], sm.scale[team][1]), fmaxf(sm.scale[team][2], sm.scale[team][3])));
-                    const float by_scale = most_scale > 0.0f ? most_scale / new_scale : 1.0f;
-                    most_scale = new_scale;
-                    lift_by = new_scale > 0.0f ? 64.0f / new_scale : 0.0f;
                     bool none = false;                                 // has row `me` not seen a token?
                     if (me < R) {
                         float up = fmaxf(fmaxf(sm.peak[team][0][me], sm.peak[team][1][me]), fmaxf(sm.peak[team][2][me], sm.peak[team][3][me]));
@@ -721,8 +717,10 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                         none = up == kNone;
                         first = none;
                         if (none) up = 0.0f;
-                        sm.by[team][me] = up;
-                        lows[me] -= up;
+                        // what the maximum moves by once it is rounded is what the sums are told
+                        const float low = lows[me], now = __fsub_rd(low, up);
+                        sm.by[team][me] = low - now;
+                        lows[me] = now;
                     }
                     unset = team_any(none, team);                      // also: the new maxima are there
                     if (any) {
@@ -736,7 +734,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                                 tensor_wait_load();
                                 tensor_hold(y);
 #pragma unroll
-                                for (uint32_t i = 0; i < 8; ++i) y[i] *= exp2_fast(fminf(-sm.by[team][r + i], 0.0f)) * by_scale;
+                                for (uint32_t i = 0; i < 8; ++i) y[i] *= exp2_fast(fminf(-sm.by[team][r + i], 0.0f));
                                 tensor_store(at, y);
                             }
                         tensor_wait_store();
@@ -781,7 +779,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 }
                 // the weights as the right operand; the buffer is free when the products with what it held are done
                 if (it >= 2) ok = ok && barrier_wait(bar(sm.summed[pb.at]), pb.parity ^ 1u, gave_up);
-                const float by = scale * lift_by;
+                const float by = scale * 64.0f;
                 uint8_t* const to = weights + pb.at * S::kPBytes + me * 16;
                 uint32_t term[3][R / 4];
 #pragma unroll
@@ -841,7 +839,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 sum_neighbours<R, 5>(l, lane, from);                   // R <= 16: one row a lane is left
                 sm.peak[team][part][from] = l[0];                      // the same from lanes of the same row
             }
-            if (lane == 0) sm.scale[team][part] = ok ? 0.0f : NAN;
+            if (lane == 0) sm.gone[team][part] = ok ? 0.0f : NAN;
             teams_sync<S::kTeams>();
             tensor_after_sync();
             const bool whole = walk.take == walk.count;
@@ -853,27 +851,31 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 return ((uint64_t)walk.b * p.queries + query) * (p.heads.d * p.group.d) + walk.h * p.group.d + (row - query * p.group.d);
             };
             if (me < F) {
-                // row mine + me: its maximum and sum over the turns
-                float m = kNone, sum = 0.0f, one[S::kTurns];
+                // row mine + me: its maximum and sum over the turns. Sums come with powers of two of their own (the scales of the values at the maximum): such a power goes over to
+                // the maximum, so that those of other turns and other parts can be compared with it.
+                float m = kNone, sum = 0.0f, one[S::kTurns], high[S::kTurns];
 #pragma unroll
                 for (uint32_t u = 0; u < S::kTurns; ++u) {
                     const float* x = &sm.peak[team0 + u][0][mine + me];
-                    const float* gone = sm.scale[team0 + u];
+                    const float* gone = sm.gone[team0 + u];
                     one[u] = ((x[0] + x[R]) + (x[2 * R] + x[3 * R])) + ((gone[0] + gone[1]) + (gone[2] + gone[3]));
-                    if (one[u] != 0.0f) m = fmaxf(m, -sm.low[team0 + u][mine + me]);
+                    const int power = min(max((__float_as_int(one[u]) >> 23 & 0xFF) - 127, -126), 126);
+                    high[u] = (float)power - sm.low[team0 + u][mine + me];
+                    if (one[u] != 0.0f) m = fmaxf(m, high[u]);
+                    one[u] *= __int_as_float((127 - power) << 23);
                 }
 #pragma unroll
                 for (uint32_t u = 0; u < S::kTurns; ++u) {
-                    const float k = one[u] != 0.0f ? exp2_fast(-sm.low[team0 + u][mine + me] - m) : 0.0f;
-                    sum = fmaf(one[u], k, sum);
-                    sm.last[team0 + u][mine + me].x = k;
+                    const bool some = one[u] != 0.0f;
+                    sum = fmaf(one[u], some ? exp2_fast(high[u] - m) : 0.0f, sum);
+                    sm.last[team0 + u][mine + me].x = some ? 0x1p-6f * exp2_fast(-sm.low[team0 + u][mine + me] - m) : 0.0f;
                 }
                 const float by = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
                 sm.last[team0][mine + me].y = by;
                 p.ml[slot * ROWS + row0 + mine + me] = make_float2(m, sum);
                 if (whole && p.lse && row_at + me < p.rows) p.lse[place(row_at + me)] = sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
             }
-            if (me == 0) sm.by[team][0] = any ? most_scale * 0x1p-6f : -1.0f;          // a turn's units; below 0: it had no group
+            if (me == 0) sm.by[team][0] = any ? 0.0f : -1.0f;
             teams_sync<S::kTeams>();
 #pragma unroll 1
             for (uint32_t i = 0; i < S::kHalves * F / 4; ++i) {
@@ -881,8 +883,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 float y[4] = {0, 0, 0, 0};
 #pragma unroll
                 for (uint32_t u = 0; u < S::kTurns; ++u) {
-                    const float units = sm.by[team0 + u][0];
-                    if (units < 0.0f) continue;                        // uniform: nothing was written there
+                    if (sm.by[team0 + u][0] < 0.0f) continue;          // uniform: nothing was written there
                     float x[3][4];
 #pragma unroll
                     for (uint32_t c = 0; c < 3; ++c) tensor_load(sums_at + lanes + u * S::kSumCols + half * S::kPCols + c * ROWS + row0 + r, x[c]);
@@ -891,7 +892,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                     for (uint32_t c = 0; c < 3; ++c) tensor_hold(x[c]);
 #pragma unroll
                     for (uint32_t k = 0; k < 4; ++k)
-                        y[k] = fmaf(fmaf(fmaf(x[2][k], 0x1p-5f, x[1][k]), 0x1p-5f, x[0][k]), units * sm.last[team0 + u][r + k].x, y[k]);
+                        y[k] = fmaf(fmaf(fmaf(x[2][k], 0x1p-5f, x[1][k]), 0x1p-5f, x[0][k]), sm.last[team0 + u][r + k].x, y[k]);
                 }
                 if (d < D) {
 #pragma unroll

@@ -1,0 +1,162 @@
+"""Attention over the cache in 8 bits where values differ in size from block to block: what a row does not see, or gives no weight, does not change it.
+
+Tolerance of out, per row, with u the half-step of its type, `score` as in test_gpu_attend8.py (how far a score may be off), size = sum of p |v| and
+most = the largest product of a weight p and a scale of values over the tokens that the row sees: u |out| for its own rounding; (2^-11 for a weight's three
+terms + 2 score + count * 2^-29 for what the matrix unit cuts of the sums) * size; a weight times a scale is held to 2^-26 of most, for values of at most 448
+scales: 2^-17 * count * most.
+"""
+import os
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import cache8_plain as plain  # noqa: E402
+from test_gpu_attend8 import BF16, F16, cuda, kvp  # noqa: E402,F401
+
+pytestmark = pytest.mark.gpu
+
+
+def filled(kvp, k, v, page=16):  # noqa: F811
+    """One sequence's cache, its pages out of order, NaN where no token is."""
+    n, heads, d = k.shape
+    columns = -(-n // page)
+    table = np.random.default_rng(n).permutation(columns + 1)[:columns].astype(np.int32)[None]
+    cache = torch.full((columns + 1, heads, kvp.cache8_page_bytes(d, page)), 255, dtype=torch.uint8, device="cuda")
+    slots = table[0].astype(np.int64)[np.arange(n) // page] * page + np.arange(n) % page
+    kvp.cache8_append(cache, cuda(k.astype(np.float32)), cuda(v.astype(np.float32)), cuda(slots))
+    return cache, table, np.array([n], np.int32)
+
+
+def near(got, q, cache, table, lens, terms=2.0 ** -11, window=0, keep=None):
+    """out of one sequence against 64 bits; keep: units of 16 tokens that are read"""
+    b, t, hq, d = q.shape
+    (keys, _), (vals, vscale) = plain.held(cache.cpu().numpy(), d)
+    n, h = int(lens[0]), cache.shape[1]
+    ids, page = np.arange(n), keys.shape[2]
+    k, v, size = (x[table[0][ids // page], :, ids % page] for x in (keys, vals, vscale))
+    out, x, scale = got["out"].double().cpu().numpy()[0], q.double().cpu().numpy()[0], float(np.float32(d ** -0.5))
+    u = 2.0 ** -8 if q.dtype == BF16 else 2.0 ** -11
+    for j in range(t):
+        at = n - t + j
+        see = ids <= at
+        if window:
+            see &= ids > at - window
+        if keep is not None:
+            see &= keep[ids // 16]
+        for r in range(hq):
+            a, w, s = k[see, r * h // hq], v[see, r * h // hq], size[see, r * h // hq]
+            y = a @ x[j, r] * scale
+            p = np.exp(y - y.max())
+            p /= p.sum()
+            score = 16 * 2.0 ** -23 * (np.abs(a) @ np.abs(x[j, r]) * scale).max() + 2.0 ** -22 * (np.abs(x[j, r]).max() * np.abs(a).sum(-1).max() * scale + np.abs(y).max() + 1)
+            want = p @ w
+            room = u * np.abs(want) + (terms + 2 * score + len(p) * 2.0 ** -29) * (p @ np.abs(w)) + 2.0 ** -17 * len(p) * (p * s).max() + 2.0 ** -25
+            off = np.abs(out[j, r] - want)
+            worst = float((off / room).max())
+            assert worst <= 1, (j, r)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("d,group,queries", [(128, 1, 20), (128, 4, 24), (64, 2, 40), (256, 3, 18), (128, 8, 18)])
+@pytest.mark.parametrize("large", [2.0 ** 12, 2.0 ** 20, np.inf])
+def test_a_later_token_with_large_values_leaves_earlier_queries_alone(kvp, d, group, queries, dtype, large):  # noqa: F811
+    """The last query's token has values many times the others', also cut infinities: the queries before it, that do not see it, are as without it."""
+    rng = np.random.default_rng(d + group)
+    n = 320 + 1                                                # the last token has a block of its own
+    k, v = rng.standard_normal((2, n, 1, d))
+    v[-1] = large if np.isinf(large) else v[-1] * large
+    cache, table, lens = filled(kvp, k, v)
+    q = cuda(rng.standard_normal((1, queries, group, d)).astype(np.float32)).to(dtype)
+    got = kvp.attend8(q, cache, cuda(table), cuda(lens), want_lse=True)
+    before = dict(got, out=got["out"][:, :-1])
+    near(before, q[:, :-1], cache, table, lens - 1)
+    without = kvp.attend8(q[:, :-1], cache, cuda(table), cuda(lens - 1), want_lse=True)
+    near(without, q[:, :-1], cache, table, lens - 1)
+    if not np.isinf(large) and dtype == BF16:                  # fp16 does not hold 2^20 of the last row
+        near(dict(out=got["out"][:, -1:]), q[:, -1:], cache, table, lens)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows", [1, 8, 12, 40])
+def test_blocks_with_large_values_and_no_weight(kvp, dtype, rows):  # noqa: F811
+    """A token that takes most of the weight, a long tail that takes the rest, and blocks of values 2^12 or 2^20 times the others' that no row gives weight: out holds the tail.
+    The sequence is there many times, so that a CTA goes through all of it."""
+    d, n, batch = 128, 6000, 1200
+    rng = np.random.default_rng(rows)
+    for large, where in ((2.0 ** 12, 0), (2.0 ** 20, 0), (2.0 ** 12, n - 16), (2.0 ** 20, 2992)):
+        k = rng.standard_normal((n, 1, d)) * 0.05
+        k[..., 0] = 0.0
+        k[1000, 0, 0] = 100.0                                  # score 100 * 1.1 * scale = 9.7 over the tail's: e^9.7 tail tokens weigh as much
+        k[where: where + 16, 0, 0] = -400.0                    # e^-39
+        v = 1.0 + 0.1 * rng.standard_normal((n, 1, d))
+        v[992: 1008] *= 2.0 ** -10                             # what has most weight is small
+        v[where: where + 16] *= large
+        cache, table, lens = filled(kvp, k, v)
+        q = rng.standard_normal((1, 1, rows, d)) * 0.2
+        q[..., 0] = 1.1
+        q = cuda(q.astype(np.float32)).to(dtype)
+        got = kvp.attend8(q.expand(batch, -1, -1, -1), cache, cuda(np.repeat(table, batch, 0)), cuda(np.repeat(lens, batch)))
+        for i in (0, 7, batch // 2, batch - 1):
+            near(dict(out=got["out"][i: i + 1]), q, cache, table, lens)
+
+
+def test_what_windows_and_bitmaps_leave_out(kvp):  # noqa: F811
+    """Large values behind a window, or in units that are not read, beside small ones that are."""
+    d, n = 64, 700
+    rng = np.random.default_rng(5)
+    k, v = rng.standard_normal((2, n, 1, d))
+    v[: 300] *= 2.0 ** 18
+    cache, table, lens = filled(kvp, k, v)
+    q = cuda(rng.standard_normal((1, 3, 4, d)).astype(np.float32)).to(BF16)
+    # one query sees through the window the last token of the large ones' block, the others do not
+    window = n - 3 + 1 - 303
+    near(kvp.attend8(q, cache, cuda(table), cuda(lens), window=window), q, cache, table, lens, window=window)
+    keep = np.arange(-(-n // 16)) >= 19
+    units = cuda(np.packbits(np.pad(keep, (0, -len(keep) % 32)), bitorder="little").view(np.int32))
+    near(kvp.attend8(q, cache, cuda(table), cuda(lens), unit_tokens=16, units=units), q, cache, table, lens, keep=keep)
+
+
+def test_values_that_are_all_zero_or_tiny(kvp):  # noqa: F811
+    """Rows whose heaviest tokens have values 0, or 2^-90 of the others': zeros add nothing, and what has a value is kept."""
+    d, n = 128, 400
+    rng = np.random.default_rng(6)
+    for small in (0.0, 2.0 ** -90):
+        for first in (0, 384):
+            k, v = rng.standard_normal((2, n, 2, d)) * 0.3
+            k[first: first + 16] = 0.0
+            k[first: first + 16, :, 0] = 200.0                 # e^35 of the others
+            v[first: first + 16] *= small
+            cache, table, lens = filled(kvp, k, v)
+            q = rng.standard_normal((1, 1, 8, d)) * 0.2
+            q[..., 0] = 2.0
+            q = cuda(q.astype(np.float32)).to(BF16)
+            got = kvp.attend8(q, cache, cuda(table), cuda(lens))
+            near(got, q, cache, table, lens)
+            assert bool(got["out"].abs().amax() > 0)
+    k = np.zeros((n, 2, d))
+    cache, table, lens = filled(kvp, k, k)
+    assert not kvp.attend8(q, cache, cuda(table), cuda(lens))["out"].any()
+
+
+def test_parts_whose_values_differ_by_many_powers(kvp):  # noqa: F811
+    """The heaviest tokens have values 0 and a CTA of their own, what has values of 2^50 or 2^90 is elsewhere: the parts are joined all the same."""
+    d, n = 128, 3000
+    rng = np.random.default_rng(7)
+    for high in (1.0, 2.0 ** 50, 2.0 ** 90):
+        for first, last in ((0, 640), (2000, 3000)):
+            k, v = rng.standard_normal((2, n, 1, d)) * 0.3
+            k[first: last, :, 0] = 60.0                        # e^10 of the others
+            v[first: last] = 0.0
+            v[1000: 1500] *= high
+            cache, table, lens = filled(kvp, k, v)
+            for rows in (4, 20):
+                q = rng.standard_normal((1, 1, rows, d)) * 0.2
+                q[..., 0] = 2.0
+                q = cuda(q.astype(np.float32)).to(BF16)
+                got = kvp.attend8(q, cache, cuda(table), cuda(lens), want_lse=True, want_weights=True)
+                near(got, q, cache, table, lens)
+                # 500 tokens of at most 1000 that weigh e^10.6 each: 1.2e-5 of the weight, of values that average 0.3 / sqrt(500) over them: 1.7e-7 = 2^-22.5 a dim, of 128 dims and more
+                assert bool(got["out"].abs().amax() > high * 2.0 ** -24) and abs(float(got["weights"].sum()) - rows) < 1e-4 * rows
