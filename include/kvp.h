@@ -535,7 +535,7 @@ typedef struct {
  *   slopes  (device) [kv_heads * group] float or NULL: a score gets slope * (position of the token - position of the query) added, behind the cap
  * The scores of a query that sees a token are cap(scale * q . k) + bias in fp32. A query that sees no token gives out 0 and lse -infinity; a row of q
  * with a value that is not finite gives NaN. The products run in e4m3 with fp32 sums: a bf16 value of q enters exactly as two terms and an fp16 one as three (values
- * below 2^-14 of the row's largest to within 2^-22 of that), a weight times the scale of its block's values, rounded to fp16 (2^-11 of itself), as three, to within 2^-26 of
+ * below 2^-14 of the row's largest to within 2^-22 of that), a weight times the scale of its block's values as three (2^-13 of itself), to within 2^-26 of
  * the row's largest such product over the tokens that it sees (scales below 2^-90 count as that there). A chunk of a prompt (many queries) reads the cache once for every 64 rows.
  * A wait inside the kernel that takes two seconds, which only a fault can cause, ends it with NaN in out.
  * Errors: as of kvp_attend, and a cap that is negative or not finite or so small that scale / cap is not finite (KVP_ERR_ARG).

@@ -160,3 +160,19 @@ def test_parts_whose_values_differ_by_many_powers(kvp):  # noqa: F811
                 near(got, q, cache, table, lens)
                 # 500 tokens of at most 1000 that weigh e^10.6 each: 1.2e-5 of the weight, of values that average 0.3 / sqrt(500) over them: 1.7e-7 = 2^-22.5 a dim, of 128 dims and more
                 assert bool(got["out"].abs().amax() > high * 2.0 ** -24) and abs(float(got["weights"].sum()) - rows) < 1e-4 * rows
+
+
+@pytest.mark.parametrize("d,rows", [(64, 8), (64, 16), (128, 6), (128, 12), (128, 33), (256, 8), (256, 20)])
+def test_a_weight_keeps_fourteen_bits(kvp, d, rows):  # noqa: F811
+    """A few tokens with values in dims of their own: out is the weights themselves, times numbers that 8 bits hold. A weight is three terms, each the nearest of four significant bits to
+    what the ones before leave, 2^-5 of it at most: the third is off by 2^-14 of the weight, and the first remainder is rounded to fp16, 2^-16 of the weight. Together below 2^-13.
+    fp16 outputs are rounded by 2^-11 themselves; weights that are as well would add as much again."""
+    rng = np.random.default_rng(d + rows)
+    for n in (2, 3, 5, 8):
+        k, v = rng.standard_normal((n, 1, d)), np.zeros((n, 1, d))
+        for i in range(n):
+            v[i, 0, i::n] = 1.0
+        cache, table, lens = filled(kvp, k, v)
+        for _ in range(4):
+            q = cuda((rng.standard_normal((1, 1, rows, d)) * 1.5).astype(np.float32)).to(F16)
+            near(kvp.attend8(q, cache, cuda(table), cuda(lens)), q, cache, table, lens, terms=2.0 ** -13)
