@@ -582,7 +582,8 @@ int kvp_rope(const kvp_rope_params* params, const void* q, void* q_out, const vo
 #define KVP_ROPE_LINEAR 1u   /* all divided by factor                                                                  */
 #define KVP_ROPE_BASE   2u   /* base * factor^(rotary_dim / (rotary_dim - 2)): the highest stays, the lowest is divided */
 #define KVP_ROPE_PARTS  3u   /* by the turns t = original_tokens * frequency / 2 pi: t >= high stays, t <= low is divided, between linear in t */
-#define KVP_ROPE_RAMP   4u   /* the same borders, between them linear in j (their dims rounded outwards); scale = 0.1 ln(factor) + 1 */
+#define KVP_ROPE_RAMP   4u   /* the same borders, between them linear in j (their dims rounded outwards; the first not before pair 0, and with
+                             * low = 0 the second at the last pair, else it may lie behind that); scale = 0.1 ln(factor) + 1 */
 
 typedef struct {
     uint32_t kind;              /* KVP_ROPE_PLAIN .. KVP_ROPE_RAMP                              */

@@ -224,11 +224,11 @@ extern "C" int kvp_rope_frequencies(const kvp_rope_scaling* r, uint32_t rotary_d
             f = f * keep + f / r->factor * (1.0 - keep);
         }
         if (r->kind == KVP_ROPE_RAMP) {
-            // the same borders, but linear in the dim between those that turn `high` and `low` times, cut to whole dims
+            // the same borders, but linear in the dim between those that turn `high` and `low` times, rounded outwards to whole dims. The second may lie behind the last pair, which
+            // then is not divided in full.
             auto dim_of = [&](double turns) { return half * std::log(r->original_tokens / (turns * two_pi)) / std::log(base); };
             double from = std::floor(dim_of(r->high)), to = r->low > 0.0 ? std::ceil(dim_of(r->low)) : half - 1.0;
             if (!(from > 0.0)) from = 0.0;
-            if (!(to < half - 1.0)) to = half - 1.0;
             if (!(to > from)) to = from + 0.001;
             double divide = ((double)j - from) / (to - from);
             divide = divide < 0.0 ? 0.0 : divide > 1.0 ? 1.0 : divide;
