@@ -588,7 +588,7 @@ int kvp_rope(const kvp_rope_params* params, const void* q, void* q_out, const vo
 typedef struct {
     uint32_t kind;              /* KVP_ROPE_PLAIN .. KVP_ROPE_RAMP                              */
     uint32_t reserved;          /* must be 0 */
-    double   base;              /* usually 10000                                                */
+    double   base;              /* usually 10000; RAMP: above 1                                 */
     double   factor;            /* >= 1                                                         */
     double   original_tokens;   /* PARTS, RAMP: the context that the model was trained on       */
     double   low, high;         /* PARTS, RAMP: turns, 0 <= low < high (often 1 and 4, 1 and 32) */

@@ -213,6 +213,7 @@ extern "C" int kvp_rope_frequencies(const kvp_rope_scaling* r, uint32_t rotary_d
     const double two_pi = 6.283185307179586476925;
     double base = r->base;
     if (r->kind == KVP_ROPE_BASE) base *= std::pow(r->factor, (double)rotary_dim / (rotary_dim - 2));
+    if (!std::isnormal(base) || (r->kind == KVP_ROPE_RAMP && !(base > 1.0))) return KVP_ERR_ARG;     // frequencies of 0 or infinity; no borders
     for (uint32_t j = 0; j < half; ++j) {
         double f = std::pow(base, -(double)j / half);
         if (r->kind == KVP_ROPE_LINEAR) f /= r->factor;

@@ -37,3 +37,22 @@ def test_ramp_without_a_lower_border_ends_at_the_last_pair():
     first = math.floor(32 * math.log(8192 / (64 * math.pi)) / math.log(1e4))
     divided = np.clip((np.arange(32) - first) / (31 - first), 0, 1)
     assert np.allclose(got.numpy(), f / 8 * divided + f * (1 - divided), rtol=1e-13, atol=0) and math.isclose(float(got[-1]), f[-1] / 8, rel_tol=1e-13)
+
+
+@pytest.mark.parametrize("kw", [dict(scaling="ramp", base=1.0), dict(scaling="ramp", base=0.5), dict(scaling="base", base=1e300, factor=1e20), dict(scaling="base", base=2.0, factor=1e308),
+                                dict(scaling="linear", base=1e-320)])
+def test_frequencies_that_are_no_numbers_are_refused(kw):
+    """A base of 1 has no borders between its pairs, one beyond 64 bits leaves frequencies of 0, one of almost 0 infinite ones: never NaN, infinity or 0 for a frequency."""
+    from paper_2508_13231_b200 import kvp
+    kw = dict(dict(factor=4.0, original_tokens=4096), **kw)
+    with pytest.raises(kvp.KvpError) as e:
+        kvp.rope_frequencies(4, **kw)
+    assert e.value.code == kvp.ERR_ARG
+
+
+def test_frequencies_of_bases_below_one():
+    from paper_2508_13231_b200 import kvp
+    got, _ = kvp.rope_frequencies(8, base=0.5)
+    assert np.allclose(got.numpy(), 0.5 ** (-np.arange(4) / 4), rtol=1e-14, atol=0)
+    got, _ = kvp.rope_frequencies(8, base=0.5, scaling="parts", factor=2.0, original_tokens=64)
+    assert np.all(np.isfinite(got.numpy())) and np.all(got.numpy() > 0)
