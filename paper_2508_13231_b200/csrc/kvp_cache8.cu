@@ -215,9 +215,10 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
                 const uint64_t at = block_at<D>((uint64_t)mine, head, p);
                 const float2 old = *reinterpret_cast<const float2*>(p.cache + at + L::kScale);
                 runs.block[run] = at;
-                // a scale that is no power of two is none: nothing is held
-                runs.old[0][run] = old.x >= 0x1p-126f && old.x < INFINITY && !(__float_as_int(old.x) & 0x7FFFFF) ? old.x : 0.0f;
-                runs.old[1][run] = old.y >= 0x1p-126f && old.y < INFINITY && !(__float_as_int(old.y) & 0x7FFFFF) ? old.y : 0.0f;
+                // a scale that is no power of two is none: nothing is held, and -1 is changed whatever comes
+                const auto valid = [](float x) { return x == 0.0f || (x >= 0x1p-126f && x < INFINITY && !(__float_as_int(x) & 0x7FFFFF)); };
+                runs.old[0][run] = valid(old.x) ? old.x : -1.0f;
+                runs.old[1][run] = valid(old.y) ? old.y : -1.0f;
             }
         }
     }
@@ -275,7 +276,7 @@ __global__ void __launch_bounds__(2 * D, 1024 / (2 * D)) append8_kernel(const Ro
             mask |= (t != kNobody) << i;
         }
         if (u == 0) runs.mask[run] = mask;
-        const float now = fmaxf(old, scale_for(__uint_as_float(m)));
+        const float now = fmaxf(fmaxf(old, 0.0f), scale_for(__uint_as_float(m)));
         runs.old[u][run] = old;
         runs.now[u][run] = now;
         if (now != old || begins) *reinterpret_cast<float*>(p.cache + runs.block[run] + L::kScale + 4 * u) = now;
