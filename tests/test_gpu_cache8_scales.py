@@ -38,3 +38,31 @@ def test_zeros_into_a_block_without_a_scale(kvp, heads, d):  # noqa: F811
                     kvp.cache8_append(c, y, y, cuda(np.array([9])))
                 for a, b in zip(kvp.cache8_read(dev, cuda(np.arange(16)), d, F32), kvp.cache8_read(clean, cuda(np.arange(16)), d, F32)):
                     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("d,page,heads", [(64, 16, 2), (128, 32, 1), (256, 48, 1)])
+def test_blocks_that_begin_anew_with_some_of_their_tokens(kvp, d, page, heads):  # noqa: F811
+    """Runs that contain their block's first place, over blocks that held others: the scales are those of the new tokens alone, the bytes of the places behind them stay as they were
+    (nothing reads them), and the other blocks are not touched."""
+    rng = np.random.default_rng(d)
+    pages = 6
+    cache = random_cache(rng, pages, heads, d, page)
+    blocks = rng.permutation(pages * page // 16)[:5]
+    many = rng.integers(1, 16, 5)
+    slots = np.concatenate([b * 16 + np.arange(n) for b, n in zip(blocks, many)]).astype(np.int64)
+    k, v = (cuda(x).float() for x in rng.standard_normal((2, len(slots), heads, d)) * 2.0 ** -9)
+    dev, before = cuda(cache), cache.copy()
+    kvp.cache8_append(dev, k, v, cuda(slots))
+    plain.append(cache, f64(k), f64(v), slots)
+    got = dev.cpu().numpy()
+    assert np.array_equal(got, cache)
+    raw, old = (x.reshape(pages, heads, page // 16, -1).transpose(0, 2, 1, 3).reshape(pages * page // 16, heads, -1) for x in (got, before))
+    keys, values = plain.places(d)
+    for b, n in zip(blocks, many):
+        for where in (keys, values):
+            assert np.array_equal(raw[b][:, where[n:]], old[b][:, where[n:]])
+        for x, field in ((k, 32 * d), (v, 32 * d + 4)):
+            scale = np.ascontiguousarray(raw[b][:, field: field + 4]).view(np.float32)[:, 0]
+            assert scale.tolist() == [plain.scale_of(float(np.abs(f64(x)[slots // 16 == b][:, j]).max())) for j in range(heads)]
+    rest = np.setdiff1d(np.arange(len(raw)), blocks)
+    assert np.array_equal(raw[rest], old[rest])
