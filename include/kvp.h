@@ -538,7 +538,7 @@ typedef struct {
  * below 2^-14 of the row's largest to within 2^-22 of that), a weight times the scale of its block's values as three (2^-13 of itself), to within 2^-26 of
  * the row's largest such product over the tokens that it sees (scales below 2^-90 count as that there). A chunk of a prompt (many queries) reads the cache once for every 64 rows.
  * A wait inside the kernel that takes two seconds, which only a fault can cause, ends it with NaN in out.
- * Errors: as of kvp_attend, and a cap that is negative or not finite or so small that scale / cap is not finite (KVP_ERR_ARG).
+ * Errors: as of kvp_attend, and a cap that is negative or not finite, or so small or large that scale / cap or cap / ln 2 is no normal number (KVP_ERR_ARG).
  */
 int kvp_attend8_workspace(const kvp_attend8_params* params, int want_weights, int has_units, uint64_t* bytes);
 int kvp_attend8(const kvp_attend8_params* params, const void* q, const void* cache, const int32_t* table, const int32_t* lens,

@@ -963,7 +963,8 @@ int check_attend8(const kvp_attend8_params* a)
     const uint32_t u = a->unit_tokens;
     if (!u || a->cache.page_tokens % u || (u < kTileTokens ? kTileTokens % u : u % kTileTokens)) return KVP_ERR_ARG;
     if (!(a->scale > -INFINITY && a->scale < INFINITY) || !(a->cap >= 0.0f && a->cap < INFINITY)) return KVP_ERR_ARG;
-    if (a->cap > 0.0f && !(fabsf(a->scale / a->cap) < INFINITY)) return KVP_ERR_ARG;
+    // scores in units of the cap, and the cap to the base 2, are normal numbers
+    if (a->cap > 0.0f && (!(fabsf(a->scale / a->cap) < INFINITY) || !(a->cap * kLog2e < INFINITY) || (a->scale != 0.0f && fabsf(a->scale / a->cap) < 0x1p-126f))) return KVP_ERR_ARG;
     if (!head_dim_served(a->cache.head_dim)) return KVP_ERR_RANGE;
     const uint64_t rows = (uint64_t)a->queries * a->group, bh = (uint64_t)a->batch * a->cache.kv_heads;
     const uint64_t tokens = (uint64_t)a->table_pages * a->cache.page_tokens;
