@@ -1,8 +1,8 @@
 // Rotary positions (include/kvp.h, kvp_rope): pairs of dims of queries and keys turned by position * frequency.
 //
-// An angle is kept as a fraction of a turn, in 2^-64 turns: frequency / 2 pi as a 64-bit fraction times the position, modulo 2^64,
-// is the exact remainder of the frequency as it is held (53 bits), however far the position. Its upper bits give the quadrant and what is left, at most an eighth
-// of a turn, whose fp32 form is off by 2^-27 turns at most.
+// An angle is kept as a fraction of a turn, in 2^-64 turns: frequency / 2 pi, to 2^-64 turns, times the position, modulo 2^64. A double holds 53 bits of that quotient, which
+// is not enough (2^31 tokens at a radian each would be off by 2^-21), so it is two: the product with the double next to 1 / 2 pi, and what that leaves out. An angle is off by 2^-65 turns a token,
+// 2^-34 at the farthest. Its upper bits give the quadrant and what is left, at most an eighth of a turn, whose fp32 form is off by 2^-27 turns at most.
 //
 // What bounds it is memory: a thread computes the sines and cosines of its pairs once and goes through several heads with them,
 // 16 bytes at a time, four heads' loads under way. 32768 tokens x 40 heads of 128 dims, bf16 (671 MB): 103 us, 6.5 TB/s; one head's loads at a time 203, elements
@@ -84,8 +84,10 @@ struct Vec<T, 1> {
 
 __device__ __forceinline__ void turn_of(int32_t position, double frequency, float scale, bool inverse, float& c, float& s)
 {
-    const double turns = frequency * 0.15915494309189533577, part = (turns - floor(turns)) * 18446744073709551616.0;
-    const uint64_t angle = (uint64_t)(int64_t)position * __double2ull_rn(part) + (1ull << 61);        // + an eighth, so that quadrants are cut there
+    constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;                // 1 / 2 pi
+    const double turns = __dmul_rn(frequency, kTurn), rest = fma(frequency, kTurnRest, fma(frequency, kTurn, -turns));
+    const uint64_t part = (uint64_t)__double2ll_rn((turns - rint(turns)) * 0x1p64) + (uint64_t)__double2ll_rn((rest - rint(rest)) * 0x1p64);
+    const uint64_t angle = (uint64_t)(int64_t)position * part + (1ull << 61);               // + an eighth, so that quadrants are cut there
     const uint32_t quadrant = (uint32_t)(angle >> 62);
     const int32_t left = (int32_t)((uint32_t)(angle >> 30) ^ 0x80000000u);                            // what is below it, 2^-34 turns, the eighth taken off again
     const float x = (float)left * 0x1p-33f;                                                           // half turns, -1/4 .. 1/4
