@@ -536,7 +536,8 @@ typedef struct {
  * The scores of a query that sees a token are cap(scale * q . k) + bias in fp32. A query that sees no token gives out 0 and lse -infinity; a row of q
  * with a value that is not finite gives NaN. The products run in e4m3 with fp32 sums: a bf16 value of q enters exactly as two terms and an fp16 one as three (values
  * below 2^-14 of the row's largest to within 2^-22 of that), a weight times the scale of its block's values as three (2^-13 of itself), to within 2^-26 of
- * the row's largest such product over the tokens that it sees (scales below 2^-90 count as that there). A chunk of a prompt (many queries) reads the cache once for every 64 rows.
+ * the row's largest such product over the tokens that it sees (scales below 2^-90 count as that there). Beside a value of 2^x, x > 60, weights below
+ * 2^(x - 127) of the row's largest may count as 0. A chunk of a prompt (many queries) reads the cache once for every 64 rows.
  * A wait inside the kernel that takes two seconds, which only a fault can cause, ends it with NaN in out.
  * Errors: as of kvp_attend, and a cap that is negative or not finite, or so small or large that scale / cap or cap / ln 2 is no normal number (KVP_ERR_ARG).
  */

@@ -11,9 +11,11 @@
 // half step 2^-14, and what the first one leaves is rounded to fp16), down to 2^-26 of the largest. Products of e4m3 numbers are exact and the unit keeps 25 bits of their sums; terms have sums of their own, joined in fp32.
 // No byte of the cache goes through a register, and a chunk of a prompt reads it once for 64 rows.
 //
-// exp runs in fp32 against a running maximum M of s_i + e_i, with 2^e_i the scale of token i's values, over the tokens that the row sees: 2^(s_i - M) times 2^6 and the scale is
+// exp runs in fp32 against a running maximum M of s_i + e_i - E, with 2^e_i the scale of token i's values, over the tokens that the row sees: 2^(s_i - M) times 2^(6 - E) and the scale is
 // what is split. It is at most 64, and 256 before M moves: that happens only when a token passes it by 2^2 (kSlack). So neither values behind a row's mask nor large ones that get no
-// weight take bits from the others. The weights' sum has the same M; what it holds (up to 2^92 times as many as there are tokens, 2^-94 at least) fp32 does.
+// weight take bits from the others. The weights' sum has the same M and so is 2^(E - e) times as large as with the largest score for M: fp32 has room for scales of 2^-90 to 2^92 (beside the
+// largest, weights below 2^-27 of the row's largest are 0). E, a number once for all (kE), keeps s_i - M small, and as exact as s_i, for values of size 1; of size 2^x it is off by 2^-24 |x|.
+// E taken from the values of each segment made a chunk of a prompt 822 us instead of 797 and a batch 68.6 instead of 66.5.
 //
 // Split over CTAs as in kvp_attend: one line of all tiles (16 tokens), cut into equal parts on the device; the join is its join.
 //
@@ -42,7 +44,9 @@ constexpr uint32_t kGroup = 8;                // tiles of a stage
 constexpr uint32_t kOthers = 3;               // warps that are in no team
 constexpr uint32_t kListCap8 = 1024;          // units of a bitmap row that are listed at a time: 32 words
 constexpr float kSlack = 2.0f;
-constexpr float kLeastPower = -90.0f;         // smaller scales count as 2^this where the maximum is looked for, also 0
+constexpr int kE = -7;                        // log2 of the scale of a block of normal values
+constexpr float kUnit = 64.0f * (1 << -kE);   // 2^(6 - E)
+constexpr float kLeastPower = -83.0f;         // e_i - E counts as no less where the maximum is looked for, also where a scale is 0
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Attend8K : LineK<kFixed8> {
@@ -655,7 +659,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 const float2 scales = *reinterpret_cast<const float2*>(block + 16 * D);        // of keys, of values
                 bool live = tile != ~0u && pos < (int32_t)len;
                 if (live && p.units && p.unit < kTileTokens) live = bits_at(p, (uint64_t)walk.bh * p.row_units + ((uint32_t)pos >> p.unit_log2)) & 1u;
-                const float scale = live ? scales.y : 0.0f, power = fmaxf((float)((__float_as_int(scale) >> 23) - 127), kLeastPower);
+                const float scale = live ? scales.y : 0.0f, power = fmaxf((float)((__float_as_int(scale) >> 23) - 127 - kE), kLeastPower);
                 // does every row see every token of the warp?
                 const bool all_seen = __all_sync(0xFFFFFFFFu, live && pos < see_least && (pos >= see_most - window || pos < sink));
                 ok = ok && barrier_wait(bar(sm.scored[sb.at]), sb.parity, gave_up);
@@ -791,7 +795,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 }
                 // the weights as the right operand; the buffer is free when the products with what it held are done
                 if (it >= 2) ok = ok && barrier_wait(bar(sm.summed[pb.at]), pb.parity ^ 1u, gave_up);
-                const float by = scale * 64.0f;
+                const float by = scale * kUnit;
                 uint8_t* const to = weights + pb.at * S::kPBytes + me * 16;
                 uint32_t term[3][R / 4];
 #pragma unroll
@@ -877,7 +881,7 @@ __global__ void __launch_bounds__(S::kBlock, S::kCtas) attend8_kernel(const Atte
                 for (uint32_t u = 0; u < S::kTurns; ++u) {
                     const bool some = one[u] != 0.0f;
                     sum = fmaf(one[u], some ? exp2_fast(high[u] - m) : 0.0f, sum);
-                    sm.last[team0 + u][mine + me].x = some ? 0x1p-6f * exp2_fast(-sm.low[team0 + u][mine + me] - m) : 0.0f;
+                    sm.last[team0 + u][mine + me].x = some ? 1.0f / kUnit * exp2_fast(-sm.low[team0 + u][mine + me] - m) : 0.0f;
                 }
                 const float by = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
                 sm.last[team0][mine + me].y = by;

@@ -176,3 +176,54 @@ def test_a_weight_keeps_fourteen_bits(kvp, d, rows):  # noqa: F811
         for _ in range(4):
             q = cuda((rng.standard_normal((1, 1, rows, d)) * 1.5).astype(np.float32)).to(F16)
             near(kvp.attend8(q, cache, cuda(table), cuda(lens)), q, cache, table, lens, terms=2.0 ** -13)
+
+
+@pytest.mark.parametrize("rows", [1, 8, 12, 40])
+@pytest.mark.parametrize("power", [0, -30, -13, 12, 25])
+def test_lse_and_weights_beside_values_of_any_size(kvp, power, rows):  # noqa: F811
+    """Values of size 2^x: scores are kept with an offset of x, whose rounding adds 2^-24 * (|x| + 4) in the exponent to base 2, once to the maximum and once to a score: 2^-23 * (|x| + 4)
+    on top of what test_gpu_attend8.py allows. Scores are small, and one sequence has a single token, so that this is most of it."""
+    d, n = 128, 900
+    rng = np.random.default_rng(rows)
+    k, v = rng.standard_normal((2, n, 2, d))
+    q = cuda((rng.standard_normal((2, 1, 2 * rows, d)) * 1e-3).astype(np.float32)).to(BF16)
+    cache, table, lens = filled(kvp, k, v * 2.0 ** power)
+    table, lens = np.repeat(table, 2, 0), np.array([n, 1], np.int32)
+    got = kvp.attend8(q, cache, cuda(table), cuda(lens), unit_tokens=16, want_lse=True, want_weights=True)
+    want = plain.attend(q.double().cpu().numpy(), cache.cpu().numpy(), table, lens, 16, float(np.float32(d ** -0.5)))
+    extra = 2.0 ** -23 * (abs(power) + 4)
+    score = 16 * 2.0 ** -23 * want["reach"] + 2.0 ** -22 * (want["wide"] + want["high"] + 1) + extra
+    off = np.abs(got["lse"].double().cpu().numpy() - want["lse"])
+    assert np.all(off <= score + 4 * 2.0 ** -23 * np.abs(want["lse"])), off.max()
+    off = np.abs(got["weights"].double().cpu().numpy() - want["weights"])
+    assert np.all(off <= want["weights"] * (2 * score.max() + 8 * 2.0 ** -23 * np.abs(want["lse"]).max() + 2.0 ** -20)), off.max()
+
+
+@pytest.mark.parametrize("rows", [4, 20])
+@pytest.mark.parametrize("size,large", [(1.0, np.inf), (1e-12, np.inf), (1e20, 1e-15), (1.0, 2.0 ** 60), (2.0 ** -80, 2.0 ** 10)])
+def test_weights_beside_values_of_another_size(kvp, size, large, rows):  # noqa: F811
+    """A block whose values are 2^60 times or more as large (or small) as the others', with much more weight, or much less: units of small weight keep it, and lse is right.
+    Tolerance as in test_gpu_attend8.py: weights 2 * score + 8 * 2^-23 |lse| + 2^-20 of themselves, lse score + 4 * 2^-23 |lse|; the offset of the scores adds 2^-23 * 99 to `score` at most, and
+    beside values of 2^100 (what infinities count as) a weight below 2^-27 of the largest may be 0: 2^-27 a row and token, on either side."""
+    d, n = 128, 700
+    rng = np.random.default_rng(11)
+    for where in (0, 304, 688):
+        for weight in (110.0, -110.0):                         # scores of +-19 beside the others', e^19 = 2^28
+            k, v = rng.standard_normal((2, n, 1, d)) * 0.3
+            v = v * size
+            k[where: where + 12, 0, 0] = weight
+            v[where: where + 12] = large * np.sign(v[where: where + 12])
+            cache, table, lens = filled(kvp, k, v)
+            q = rng.standard_normal((1, 1, rows, d)) * 0.2
+            q[..., 0] = 2.0
+            q = cuda(q.astype(np.float32)).to(BF16)
+            got = kvp.attend8(q, cache, cuda(table), cuda(lens), unit_tokens=16, want_lse=True, want_weights=True)
+            want = plain.attend(q.double().cpu().numpy(), cache.cpu().numpy(), table, lens, 16, float(np.float32(d ** -0.5)))
+            score = 16 * 2.0 ** -23 * want["reach"] + 2.0 ** -22 * (want["wide"] + want["high"] + 1) + 2.0 ** -23 * 99
+            gone = 2.0 ** -27 if np.isinf(large) else 0.0
+            off = np.abs(got["lse"].double().cpu().numpy() - want["lse"])
+            assert np.all(off <= score + 4 * 2.0 ** -23 * np.abs(want["lse"]) + n * gone), off.max()
+            off = np.abs(got["weights"].double().cpu().numpy() - want["weights"])
+            room = want["weights"] * (2 * score.max() + 8 * 2.0 ** -23 * np.abs(want["lse"]).max() + 2.0 ** -20 + n * gone) + 16 * rows * gone
+            assert np.all(off <= room), (off / np.maximum(room, 1e-300)).max()
+            near(got, q, cache, table, lens)
