@@ -538,6 +538,7 @@ typedef struct {
  * below 2^-14 of the row's largest to within 2^-22 of that), a weight times the scale of its block's values as three (2^-13 of itself), to within 2^-26 of
  * the row's largest such product over the tokens that it sees (scales below 2^-90 count as that there). Beside a value of 2^x, x > 60, weights below
  * 2^(x - 127) of the row's largest may count as 0. A chunk of a prompt (many queries) reads the cache once for every 64 rows.
+ * With weights the workspace holds a float for every query row and block of min(unit_tokens, 16) tokens, written and read once: units of 16 tokens or more where there are many queries.
  * A wait inside the kernel that takes two seconds, which only a fault can cause, ends it with NaN in out.
  * Errors: as of kvp_attend, and a cap that is negative or not finite, or so small or large that scale / cap or cap / ln 2 is no normal number (KVP_ERR_ARG).
  */
@@ -571,7 +572,7 @@ typedef struct {
  *   q, k (device) [tokens][heads or kv_heads][head_dim];  q_out, k_out (device) the same, may be q or k themselves with the same strides (another
  *        overlap is not allowed)
  *   positions (device) [tokens] int32, also negative;  frequencies (device) [rotary_dim / 2] double, radians a token, finite
- * Sums and products in fp32, rounded once. An angle is reduced in 64-bit whole numbers, so sines and cosines are good to 2^-24 at any position.
+ * Sums and products in fp32, rounded once. An angle is reduced in 64-bit whole numbers to 2^-34 turns, so sines and cosines are good to 2^-24 at any position.
  * Errors: KVP_ERR_ARG (null, sizes, dtype, flags, a scale that is not finite, alignment), KVP_ERR_RANGE (sizes). 16-byte aligned rows with
  * rotary_dim / 2 (interleaved: rotary_dim) and the rest of the head multiples of 16 bytes are moved 16 bytes at a time.
  */

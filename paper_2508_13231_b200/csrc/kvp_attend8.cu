@@ -24,8 +24,8 @@
 // shared memory whose wait ends after two seconds; a CTA that gave up writes NaN.
 //
 // What bounds it. 131072 tokens x 8 heads of 128 dims x 8 queries with weights (270 MB, 42 us at the rate of a copy) take 57 us: 12 until the first groups are through (line,
-// queries and first tiles, and the instructions' first fetch), then memory at 5.6 TB/s, 3 for the join; issue slots 36%, matrix unit 6% busy. A chunk of 512 queries x
-// 4 heads over 32768 tokens x 8 heads: 797 us, 345 TFLOP/s, issue slots 59%, matrix unit 20%: 26 instructions of a warp a score, a third of them for the terms
+// queries and first tiles, and the instructions' first fetch), then memory at 5.6 TB/s, 3 for the join; issue slots 37%, matrix unit 6% busy. A chunk of 512 queries x
+// 4 heads over 32768 tokens x 8 heads: 797 us, 345 TFLOP/s, issue slots 61%, matrix unit 20%: 26 instructions of a warp a score, a third of them for the terms
 // (a weight rounded to fp16 before it is split, 2^-11 of itself instead of 2^-13: 774).
 #include <type_traits>
 
